@@ -351,6 +351,150 @@ int32_t rip_step(rip_sched* s, const rip_replicas* r, int64_t step, const uint8_
 int32_t rip_set_max_blocks(int32_t max_blocks);
 int32_t rip_set_blocks_per_cu(int32_t blocks_per_cu);
 
+/* ------------------------------------------------------------------------
+ * Operators that fill the gradient buffers of language-model replicas
+ *
+ * A replica's training pass begins at its embedding, keeps what its layers need
+ * for the backward pass, and ends in a loss over the vocabulary.  These calls
+ * write straight into registered gradient segments (rip_replicas_create), which
+ * the next rip_step / rip_preduce reads.  Each works on one replica's buffers.
+ *
+ * Conventions beyond those at the top of this file
+ *  - A matrix is a device pointer, its type (RIP_FP32 / RIP_BF16) and its row
+ *    stride `ld` in elements (at least its width).  It need only be aligned to
+ *    its elements; columns between the width and `ld` are neither read nor
+ *    written.  Indexes into it are 64-bit.
+ *  - Arithmetic and every sum are fp32 (or wider); a result is rounded to bf16
+ *    once, to nearest even.  Nothing is added atomically: a call's result is the
+ *    same bits every time.
+ *  - Token ids and targets are RIP_INT32 or RIP_INT64 device arrays.
+ *  - `workspace` is device memory of at least the bytes that the call's
+ *    _workspace function returns for the same sizes (0 = none needed; sizes that
+ *    the call itself refuses also give 0), 16-byte aligned, free again when the
+ *    stream has passed the call.  It need not be cleared.
+ *  - A buffer that a call writes must not overlap any other of its buffers,
+ *    except where a call says that it may be the same matrix.
+ *  - Empty inputs (no tokens) are no error; their pointers may be NULL.
+ *  - All calls are only kernel launches on `stream` (no allocation, copy, memset
+ *    or wait), so they may be captured into a HIP graph.
+ * Errors of every call: RIP_E_INVAL (null pointer, size, row stride, workspace
+ * too small, a scalar out of its range), RIP_E_ALIGN, RIP_E_OVERLAP,
+ * RIP_E_UNSUPPORTED (type, size above a limit), RIP_E_HIP.
+ * ---------------------------------------------------------------------- */
+enum { RIP_INT32 = 0, RIP_INT64 = 1 };  /* types of token ids */
+
+#define RIP_MAX_TOKENS (1 << 23)    /* tokens (rows) of one call */
+#define RIP_MAX_WIDTH (1 << 24)     /* columns of a row; logits of a token */
+#define RIP_MAX_FEATURES (1 << 18)  /* rows and columns of a layer's weight */
+#define RIP_MAX_PAIRS (1 << 20)     /* pairs of sequences of one call */
+
+/* Embedding lookup: out[t] = scale * table[ids[t]] for n_tokens rows of `width`.
+ * An id outside 0 .. vocab-1 (padding) gives a row of zeros.  table and out may
+ * have different types. */
+int32_t rip_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab, int64_t width,
+                         int64_t ld_table, const void* ids, int32_t id_type, int64_t n_tokens,
+                         float scale, void* out, int32_t out_dtype, int64_t ld_out, void* stream);
+
+/* Its gradient: grad[v] = scale * sum of dout[t] over the tokens with ids[t] == v
+ * (ascending t within fixed runs of tokens, whose sums are added in order), for
+ * every row of the table: rows that no token names become zeros.  With
+ * `accumulate` nonzero the sums are added to what grad holds and the other rows
+ * are not touched.  Ids outside the vocabulary contribute nothing. */
+int64_t rip_embed_grad_workspace(int64_t n_tokens, int64_t width);
+int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t ld_dout, const void* ids,
+                       int32_t id_type, int64_t n_tokens, float scale, void* grad,
+                       int32_t grad_dtype, int64_t vocab, int64_t width, int64_t ld_grad,
+                       int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Activations kept in 8 bits.  A checkpoint of `rows` rows of `width` columns is
+ *   codes [rows][32 * ceil(width / 32)] int8, 16-byte aligned
+ *   exps  [rows][ceil(width / 32)] uint8
+ * A block is 32 columns of a row (the last may be short; its other codes are 0).
+ * With e = exp - 127, code q stands for q * 2^e, q in -127 .. 127: e is the
+ * smallest integer in -126 .. 121 for which the block's largest magnitude is at
+ * most 127 * 2^e (121 for a magnitude beyond 127 * 2^121), and q is x / 2^e
+ * rounded to nearest, ties to even, and cut to -127 .. 127.  A block with an
+ * infinity or a NaN has exp 255 and codes 0 and stands for NaN throughout, so
+ * that a diverged value is not lost.
+ * rip_ckpt_unpack writes the values it stands for (exact in bf16 too). */
+int32_t rip_ckpt_pack(const void* x, int32_t dtype, int64_t ld, int64_t rows, int64_t width,
+                      int8_t* codes, uint8_t* exps, void* stream);
+int32_t rip_ckpt_unpack(const int8_t* codes, const uint8_t* exps, int64_t rows, int64_t width,
+                        void* x, int32_t dtype, int64_t ld, void* stream);
+
+/* Gated unit of a feed-forward layer: h = silu(gate) * up, silu(z) = z / (1 +
+ * e^-z), from the inputs as given; gate and up are kept as checkpoints in the
+ * same pass.  gate and up may lie side by side in the rows of one buffer; h may
+ * be the same matrix as gate or up. */
+int32_t rip_gate_forward(const void* gate, int64_t ld_gate, const void* up, int64_t ld_up,
+                         int32_t dtype, int64_t rows, int64_t width, void* h, int64_t ld_h,
+                         int8_t* gate_codes, uint8_t* gate_exps, int8_t* up_codes,
+                         uint8_t* up_exps, void* stream);
+
+/* Its backward pass from the checkpoints' values g, u, with s = 1 / (1 + e^-g):
+ *   dgate = dh * u * s * (1 + g * (1 - s)),   dup = dh * g * s
+ * and, unless h_codes and h_exps are both NULL, a checkpoint of g * s * u: the
+ * next layer's input, so that no forward pass need keep it.  dgate and dup may
+ * lie side by side in the rows of one buffer; one of them may be dh. */
+int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtype, const int8_t* gate_codes,
+                          const uint8_t* gate_exps, const int8_t* up_codes,
+                          const uint8_t* up_exps, int64_t rows, int64_t width, void* dgate,
+                          int64_t ld_dgate, void* dup, int64_t ld_dup, int8_t* h_codes,
+                          uint8_t* h_exps, void* stream);
+
+/* Weight gradient of a linear layer y = x W^T from the checkpoint of x:
+ *   grad[n][k] = sum_t dy[t][n] * x'[t][k]     (out_features x in_features)
+ * added to what grad holds if `accumulate` is nonzero.  x' is what the
+ * checkpoint stands for; products are exact and sums fp32 for either type of dy. */
+int64_t rip_ckpt_wgrad_workspace(int32_t dy_dtype, int64_t rows, int64_t out_features,
+                                 int64_t in_features);
+int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_dy, int64_t rows,
+                       int64_t out_features, const int8_t* codes, const uint8_t* exps,
+                       int64_t in_features, void* grad, int32_t grad_dtype, int64_t ld_grad,
+                       int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Preference loss over pairs of sequences, and the gradient of the logits.
+ *   logits   [n_tokens][vocab]; targets[t] is the token that row t predicts
+ *   seq_offsets [2 * n_pairs + 1] int32 on the device, ascending: sequence q is
+ *            the tokens seq_offsets[q] .. seq_offsets[q+1]-1; 2p is the chosen
+ *            and 2p+1 the rejected one of pair p.  Offsets outside 0..n_tokens or
+ *            out of order are cut to fit.
+ *   ref_logp [2 * n_pairs] log-probabilities of the sequences under the reference
+ * A token counts unless its target lies outside 0 .. vocab-1 (prompt, padding),
+ * it belongs to no sequence, or every logit of its row is -inf.  With
+ *   logp[t] = log softmax(logits[t])[targets[t]]   (0 where it does not count)
+ *   seq_logp[q] = sum of logp over sequence q (in 64 bits, then rounded)
+ *   z_p = beta * ((seq_logp[2p] - ref_logp[2p]) - (seq_logp[2p+1] - ref_logp[2p+1]))
+ *   loss = mean over p of -(1 - smoothing) log sigmoid(z_p) - smoothing log sigmoid(-z_p)
+ * grad is grad_scale * d loss / d logits, zeros in the rows that do not count,
+ * whatever those rows hold.  Outputs: loss [1], seq_logp [2 * n_pairs], logp
+ * [n_tokens] or NULL, grad or NULL (only the loss), which may be the same matrix
+ * as logits. */
+int64_t rip_pref_loss_workspace(int64_t n_tokens, int64_t vocab, int32_t n_pairs);
+int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,
+                      int64_t vocab, const void* targets, int32_t id_type,
+                      const int32_t* seq_offsets, int32_t n_pairs, const float* ref_logp,
+                      float beta, float smoothing, float grad_scale, float* loss, float* seq_logp,
+                      float* logp, void* grad, int64_t ld_grad, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
+/* Clipped policy loss with a KL term, and the gradient of the logits.  logp and
+ * which tokens count are as above (there are no sequences).  For a counted token
+ *   r = e^(logp - old_logp),  c = min(max(r, 1 - clip_low), 1 + clip_high)
+ *   loss_t = -min(r * advantage, c * advantage) + kl * (e^d - d - 1),  d = ref_logp - logp
+ *   loss = sum over the counted t of weight[t] * loss_t
+ * The derivative by logp of the first term is -r * advantage where r * advantage
+ * <= c * advantage, else 0.  old_logp, advantage, weight and ref_logp are fp32
+ * [n_tokens]; weight NULL stands for 1 / n_tokens, ref_logp may be NULL if kl is
+ * 0.  0 <= clip_low <= 1, clip_high >= 0.  Outputs as above. */
+int64_t rip_policy_loss_workspace(int64_t n_tokens, int64_t vocab);
+int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,
+                        int64_t vocab, const void* targets, int32_t id_type, const float* old_logp,
+                        const float* advantage, const float* weight, const float* ref_logp,
+                        float clip_low, float clip_high, float kl, float grad_scale, float* loss,
+                        float* logp, void* grad, int64_t ld_grad, void* workspace,
+                        int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -380,3 +380,9 @@ def abi_version() -> int:
 def rip_last_launch_count() -> int:
     """Kernel launches the calling thread's last step call enqueued (0-2)."""
     return lib.rip_last_launch_count()
+
+
+# operators that fill a replica's gradient buffers (they need the names above)
+from ._train_ops import (  # noqa: E402,F401
+    Ckpt, rip_ckpt_pack, rip_ckpt_unpack, rip_ckpt_wgrad, rip_embed_grad, rip_embed_lookup,
+    rip_gate_backward, rip_gate_forward, rip_policy_loss, rip_pref_loss)

@@ -1,0 +1,69 @@
+// The 8-bit checkpoint format: how a block of 32 values becomes 32 integers and
+// one exponent, and back (device code shared by rip_ckpt.hip and rip_wgrad.hip).
+//
+// A block's step is the smallest power of two 2^e, -126 <= e <= 121, for which its
+// largest magnitude is at most 127 steps (or 2^121, where there is none: the few
+// fp32 numbers beyond are cut to 127 steps, as 2^122 would round them to 2^128).
+// A power of two instead of a free
+// scale costs at most one of the eight bits and buys two things: the value
+// q * 2^e has at most seven significant bits, so it is exact in bf16 and goes
+// into the matrix cores as it is, and packing is exact up to the one rounding
+// of x / 2^e, the same on every machine.
+#pragma once
+
+#include "rip_ops_common.h"
+
+namespace rip {
+
+constexpr int kCkptBlock = 32;                 // columns of a block
+constexpr int kCkptLanes = kCkptBlock / kLane; // lanes that hold a block
+constexpr uint32_t kCkptMax = 121 + 127;       // largest exponent byte of a finite block
+constexpr uint32_t kCkptNan = 255;             // exponent byte of a block with an inf or NaN
+
+// Exponent byte (e + 127, 1..248) of a block whose largest magnitude has the
+// bits `top`; kCkptNan if that is an infinity or a NaN.
+__device__ __forceinline__ uint32_t ckpt_exponent(uint32_t top) {
+  // |x| = m * 2^k, 1 <= m < 2: 127 steps of 2^(k-6) reach 1.984375 * 2^k
+  const int e = (int)(top >> 23) - 6 + ((top & 0x7fffffu) > 0x7e0000u ? 1 : 0);
+  return top >= 0x7f800000u ? kCkptNan : (uint32_t)max(1, min(e, (int)kCkptMax));
+}
+
+// Exponent byte and codes (8 bytes) of the lane's eight values; the four lanes
+// of a block are consecutive and all active.
+__device__ __forceinline__ uint32_t ckpt_pack(const float (&x)[kLane], uint2& codes) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  const uint32_t e = ckpt_exponent(top);
+  // x / 2^e + 1.5 * 2^23, rounded once to nearest even: its low byte is q
+  const float inv = e == kCkptNan ? 0.0f : __uint_as_float((254 - e) << 23);
+  uint32_t q[kLane];
+#pragma unroll
+  for (int j = 0; j < kLane; ++j)
+    q[j] = __float_as_uint(__builtin_fmaf(x[j], inv, 12582912.0f)) & 0xff;
+  if (e == kCkptMax) {  // the one step that a magnitude may exceed
+#pragma unroll
+    for (int j = 0; j < kLane; ++j)
+      q[j] = (uint32_t)(int)fminf(fmaxf(rintf(x[j] * inv), -127.0f), 127.0f) & 0xff;
+  }
+  codes.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+  codes.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
+  if (e == kCkptNan) codes.x = codes.y = 0;
+  return e;
+}
+
+// 2^e, NaN for a block that held an inf or a NaN (its codes are zeros).
+__device__ __forceinline__ float ckpt_step(uint32_t e) {
+  return __uint_as_float(e == kCkptNan ? 0x7fc00000u : e << 23);
+}
+
+__device__ __forceinline__ void ckpt_unpack(uint2 codes, uint32_t e, float (&x)[kLane]) {
+  const float step = ckpt_step(e);
+#pragma unroll
+  for (int j = 0; j < kLane; ++j)
+    x[j] = (float)(int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j % 4))) * step;
+}
+
+}  // namespace rip

@@ -1,0 +1,509 @@
+// Embedding lookup with scaling and its gradient by sorted tokens (gfx950).
+//
+//   out[t]  = scale * table[id_t]
+//   grad[v] = scale * sum over {t : id_t = v}, ascending t, of dout[t]
+//
+// Both are bound by memory: the lookup reads and writes a row a token, the
+// gradient reads a row a token and writes the whole table's gradient (P-Reduce
+// reads every element of it).
+//
+// The gradient runs over the tokens sorted by id, a fixed number of them to a
+// wave, however often an id occurs: a frequent id is shared by many waves
+// instead of making one wave long.  A wave adds a run of equal ids in
+// registers and writes the row if the run is its own; a run that passes the
+// wave's ends leaves its partial sums in the workspace, and a last launch adds
+// those.  Nothing is added atomically, so the result is the same in every call.
+
+#include "rip_ops_common.h"
+
+namespace rip {
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kLookupBlock = 256;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
+constexpr int kSortItems = 4;                          // tokens of a thread
+constexpr int kChunk = kSortThreads * kSortItems;      // tokens sorted by one workgroup
+constexpr int kMaxDigit = 8;                           // bits of a pass of the sort
+constexpr int kColumns = kWave * kLane;                // columns of a wave
+constexpr int kFillBytes = 1 << 16;                    // bytes zeroed by a workgroup of the fill
+
+template <int TD, int OD>
+__global__ __launch_bounds__(kLookupBlock) void lookup_kernel(
+    const typename Elem<TD>::T* table, int64_t vocab, int width, int64_t ld, const void* ids,
+    int wide, uint32_t units, FastDiv per_row, float scale, typename Elem<OD>::T* out,
+    int64_t ld_out) {
+  const uint32_t unit = blockIdx.x * kLookupBlock + threadIdx.x;
+  if (unit >= units) return;
+  const uint32_t t = per_row.div(unit);
+  const int c = (int)(unit - t * per_row.d) * kLane;
+  const int64_t id = load_id(ids, wide, t);
+  float f[kLane];
+  if (id >= 0 && id < vocab) {
+    load_unit<TD>(table + id * ld, c, width, f);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[j] *= scale;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[j] = 0.0f;
+  }
+  store_unit<OD>(out + (int64_t)t * ld_out, c, width, f);
+}
+
+// Sort of up to kChunk (id, position) pairs by id in one workgroup: passes over
+// digits of `bits` bits from the lowest, each stable.  A wave holds consecutive
+// elements; equal digits in a wave find each other with one ballot a bit.
+struct SortShared {
+  uint32_t key[kChunk];
+  uint16_t pos[kChunk];
+  uint32_t count[kSortWaves << kMaxDigit];
+  uint32_t wave_sum[kSortWaves];
+};
+
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ void sort_chunk(SortShared& sh, int passes, int bits) {
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int buckets = 1 << bits, cells = kSortWaves << bits;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int p = 0; p < passes; ++p) {
+    for (int i = tid; i < cells; i += kSortThreads) sh.count[i] = 0;
+    __syncthreads();
+    uint32_t key[kSortItems], rank[kSortItems];
+    uint16_t pos[kSortItems];
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+      const int i = (wave * kSortItems + r) * kWave + lane;
+      key[r] = sh.key[i];
+      pos[r] = sh.pos[i];
+      const uint32_t d = (key[r] >> (p * bits)) & (buckets - 1);
+      uint64_t same = ~(uint64_t)0;
+      for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot((d >> b) & 1);
+        same &= (d >> b) & 1 ? set : ~set;
+      }
+      // counters are laid out digit by digit, the waves of a digit in a row
+      const uint32_t cell = d * kSortWaves + wave;
+      const uint32_t before = sh.count[cell];
+      rank[r] = before + __popcll(same & below);
+      // a wave's accesses to LDS happen in order; the fences keep the compiler's
+      wave_fence();
+      if (!(same & below)) sh.count[cell] = before + __popcll(same);
+      wave_fence();
+    }
+    __syncthreads();
+    // exclusive sums of the counters, a run of them to each thread
+    const int per = (cells + kSortThreads - 1) / kSortThreads;
+    uint32_t sum = 0;
+    for (int i = 0; i < per; ++i) {
+      const int cell = tid * per + i;
+      if (cell < cells) sum += sh.count[cell];
+    }
+    uint32_t scan = sum;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t up = __shfl_up(scan, o);
+      if (lane >= o) scan += up;
+    }
+    if (lane == kWave - 1) sh.wave_sum[wave] = scan;
+    __syncthreads();
+    uint32_t base = scan - sum;
+    for (int w = 0; w < wave; ++w) base += sh.wave_sum[w];
+    for (int i = 0; i < per; ++i) {
+      const int cell = tid * per + i;
+      if (cell < cells) {
+        const uint32_t c = sh.count[cell];
+        sh.count[cell] = base;
+        base += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSortItems; ++r) {
+      const uint32_t d = (key[r] >> (p * bits)) & (buckets - 1);
+      const uint32_t to = sh.count[d * kSortWaves + wave] + rank[r];
+      sh.key[to] = key[r];
+      sh.pos[to] = pos[r];
+    }
+    __syncthreads();
+  }
+}
+
+// Workgroups below `chunks` each sort kChunk tokens (ids outside the vocabulary
+// become `vocab` and go last); the others zero the gradient's rows meanwhile,
+// which takes longer than the sort for all but the smallest tables.
+template <int GD>
+__global__ __launch_bounds__(kSortThreads) void sort_fill_kernel(
+    const void* ids, int wide, int64_t n, uint32_t vocab, int passes, int bits, int chunks,
+    uint32_t* sorted_id, uint32_t* sorted_pos, typename Elem<GD>::T* grad, int width, int64_t ld,
+    int rows_per_block) {
+  __shared__ SortShared sh;
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x < chunks) {
+    const int64_t base = (int64_t)blockIdx.x * kChunk;
+    const int count = (int)(n - base < kChunk ? n - base : kChunk);
+    for (int i = tid; i < kChunk; i += kSortThreads) {
+      int64_t id = i < count ? load_id(ids, wide, base + i) : (int64_t)vocab;
+      if (id < 0 || id > (int64_t)vocab) id = vocab;
+      sh.key[i] = (uint32_t)id;
+      sh.pos[i] = (uint16_t)i;
+    }
+    __syncthreads();
+    sort_chunk(sh, passes, bits);
+    for (int i = tid; i < count; i += kSortThreads) {
+      sorted_id[base + i] = sh.key[i];
+      sorted_pos[base + i] = (uint32_t)base + sh.pos[i];
+    }
+    return;
+  }
+  const int64_t row0 = (int64_t)(blockIdx.x - chunks) * rows_per_block;
+  const int64_t row1 = row0 + rows_per_block < vocab ? row0 + rows_per_block : vocab;
+  const float zero[kLane] = {};
+  if (ld == width) {  // rows without gaps are one range
+    typename Elem<GD>::T* p = grad + row0 * ld;
+    const int64_t m = (row1 - row0) * (int64_t)width;
+    for (int64_t c = (int64_t)tid * kLane; c < m; c += (int64_t)kSortThreads * kLane) {
+      if (c + kLane <= m) {
+        Elem<GD>::store8(p + c, zero);
+      } else {
+        for (int64_t j = c; j < m; ++j) Elem<GD>::store(p + j, 0.0f);
+      }
+    }
+  } else {
+    for (int64_t r = row0; r < row1; ++r)
+      for (int c = tid * kLane; c < width; c += kSortThreads * kLane)
+        store_unit<GD>(grad + r * ld, c, width, zero);
+  }
+}
+
+// Number of entries of a sorted run that come before `id` (equal ones too with
+// `after`).
+__device__ __forceinline__ int rank_in(const uint32_t* run, int n, uint32_t id, bool after) {
+  int lo = 0;
+  for (int len = n; len > 0;) {
+    const int half = len / 2;
+    const uint32_t x = run[lo + half];
+    if (x < id || (after && x == id)) {
+      lo += half + 1;
+      len -= half + 1;
+    } else {
+      len = half;
+    }
+  }
+  return lo;
+}
+
+// The sorted chunks become one sorted list: an entry's place is its place in its
+// own chunk and its rank in every other (equal ids of earlier chunks go first).
+__global__ __launch_bounds__(256) void merge_kernel(const uint32_t* id_in, const uint32_t* pos_in,
+                                                    int64_t n, int chunks, uint32_t* id_out,
+                                                    uint32_t* pos_out) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int own = (int)(i / kChunk);
+  const uint32_t id = id_in[i];
+  int64_t at = i - (int64_t)own * kChunk;
+  for (int c = 0; c < chunks; ++c) {
+    if (c == own) continue;
+    const int64_t base = (int64_t)c * kChunk;
+    const int len = (int)(n - base < kChunk ? n - base : kChunk);
+    at += rank_in(id_in + base, len, id, c < own);
+  }
+  id_out[at] = id;
+  pos_out[at] = pos_in[i];
+}
+
+template <int GD>
+__device__ __forceinline__ void write_row(typename Elem<GD>::T* row, int c, int width, float scale,
+                                          int accumulate, const float (&acc)[kLane]) {
+  float f[kLane];
+  if (accumulate) {
+    load_unit<GD>(row, c, width, f);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[j] = f[j] + scale * acc[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[j] = scale * acc[j];
+  }
+  store_unit<GD>(row, c, width, f);
+}
+
+// One wave: entries [a, b) of the sorted list, 512 columns.  Partial sums of a
+// run that began before `a` go to slot 0 of the wave's share, those of a run
+// that begins here and goes on to slot 1.
+template <int DD, int GD>
+__global__ __launch_bounds__(kWave) void sum_kernel(
+    const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id, const uint32_t* pos,
+    int64_t n, uint32_t vocab, int per, float scale, typename Elem<GD>::T* grad, int width,
+    int64_t ld, int accumulate, float* partial) {
+  const int64_t a = (int64_t)blockIdx.x * per;
+  const int64_t b = a + per < n ? a + per : n;
+  const int c = blockIdx.y * kColumns + threadIdx.x * kLane;
+  if (id[a] >= vocab) return;  // only ids outside the vocabulary from here on
+  float acc[kLane] = {};
+  bool begins = a == 0 || id[a - 1] != id[a];
+  for (int64_t i = a; i < b; ++i) {
+    const uint32_t v = id[i];
+    if (v >= vocab) break;
+    float f[kLane] = {};
+    if (c < width) load_unit<DD>(dout + (int64_t)pos[i] * ld_dout, c, width, f);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) acc[j] += f[j];
+    const bool ends = i + 1 >= n || id[i + 1] != v;
+    if (!ends && i + 1 < b) continue;
+    if (c < width) {
+      if (begins && ends) {
+        write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
+      } else {
+        float* p = partial + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * width;
+        store_unit<RIP_FP32>(p, c, width, acc);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) acc[j] = 0.0f;
+    begins = true;
+  }
+}
+
+constexpr int kJoinWaves = 8;
+
+// The workgroup of the wave in which a long run begins adds that run's partial
+// sums: its own slot 1 and slot 0 of the waves that the run passes through.
+template <int GD>
+__global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
+    const uint32_t* id, int64_t n, uint32_t vocab, int per, int waves, const float* partial,
+    float scale, typename Elem<GD>::T* grad, int width, int64_t ld, int accumulate) {
+  __shared__ float part[kJoinWaves][kColumns];
+  const int64_t a = (int64_t)blockIdx.x * per;
+  const int64_t b = a + per;
+  if (b >= n) return;
+  const uint32_t v = id[b - 1];
+  if (v >= vocab || id[b] != v) return;       // the last run ends here
+  if (id[a] == v && a > 0 && id[a - 1] == v) return;  // it began in an earlier wave
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  // last wave that the run reaches: the first whose own last entry differs
+  int last = blockIdx.x + 1;
+  for (;; last += kWave) {
+    const int w = last + lane;
+    const int64_t end = ((int64_t)w + 1) * per < n ? ((int64_t)w + 1) * per : n;
+    const bool on = w < waves - 1 && id[end - 1] == v && id[end] == v;
+    const uint64_t stop = ~__ballot(on);
+    if (stop) {
+      last += __ffsll((unsigned long long)stop) - 1;
+      break;
+    }
+  }
+  const int c = blockIdx.y * kColumns + lane * kLane;
+  const int count = last - (int)blockIdx.x;  // partial sums after the first
+  const int share = (count + kJoinWaves - 1) / kJoinWaves;
+  float acc[kLane] = {}, f[kLane];
+  if (c < width) {
+    if (wave == 0) load_unit<RIP_FP32>(partial + ((int64_t)blockIdx.x * 2 + 1) * width, c, width, acc);
+    const int w1 = min(count, (wave + 1) * share);
+    for (int w = wave * share; w < w1; ++w) {
+      load_unit<RIP_FP32>(partial + ((int64_t)blockIdx.x + 1 + w) * 2 * width, c, width, f);
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) acc[j] += f[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) part[wave][lane * kLane + j] = acc[j];
+  __syncthreads();
+  if (wave != 0 || c >= width) return;
+  for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) acc[j] += part[w][lane * kLane + j];
+  write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
+}
+
+// Entries of the sorted list that a wave adds up.
+int entries_per_wave(int64_t n, int64_t width) {
+  const int64_t columns = ceil_div(width, kColumns);
+  int per = 4;
+  while (per < 32 && ceil_div(n, 2 * per) * columns >= 4096) per *= 2;
+  return per;
+}
+
+struct GradPlan {
+  int per, waves, chunks;
+  int64_t id_bytes, partial_bytes, total;
+};
+GradPlan grad_plan(int64_t n, int64_t width) {
+  GradPlan p{};
+  p.per = entries_per_wave(n, width);
+  p.waves = (int)ceil_div(n, p.per);
+  p.chunks = (int)ceil_div(n, kChunk);
+  p.id_bytes = ceil_div(n * 4, 256) * 256;
+  p.partial_bytes = (int64_t)p.waves * 2 * width * 4;
+  // ids and positions, once more where chunks are merged, and the partial sums
+  p.total = p.id_bytes * (p.chunks > 1 ? 4 : 2) + p.partial_bytes;
+  return p;
+}
+
+int32_t check_ids(const void* ids, int32_t id_type, int64_t n) {
+  if (id_type != RIP_INT32 && id_type != RIP_INT64)
+    return fail(RIP_E_UNSUPPORTED, "unknown id type %d", id_type);
+  if (n < 0) return fail(RIP_E_INVAL, "n_tokens %lld < 0", (long long)n);
+  if (n > RIP_MAX_TOKENS)
+    return fail(RIP_E_UNSUPPORTED, "n_tokens %lld > %d", (long long)n, RIP_MAX_TOKENS);
+  if (n && !ids) return fail(RIP_E_INVAL, "ids is NULL");
+  if (reinterpret_cast<uintptr_t>(ids) % (id_type == RIP_INT64 ? 8 : 4))
+    return fail(RIP_E_ALIGN, "ids = %p is not aligned to its type", ids);
+  return RIP_OK;
+}
+
+int32_t check_table(int64_t vocab, int64_t width) {
+  if (vocab < 1 || width < 1)
+    return fail(RIP_E_INVAL, "vocab %lld and width %lld must be >= 1", (long long)vocab,
+                (long long)width);
+  if (vocab > INT32_MAX - 1 || width > RIP_MAX_WIDTH)
+    return fail(RIP_E_UNSUPPORTED, "vocab %lld or width %lld above the limit", (long long)vocab,
+                (long long)width);
+  return RIP_OK;
+}
+
+}  // namespace
+
+int32_t check_matrix(const void* p, const char* what, int32_t dtype, int64_t rows, int64_t width,
+                     int64_t ld) {
+  if (!known_dtype(dtype)) return fail(RIP_E_UNSUPPORTED, "%s: unknown dtype %d", what, dtype);
+  if (rows < 0 || width < 0 || ld < width)
+    return fail(RIP_E_INVAL, "%s: %lld rows of %lld with row stride %lld", what, (long long)rows,
+                (long long)width, (long long)ld);
+  if (rows && width && !p) return fail(RIP_E_INVAL, "%s is NULL", what);
+  if (reinterpret_cast<uintptr_t>(p) % elem_bytes(dtype))
+    return fail(RIP_E_ALIGN, "%s = %p is not aligned to its type", what, p);
+  return RIP_OK;
+}
+
+}  // namespace rip
+
+using namespace rip;
+
+extern "C" int32_t rip_embed_lookup(const void* table, int32_t table_dtype, int64_t vocab,
+                                    int64_t width, int64_t ld_table, const void* ids,
+                                    int32_t id_type, int64_t n_tokens, float scale, void* out,
+                                    int32_t out_dtype, int64_t ld_out, void* stream) {
+  clear_error();
+  int32_t rc;
+  if ((rc = check_ids(ids, id_type, n_tokens)) || (rc = check_table(vocab, width)) ||
+      (rc = check_matrix(table, "table", table_dtype, vocab, width, ld_table)) ||
+      (rc = check_matrix(out, "out", out_dtype, n_tokens, width, ld_out)))
+    return rc;
+  if (overlap(out, span(out_dtype, n_tokens, width, ld_out), table,
+              span(table_dtype, vocab, width, ld_table)) ||
+      overlap(out, span(out_dtype, n_tokens, width, ld_out), ids,
+              n_tokens * (id_type == RIP_INT64 ? 8 : 4)))
+    return fail(RIP_E_OVERLAP, "out overlaps table or ids");
+  if (n_tokens == 0) return RIP_OK;
+  const int64_t per_row = ceil_div(width, kLane);
+  if (n_tokens * per_row >= (int64_t)1 << 31)
+    return fail(RIP_E_UNSUPPORTED, "%lld tokens of width %lld are above the limit",
+                (long long)n_tokens, (long long)width);
+  uint32_t units = (uint32_t)(n_tokens * per_row);
+  FastDiv div = FastDiv::make((uint32_t)per_row);
+  int w = (int)width, wide = id_type == RIP_INT64;
+  void* args[] = {&table, &vocab, &w,     &ld_table, &ids, &wide,
+                  &units, &div,   &scale, &out,      &ld_out};
+  const void* fn =
+      table_dtype == RIP_FP32
+          ? (out_dtype == RIP_FP32 ? (const void*)lookup_kernel<RIP_FP32, RIP_FP32>
+                                   : (const void*)lookup_kernel<RIP_FP32, RIP_BF16>)
+          : (out_dtype == RIP_FP32 ? (const void*)lookup_kernel<RIP_BF16, RIP_FP32>
+                                   : (const void*)lookup_kernel<RIP_BF16, RIP_BF16>);
+  return launch(fn, dim3((uint32_t)ceil_div(units, kLookupBlock)), dim3(kLookupBlock), args, 0,
+                stream, "rip_embed_lookup");
+}
+
+extern "C" int64_t rip_embed_grad_workspace(int64_t n_tokens, int64_t width) {
+  if (n_tokens < 1 || n_tokens > RIP_MAX_TOKENS || width < 1 || width > RIP_MAX_WIDTH) return 0;
+  return grad_plan(n_tokens, width).total;
+}
+
+extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t ld_dout,
+                                  const void* ids, int32_t id_type, int64_t n_tokens, float scale,
+                                  void* grad, int32_t grad_dtype, int64_t vocab, int64_t width,
+                                  int64_t ld_grad, int32_t accumulate, void* workspace,
+                                  int64_t workspace_bytes, void* stream) {
+  clear_error();
+  int32_t rc;
+  if ((rc = check_ids(ids, id_type, n_tokens)) || (rc = check_table(vocab, width)) ||
+      (rc = check_matrix(dout, "dout", dout_dtype, n_tokens, width, ld_dout)) ||
+      (rc = check_matrix(grad, "grad", grad_dtype, vocab, width, ld_grad)))
+    return rc;
+  const int64_t grad_span = span(grad_dtype, vocab, width, ld_grad);
+  const int64_t ids_span = n_tokens * (id_type == RIP_INT64 ? 8 : 4);
+  if (overlap(grad, grad_span, dout, span(dout_dtype, n_tokens, width, ld_dout)) ||
+      overlap(grad, grad_span, ids, ids_span))
+    return fail(RIP_E_OVERLAP, "grad overlaps dout or ids");
+  const int64_t need = rip_embed_grad_workspace(n_tokens, width);
+  if (need > 0) {
+    if (!workspace || workspace_bytes < need)
+      return fail(RIP_E_INVAL, "workspace of %lld bytes, %lld needed", (long long)workspace_bytes,
+                  (long long)need);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16)
+      return fail(RIP_E_ALIGN, "workspace = %p is not 16-byte aligned", workspace);
+    if (overlap(workspace, need, grad, grad_span) || overlap(workspace, need, ids, ids_span) ||
+        overlap(workspace, need, dout, span(dout_dtype, n_tokens, width, ld_dout)))
+      return fail(RIP_E_OVERLAP, "workspace overlaps another buffer");
+  }
+  if (n_tokens == 0 && accumulate) return RIP_OK;
+
+  GradPlan p = grad_plan(n_tokens, width);
+  char* ws = static_cast<char*>(workspace);
+  uint32_t* id_a = (uint32_t*)ws;
+  uint32_t* pos_a = (uint32_t*)(ws + p.id_bytes);
+  uint32_t* id_b = p.chunks > 1 ? (uint32_t*)(ws + 2 * p.id_bytes) : id_a;
+  uint32_t* pos_b = p.chunks > 1 ? (uint32_t*)(ws + 3 * p.id_bytes) : pos_a;
+  float* partial = (float*)(ws + p.id_bytes * (p.chunks > 1 ? 4 : 2));
+
+  // Keys run to `vocab` itself (ids outside the vocabulary).
+  int key_bits = 1;
+  while (((int64_t)1 << key_bits) <= vocab) ++key_bits;
+  int passes = (key_bits + kMaxDigit - 1) / kMaxDigit;
+  int bits = (key_bits + passes - 1) / passes;
+  int w = (int)width, wide = id_type == RIP_INT64;
+  uint32_t v32 = (uint32_t)vocab;
+  int rows_per_block = (int)(kFillBytes / (width * elem_bytes(grad_dtype)));
+  if (rows_per_block < 1) rows_per_block = 1;
+  const int64_t fill = accumulate ? 0 : ceil_div(vocab, rows_per_block);
+  {
+    void* args[] = {&ids,  &wide,  &n_tokens, &v32, &passes,  &bits,          &p.chunks,
+                    &id_a, &pos_a, &grad,     &w,   &ld_grad, &rows_per_block};
+    const void* fn = grad_dtype == RIP_FP32 ? (const void*)sort_fill_kernel<RIP_FP32>
+                                            : (const void*)sort_fill_kernel<RIP_BF16>;
+    if ((rc = launch(fn, dim3((uint32_t)(p.chunks + fill)), dim3(kSortThreads), args, 0, stream,
+                     "rip_embed_grad: sort")))
+      return rc;
+  }
+  if (n_tokens == 0) return RIP_OK;
+  if (p.chunks > 1) {
+    void* args[] = {&id_a, &pos_a, &n_tokens, &p.chunks, &id_b, &pos_b};
+    if ((rc = launch((const void*)merge_kernel, dim3((uint32_t)ceil_div(n_tokens, 256)), dim3(256),
+                     args, 0, stream, "rip_embed_grad: merge")))
+      return rc;
+  }
+  const uint32_t columns = (uint32_t)ceil_div(width, kColumns);
+  {
+    void* args[] = {&dout,  &ld_dout, &id_b, &pos_b,   &n_tokens,   &v32,    &p.per,
+                    &scale, &grad,    &w,    &ld_grad, &accumulate, &partial};
+    const void* fn =
+        dout_dtype == RIP_FP32
+            ? (grad_dtype == RIP_FP32 ? (const void*)sum_kernel<RIP_FP32, RIP_FP32>
+                                      : (const void*)sum_kernel<RIP_FP32, RIP_BF16>)
+            : (grad_dtype == RIP_FP32 ? (const void*)sum_kernel<RIP_BF16, RIP_FP32>
+                                      : (const void*)sum_kernel<RIP_BF16, RIP_BF16>);
+    if ((rc = launch(fn, dim3((uint32_t)p.waves, columns), dim3(kWave), args, 0, stream,
+                     "rip_embed_grad: sum")))
+      return rc;
+  }
+  if (p.waves < 2) return RIP_OK;
+  void* args[] = {&id_b, &n_tokens, &v32, &p.per,   &p.waves,   &partial,
+                  &scale, &grad,    &w,   &ld_grad, &accumulate};
+  const void* fn = grad_dtype == RIP_FP32 ? (const void*)join_kernel<RIP_FP32>
+                                          : (const void*)join_kernel<RIP_BF16>;
+  return launch(fn, dim3((uint32_t)p.waves, columns), dim3(kWave * kJoinWaves), args, 0, stream,
+                "rip_embed_grad: join");
+}

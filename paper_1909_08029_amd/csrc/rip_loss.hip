@@ -1,0 +1,486 @@
+// Losses over the vocabulary with the gradient of the logits (gfx950): a
+// preference loss over pairs of sequences, and a clipped policy loss with a KL
+// term.  With x a token's row of logits and y its target,
+//
+//   logp = x[y] - log sum_v e^x[v]
+//   d logp / d x[v] = (v == y) - softmax(x)[v]
+//
+// and either loss gives each counted token one number, coef = d loss / d logp,
+// so the gradient's row is coef * ((v == y) - softmax(x)[v]).
+//
+//   1. stats   a row's largest logit and the sum of e^(x - largest), in one pass
+//              (each lane keeps a running pair); few rows are split over several
+//              workgroups, whose pairs the next launch joins
+//   2. pairs / tokens   log-probabilities, the loss and coef
+//   3. grad    one pass over the logits, writing the gradient; rows that do not
+//              count are written as zeros without being read
+//
+// Bound by memory: the logits are read twice and the gradient written once.
+
+#include "rip_ops_common.h"
+
+namespace rip {
+namespace {
+
+constexpr int kWave = 64;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kStep = kThreads * kLane;  // elements of a workgroup's round
+constexpr float kLowest = -3.402823466e38f;
+
+// A row's largest logit and sum of e^(x - top).  sum == 0 only where every
+// logit is -inf (or there is none): then top is the lowest number.
+struct Stat {
+  float top, sum;
+};
+__device__ __forceinline__ float exp_fast(float x) {
+  return __builtin_amdgcn_exp2f(x * 1.44269502f);
+}
+__device__ __forceinline__ Stat join(Stat a, Stat b) {
+  const float top = fmaxf(a.top, b.top);
+  return {top, a.sum * exp_fast(a.top - top) + b.sum * exp_fast(b.top - top)};
+}
+__device__ __forceinline__ void add8(Stat& s, const float (&f)[kLane]) {
+  float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])),
+                    fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
+  top = fmaxf(top, s.top);
+  float sum = s.sum * exp_fast(s.top - top);
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) sum += exp_fast(f[j] - top);
+  s = {top, sum};
+}
+// The workgroup's joined pair, in every thread.
+__device__ __forceinline__ Stat join_block(Stat s, Stat* shared) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) s = join(s, {__shfl_xor(s.top, o), __shfl_xor(s.sum, o)});
+  if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = s;
+  __syncthreads();
+  Stat r = shared[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) r = join(r, shared[w]);
+  return r;
+}
+
+struct Rows {
+  int64_t n, ld;
+  int vocab;
+  int splits;   // workgroups of a row
+  int columns;  // of a workgroup, a multiple of kLane
+  const void* targets;
+  int wide;
+};
+__device__ __forceinline__ bool counts(const Rows& r, int64_t t, int64_t* target) {
+  *target = load_id(r.targets, r.wide, t);
+  return *target >= 0 && *target < r.vocab;
+}
+
+// What the grad launch needs of a token: gradient[v] = scale * e^(x[v] - top),
+// plus coef at the target.
+struct Token {
+  float top, scale, coef;
+  int target;
+};
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
+                                                         const typename Elem<DT>::T* logits,
+                                                         Stat* stat, Token* token, float* logp) {
+  __shared__ Stat shared[kWaves];
+  const int64_t t = blockIdx.x / r.splits;
+  const int split = blockIdx.x - (uint32_t)t * r.splits;
+  if (split == 0 && threadIdx.x == 0) {  // stands for tokens that do not count
+    token[t] = {0.0f, 0.0f, 0.0f, -1};
+    if (logp) logp[t] = 0.0f;
+  }
+  int64_t target;
+  if (!counts(r, t, &target)) return;
+  const int end = min(r.vocab, (split + 1) * r.columns);
+  const typename Elem<DT>::T* row = logits + t * r.ld;
+  Stat s{kLowest, 0.0f};
+  int c = split * r.columns + threadIdx.x * kLane;
+  for (; c + 3 * kStep + kLane <= end; c += 4 * kStep) {
+    float f[4][kLane];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) Elem<DT>::load8(row + c + u * kStep, f[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) add8(s, f[u]);
+  }
+  for (; c < end; c += kStep) {
+    float f[kLane];
+    if (c + kLane <= end) {
+      Elem<DT>::load8(row + c, f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j)
+        f[j] = c + j < end ? Elem<DT>::load(row + c + j) : -__builtin_huge_valf();
+    }
+    add8(s, f);
+  }
+  s = join_block(s, shared);
+  if (threadIdx.x == 0) stat[blockIdx.x] = s;
+}
+
+// log-probability of a counted token's target; false where the row has no
+// logit above -inf, which leaves the token out.
+template <int DT>
+__device__ __forceinline__ bool token_logp(const Rows& r, const typename Elem<DT>::T* logits,
+                                           const Stat* stat, int64_t t, int64_t target, Stat* s,
+                                           float* logp) {
+  *s = stat[t * r.splits];
+  for (int i = 1; i < r.splits; ++i) *s = join(*s, stat[t * r.splits + i]);
+  if (s->sum == 0.0f) return false;
+  *logp = Elem<DT>::load(logits + t * r.ld + target) - s->top - logf(s->sum);
+  return true;
+}
+
+__device__ __forceinline__ double sum_block(double x, double* shared) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = x;
+  __syncthreads();
+  double s = shared[0];
+  for (int w = 1; w < kWaves; ++w) s += shared[w];
+  return s;
+}
+
+__device__ __forceinline__ float log_sigmoid(float z) {
+  return fminf(z, 0.0f) - log1pf(expf(-fabsf(z)));
+}
+
+// One workgroup a pair.  The sums over a sequence are held in 64 bits: they run
+// to thousands while the loss depends on differences of a few.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void pairs_kernel(
+    Rows r, const typename Elem<DT>::T* logits, const Stat* stat, const int32_t* offsets, int pairs,
+    const float* ref, float beta, float smoothing, float grad_scale, float* seq_logp, Token* token,
+    float* logp, double* pair_loss) {
+  __shared__ double shared[kWaves];
+  int64_t at[3];
+  for (int i = 0; i < 3; ++i) {  // within the tokens and ascending, whatever the offsets say
+    int64_t o = offsets[2 * blockIdx.x + i];
+    o = o < 0 ? 0 : o > r.n ? r.n : o;
+    at[i] = i && o < at[i - 1] ? at[i - 1] : o;
+  }
+  double margin[2];
+  for (int q = 0; q < 2; ++q) {
+    double sum = 0.0;
+    for (int64_t t = at[q] + threadIdx.x; t < at[q + 1]; t += kThreads) {
+      int64_t target;
+      Stat s;
+      float lp;
+      if (!counts(r, t, &target) || !token_logp<DT>(r, logits, stat, t, target, &s, &lp)) continue;
+      sum += lp;
+      if (logp) logp[t] = lp;
+      token[t] = {s.top, 1.0f / s.sum, 1.0f, (int)target};
+    }
+    sum = sum_block(sum, shared);
+    const int q2 = 2 * blockIdx.x + q;
+    margin[q] = sum - (double)ref[q2];
+    if (threadIdx.x == 0) seq_logp[q2] = (float)sum;
+  }
+  const float z = (float)((double)beta * (margin[0] - margin[1]));
+  const float good = expf(log_sigmoid(z)), bad = expf(log_sigmoid(-z));
+  const float coef =
+      grad_scale * beta / (float)pairs * (smoothing * good - (1.0f - smoothing) * bad);
+  if (threadIdx.x == 0) {  // a term of weight 0 stays out, also where it is infinite
+    double l = 0.0;
+    if (smoothing < 1.0f) l -= (1.0 - smoothing) * log_sigmoid(z);
+    if (smoothing > 0.0f) l -= (double)smoothing * log_sigmoid(-z);
+    pair_loss[blockIdx.x] = l / pairs;
+  }
+  for (int q = 0; q < 2; ++q)
+    for (int64_t t = at[q] + threadIdx.x; t < at[q + 1]; t += kThreads) {
+      Token k = token[t];
+      if (k.target < 0) continue;
+      k.coef = q ? -coef : coef;
+      k.scale *= -k.coef;
+      token[t] = k;
+    }
+}
+
+struct Policy {
+  const float *old_logp, *advantage, *weight, *ref_logp;
+  float low, high, kl, grad_scale;
+};
+
+// A counted token's loss and its derivative by logp.  ratio * A is flat where
+// the clipped value is the smaller one; a NaN stays on the other branch.
+__device__ __forceinline__ float policy_token(const Policy& p, int64_t t, int64_t n, float lp,
+                                              float* coef) {
+  const float a = p.advantage[t], w = p.weight ? p.weight[t] : 1.0f / (float)n;
+  const float ratio = expf(lp - p.old_logp[t]);
+  const float bound = fminf(fmaxf(ratio, p.low), p.high) * a;
+  const bool flat = ratio * a > bound;
+  float loss = flat ? -bound : -(ratio * a), slope = flat ? 0.0f : -(ratio * a);
+  if (p.ref_logp) {
+    const float d = p.ref_logp[t] - lp, e = expf(d);
+    loss += p.kl * (e - d - 1.0f);
+    slope += p.kl * (1.0f - e);
+  }
+  *coef = w * slope * p.grad_scale;
+  return w * loss;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void tokens_kernel(Rows r,
+                                                          const typename Elem<DT>::T* logits,
+                                                          const Stat* stat, Policy p, Token* token,
+                                                          float* logp, double* part_loss) {
+  __shared__ double shared[kWaves];
+  const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  double loss = 0.0;
+  int64_t target;
+  Stat s;
+  float lp;
+  if (t < r.n && counts(r, t, &target) && token_logp<DT>(r, logits, stat, t, target, &s, &lp)) {
+    float coef;
+    loss = policy_token(p, t, r.n, lp, &coef);
+    if (logp) logp[t] = lp;
+    token[t] = {s.top, -coef / s.sum, coef, (int)target};
+  }
+  loss = sum_block(loss, shared);
+  if (threadIdx.x == 0) part_loss[blockIdx.x] = loss;
+}
+
+// The loss: the sum of `parts` numbers, by one workgroup.
+__device__ __forceinline__ void total_loss(const double* part, int parts, float* loss,
+                                           double* shared) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += kThreads) sum += part[i];
+  sum = sum_block(sum, shared);
+  if (threadIdx.x == 0) *loss = (float)sum;
+}
+__global__ __launch_bounds__(kThreads) void total_kernel(const double* part, int parts,
+                                                         float* loss) {
+  __shared__ double shared[kWaves];
+  total_loss(part, parts, loss, shared);
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
+                                                        const typename Elem<DT>::T* logits,
+                                                        const Token* token,
+                                                        typename Elem<DT>::T* grad, int64_t ld_grad,
+                                                        const double* part, int parts,
+                                                        float* loss) {
+  __shared__ double shared[kWaves];
+  if (blockIdx.x == 0) total_loss(part, parts, loss, shared);
+  const int64_t t = blockIdx.x / r.splits;
+  const int split = blockIdx.x - (uint32_t)t * r.splits;
+  const int end = min(r.vocab, (split + 1) * r.columns);
+  const typename Elem<DT>::T* row = logits + t * r.ld;
+  typename Elem<DT>::T* out = grad + t * ld_grad;
+  const Token k = token[t];
+  int c = split * r.columns + threadIdx.x * kLane;
+  if (k.coef == 0.0f) {
+    const float zero[kLane] = {};
+    for (; c < end; c += kStep) store_unit<DT>(out, c, end, zero);
+    return;
+  }
+  for (; c < end; c += kStep) {
+    float f[kLane];
+    load_unit<DT>(row, c, end, f);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      f[j] = k.scale * exp_acc(f[j] - k.top);
+      if (c + j == k.target) f[j] += k.coef;
+    }
+    store_unit<DT>(out, c, end, f);
+  }
+}
+
+// Workgroups of a row: enough to fill the card where there are few rows, each
+// with a round of its threads at least.
+Rows make_rows(int64_t n, int64_t vocab, int64_t ld, const void* targets, int32_t id_type) {
+  Rows r{n, ld, (int)vocab, 1, 0, targets, id_type == RIP_INT64};
+  const int64_t most = ceil_div(vocab, kStep);
+  int64_t splits = n > 0 ? 2048 / n : 1;
+  splits = splits < 1 ? 1 : splits > most ? most : splits;
+  r.columns = (int)(ceil_div(ceil_div(vocab, splits), kLane) * kLane);
+  r.splits = (int)ceil_div(vocab, r.columns);
+  return r;
+}
+
+struct Work {
+  Stat* stat;
+  Token* token;
+  double* part;
+  int64_t bytes;
+};
+Work make_work(const Rows& r, int64_t parts, void* workspace) {
+  char* p = static_cast<char*>(workspace);
+  Work w{};
+  w.stat = (Stat*)p;
+  int64_t at = ceil_div(r.n * r.splits * (int64_t)sizeof(Stat), 256) * 256;
+  w.token = (Token*)(p + at);
+  at += ceil_div(r.n * (int64_t)sizeof(Token), 256) * 256;
+  w.part = (double*)(p + at);
+  w.bytes = at + (parts + 1) * (int64_t)sizeof(double);
+  return w;
+}
+int64_t policy_parts(int64_t n) { return ceil_div(n, kThreads); }
+
+int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t ld, int64_t n,
+                   int64_t vocab, const void* targets, int32_t id_type, const void* loss,
+                   const void* grad, int64_t ld_grad, const void* workspace,
+                   int64_t workspace_bytes, int64_t need) {
+  int32_t rc;
+  if (vocab < 1) return fail(RIP_E_INVAL, "%s: vocab %lld < 1", name, (long long)vocab);
+  if (vocab > RIP_MAX_WIDTH || n > RIP_MAX_TOKENS)
+    return fail(RIP_E_UNSUPPORTED, "%s: %lld tokens of vocabulary %lld are above the limit", name,
+                (long long)n, (long long)vocab);
+  if ((rc = check_matrix(logits, "logits", dtype, n, vocab, ld))) return rc;
+  if (grad && (rc = check_matrix(grad, "grad", dtype, n, vocab, ld_grad))) return rc;
+  if (id_type != RIP_INT32 && id_type != RIP_INT64)
+    return fail(RIP_E_UNSUPPORTED, "%s: unknown id type %d", name, id_type);
+  const int id_bytes = id_type == RIP_INT64 ? 8 : 4;
+  if (n && !targets) return fail(RIP_E_INVAL, "%s: targets is NULL", name);
+  if (reinterpret_cast<uintptr_t>(targets) % id_bytes)
+    return fail(RIP_E_ALIGN, "%s: targets = %p is not aligned to its type", name, targets);
+  if (!loss) return fail(RIP_E_INVAL, "%s: loss is NULL", name);
+  if (!workspace || workspace_bytes < need)
+    return fail(RIP_E_INVAL, "%s: workspace of %lld bytes, %lld needed", name,
+                (long long)workspace_bytes, (long long)need);
+  if (reinterpret_cast<uintptr_t>(workspace) % 16)
+    return fail(RIP_E_ALIGN, "%s: workspace = %p is not 16-byte aligned", name, workspace);
+  const int64_t ls = span(dtype, n, vocab, ld);
+  if (grad) {
+    const int64_t gs = span(dtype, n, vocab, ld_grad);
+    if (overlap(grad, gs, logits, ls) && !(grad == logits && ld == ld_grad))
+      return fail(RIP_E_OVERLAP, "%s: grad overlaps logits without being the same matrix", name);
+    if (overlap(grad, gs, targets, n * id_bytes) || overlap(grad, gs, workspace, need))
+      return fail(RIP_E_OVERLAP, "%s: grad overlaps targets or workspace", name);
+  }
+  if (overlap(workspace, need, logits, ls) || overlap(workspace, need, targets, n * id_bytes))
+    return fail(RIP_E_OVERLAP, "%s: workspace overlaps logits or targets", name);
+  return RIP_OK;
+}
+
+template <int DT>
+int32_t run_stats(Rows& r, const void* logits, Work& w, float* logp, void* stream) {
+  if (r.n == 0) return RIP_OK;
+  void* args[] = {&r, &logits, &w.stat, &w.token, &logp};
+  return launch((const void*)stats_kernel<DT>, dim3((uint32_t)(r.n * r.splits)), dim3(kThreads),
+                args, 0, stream, "loss: stats");
+}
+template <int DT>
+int32_t run_grad(Rows& r, const void* logits, Work& w, void* grad, int64_t ld_grad, int parts,
+                 float* loss, void* stream) {
+  if (!grad || r.n == 0) {
+    void* args[] = {&w.part, &parts, &loss};
+    return launch((const void*)total_kernel, dim3(1), dim3(kThreads), args, 0, stream,
+                  "loss: total");
+  }
+  void* args[] = {&r, &logits, &w.token, &grad, &ld_grad, &w.part, &parts, &loss};
+  return launch((const void*)grad_kernel<DT>, dim3((uint32_t)(r.n * r.splits)), dim3(kThreads),
+                args, 0, stream, "loss: grad");
+}
+
+template <int DT>
+int32_t run_pref(Rows r, const void* logits, const int32_t* offsets, int pairs, const float* ref,
+                 float beta, float smoothing, float grad_scale, float* loss, float* seq_logp,
+                 float* logp, void* grad, int64_t ld_grad, void* workspace, void* stream) {
+  Work w = make_work(r, pairs, workspace);
+  int32_t rc;
+  if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
+  void* args[] = {&r,    &logits,    &w.stat,     &offsets,  &pairs,   &ref,  &beta,
+                  &smoothing, &grad_scale, &seq_logp, &w.token, &logp, &w.part};
+  if ((rc = launch((const void*)pairs_kernel<DT>, dim3((uint32_t)pairs), dim3(kThreads), args, 0,
+                   stream, "rip_pref_loss: pairs")))
+    return rc;
+  return run_grad<DT>(r, logits, w, grad, ld_grad, pairs, loss, stream);
+}
+
+template <int DT>
+int32_t run_policy(Rows r, const void* logits, Policy p, float* loss, float* logp, void* grad,
+                   int64_t ld_grad, void* workspace, void* stream) {
+  int parts = (int)policy_parts(r.n);
+  Work w = make_work(r, parts, workspace);
+  int32_t rc;
+  if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
+  if (r.n) {
+    void* args[] = {&r, &logits, &w.stat, &p, &w.token, &logp, &w.part};
+    if ((rc = launch((const void*)tokens_kernel<DT>, dim3((uint32_t)parts), dim3(kThreads), args, 0,
+                     stream, "rip_policy_loss: tokens")))
+      return rc;
+  }
+  return run_grad<DT>(r, logits, w, grad, ld_grad, parts, loss, stream);
+}
+
+}  // namespace
+}  // namespace rip
+
+using namespace rip;
+
+extern "C" int64_t rip_pref_loss_workspace(int64_t n_tokens, int64_t vocab, int32_t n_pairs) {
+  if (n_tokens < 0 || n_tokens > RIP_MAX_TOKENS || vocab < 1 || vocab > RIP_MAX_WIDTH ||
+      n_pairs < 0 || n_pairs > RIP_MAX_PAIRS)
+    return 0;
+  return make_work(make_rows(n_tokens, vocab, vocab, nullptr, 0), n_pairs, nullptr).bytes;
+}
+extern "C" int64_t rip_policy_loss_workspace(int64_t n_tokens, int64_t vocab) {
+  if (n_tokens < 0 || n_tokens > RIP_MAX_TOKENS || vocab < 1 || vocab > RIP_MAX_WIDTH) return 0;
+  return make_work(make_rows(n_tokens, vocab, vocab, nullptr, 0), policy_parts(n_tokens), nullptr)
+      .bytes;
+}
+
+extern "C" int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,
+                                 int64_t vocab, const void* targets, int32_t id_type,
+                                 const int32_t* seq_offsets, int32_t n_pairs,
+                                 const float* ref_logp, float beta, float smoothing,
+                                 float grad_scale, float* loss, float* seq_logp, float* logp,
+                                 void* grad, int64_t ld_grad, void* workspace,
+                                 int64_t workspace_bytes, void* stream) {
+  clear_error();
+  if (n_pairs < 1) return fail(RIP_E_INVAL, "rip_pref_loss: n_pairs %d < 1", n_pairs);
+  if (n_pairs > RIP_MAX_PAIRS)
+    return fail(RIP_E_UNSUPPORTED, "rip_pref_loss: n_pairs %d > %d", n_pairs, RIP_MAX_PAIRS);
+  int32_t rc;
+  if ((rc = check_loss("rip_pref_loss", logits, dtype, ld, n_tokens, vocab, targets, id_type, loss,
+                       grad, ld_grad, workspace, workspace_bytes,
+                       rip_pref_loss_workspace(n_tokens, vocab, n_pairs))))
+    return rc;
+  if (!seq_offsets || !ref_logp || !seq_logp)
+    return fail(RIP_E_INVAL, "rip_pref_loss: seq_offsets, ref_logp or seq_logp is NULL");
+  if (!(smoothing >= 0.0f && smoothing <= 1.0f))
+    return fail(RIP_E_INVAL, "rip_pref_loss: smoothing %g is not in 0..1", (double)smoothing);
+  if (!(beta == beta) || !(grad_scale == grad_scale))
+    return fail(RIP_E_INVAL, "rip_pref_loss: beta or grad_scale is NaN");
+  Rows r = make_rows(n_tokens, vocab, ld, targets, id_type);
+  return dtype == RIP_FP32
+             ? run_pref<RIP_FP32>(r, logits, seq_offsets, n_pairs, ref_logp, beta, smoothing,
+                                  grad_scale, loss, seq_logp, logp, grad, ld_grad, workspace, stream)
+             : run_pref<RIP_BF16>(r, logits, seq_offsets, n_pairs, ref_logp, beta, smoothing,
+                                  grad_scale, loss, seq_logp, logp, grad, ld_grad, workspace,
+                                  stream);
+}
+
+extern "C" int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,
+                                   int64_t vocab, const void* targets, int32_t id_type,
+                                   const float* old_logp, const float* advantage,
+                                   const float* weight, const float* ref_logp, float clip_low,
+                                   float clip_high, float kl, float grad_scale, float* loss,
+                                   float* logp, void* grad, int64_t ld_grad, void* workspace,
+                                   int64_t workspace_bytes, void* stream) {
+  clear_error();
+  int32_t rc;
+  if (n_tokens < 0) return fail(RIP_E_INVAL, "rip_policy_loss: n_tokens %lld < 0", (long long)n_tokens);
+  if ((rc = check_loss("rip_policy_loss", logits, dtype, ld, n_tokens, vocab, targets, id_type,
+                       loss, grad, ld_grad, workspace, workspace_bytes,
+                       rip_policy_loss_workspace(n_tokens, vocab))))
+    return rc;
+  if (n_tokens && (!old_logp || !advantage))
+    return fail(RIP_E_INVAL, "rip_policy_loss: old_logp or advantage is NULL");
+  if (kl != 0.0f && n_tokens && !ref_logp)
+    return fail(RIP_E_INVAL, "rip_policy_loss: a KL term needs ref_logp");
+  if (!(clip_low >= 0.0f && clip_low <= 1.0f && clip_high >= 0.0f))
+    return fail(RIP_E_INVAL, "rip_policy_loss: clip_low %g is not in 0..1 or clip_high %g < 0",
+                (double)clip_low, (double)clip_high);
+  if (!(kl == kl) || !(grad_scale == grad_scale))
+    return fail(RIP_E_INVAL, "rip_policy_loss: kl or grad_scale is NaN");
+  Rows r = make_rows(n_tokens, vocab, ld, targets, id_type);
+  Policy p{old_logp,         advantage,         weight, kl != 0.0f ? ref_logp : nullptr,
+           1.0f - clip_low, 1.0f + clip_high, kl,     grad_scale};
+  return dtype == RIP_FP32 ? run_policy<RIP_FP32>(r, logits, p, loss, logp, grad, ld_grad, workspace, stream)
+                           : run_policy<RIP_BF16>(r, logits, p, loss, logp, grad, ld_grad, workspace, stream);
+}

@@ -1,0 +1,309 @@
+"""Preference and policy losses and the gradient of their logits against plain
+64-bit forms.
+
+Tolerances.  A row's sum of exponentials is fp32, a lane adding vocab / 256 terms
+at least: a log-probability is good to
+    delta = (vocab / 256 + 64) 2^-24 + 2^-22 max |x|.
+Sequence sums are 64-bit: count * delta.  A loss's derivative by logp then has a
+relative error of beta * that, or for the policy's ratio of delta, and 2^-20 for
+its own few operations; a softmax has the row sum's error, 2^-14 at the
+vocabularies here, on the magnitudes of its two terms.
+"""
+import numpy as np
+import pytest
+
+import train_ops_ref as ref
+from train_ops_ref import BF16, F32
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # tokens, vocab, pad, offset, wide ids
+    (1, 1, 0, 0, True), (2, 3, 0, 0, False), (4, 7, 1, 1, True), (9, 64, 0, 3, True),
+    (40, 1031, 0, 0, False), (101, 333, 7, 1, True), (3, 70001, 0, 0, True),
+    (17, 20000, 64, 5, False), (600, 97, 0, 0, True), (2500, 40, 0, 0, True)]
+
+
+def make(rng, tokens, vocab, pad, offset, wide, dtype, special=True):
+    """Logits, targets (some out of range), as arrays of what the device holds."""
+    import torch
+    x = rng.standard_normal((tokens, vocab)) * 3
+    targets = rng.integers(0, vocab, tokens)
+    targets[rng.random(tokens) < 0.2] = -100
+    if special and tokens >= 9:
+        x[1] = -np.inf                                # nothing left
+        x[2, : vocab // 2] = -np.inf                  # half of the vocabulary masked
+        targets[2] = vocab - 1
+        x[3] = float(torch.finfo(dtype).min)          # the type's lowest everywhere
+        targets[3] = 0
+        x[4], targets[4] = np.nan, -1                 # a token that does not count
+        x[5], targets[5] = np.inf, vocab              # another
+        x[6, 0] = float(torch.finfo(dtype).min)
+    dev, _ = ref.device_matrix(x, dtype, pad, offset)
+    t = torch.from_numpy(targets.astype(np.int64 if wide else np.int32)).cuda()
+    return dev, t, ref.host(dev), targets
+
+
+def offsets_of(rng, tokens, pairs):
+    cuts = np.sort(rng.integers(0, tokens + 1, 2 * pairs + 1))
+    return cuts.astype(np.int32)
+
+
+def delta(x, vocab):
+    finite = x[np.isfinite(x) & (np.abs(x) < 1e30)]
+    return (vocab / 256 + 64) * 2.0 ** -24 + 2.0 ** -22 * (np.abs(finite).max() if finite.size else 0)
+
+
+def check_grad(got, want, targets, rel, dtype):
+    """want: dict of the plain form; rel: relative error of coef."""
+    hot = np.zeros(want["grad"].shape)
+    on = np.flatnonzero(want["counted"])
+    hot[on, targets[on]] = 1
+    tol = np.abs(want["coef"])[:, None] * (want["soft"] + hot) * (2.0 ** -14 + rel)
+    tol = tol + ref.HALF_ULP[dtype] * np.abs(want["grad"]) + 1e-37
+    ref.close(got, want["grad"], tol, "grad")
+    assert (got[~want["counted"]] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_pref_loss(shape, dtype):
+    import torch
+    import paper_1909_08029_amd as rip
+    tokens, vocab, pad, offset, wide = shape
+    rng = np.random.default_rng(tokens * 31 + vocab)
+    x, t, xh, targets = make(rng, *shape, dtype)
+    for pairs, beta, smoothing in ((1, 0.1, 0.0), (3, 0.5, 0.2)):
+        offsets = offsets_of(rng, tokens, pairs)
+        logp = ref.log_softmax_at(xh, targets)[0]
+        seq = np.array([logp[a:b].sum() for a, b in zip(offsets, offsets[1:])])
+        r = (seq + rng.standard_normal(2 * pairs) * 3).astype(np.float32)
+        scale = float(np.float32(0.7))
+        beta, smoothing = float(np.float32(beta)), float(np.float32(smoothing))
+        want = ref.pref_loss(xh, targets, offsets, r.astype(np.float64), beta, smoothing, scale)
+        od, rd = torch.from_numpy(offsets).cuda(), torch.from_numpy(r).cuda()
+        grad, buf = ref.device_matrix(np.zeros((tokens, vocab)), dtype, pad, offset)
+        loss, got_seq, got_logp = rip.rip_pref_loss(x, t, od, rd, beta, smoothing, grad=grad,
+                                                    grad_scale=scale)
+        d = delta(xh, vocab)
+        ref.close(ref.host(got_logp), want["logp"], d + 2.0 ** -23 * np.abs(want["logp"]), "logp")
+        count = np.diff(offsets) * d
+        ref.close(ref.host(got_seq), want["seq"], count + 2.0 ** -23 * np.abs(want["seq"]), "seq")
+        dz = beta * 2 * count.sum()
+        ref.close(ref.host(loss), want["loss"], dz + 2.0 ** -20 * (1 + abs(want["loss"])), "loss")
+        check_grad(ref.host(grad), want, targets, dz + 2.0 ** -20, dtype)
+        assert ref.guards_intact(grad, buf)
+        alone = rip.rip_pref_loss(x, t, od, rd, beta, smoothing)
+        assert torch.equal(alone[0], loss) and torch.equal(alone[1], got_seq)
+        own = x.clone()
+        if own.stride() == grad.stride():
+            rip.rip_pref_loss(own, t, od, rd, beta, smoothing, grad=own, grad_scale=scale)
+            assert torch.equal(own, grad)
+            rip.rip_pref_loss(x, t, od, rd, beta, smoothing, grad=own, grad_scale=scale)
+            assert torch.equal(own, grad)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_policy_loss(shape, dtype):
+    import torch
+    import paper_1909_08029_amd as rip
+    tokens, vocab, pad, offset, wide = shape
+    rng = np.random.default_rng(tokens * 17 + vocab)
+    x, t, xh, targets = make(rng, *shape, dtype)
+    logp = ref.log_softmax_at(xh, targets)[0]
+    # ratios well away from the clip's ends
+    ratio = rng.choice([0.4, 0.7, 0.9, 1.0, 1.1, 1.35, 2.0], tokens)
+    old = (logp - np.log(ratio)).astype(np.float32)
+    adv = rng.standard_normal(tokens).astype(np.float32)
+    adv[rng.random(tokens) < 0.1] = 0
+    weight = rng.random(tokens).astype(np.float32)
+    refp = (logp + rng.standard_normal(tokens) * 0.5).astype(np.float32)
+    cuda = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    f = lambda v: float(np.float32(v))  # noqa: E731
+    d = delta(xh, vocab)
+    for use_w, kl, low, high in ((True, f(0.1), f(0.2), f(0.28)), (False, 0.0, 1.0, 0.0)):
+        w = weight.astype(np.float64) if use_w else np.full(tokens, 1.0 / tokens)
+        if not use_w:   # clipped to 0..1: ratios of exactly 1 lie at an end, where the sides differ
+            old = np.where(ratio == 1.0, old - np.float32(0.25), old).astype(np.float32)
+        want = ref.policy_loss(xh, targets, old.astype(np.float64), adv.astype(np.float64), w,
+                               refp.astype(np.float64), low, high, kl)
+        grad, buf = ref.device_matrix(np.zeros((tokens, vocab)), dtype, pad, offset)
+        args = dict(weight=cuda(weight) if use_w else None, ref_logp=cuda(refp) if kl else None,
+                    clip_low=low, clip_high=high, kl=kl)
+        loss, got = rip.rip_policy_loss(x, t, cuda(old), cuda(adv), grad=grad, **args)
+        ref.close(ref.host(got), want["logp"], d + 2.0 ** -23 * np.abs(want["logp"]), "logp")
+        r = np.exp(want["logp"] - old)
+        e = np.exp(refp - want["logp"]) if kl else 0 * r
+        size = np.abs(w) * (r * np.abs(adv) + kl * (e + np.abs(refp - want["logp"]) + 1))
+        err = size * (4 * d + 2.0 ** -20)
+        ref.close(ref.host(loss), want["loss"], err[want["counted"]].sum() + 2.0 ** -22, "loss")
+        # coef's own error, relative to it where it is not zero
+        rel = np.divide(err, np.abs(want["coef"]), out=np.zeros_like(err), where=want["coef"] != 0)
+        check_grad(ref.host(grad), want, targets, rel[:, None], dtype)
+        assert ref.guards_intact(grad, buf)
+        alone = rip.rip_policy_loss(x, t, cuda(old), cuda(adv), **args)
+        assert torch.equal(alone[1], got)
+        ref.close(ref.host(alone[0]), want["loss"], err[want["counted"]].sum() + 2.0 ** -22, "loss")
+        again = torch.full_like(grad, 5.0)
+        loss2, _ = rip.rip_policy_loss(x, t, cuda(old), cuda(adv), grad=again, **args)
+        assert torch.equal(again, grad) and torch.equal(loss2, loss)
+        own = x.clone()
+        rip.rip_policy_loss(own, t, cuda(old), cuda(adv), grad=own, **args)
+        assert torch.equal(own, grad)
+
+
+@pytest.mark.parametrize("which", ["pref", "policy"])
+def test_gradient_by_differences(which):
+    """The loss along a direction in the logits: central differences with step
+    2^-6, in fp32 (truncation: the step's square times a third derivative below
+    one; the loss's rounding over the step)."""
+    import torch
+    import paper_1909_08029_amd as rip
+    torch.manual_seed(8)
+    tokens, vocab, e = 24, 50, 2.0 ** -6
+    x = torch.randn(tokens, vocab, device="cuda")
+    t = torch.randint(0, vocab, (tokens,), device="cuda")
+    t[::5] = -100
+    logp = torch.log_softmax(x, 1).gather(1, t.clamp(min=0)[:, None])[:, 0]
+    if which == "pref":
+        offsets = torch.tensor([0, 5, 9, 9, 24], dtype=torch.int32, device="cuda")
+        refl = torch.randn(4, device="cuda") * 3 - 8
+        call = lambda z, g=None: rip.rip_pref_loss(z, t, offsets, refl, 0.5, 0.1, grad=g)[0]  # noqa: E731
+    else:
+        old = logp + 0.02 * torch.randn(tokens, device="cuda")   # stays inside the clip
+        refp = logp + 0.3 * torch.randn(tokens, device="cuda")
+        adv, w = torch.randn(tokens, device="cuda"), torch.rand(tokens, device="cuda")
+        call = lambda z, g=None: rip.rip_policy_loss(z, t, old, adv, w, refp, 0.3, 0.3, 0.2, grad=g)[0]  # noqa: E731
+    grad = torch.empty_like(x)
+    call(x, grad)
+    for _ in range(4):
+        d = torch.randn_like(x)
+        d /= d.abs().max()
+        quotient = float(call(x + e * d).double() - call(x - e * d).double()) / (2 * e)
+        exact = float((grad.double() * d.double()).sum())
+        assert abs(quotient - exact) <= tokens * e * e + 2.0 ** -20 / e
+
+
+def test_pairs_with_an_impossible_token():
+    import torch
+    import paper_1909_08029_amd as rip
+    x = torch.zeros(4, 6, device="cuda")
+    t = torch.zeros(4, dtype=torch.int64, device="cuda")
+    offsets = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    z = torch.zeros(2, device="cuda")
+    for row, loss in ((3, 0.0), (1, float("inf"))):   # in the rejected, in the chosen
+        y = x.clone()
+        y[row, 0] = float("-inf")
+        g = torch.empty_like(y)
+        got, seq, _ = rip.rip_pref_loss(y, t, offsets, z, 1.0, 0.0, grad=g)
+        assert got == loss and seq[row // 2] == float("-inf")
+        assert torch.isfinite(g).all()
+        assert (g == 0).all() if row == 3 else bool((g[0, 0] < 0) and (g[1, 0] == -1))
+
+
+def test_a_nan_stays_in_its_pair():
+    import torch
+    import paper_1909_08029_amd as rip
+    torch.manual_seed(2)
+    for bad in (float("nan"), float("inf")):
+        x = torch.randn(12, 40, device="cuda")
+        x[1, 7] = bad
+        t = torch.randint(0, 40, (12,), device="cuda")
+        offsets = torch.tensor([0, 3, 6, 9, 12], dtype=torch.int32, device="cuda")
+        g = torch.empty_like(x)
+        loss, seq, logp = rip.rip_pref_loss(x, t, offsets, torch.zeros(4, device="cuda"), grad=g)
+        assert torch.isnan(loss) and torch.isnan(logp[1]) and torch.isfinite(seq[1:]).all()
+        assert torch.isnan(g[:6]).any(1).all() and torch.isfinite(g[6:]).all()
+        zero = torch.zeros(12, device="cuda")
+        rip.rip_policy_loss(x, t, zero - 3, zero + 1, grad=g)
+        assert torch.isnan(g[1]).all() and torch.isfinite(g[[0, *range(2, 12)]]).all()
+
+
+def test_offsets_are_cut_to_fit():
+    """Offsets that leave the tokens or run backwards never reach other memory;
+    tokens outside every sequence do not count."""
+    import torch
+    import paper_1909_08029_amd as rip
+    torch.manual_seed(4)
+    x, t = torch.randn(10, 30, device="cuda"), torch.randint(0, 30, (10,), device="cuda")
+    refl = torch.zeros(2, device="cuda")
+
+    def run(o):
+        g = torch.full_like(x, 3.0)
+        out = rip.rip_pref_loss(x, t, torch.tensor(o, dtype=torch.int32, device="cuda"), refl, grad=g)
+        return [a.clone() for a in (*out, g)]
+    for wild, fit in (([-5, 4, 1000], [0, 4, 10]), ([6, 2, 8], [6, 6, 8]), ([2, 2 ** 31 - 1, 5], [2, 10, 10])):
+        for a, b in zip(run(wild), run(fit)):
+            assert torch.equal(a, b)
+    out = run([3, 5, 8])
+    assert (out[2][[0, 1, 2, 8, 9]] == 0).all() and (out[3][[0, 1, 2, 8, 9]] == 0).all()
+    assert (out[3][3:8] != 0).any(1).all()
+
+
+def test_no_tokens():
+    import torch
+    import paper_1909_08029_amd as rip
+    x = torch.empty(0, 30, device="cuda")
+    t = torch.empty(0, dtype=torch.int64, device="cuda")
+    o = torch.zeros(3, dtype=torch.int32, device="cuda")
+    loss, seq, logp = rip.rip_pref_loss(x, t, o, torch.tensor([1.0, 3.0], device="cuda"), 0.5, grad=x)
+    assert abs(float(loss) - np.log1p(np.exp(-1.0))) < 1e-6 and (seq == 0).all() and logp.numel() == 0
+    f = torch.empty(0, device="cuda")
+    loss, logp = rip.rip_policy_loss(x, t, f, f, grad=x)
+    assert loss == 0 and logp.numel() == 0
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 logits; the tokens that count lie at the end."""
+    import torch
+    import paper_1909_08029_amd as rip
+    tokens, vocab = 33000, 70001
+    x = torch.zeros((tokens, vocab), dtype=BF16, device="cuda")
+    t = torch.full((tokens,), -100, dtype=torch.int32, device="cuda")
+    t[-3:] = torch.tensor([5, 70000, 35000], dtype=torch.int32)
+    x[-3:] = torch.randn(3, vocab, device="cuda")
+    tail = x[-3:].clone()
+    adv, old = torch.ones(tokens, device="cuda"), torch.full((tokens,), -11.0, device="cuda")
+    small = torch.empty_like(tail)
+    w = torch.ones(tokens, device="cuda")
+    want, _ = rip.rip_policy_loss(tail, t[-3:].clone(), old[-3:].clone(), adv[-3:].clone(),
+                                  w[-3:].clone(), grad=small)
+    loss, logp = rip.rip_policy_loss(x, t, old, adv, w, grad=x)
+    assert abs(float(loss) - float(want)) <= 1e-5 * abs(float(want))
+    assert torch.allclose(x[-3:].float(), small.float(), rtol=2 ** -7, atol=0)
+    assert not x[:-3].any() and not logp[:-3].any()
+
+
+def test_refusals():
+    import torch
+    import paper_1909_08029_amd as rip
+    x = torch.zeros(8, 20, device="cuda")
+    t = torch.zeros(8, dtype=torch.int64, device="cuda")
+    o = torch.tensor([0, 4, 8], dtype=torch.int32, device="cuda")
+    r, f = torch.zeros(2, device="cuda"), torch.zeros(8, device="cuda")
+    for call in (lambda: rip.rip_pref_loss(x, t[:7], o, r),
+                 lambda: rip.rip_pref_loss(x, t, o[:2], r),
+                 lambda: rip.rip_pref_loss(x, t, o.long(), r),
+                 lambda: rip.rip_pref_loss(x, t, o, r.double()),
+                 lambda: rip.rip_pref_loss(x, t, o, f),
+                 lambda: rip.rip_pref_loss(x, t, o, r, grad=x.to(BF16)),
+                 lambda: rip.rip_pref_loss(x.cpu(), t, o, r),
+                 lambda: rip.rip_policy_loss(x, t, None, f),
+                 lambda: rip.rip_policy_loss(x, t, f, f[:4]),
+                 lambda: rip.rip_policy_loss(x.t(), t, f, f)):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        rip.rip_pref_loss(x.half(), t, o, r)
+    for call, code in ((lambda: rip.rip_pref_loss(x, t, o, r, smoothing=1.5), rip.RIP_E_INVAL),
+                       (lambda: rip.rip_pref_loss(x, t, o, r, beta=float("nan")), rip.RIP_E_INVAL),
+                       (lambda: rip.rip_policy_loss(x, t, f, f, kl=0.1), rip.RIP_E_INVAL),
+                       (lambda: rip.rip_policy_loss(x, t, f, f, clip_low=-0.1), rip.RIP_E_INVAL),
+                       (lambda: rip.rip_policy_loss(x, t, f, f, clip_low=1.1), rip.RIP_E_INVAL),
+                       (lambda: rip.rip_policy_loss(x[:4], t[:4], f[:4], f[:4], grad=x[1:5]),
+                        rip.RIP_E_OVERLAP),
+                       (lambda: rip.rip_policy_loss(x[:1].expand(8, 20), t, f, f), rip.RIP_E_INVAL)):
+        with pytest.raises(rip.RipError) as e:
+            call()
+        assert e.value.code == code
+    assert (x == 0).all()

@@ -1,0 +1,181 @@
+"""Argument checks of the operators that fill gradient buffers, which run before
+any launch (CPU only; the addresses are never used), and their plain forms against
+the definitions."""
+import numpy as np
+import pytest
+
+import paper_1909_08029_amd as rip
+import train_ops_ref as ref
+
+A, B, C, D, E, W = (0x10_0000_0000 * i for i in range(1, 7))   # far apart
+BIG = 1 << 40
+INVAL, ALIGN, OVERLAP, UNSUP = (rip.RIP_E_INVAL, rip.RIP_E_ALIGN, rip.RIP_E_OVERLAP,
+                                rip.RIP_E_UNSUPPORTED)
+
+
+def call(fn, defaults, **change):
+    args = dict(defaults, **change)
+    return getattr(rip.lib, fn)(*args.values())
+
+
+LOOKUP = dict(table=A, tt=0, vocab=100, width=16, ld=16, ids=B, idt=1, n=8, scale=1.0, out=C,
+              ot=1, ld_out=16, stream=None)
+GRAD = dict(dout=A, dt=0, ld=16, ids=B, idt=0, n=8, scale=1.0, grad=C, gt=0, vocab=100, width=16,
+            ld_g=16, acc=0, ws=W, nbytes=BIG, stream=None)
+PACK = dict(x=A, dt=1, ld=40, rows=8, width=40, codes=B, exps=C, stream=None)
+UNPACK = dict(codes=B, exps=C, rows=8, width=40, x=A, dt=1, ld=40, stream=None)
+FORWARD = dict(gate=A, ldg=40, up=A + 4096, ldu=40, dt=1, rows=8, width=40, h=B, ldh=40, gc=C,
+               ge=C + 4096, uc=D, ue=D + 4096, stream=None)
+BACKWARD = dict(dh=A, ld=40, dt=1, gc=C, ge=C + 4096, uc=D, ue=D + 4096, rows=8, width=40, dg=B,
+                ldg=40, du=B + 4096, ldu=40, hc=None, he=None, stream=None)
+WGRAD = dict(dy=A, dt=1, ld=24, rows=9000, n=24, codes=B, exps=C, k=40, grad=D, gt=0, ld_g=40,
+             acc=0, ws=W, nbytes=BIG, stream=None)
+PREF = dict(x=A, dt=1, ld=50, n=8, vocab=50, t=B, idt=1, off=C, pairs=2, ref=C + 4096, beta=0.1,
+            smooth=0.0, gs=1.0, loss=D, seq=D + 64, logp=D + 128, grad=E, ld_g=50, ws=W, nbytes=BIG,
+            stream=None)
+POLICY = dict(x=A, dt=1, ld=50, n=8, vocab=50, t=B, idt=1, old=C, adv=C + 4096, w=None, ref=None,
+              lo=0.2, hi=0.2, kl=0.0, gs=1.0, loss=D, logp=D + 128, grad=E, ld_g=50, ws=W,
+              nbytes=BIG, stream=None)
+
+
+@pytest.mark.parametrize("fn,defaults,change,code", [
+    ("rip_embed_lookup", LOOKUP, dict(table=None), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(ids=None), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(out=None), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(n=-1), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(vocab=0), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(ld=15), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(width=0, ld=0, ld_out=0), INVAL),
+    ("rip_embed_lookup", LOOKUP, dict(tt=2), UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(ot=-1), UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(idt=2), UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(n=(1 << 23) + 1), UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(vocab=1 << 31), UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(n=1 << 23, width=1 << 20, ld=1 << 20, ld_out=1 << 20, vocab=2),
+     UNSUP),
+    ("rip_embed_lookup", LOOKUP, dict(table=A + 2), ALIGN),
+    ("rip_embed_lookup", LOOKUP, dict(out=C + 1), ALIGN),
+    ("rip_embed_lookup", LOOKUP, dict(ids=B + 4), ALIGN),
+    ("rip_embed_lookup", LOOKUP, dict(out=A + 64), OVERLAP),
+    ("rip_embed_lookup", LOOKUP, dict(out=B + 32), OVERLAP),
+    ("rip_embed_grad", GRAD, dict(dout=None), INVAL),
+    ("rip_embed_grad", GRAD, dict(grad=None), INVAL),
+    ("rip_embed_grad", GRAD, dict(ws=None), INVAL),
+    ("rip_embed_grad", GRAD, dict(nbytes=64), INVAL),
+    ("rip_embed_grad", GRAD, dict(ld_g=8), INVAL),
+    ("rip_embed_grad", GRAD, dict(ws=W + 4), ALIGN),
+    ("rip_embed_grad", GRAD, dict(grad=A), OVERLAP),
+    ("rip_embed_grad", GRAD, dict(ws=C + 64), OVERLAP),
+    ("rip_embed_grad", GRAD, dict(ws=A), OVERLAP),
+    ("rip_embed_grad", GRAD, dict(gt=7), UNSUP),
+    ("rip_ckpt_pack", PACK, dict(x=None), INVAL),
+    ("rip_ckpt_pack", PACK, dict(codes=None), INVAL),
+    ("rip_ckpt_pack", PACK, dict(exps=None), INVAL),
+    ("rip_ckpt_pack", PACK, dict(rows=-1), INVAL),
+    ("rip_ckpt_pack", PACK, dict(width=0), INVAL),
+    ("rip_ckpt_pack", PACK, dict(ld=39), INVAL),
+    ("rip_ckpt_pack", PACK, dict(codes=B + 8), ALIGN),
+    ("rip_ckpt_pack", PACK, dict(x=A + 1), ALIGN),
+    ("rip_ckpt_pack", PACK, dict(dt=3), UNSUP),
+    ("rip_ckpt_pack", PACK, dict(rows=1 << 23, width=1 << 12, ld=1 << 12), UNSUP),
+    ("rip_ckpt_pack", PACK, dict(codes=A), OVERLAP),
+    ("rip_ckpt_pack", PACK, dict(exps=B + 100), OVERLAP),
+    ("rip_ckpt_unpack", UNPACK, dict(x=B), OVERLAP),
+    ("rip_ckpt_unpack", UNPACK, dict(x=None), INVAL),
+    ("rip_gate_forward", FORWARD, dict(up=None), INVAL),
+    ("rip_gate_forward", FORWARD, dict(ue=None), INVAL),
+    ("rip_gate_forward", FORWARD, dict(ldh=39), INVAL),
+    ("rip_gate_forward", FORWARD, dict(h=A + 80), OVERLAP),
+    ("rip_gate_forward", FORWARD, dict(h=A, ldh=41), OVERLAP),
+    ("rip_gate_forward", FORWARD, dict(uc=C), OVERLAP),
+    ("rip_gate_forward", FORWARD, dict(uc=D + 1), ALIGN),
+    ("rip_gate_backward", BACKWARD, dict(gc=None), INVAL),
+    ("rip_gate_backward", BACKWARD, dict(hc=E), INVAL),
+    ("rip_gate_backward", BACKWARD, dict(du=B), OVERLAP),
+    ("rip_gate_backward", BACKWARD, dict(ldg=80, ldu=80, du=B + 78), OVERLAP),
+    ("rip_gate_backward", BACKWARD, dict(hc=C, he=E), OVERLAP),
+    ("rip_gate_backward", BACKWARD, dict(dh=None), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(dy=None), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(codes=None), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(grad=None), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(nbytes=16), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(rows=-1), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(n=0), INVAL),
+    ("rip_ckpt_wgrad", WGRAD, dict(k=1 << 19, ld_g=1 << 19), UNSUP),
+    ("rip_ckpt_wgrad", WGRAD, dict(dt=5), UNSUP),
+    ("rip_ckpt_wgrad", WGRAD, dict(codes=B + 4), ALIGN),
+    ("rip_ckpt_wgrad", WGRAD, dict(ws=W + 1), ALIGN),
+    ("rip_ckpt_wgrad", WGRAD, dict(grad=B), OVERLAP),
+    ("rip_ckpt_wgrad", WGRAD, dict(ws=D), OVERLAP),
+    ("rip_pref_loss", PREF, dict(pairs=0), INVAL),
+    ("rip_pref_loss", PREF, dict(off=None), INVAL),
+    ("rip_pref_loss", PREF, dict(ref=None), INVAL),
+    ("rip_pref_loss", PREF, dict(loss=None), INVAL),
+    ("rip_pref_loss", PREF, dict(t=None), INVAL),
+    ("rip_pref_loss", PREF, dict(vocab=0), INVAL),
+    ("rip_pref_loss", PREF, dict(smooth=-0.1), INVAL),
+    ("rip_pref_loss", PREF, dict(ld=49), INVAL),
+    ("rip_pref_loss", PREF, dict(nbytes=8), INVAL),
+    ("rip_pref_loss", PREF, dict(pairs=(1 << 20) + 1), UNSUP),
+    ("rip_pref_loss", PREF, dict(idt=4), UNSUP),
+    ("rip_pref_loss", PREF, dict(grad=A + 2), OVERLAP),
+    ("rip_pref_loss", PREF, dict(grad=A, ld_g=51), OVERLAP),
+    ("rip_pref_loss", PREF, dict(ws=E), OVERLAP),
+    ("rip_pref_loss", PREF, dict(t=B + 4), ALIGN),
+    ("rip_policy_loss", POLICY, dict(old=None), INVAL),
+    ("rip_policy_loss", POLICY, dict(kl=0.1), INVAL),
+    ("rip_policy_loss", POLICY, dict(lo=1.5), INVAL),
+    ("rip_policy_loss", POLICY, dict(hi=-0.5), INVAL),
+    ("rip_policy_loss", POLICY, dict(kl=float("nan")), INVAL),
+    ("rip_policy_loss", POLICY, dict(n=-1), INVAL),
+    ("rip_policy_loss", POLICY, dict(grad=E + 1), ALIGN),
+    ("rip_policy_loss", POLICY, dict(n=(1 << 23) + 1), UNSUP),
+])
+def test_refused_before_any_launch(fn, defaults, change, code):
+    assert call(fn, defaults, **change) == code
+    assert rip.lib.rip_last_error()
+
+
+def test_workspace_sizes():
+    lib = rip.lib
+    assert lib.rip_embed_grad_workspace(0, 16) == 0
+    assert lib.rip_embed_grad_workspace(1, 16) > 0
+    assert lib.rip_embed_grad_workspace(-1, 16) == 0 == lib.rip_embed_grad_workspace(1, 0)
+    assert lib.rip_pref_loss_workspace(0, 10, 1) > 0
+    assert lib.rip_policy_loss_workspace(0, 10) > 0
+    assert lib.rip_pref_loss_workspace(-1, 10, 1) == 0
+    assert lib.rip_ckpt_wgrad_workspace(0, 0, 4, 4) == 0
+    assert lib.rip_ckpt_wgrad_workspace(9, 100, 4, 4) == 0
+    for n in (1, 63, 4096, 4097, 100_000, 1 << 23):
+        for width in (1, 512, 513, 5000):
+            assert lib.rip_embed_grad_workspace(n, width) >= 8 * n
+    # a small gradient summed over many tokens is split, a large one is not
+    assert lib.rip_ckpt_wgrad_workspace(1, 40000, 64, 64) >= 2 * 64 * 64 * 4
+
+
+def test_plain_forms():
+    """The tests' own 64-bit forms: packing keeps the format's bounds, and the
+    losses' gradients equal difference quotients."""
+    rng = np.random.default_rng(1)
+    x = (rng.standard_normal((40, 70)) * 2.0 ** rng.integers(-140, 120, (40, 1))).astype(np.float32)
+    codes, exps = ref.pack(x)
+    step = np.repeat(2.0 ** (exps.astype(np.float64) - 127), 32, 1)[:, :70]
+    assert np.abs(ref.unpack(codes, exps, 70) - x).max(initial=0) <= (0.5 * step).max()
+    assert (np.abs(ref.unpack(codes, exps, 70) - x) <= 0.5 * step).all()
+    top = np.abs(codes.astype(int)).reshape(40, 3, 32).max(2)
+    assert ((top >= 63) | (exps == 1)).all() and (codes >= -127).all()
+
+    logits, targets = rng.standard_normal((9, 12)), rng.integers(0, 12, 9)
+    targets[2] = -100
+    offsets, r = [0, 3, 5, 7, 9], rng.standard_normal(4) - 6
+    w, adv = rng.random(9), rng.standard_normal(9)
+    old = ref.log_softmax_at(logits, targets)[0] + 0.01 * rng.standard_normal(9)
+    refp = old + rng.standard_normal(9)
+    for f in (lambda z: ref.pref_loss(z, targets, offsets, r, 0.5, 0.1),
+              lambda z: ref.policy_loss(z, targets, old, adv, w, refp, 0.2, 0.3, 0.1)):
+        g = f(logits)["grad"]
+        for t, v in ((0, targets[0]), (1, 4), (4, 0), (8, targets[8]), (2, 3)):
+            d = np.zeros_like(logits)
+            d[t, v] = 1e-5
+            q = (f(logits + d)["loss"] - f(logits - d)["loss"]) / 2e-5
+            assert abs(q - g[t, v]) < 1e-8
