@@ -59,11 +59,16 @@ __device__ __forceinline__ float ckpt_step(uint32_t e) {
   return __uint_as_float(e == kCkptNan ? 0x7fc00000u : e << 23);
 }
 
+// Byte j of a word as a signed integer, widened to fp32 (one instruction, which
+// picks the byte itself; written so that the compiler finds it).
+__device__ __forceinline__ float widen(uint32_t w, int j) {
+  return (float)((int)(w << (24 - 8 * j)) >> 24);
+}
+
 __device__ __forceinline__ void ckpt_unpack(uint2 codes, uint32_t e, float (&x)[kLane]) {
   const float step = ckpt_step(e);
 #pragma unroll
-  for (int j = 0; j < kLane; ++j)
-    x[j] = (float)(int8_t)((j < 4 ? codes.x : codes.y) >> (8 * (j % 4))) * step;
+  for (int j = 0; j < kLane; ++j) x[j] = widen(j < 4 ? codes.x : codes.y, j % 4) * step;
 }
 
 }  // namespace rip
