@@ -23,10 +23,9 @@ namespace rip {
 namespace {
 
 constexpr int kTokens = 32;  // tokens of a step
-constexpr int kThreads = 256;
+constexpr int kReduce = 256; // threads of a workgroup of the second launch
 constexpr int kCodes = 16;   // codes that a lane loads at once
-constexpr int kStages = 4;   // steps that LDS holds
-constexpr int kLoads = 2;    // steps that are on their way in registers
+constexpr int kStages = 3;   // steps that LDS holds, and that are on their way in registers
 
 // Elements between LDS rows of a tile's `n` columns.  A group of 16 lanes reads 32
 // bytes of each of four rows: with rows 64 bytes past a multiple of 128 (or of 256,
@@ -52,21 +51,19 @@ __device__ __forceinline__ bf16x8 read_columns(const uint16_t* tile, int t, int 
   return __builtin_bit_cast(bf16x8, v);
 }
 
-// x as three bf16 numbers that add up to it: the leading bits, cut, and what
-// that leaves, twice.  Infinities and NaNs are the first part alone.
+// x as three bf16 numbers that add up to it, each in the high half of a word: the
+// leading bits, cut, and what that leaves, twice.  An infinity is the first part
+// alone; a NaN's difference from its first part is a NaN whatever that part is.
 __device__ __forceinline__ void cut3(float x, uint32_t (&part)[3]) {
-  const uint32_t b = __float_as_uint(x);
-  if ((b & 0x7f800000u) == 0x7f800000u) {
-    part[0] = (b >> 16) | ((b & 0x7fffffu) ? 0x40u : 0u);
-    part[1] = part[2] = 0;
-    return;
-  }
-  const float r1 = x - __uint_as_float(b & 0xffff0000u);
-  const uint32_t b1 = __float_as_uint(r1);
-  const float r2 = r1 - __uint_as_float(b1 & 0xffff0000u);
-  part[0] = b >> 16;
-  part[1] = b1 >> 16;
-  part[2] = __float_as_uint(r2) >> 16;
+  part[0] = __float_as_uint(x);
+  float r = x - __uint_as_float(part[0] & 0xffff0000u);
+  r = __builtin_isinf(x) ? 0.0f : r;
+  part[1] = __float_as_uint(r);
+  part[2] = __float_as_uint(r - __uint_as_float(part[1] & 0xffff0000u));
+}
+// High halves of two words as one, the first below.
+__device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
 }
 
 struct Product {
@@ -75,21 +72,50 @@ struct Product {
   int blocks;        // checkpoint blocks of a row
   int tiles_n, tiles_k;
   int64_t share;     // tokens of a split, a multiple of kTokens
+  int part_k;        // columns of a split's part in the workspace, a multiple of four
   int accumulate;
 };
 
-// A tile of 64 MN rows (along dy's columns) and 64 MK columns (along x's), a
-// quarter of it to each wave.
-template <int DD, int MN, int MK>
+// The workgroup's tile and split.  Workgroups go to the eight XCDs in turn; each
+// XCD, whose workgroups share an L2, takes a run of consecutive places, and places
+// run through bands of four tiles along n and all tiles along k, split by split:
+// 32 of them read the same tokens of four panels of dy and up to eight of x.
+// 16384 x 5504 x 2048 bf16: 528 us with tiles in row order, 455 so.
+struct Place {
+  int tile_n, tile_k, split;
+};
+__device__ __forceinline__ Place place(const Product& p) {
+  constexpr uint32_t kXcds = 8, kBand = 4;
+  const uint32_t all = gridDim.x, xcd = blockIdx.x % kXcds, rest = all % kXcds;
+  const uint32_t at = xcd * (all / kXcds) + (xcd < rest ? xcd : rest) + blockIdx.x / kXcds;
+  const uint32_t tiles = p.tiles_n * p.tiles_k, split = at / tiles, tile = at - split * tiles;
+  const uint32_t band = tile / (kBand * p.tiles_k), in = tile - band * kBand * p.tiles_k;
+  const uint32_t width = min(kBand, p.tiles_n - band * kBand);
+  return {(int)(band * kBand + in % width), (int)(in / width), (int)split};
+}
+
+// A tile of grad for WN x WK waves: each has 32 MN rows (along dy's columns) and
+// 32 MK columns (along x's).
+template <int DD, int MN_, int MK_, int WN_, int WK_>
 struct Tile {
   typedef typename Elem<DD>::T T;
+  static constexpr int MN = MN_, MK = MK_, WN = WN_, WK = WK_, kThreads = 64 * WN * WK;
   static constexpr int kParts = DD == RIP_FP32 ? 3 : 1;
-  static constexpr int kN = 64 * MN, kK = 64 * MK;
+  static constexpr int kN = 32 * MN * WN, kK = 32 * MK * WK;
   static constexpr int kPitchN = pitch(kN), kPitchK = pitch(kK);
-  static constexpr int kYUnits = kTokens * kN / kLane / kThreads;   // of eight elements
-  static constexpr int kXUnits = kTokens * kK / kCodes / kThreads;  // of sixteen codes
+  // Units of a thread: eight elements of dy, sixteen codes.  Where there are
+  // half a round's too few, the last ones are loaded and written twice, alike.
+  static constexpr int kYAll = kTokens * kN / kLane, kXAll = kTokens * kK / kCodes;
+  static constexpr int kYUnits = (kYAll + kThreads - 1) / kThreads;
+  static constexpr int kXUnits = (kXAll + kThreads - 1) / kThreads;
   static constexpr int kYRegs = DD == RIP_FP32 ? 2 : 1;
-  static constexpr int kProducts = kParts * MN * MK, kOperands = kParts * MN + MK;  // of 16 tokens
+  static constexpr int kOperands = kParts * MN + MK;  // of 16 tokens
+  static_assert(kXAll * 2 % kThreads == 0 && kYAll * 2 % kThreads == 0, "units of a thread");
+  template <int ALL>
+  static __device__ __forceinline__ int unit(int i) {
+    const int u = threadIdx.x + i * kThreads;
+    return u - (int)threadIdx.x + kThreads > ALL ? ALL - kThreads / 2 + u % (kThreads / 2) : u;
+  }
 
   struct Shared {
     uint16_t y[kParts][kTokens * kPitchN];
@@ -100,8 +126,11 @@ struct Tile {
     u32x4 x[kXUnits];
     uint32_t e[kXUnits];
   };
-  struct Offsets {  // a thread's elements in the 32 rows of a step
+  struct Offsets {  // bytes of a thread's elements in the 32 rows of a step
     uint32_t y[kYUnits], x[kXUnits], e[kXUnits];
+  };
+  struct Rows {  // where a step's rows begin
+    const char *y, *x, *e;
   };
 
   // Columns past the last are read as the last ones' neighbours: whatever is there
@@ -110,13 +139,13 @@ struct Tile {
     Offsets o;
 #pragma unroll
     for (int i = 0; i < kYUnits; ++i) {
-      const int u = threadIdx.x + i * kThreads;
+      const int u = unit<kYAll>(i);
       const int c = min(n0 + u % (kN / kLane) * kLane, (p.n - 1) / kLane * kLane);
-      o.y[i] = (uint32_t)(u / (kN / kLane)) * (uint32_t)p.ld_dy + c;
+      o.y[i] = ((uint32_t)(u / (kN / kLane)) * (uint32_t)p.ld_dy + c) * (uint32_t)sizeof(T);
     }
 #pragma unroll
     for (int i = 0; i < kXUnits; ++i) {
-      const int u = threadIdx.x + i * kThreads, row = u / (kK / kCodes);
+      const int u = unit<kXAll>(i), row = u / (kK / kCodes);
       const int c = min(k0 + u % (kK / kCodes) * kCodes, p.blocks * kCkptBlock - kCodes);
       o.x[i] = (uint32_t)row * (uint32_t)(p.blocks * kCkptBlock) + c;
       o.e[i] = (uint32_t)row * (uint32_t)p.blocks + c / kCkptBlock;
@@ -124,26 +153,21 @@ struct Tile {
     return o;
   }
 
-  // Rows t .. t+31, all of them tokens of the split, sixteen bytes from any
-  // column's start inside dy.
-  static __device__ __forceinline__ void load(const Product& p, const Offsets& o, const T* dy,
-                                              const int8_t* codes, const uint8_t* exps, int64_t t,
-                                              Regs& r) {
-    const T* y = dy + t * p.ld_dy;
-    const int8_t* x = codes + t * (p.blocks * kCkptBlock);
-    const uint8_t* e = exps + t * p.blocks;
+  // A step's rows, all of them tokens of the split, sixteen bytes from any column's
+  // start inside dy.
+  static __device__ __forceinline__ void load(const Offsets& o, const Rows& rows, Regs& r) {
+#pragma unroll
+    for (int i = 0; i < kXUnits; ++i) {
+      r.x[i] = *(const u32x4*)(rows.x + o.x[i]);
+      r.e[i] = *(const uint8_t*)(rows.e + o.e[i]);
+    }
 #pragma unroll
     for (int i = 0; i < kYUnits; ++i)
 #pragma unroll
-      for (int h = 0; h < kYRegs; ++h) r.y[i][h] = *(const u32x4_any*)(y + o.y[i] + 4 * h);
-#pragma unroll
-    for (int i = 0; i < kXUnits; ++i) {
-      r.x[i] = *(const u32x4*)(x + o.x[i]);
-      r.e[i] = e[o.e[i]];
-    }
+      for (int h = 0; h < kYRegs; ++h) r.y[i][h] = *(const u32x4_any*)(rows.y + o.y[i] + 16 * h);
   }
 
-  // The same with rows from `end` on and columns past the last as zeros.
+  // Rows t .. t+31 with those from `end` on and columns past the last as zeros.
   static __device__ __forceinline__ void load_checked(const Product& p, const T* dy,
                                                       const int8_t* codes, const uint8_t* exps,
                                                       int n0, int k0, int64_t t, int64_t end,
@@ -151,7 +175,7 @@ struct Tile {
     const int width = p.blocks * kCkptBlock;
 #pragma unroll
     for (int i = 0; i < kYUnits; ++i) {
-      const int u = threadIdx.x + i * kThreads, row = u / (kN / kLane);
+      const int u = unit<kYAll>(i), row = u / (kN / kLane);
       const int c = n0 + u % (kN / kLane) * kLane;
       float f[kLane] = {};
       if (t + row < end && c < p.n) load_unit<DD>(dy + (t + row) * p.ld_dy, c, p.n, f);
@@ -161,12 +185,12 @@ struct Tile {
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          r.y[i][0][j] = __float_as_uint(f[2 * j]) >> 16 | (__float_as_uint(f[2 * j + 1]) & 0xffff0000u);
+          r.y[i][0][j] = high_halves(__float_as_uint(f[2 * j]), __float_as_uint(f[2 * j + 1]));
       }
     }
 #pragma unroll
     for (int i = 0; i < kXUnits; ++i) {
-      const int u = threadIdx.x + i * kThreads, row = u / (kK / kCodes);
+      const int u = unit<kXAll>(i), row = u / (kK / kCodes);
       const int c = min(k0 + u % (kK / kCodes) * kCodes, width - kCodes);
       r.x[i] = u32x4{0, 0, 0, 0};
       r.e[i] = 0;
@@ -177,27 +201,30 @@ struct Tile {
     }
   }
 
-  static __device__ __forceinline__ void store(Regs& r, Shared& sh) {
+  // What a step writes to LDS, in items: eight codes widened to bf16, or a unit of
+  // dy.  [from, to) are known when the code is compiled.
+  static constexpr int kItems = 2 * kXUnits + kYUnits;
+  static __device__ __forceinline__ void store(Regs& r, Shared& sh, int from = 0, int to = kItems) {
 #pragma unroll
-    for (int i = 0; i < kXUnits; ++i) {
+    for (int i = 0; i < 2 * kXUnits; ++i) {
+      if (i < from || i >= to) continue;
       // keeps the widening of the codes here, behind the wait for their load,
       // where otherwise it would move up to the load
-      asm("" : "+v"(r.x[i]), "+v"(r.e[i]));
-      const int u = threadIdx.x + i * kThreads, row = u / (kK / kCodes), c = u % (kK / kCodes) * kCodes;
+      if (i % 2 == 0) asm("" : "+v"(r.x[i / 2]), "+v"(r.e[i / 2]));
+      const int u = unit<kXAll>(i / 2), row = u / (kK / kCodes);
+      const int c = u % (kK / kCodes) * kCodes + i % 2 * kLane;
+      float x[kLane];
+      ckpt_unpack(make_uint2(r.x[i / 2][i % 2 * 2], r.x[i / 2][i % 2 * 2 + 1]), r.e[i / 2], x);
+      u32x4 v;  // the values' low halves are zeros
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float x[kLane];
-        ckpt_unpack(make_uint2(r.x[i][2 * h], r.x[i][2 * h + 1]), r.e[i], x);
-        u32x4 v;  // the values' low halves are zeros
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          v[j] = __builtin_amdgcn_perm(__float_as_uint(x[2 * j + 1]), __float_as_uint(x[2 * j]), 0x07060302u);
-        *(u32x4*)&sh.x[row * kPitchK + c + h * kLane] = v;
-      }
+      for (int j = 0; j < 4; ++j)
+        v[j] = high_halves(__float_as_uint(x[2 * j]), __float_as_uint(x[2 * j + 1]));
+      *(u32x4*)&sh.x[row * kPitchK + c] = v;
     }
 #pragma unroll
     for (int i = 0; i < kYUnits; ++i) {
-      const int u = threadIdx.x + i * kThreads, row = u / (kN / kLane), c = u % (kN / kLane) * kLane;
+      if (i + 2 * kXUnits < from || i + 2 * kXUnits >= to) continue;
+      const int u = unit<kYAll>(i), row = u / (kN / kLane), c = u % (kN / kLane) * kLane;
       if constexpr (DD == RIP_FP32) {
         asm("" : "+v"(r.y[i][0]), "+v"(r.y[i][1]));
         u32x4 v[3];
@@ -207,7 +234,7 @@ struct Tile {
           cut3(__uint_as_float(r.y[i][j / 2][2 * j % 4]), a);
           cut3(__uint_as_float(r.y[i][j / 2][2 * j % 4 + 1]), b);
 #pragma unroll
-          for (int q = 0; q < 3; ++q) v[q][j] = a[q] | b[q] << 16;
+          for (int q = 0; q < 3; ++q) v[q][j] = high_halves(a[q], b[q]);
         }
 #pragma unroll
         for (int q = 0; q < 3; ++q) *(u32x4*)&sh.y[q][row * kPitchN + c] = v[q];
@@ -217,27 +244,34 @@ struct Tile {
     }
   }
 
-  // Operands of sixteen tokens of a wave's part of the tile.
+  // Operands of sixteen tokens of a wave's part of the tile: MK of x, then those
+  // of dy.
   struct Frags {
     bf16x8 a[kParts][MN], b[MK];
   };
   static __device__ __forceinline__ void read(const Shared& sh, int s, int wn, int wk, int lane,
-                                              Frags& f) {
+                                              Frags& f, int from = 0, int to = kOperands) {
 #pragma unroll
-    for (int j = 0; j < MK; ++j) f.b[j] = read_columns<kPitchK>(sh.x, s, wk + j * 32, lane);
+    for (int j = 0; j < MK; ++j)
+      if (j >= from && j < to) f.b[j] = read_columns<kPitchK>(sh.x, s, wk + j * 32, lane);
 #pragma unroll
     for (int q = 0; q < kParts; ++q)
 #pragma unroll
-      for (int i = 0; i < MN; ++i) f.a[q][i] = read_columns<kPitchN>(sh.y[q], s, wn + i * 32, lane);
+      for (int i = 0; i < MN; ++i)
+        if (MK + q * MN + i >= from && MK + q * MN + i < to)
+          f.a[q][i] = read_columns<kPitchN>(sh.y[q], s, wn + i * 32, lane);
+  }
+  // Row i of part q with all columns: MK matrix instructions.
+  static __device__ __forceinline__ void multiply(const Frags& f, int q, int i, f32x16 (&acc)[MN][MK]) {
+#pragma unroll
+    for (int j = 0; j < MK; ++j)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[q][i], f.b[j], acc[i][j], 0, 0, 0);
   }
   static __device__ __forceinline__ void multiply(const Frags& f, f32x16 (&acc)[MN][MK]) {
 #pragma unroll
     for (int q = 0; q < kParts; ++q)
 #pragma unroll
-      for (int i = 0; i < MN; ++i)
-#pragma unroll
-        for (int j = 0; j < MK; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.a[q][i], f.b[j], acc[i][j], 0, 0, 0);
+      for (int i = 0; i < MN; ++i) multiply(f, q, i, acc);
   }
 };
 
@@ -249,35 +283,59 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Order of a step's instructions: beside each matrix instruction, which keeps its
-// unit busy for 32 cycles, an equal share of the LDS reads, of the arithmetic and
-// of the rest.
-template <typename Tl, int I = 0>
+// Half of a step: the products of the operands in `f`, and beside every MK matrix
+// instructions (each keeps its unit busy for 32 cycles) a share of the reads of the
+// next operands and of the writes of a later step, spread between them.
+template <int MFMA, int READS, int VALU, int WRITES, int LOADS, int I = 0>
 __device__ __forceinline__ void interleave() {
-  constexpr int kMfma = 2 * Tl::kProducts, kReads = 4 * Tl::kOperands;
-  constexpr int kWrites = Tl::kXUnits * 2 + Tl::kYUnits * Tl::kParts;
-  if constexpr (I < kMfma) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
-    constexpr int kRead = (I + 1) * kReads / kMfma - I * kReads / kMfma;
+  if constexpr (I < MFMA) {
+    constexpr int kRead = (I + 1) * READS / MFMA - I * READS / MFMA;
+    constexpr int kValu = (I + 1) * VALU / MFMA - I * VALU / MFMA;
+    constexpr int kWrite = (I + 1) * WRITES / MFMA - I * WRITES / MFMA;
+    constexpr int kLoad = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     if constexpr (kRead > 0) __builtin_amdgcn_sched_group_barrier(0x100, kRead, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // vector arithmetic
-    constexpr int kWrite = (I + 1) * kWrites / kMfma - I * kWrites / kMfma;
+    if constexpr (kLoad > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoad, 0);
+    if constexpr (kValu > 0) __builtin_amdgcn_sched_group_barrier(0x002, kValu, 0);
     if constexpr (kWrite > 0) __builtin_amdgcn_sched_group_barrier(0x200, kWrite, 0);
-    interleave<Tl, I + 1>();
+    interleave<MFMA, READS, VALU, WRITES, LOADS, I + 1>();
+  }
+}
+template <typename Tl, int HALF, int C = 0, typename Load>
+__device__ __forceinline__ void half(const typename Tl::Frags& f, f32x16 (&acc)[Tl::MN][Tl::MK],
+                                     const typename Tl::Shared& from, int at, int wn, int wk,
+                                     int lane, typename Tl::Frags& next, typename Tl::Regs& regs,
+                                     typename Tl::Shared& to, Load& load) {
+  constexpr int MN = Tl::MN, MK = Tl::MK, kRows = Tl::kParts * MN, kLast = 2 * kRows - 1;
+  if constexpr (C < kRows) {
+    constexpr int r0 = C * Tl::kOperands / kRows, r1 = (C + 1) * Tl::kOperands / kRows;
+    constexpr int g = HALF * kRows + C;  // the last one starts the loads instead of writing
+    constexpr int i0 = g * Tl::kItems / kLast, i1 = g < kLast ? (g + 1) * Tl::kItems / kLast : i0;
+    Tl::read(from, at, wn, wk, lane, next, r0, r1);
+    if constexpr (g < kLast)
+      Tl::store(regs, to, i0, i1);
+    else
+      load(regs);
+    Tl::multiply(f, C / MN, C % MN, acc);
+    interleave<MK, 2 * (r1 - r0), 22 * (i1 - i0), i1 - i0,
+               g < kLast ? 0 : 2 * Tl::kXUnits + Tl::kYUnits * Tl::kYRegs>();
+    __builtin_amdgcn_sched_barrier(0);
+    half<Tl, HALF, C + 1>(f, acc, from, at, wn, wk, lane, next, regs, to, load);
   }
 }
 
-template <int DD, int GD, int MN, int MK, int WAVES, bool PART>
-__global__ __launch_bounds__(kThreads, WAVES) void wgrad_kernel(
+template <typename Tl, int DD, int GD, int RESIDENT, bool PART>
+__global__ __launch_bounds__(Tl::kThreads, RESIDENT) void wgrad_kernel(
     Product p, const typename Elem<DD>::T* dy, const int8_t* codes, const uint8_t* exps,
     typename Elem<GD>::T* grad, float* partial) {
-  typedef Tile<DD, MN, MK> Tl;
+  constexpr int MN = Tl::MN, MK = Tl::MK;
   __shared__ __align__(16) typename Tl::Shared sh[kStages];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int n0 = (int)blockIdx.x % p.tiles_n * Tl::kN, k0 = (int)blockIdx.x / p.tiles_n * Tl::kK;
-  const int64_t t0 = (int64_t)blockIdx.y * p.share;
+  const Place at = place(p);
+  const int n0 = at.tile_n * Tl::kN, k0 = at.tile_k * Tl::kK;
+  const int64_t t0 = (int64_t)at.split * p.share;
   const int64_t t1 = t0 + p.share < p.tokens ? t0 + p.share : p.tokens;
-  const int wn = wave / 2 * (Tl::kN / 2), wk = wave % 2 * (Tl::kK / 2);
+  const int wn = wave / Tl::WK * (32 * MN), wk = wave % Tl::WK * (32 * MK);
   const int steps = (int)((t1 - t0 + kTokens - 1) / kTokens);
   // The steps whose loads cannot leave dy are loaded well ahead of their use; the
   // few at the end of the tokens are not.
@@ -289,42 +347,50 @@ __global__ __launch_bounds__(kThreads, WAVES) void wgrad_kernel(
   }
   f32x16 acc[MN][MK] = {};
   if (whole > 0) {
-    typename Tl::Regs regs[kLoads];
+    typename Tl::Regs regs[kStages];
     typename Tl::Frags f0, f1;
     const typename Tl::Offsets off = Tl::offsets(p, n0, k0);
-    auto load = [&](int s, typename Tl::Regs& r) {
+    const int row_x = p.blocks * kCkptBlock;
+    typename Tl::Rows rows = {(const char*)(dy + t0 * p.ld_dy), (const char*)(codes + t0 * row_x),
+                              (const char*)(exps + t0 * p.blocks)};
+    const int64_t step_y = kTokens * p.ld_dy * (int64_t)sizeof(typename Tl::T);
+    int left = whole;  // steps from `rows` on
+    auto load = [&](typename Tl::Regs& r) {
+      Tl::load(off, rows, r);
       // past the last whole step its rows are loaded once more, and not used
-      Tl::load(p, off, dy, codes, exps, t0 + (int64_t)min(s, whole - 1) * kTokens, r);
+      const int64_t on = left > 1;
+      left -= 1;
+      rows.y += on * step_y;
+      rows.x += on * kTokens * row_x;
+      rows.e += on * kTokens * p.blocks;
     };
     // Step s multiplies what lies in LDS stage s, writes step s + 2 to its stage
-    // and starts the loads of step s + 4.  Half of a step's operands are read
+    // and starts the loads of step s + 5.  Half of a step's operands are read
     // before the barrier that begins it.
-    auto step = [&](int s, int now) {
-      Tl::read(sh[now], 16, wn, wk, lane, f1);
-      Tl::store(regs[now % kLoads], sh[(now + 2) % kStages]);
-      load(s + 4, regs[now % kLoads]);
-      Tl::multiply(f0, acc);
-      Tl::read(sh[(now + 1) % kStages], 0, wn, wk, lane, f0);
-      Tl::multiply(f1, acc);
-      interleave<Tl>();
+    auto step = [&](int now) {
+      constexpr auto later = [](int stage, int by) { return (stage + by) % kStages; };
+      typename Tl::Regs& r = regs[later(now, 2)];
+      typename Tl::Shared& to = sh[later(now, 2)];
+      half<Tl, 0>(f0, acc, sh[now], 16, wn, wk, lane, f1, r, to, load);
+      half<Tl, 1>(f1, acc, sh[later(now, 1)], 0, wn, wk, lane, f0, r, to, load);
       lds_barrier();
     };
-    load(0, regs[0]);
-    load(1, regs[1]);
-    Tl::store(regs[0], sh[0]);
-    load(2, regs[0]);
-    Tl::store(regs[1], sh[1]);
-    load(3, regs[1]);
+    for (int i = 0; i < kStages; ++i) load(regs[i]);
+    for (int i = 0; i < 2; ++i) {
+      Tl::store(regs[i], sh[i]);
+      load(regs[i]);
+    }
     lds_barrier();
     Tl::read(sh[0], 0, wn, wk, lane, f0);
+    // all loads done: what is on its way here would otherwise be waited for in
+    // every round of the loop
+    __builtin_amdgcn_s_waitcnt(0);
     for (int s = 0;;) {
-      step(s, 0);
+      step(0);
       if (++s == whole) break;
-      step(s, 1);
+      step(1);
       if (++s == whole) break;
-      step(s, 2);
-      if (++s == whole) break;
-      step(s, 3);
+      step(2);
       if (++s == whole) break;
     }
   }
@@ -350,7 +416,7 @@ __global__ __launch_bounds__(kThreads, WAVES) void wgrad_kernel(
         const int col = k0 + wk + j * 32 + lane % 32;
         if (row >= p.n || col >= p.k) continue;
         if constexpr (PART) {
-          partial[((int64_t)blockIdx.y * p.n + row) * p.k + col] = acc[i][j][r];
+          partial[((int64_t)at.split * p.n + row) * p.part_k + col] = acc[i][j][r];
         } else {
           typename Elem<GD>::T* g = grad + (int64_t)row * p.ld_grad + col;
           Elem<GD>::store(g, p.accumulate ? Elem<GD>::load(g) + acc[i][j][r] : acc[i][j][r]);
@@ -358,40 +424,81 @@ __global__ __launch_bounds__(kThreads, WAVES) void wgrad_kernel(
       }
 }
 
-// The splits' parts, added in order.
-template <int GD>
-__global__ __launch_bounds__(kThreads) void reduce_kernel(Product p, const float* partial,
-                                                          int splits,
-                                                          typename Elem<GD>::T* grad) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)p.n * p.k;
-  if (i >= all) return;
-  float sum = partial[i];
-  for (int s = 1; s < splits; ++s) sum += partial[s * all + i];
-  typename Elem<GD>::T* g = grad + i / p.k * p.ld_grad + i % p.k;
-  Elem<GD>::store(g, p.accumulate ? Elem<GD>::load(g) + sum : sum);
+// The splits' parts added up: four columns to a thread, a run of the splits to each
+// of GROUPS groups of threads, whose sums are then added in order.
+template <int GD, int GROUPS>
+__global__ __launch_bounds__(kReduce) void reduce_kernel(Product p, const float* partial,
+                                                         int splits,
+                                                         typename Elem<GD>::T* grad) {
+  constexpr int kColumns = kReduce / GROUPS;
+  __shared__ float4 sums[GROUPS][kColumns];
+  const int in = threadIdx.x % kColumns, group = threadIdx.x / kColumns;
+  const int64_t quads = (int64_t)p.n * p.part_k / 4, i = (int64_t)blockIdx.x * kColumns + in;
+  float4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (i < quads) {
+    const float4* q = (const float4*)partial + i;
+    const int to = (group + 1) * splits / GROUPS;
+#pragma unroll 8
+    for (int s = group * splits / GROUPS; s < to; ++s) {
+      const float4 v = q[s * quads];
+      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    sums[group][in] = sum;
+    __syncthreads();
+    if (group) return;
+    for (int g = 1; g < GROUPS; ++g) {
+      const float4 v = sums[g][in];
+      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+    }
+  }
+  if (i >= quads) return;
+  const int per_row = p.part_k / 4, row = (int)(i / per_row), col = (int)(i - (int64_t)row * per_row) * 4;
+  typename Elem<GD>::T* g = grad + (int64_t)row * p.ld_grad + col;
+  const float f[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (col + j < p.k) Elem<GD>::store(g + j, p.accumulate ? Elem<GD>::load(g + j) + f[j] : f[j]);
 }
 
+// The tiles, by type of dy: rows and columns of grad, workgroups that a compute unit
+// holds, and the time (us) of a step of 32 tokens where it holds one and where it
+// holds all of them, measured on long products.
+struct Shape {
+  int n, k, resident;
+  double one, all;
+};
+constexpr Shape kF32Shapes[] = {{128, 128, 1, 0.9, 0.9}, {128, 256, 1, 1.4, 1.4}};
+constexpr Shape kBf16Shapes[] = {{128, 128, 2, 0.5, 0.7}, {192, 256, 1, 0.7, 0.7}, {256, 256, 1, 0.75, 0.75}};
+constexpr int kUnits = 256;       // compute units
+constexpr int64_t kMaxSplits = 64;
+
 struct Plan {
-  bool large;
-  int tiles_n, tiles_k, splits;
+  int shape;
+  int tiles_n, tiles_k, splits, part_k;
   int64_t share;
 };
+// The tile and the number of splits of the least time: rounds of workgroups, each
+// with its steps and the time to fill and drain the pipeline (three steps), and
+// for split products the parts' way to memory and back and the second launch.
 Plan make_plan(int32_t dy_dtype, int64_t tokens, int64_t n, int64_t k) {
+  const Shape* shapes = dy_dtype == RIP_BF16 ? kBf16Shapes : kF32Shapes;
+  const int count = dy_dtype == RIP_BF16 ? 3 : 2;
+  const int64_t steps = ceil_div(tokens, kTokens), part_k = ceil_div(k, 4) * 4;
   Plan best{};
   double least = 1e30;
-  for (int large = 0; large < (dy_dtype == RIP_BF16 ? 2 : 1); ++large) {
-    const int tn = large ? 192 : 128, tk = large ? 256 : 128;
-    const int64_t tiles_n = ceil_div(n, tn), tiles_k = ceil_div(k, tk), tiles = tiles_n * tiles_k;
-    const int64_t steps = ceil_div(tokens, kTokens);
-    const int slots = large || dy_dtype == RIP_FP32 ? 256 : 512;
-    const double step = large ? 0.5 : 0.4;
-    for (int64_t splits = 1; splits <= 64 && (splits == 1 || splits * 4 <= steps); ++splits) {
-      const int64_t per = ceil_div(steps, splits);
-      double us = (double)ceil_div(tiles * splits, slots) * per * step;
-      if (splits > 1) us += 4.0 + (double)splits * n * k * 8 / 4e6;
+  for (int i = 0; i < count; ++i) {
+    const Shape& sh = shapes[i];
+    const int64_t tiles_n = ceil_div(n, sh.n), tiles_k = ceil_div(k, sh.k), tiles = tiles_n * tiles_k;
+    for (int64_t splits = 1; splits <= kMaxSplits && (splits == 1 || splits * 2 <= steps); ++splits) {
+      const int64_t per = ceil_div(steps, splits), groups = tiles * splits;
+      const double step = groups <= kUnits ? sh.one : sh.all;
+      double us = (double)ceil_div(groups, kUnits * sh.resident) * (per + 3) * step;
+      if (splits > 1) us += 4.0 + (double)splits * n * part_k * 8 / 4e6;
       if (us < least) {
         least = us;
-        best = Plan{large != 0, (int)tiles_n, (int)tiles_k, (int)splits, per * kTokens};
+        best = Plan{i, (int)tiles_n, (int)tiles_k, (int)splits, (int)part_k, per * kTokens};
       }
     }
   }
@@ -399,27 +506,36 @@ Plan make_plan(int32_t dy_dtype, int64_t tokens, int64_t n, int64_t k) {
   return best;
 }
 
-template <int DD, int GD, int MN, int MK, int WAVES>
-const void* kernel_of(bool part) {
-  return part ? (const void*)wgrad_kernel<DD, GD, MN, MK, WAVES, true>
-              : (const void*)wgrad_kernel<DD, GD, MN, MK, WAVES, false>;
+template <int DD, int GD, int MN, int MK, int WN, int WK, int RESIDENT>
+int32_t run_tile(Product& p, const Plan& plan, void** args, void* stream) {
+  typedef Tile<DD, MN, MK, WN, WK> Tl;
+  const void* fn = plan.splits > 1 ? (const void*)wgrad_kernel<Tl, DD, GD, RESIDENT, true>
+                                   : (const void*)wgrad_kernel<Tl, DD, GD, RESIDENT, false>;
+  return launch(fn, dim3((uint32_t)(plan.tiles_n * plan.tiles_k * plan.splits)),
+                dim3(Tl::kThreads), args, 0, stream, "rip_ckpt_wgrad");
 }
 
 template <int DD, int GD>
 int32_t run(Product& p, const Plan& plan, const void* dy, const int8_t* codes, const uint8_t* exps,
             void* grad, float* partial, void* stream) {
   void* args[] = {&p, &dy, &codes, &exps, &grad, &partial};
-  const void* fn = kernel_of<DD, GD, 2, 2, DD == RIP_FP32 ? 1 : 2>(plan.splits > 1);
-  if constexpr (DD == RIP_BF16)
-    if (plan.large) fn = kernel_of<DD, GD, 3, 4, 1>(plan.splits > 1);
-  int32_t rc = launch(fn, dim3((uint32_t)(plan.tiles_n * plan.tiles_k), (uint32_t)plan.splits),
-                      dim3(kThreads), args, 0, stream, "rip_ckpt_wgrad");
+  int32_t rc;
+  if constexpr (DD == RIP_FP32)
+    rc = plan.shape == 0 ? run_tile<DD, GD, 2, 1, 2, 4, 2>(p, plan, args, stream)
+                         : run_tile<DD, GD, 2, 2, 2, 4, 2>(p, plan, args, stream);
+  else
+    rc = plan.shape == 0   ? run_tile<DD, GD, 2, 2, 2, 2, 2>(p, plan, args, stream)
+         : plan.shape == 1 ? run_tile<DD, GD, 3, 2, 2, 4, 2>(p, plan, args, stream)
+                           : run_tile<DD, GD, 4, 2, 2, 4, 2>(p, plan, args, stream);
   if (rc || plan.splits == 1) return rc;
   int splits = plan.splits;
   void* args2[] = {&p, &partial, &splits, &grad};
-  return launch((const void*)reduce_kernel<GD>,
-                dim3((uint32_t)ceil_div((int64_t)p.n * p.k, kThreads)), dim3(kThreads), args2, 0,
-                stream, "rip_ckpt_wgrad: reduce");
+  // few columns: several groups of threads share the splits
+  const int64_t quads = (int64_t)p.n * p.part_k / 4;
+  const bool few = quads < 1 << 17;
+  const void* add = few ? (const void*)reduce_kernel<GD, 8> : (const void*)reduce_kernel<GD, 1>;
+  return launch(add, dim3((uint32_t)ceil_div(quads, few ? kReduce / 8 : kReduce)), dim3(kReduce),
+                args2, 0, stream, "rip_ckpt_wgrad: reduce");
 }
 
 bool sizes_ok(int64_t tokens, int64_t n, int64_t k) {
@@ -436,7 +552,7 @@ extern "C" int64_t rip_ckpt_wgrad_workspace(int32_t dy_dtype, int64_t rows,
                                             int64_t out_features, int64_t in_features) {
   if (!known_dtype(dy_dtype) || !sizes_ok(rows, out_features, in_features)) return 0;
   const Plan plan = make_plan(dy_dtype, rows, out_features, in_features);
-  return plan.splits > 1 ? plan.splits * out_features * in_features * 4 : 0;
+  return plan.splits > 1 ? plan.splits * out_features * plan.part_k * 4 : 0;
 }
 
 extern "C" int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_dy, int64_t rows,
@@ -484,6 +600,7 @@ extern "C" int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_d
             plan.tiles_n,
             plan.tiles_k,
             plan.share,
+            plan.part_k,
             accumulate};
   float* partial = static_cast<float*>(workspace);
   if (dy_dtype == RIP_FP32)
