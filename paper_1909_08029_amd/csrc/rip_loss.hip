@@ -25,6 +25,8 @@ namespace {
 constexpr int kWave = 64;
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kStep = kThreads * kLane;  // elements of a workgroup's round
+constexpr int kRowThreads = 512;         // of the policy loss's one-launch form
+constexpr int kHold = 8;                 // units of a row that a lane of it keeps in registers
 constexpr float kLowest = -3.402823466e38f;
 
 // A row's largest logit and sum of e^(x - top).  sum == 0 only where every
@@ -49,6 +51,7 @@ __device__ __forceinline__ void add8(Stat& s, const float (&f)[kLane]) {
   s = {top, sum};
 }
 // The workgroup's joined pair, in every thread.
+template <int WAVES = kWaves>
 __device__ __forceinline__ Stat join_block(Stat s, Stat* shared) {
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) s = join(s, {__shfl_xor(s.top, o), __shfl_xor(s.sum, o)});
@@ -56,7 +59,7 @@ __device__ __forceinline__ Stat join_block(Stat s, Stat* shared) {
   __syncthreads();
   Stat r = shared[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) r = join(r, shared[w]);
+  for (int w = 1; w < WAVES; ++w) r = join(r, shared[w]);
   return r;
 }
 
@@ -123,13 +126,18 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
 // logit above -inf, which leaves the token out.
 template <int DT>
 __device__ __forceinline__ bool token_logp(const Rows& r, const typename Elem<DT>::T* logits,
-                                           const Stat* stat, int64_t t, int64_t target, Stat* s,
-                                           float* logp) {
-  *s = stat[t * r.splits];
-  for (int i = 1; i < r.splits; ++i) *s = join(*s, stat[t * r.splits + i]);
-  if (s->sum == 0.0f) return false;
-  *logp = Elem<DT>::load(logits + t * r.ld + target) - s->top - logf(s->sum);
+                                           const Stat& s, int64_t t, int64_t target, float* logp) {
+  if (s.sum == 0.0f) return false;
+  *logp = Elem<DT>::load(logits + t * r.ld + target) - s.top - logf(s.sum);
   return true;
+}
+// A row's pair from those of its splits, by `lanes` consecutive lanes (a power of
+// two); each of them gets it.
+__device__ __forceinline__ Stat row_stat(const Rows& r, const Stat* stat, int64_t t, int lanes) {
+  Stat s{kLowest, 0.0f};
+  for (int i = threadIdx.x & (lanes - 1); i < r.splits; i += lanes) s = join(s, stat[t * r.splits + i]);
+  for (int o = 1; o < lanes; o <<= 1) s = join(s, {__shfl_xor(s.top, o), __shfl_xor(s.sum, o)});
+  return s;
 }
 
 __device__ __forceinline__ double sum_block(double x, double* shared) {
@@ -147,13 +155,14 @@ __device__ __forceinline__ float log_sigmoid(float z) {
   return fminf(z, 0.0f) - log1pf(expf(-fabsf(z)));
 }
 
-// One workgroup a pair.  The sums over a sequence are held in 64 bits: they run
-// to thousands while the loss depends on differences of a few.
+// One workgroup a pair, `lanes` threads a token (they join its splits).  The sums
+// over a sequence are held in 64 bits: they run to thousands while the loss
+// depends on differences of a few.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void pairs_kernel(
     Rows r, const typename Elem<DT>::T* logits, const Stat* stat, const int32_t* offsets, int pairs,
-    const float* ref, float beta, float smoothing, float grad_scale, float* seq_logp, Token* token,
-    float* logp, double* pair_loss) {
+    const float* ref, float beta, float smoothing, float grad_scale, int lanes, float* seq_logp,
+    Token* token, float* logp, double* pair_loss) {
   __shared__ double shared[kWaves];
   int64_t at[3];
   for (int i = 0; i < 3; ++i) {  // within the tokens and ascending, whatever the offsets say
@@ -161,22 +170,29 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(
     o = o < 0 ? 0 : o > r.n ? r.n : o;
     at[i] = i && o < at[i - 1] ? at[i - 1] : o;
   }
+  const bool lead = (threadIdx.x & (lanes - 1)) == 0;
+  const int64_t begin = at[0] + threadIdx.x / lanes, round = kThreads / lanes;
+  double sum[2] = {0.0, 0.0};
+  Token mine = {0.0f, 0.0f, 0.0f, -1};  // of the first round, kept in registers
+  for (int64_t t = begin; t < at[2]; t += round) {
+    int64_t target;
+    if (!counts(r, t, &target)) continue;
+    const Stat s = row_stat(r, stat, t, lanes);
+    float lp;
+    if (!lead || !token_logp<DT>(r, logits, s, t, target, &lp)) continue;
+    sum[t >= at[1]] += lp;
+    if (logp) logp[t] = lp;
+    const Token k = {s.top, 1.0f / s.sum, 1.0f, (int)target};
+    if (t == begin)
+      mine = k;
+    else
+      token[t] = k;
+  }
   double margin[2];
   for (int q = 0; q < 2; ++q) {
-    double sum = 0.0;
-    for (int64_t t = at[q] + threadIdx.x; t < at[q + 1]; t += kThreads) {
-      int64_t target;
-      Stat s;
-      float lp;
-      if (!counts(r, t, &target) || !token_logp<DT>(r, logits, stat, t, target, &s, &lp)) continue;
-      sum += lp;
-      if (logp) logp[t] = lp;
-      token[t] = {s.top, 1.0f / s.sum, 1.0f, (int)target};
-    }
-    sum = sum_block(sum, shared);
-    const int q2 = 2 * blockIdx.x + q;
-    margin[q] = sum - (double)ref[q2];
-    if (threadIdx.x == 0) seq_logp[q2] = (float)sum;
+    const double all = sum_block(sum[q], shared);
+    margin[q] = all - (double)ref[2 * blockIdx.x + q];
+    if (threadIdx.x == 0) seq_logp[2 * blockIdx.x + q] = (float)all;
   }
   const float z = (float)((double)beta * (margin[0] - margin[1]));
   const float good = expf(log_sigmoid(z)), bad = expf(log_sigmoid(-z));
@@ -188,14 +204,14 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(
     if (smoothing > 0.0f) l -= (double)smoothing * log_sigmoid(-z);
     pair_loss[blockIdx.x] = l / pairs;
   }
-  for (int q = 0; q < 2; ++q)
-    for (int64_t t = at[q] + threadIdx.x; t < at[q + 1]; t += kThreads) {
-      Token k = token[t];
-      if (k.target < 0) continue;
-      k.coef = q ? -coef : coef;
-      k.scale *= -k.coef;
-      token[t] = k;
-    }
+  if (!lead) return;
+  for (int64_t t = begin; t < at[2]; t += round) {
+    Token k = t == begin ? mine : token[t];
+    if (k.target < 0) continue;
+    k.coef = t >= at[1] ? -coef : coef;
+    k.scale *= -k.coef;
+    token[t] = k;
+  }
 }
 
 struct Policy {
@@ -224,22 +240,139 @@ __device__ __forceinline__ float policy_token(const Policy& p, int64_t t, int64_
 template <int DT>
 __global__ __launch_bounds__(kThreads) void tokens_kernel(Rows r,
                                                           const typename Elem<DT>::T* logits,
-                                                          const Stat* stat, Policy p, Token* token,
-                                                          float* logp, double* part_loss) {
+                                                          const Stat* stat, Policy p, int lanes,
+                                                          Token* token, float* logp,
+                                                          double* part_loss) {
   __shared__ double shared[kWaves];
-  const int64_t t = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t t = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / lanes;
   double loss = 0.0;
   int64_t target;
-  Stat s;
-  float lp;
-  if (t < r.n && counts(r, t, &target) && token_logp<DT>(r, logits, stat, t, target, &s, &lp)) {
-    float coef;
-    loss = policy_token(p, t, r.n, lp, &coef);
-    if (logp) logp[t] = lp;
-    token[t] = {s.top, -coef / s.sum, coef, (int)target};
+  if (t < r.n && counts(r, t, &target)) {
+    const Stat s = row_stat(r, stat, t, lanes);
+    float lp;
+    if ((threadIdx.x & (lanes - 1)) == 0 && token_logp<DT>(r, logits, s, t, target, &lp)) {
+      float coef;
+      loss = policy_token(p, t, r.n, lp, &coef);
+      if (logp) logp[t] = lp;
+      token[t] = {s.top, -coef / s.sum, coef, (int)target};
+    }
   }
   loss = sum_block(loss, shared);
   if (threadIdx.x == 0) part_loss[blockIdx.x] = loss;
+}
+
+// A lane's eight elements as they lie in memory.
+template <int DT>
+struct Unit;
+template <>
+struct Unit<RIP_BF16> {
+  u32x4_any a;
+  __device__ __forceinline__ void load(const uint16_t* p) { a = *(const u32x4_any*)p; }
+  __device__ __forceinline__ void get(float (&f)[kLane]) const { Elem<RIP_BF16>::unpack8(a, f); }
+};
+template <>
+struct Unit<RIP_FP32> {
+  float v[kLane];
+  __device__ __forceinline__ void load(const float* p) { Elem<RIP_FP32>::load8(p, v); }
+  __device__ __forceinline__ void get(float (&f)[kLane]) const {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[j] = v[j];
+  }
+};
+
+// The policy loss of one token in one workgroup, gradient and all: coef needs
+// nothing beyond the token's own row.  The first kHold units of a lane stay in
+// registers between the two passes; the rest is read again, last first, mostly
+// from the caches: 8192 rows of 131072 bf16 took 1031 us in three launches.
+template <int DT>
+__global__ __launch_bounds__(kRowThreads) void policy_row_kernel(
+    Rows r, const typename Elem<DT>::T* logits, Policy p, float* logp, double* part,
+    typename Elem<DT>::T* grad, int64_t ld_grad) {
+  constexpr int kRound = kRowThreads * kLane;
+  __shared__ Stat shared[kRowThreads / kWave];
+  const int64_t t = blockIdx.x;
+  const int first = threadIdx.x * kLane, vocab = r.vocab;
+  const typename Elem<DT>::T* row = logits + t * r.ld;
+  typename Elem<DT>::T* out = grad + t * ld_grad;
+  float f[kLane], lp = 0.0f, coef = 0.0f;
+  Stat s{kLowest, 0.0f};
+  int64_t target;
+  double loss = 0.0;
+  Unit<DT> held[kHold];
+  const bool on = counts(r, t, &target);
+  const int whole = vocab - kLane;  // a unit from a column up to here is whole
+  if (on) {
+#pragma unroll
+    for (int u = 0; u < kHold; ++u)
+      if (first + u * kRound <= whole) held[u].load(row + first + u * kRound);
+#pragma unroll
+    for (int u = 0; u < kHold; ++u)
+      if (first + u * kRound <= whole) {
+        held[u].get(f);
+        add8(s, f);
+      }
+    int c = first + kHold * kRound;
+    for (; c + 3 * kRound <= whole; c += 4 * kRound) {
+      Unit<DT> next[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) next[u].load(row + c + u * kRound);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        next[u].get(f);
+        add8(s, f);
+      }
+    }
+    for (; c <= whole; c += kRound) {
+      Elem<DT>::load8(row + c, f);
+      add8(s, f);
+    }
+    // the last columns, fewer than a unit: one lane has them
+    const int rest = vocab / kLane * kLane;
+    if (rest < vocab && rest / kLane % kRowThreads == (int)threadIdx.x) {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j)
+        f[j] = rest + j < vocab ? Elem<DT>::load(row + rest + j) : -__builtin_huge_valf();
+      add8(s, f);
+    }
+    s = join_block<kRowThreads / kWave>(s, shared);
+    if (s.sum != 0.0f) {
+      lp = Elem<DT>::load(row + target) - s.top - logf(s.sum);
+      loss = policy_token(p, t, r.n, lp, &coef);
+    }
+  }
+  if (threadIdx.x == 0) {
+    part[t] = loss;
+    if (logp) logp[t] = lp;
+  }
+  if (!grad) return;
+  __syncthreads();  // in place, the target's logit has been read by now
+  if (coef == 0.0f) {
+    const float zero[kLane] = {};
+    for (int c = first; c < vocab; c += kRound) store_unit<DT>(out, c, vocab, zero);
+    return;
+  }
+  const float scale = -coef / s.sum;
+  const int at = (int)target;
+  auto finish = [&](int c) {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      f[j] = scale * exp_acc(f[j] - s.top);
+      if (c + j == at) f[j] += coef;
+    }
+    store_unit<DT>(out, c, vocab, f);
+  };
+  int c = first + (vocab - 1 - first) / kRound * kRound;
+  if (first < vocab)
+    for (; c >= first + kHold * kRound || (c > whole && c >= first); c -= kRound) {
+      load_unit<DT>(row, c, vocab, f);
+      finish(c);
+    }
+#pragma unroll
+  for (int u = kHold - 1; u >= 0; --u)
+    if (first + u * kRound <= whole) {
+      held[u].get(f);
+      finish(first + u * kRound);
+    }
 }
 
 // The loss: the sum of `parts` numbers, by one workgroup.
@@ -265,8 +398,10 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
                                                         float* loss) {
   __shared__ double shared[kWaves];
   if (blockIdx.x == 0) total_loss(part, parts, loss, shared);
-  const int64_t t = blockIdx.x / r.splits;
-  const int split = blockIdx.x - (uint32_t)t * r.splits;
+  // from the last row back: those that were read last are still in the caches
+  const uint32_t from_end = gridDim.x - 1 - blockIdx.x;
+  const int64_t t = from_end / r.splits;
+  const int split = from_end - (uint32_t)t * r.splits;
   const int end = min(r.vocab, (split + 1) * r.columns);
   const typename Elem<DT>::T* row = logits + t * r.ld;
   typename Elem<DT>::T* out = grad + t * ld_grad;
@@ -318,7 +453,16 @@ Work make_work(const Rows& r, int64_t parts, void* workspace) {
   w.bytes = at + (parts + 1) * (int64_t)sizeof(double);
   return w;
 }
-int64_t policy_parts(int64_t n) { return ceil_div(n, kThreads); }
+// Threads that join the splits of a row.
+int join_lanes(const Rows& r) {
+  int lanes = 1;
+  while (lanes < r.splits && lanes < kWave) lanes *= 2;
+  return lanes;
+}
+// The policy loss takes its one-launch form where the rows fill the card or are
+// short: a workgroup a row.  (512 rows of 32768: see the table of measurements.)
+bool one_launch(const Rows& r) { return r.n >= 512 || (r.n > 0 && r.vocab <= kHold * kRowThreads * kLane); }
+int64_t policy_parts(const Rows& r) { return one_launch(r) ? r.n : ceil_div(r.n * join_lanes(r), kThreads); }
 
 int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t ld, int64_t n,
                    int64_t vocab, const void* targets, int32_t id_type, const void* loss,
@@ -383,8 +527,9 @@ int32_t run_pref(Rows r, const void* logits, const int32_t* offsets, int pairs, 
   Work w = make_work(r, pairs, workspace);
   int32_t rc;
   if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
-  void* args[] = {&r,    &logits,    &w.stat,     &offsets,  &pairs,   &ref,  &beta,
-                  &smoothing, &grad_scale, &seq_logp, &w.token, &logp, &w.part};
+  int lanes = join_lanes(r);
+  void* args[] = {&r,          &logits, &w.stat,   &offsets, &pairs, &ref,   &beta, &smoothing,
+                  &grad_scale, &lanes,  &seq_logp, &w.token, &logp,  &w.part};
   if ((rc = launch((const void*)pairs_kernel<DT>, dim3((uint32_t)pairs), dim3(kThreads), args, 0,
                    stream, "rip_pref_loss: pairs")))
     return rc;
@@ -394,12 +539,22 @@ int32_t run_pref(Rows r, const void* logits, const int32_t* offsets, int pairs, 
 template <int DT>
 int32_t run_policy(Rows r, const void* logits, Policy p, float* loss, float* logp, void* grad,
                    int64_t ld_grad, void* workspace, void* stream) {
-  int parts = (int)policy_parts(r.n);
+  int parts = (int)policy_parts(r);
   Work w = make_work(r, parts, workspace);
   int32_t rc;
+  if (one_launch(r)) {
+    void* args[] = {&r, &logits, &p, &logp, &w.part, &grad, &ld_grad};
+    if ((rc = launch((const void*)policy_row_kernel<DT>, dim3((uint32_t)r.n), dim3(kRowThreads),
+                     args, 0, stream, "rip_policy_loss: rows")))
+      return rc;
+    void* total[] = {&w.part, &parts, &loss};
+    return launch((const void*)total_kernel, dim3(1), dim3(kThreads), total, 0, stream,
+                  "rip_policy_loss: total");
+  }
   if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
   if (r.n) {
-    void* args[] = {&r, &logits, &w.stat, &p, &w.token, &logp, &w.part};
+    int lanes = join_lanes(r);
+    void* args[] = {&r, &logits, &w.stat, &p, &lanes, &w.token, &logp, &w.part};
     if ((rc = launch((const void*)tokens_kernel<DT>, dim3((uint32_t)parts), dim3(kThreads), args, 0,
                      stream, "rip_policy_loss: tokens")))
       return rc;
@@ -420,8 +575,8 @@ extern "C" int64_t rip_pref_loss_workspace(int64_t n_tokens, int64_t vocab, int3
 }
 extern "C" int64_t rip_policy_loss_workspace(int64_t n_tokens, int64_t vocab) {
   if (n_tokens < 0 || n_tokens > RIP_MAX_TOKENS || vocab < 1 || vocab > RIP_MAX_WIDTH) return 0;
-  return make_work(make_rows(n_tokens, vocab, vocab, nullptr, 0), policy_parts(n_tokens), nullptr)
-      .bytes;
+  const Rows r = make_rows(n_tokens, vocab, vocab, nullptr, 0);
+  return make_work(r, policy_parts(r), nullptr).bytes;
 }
 
 extern "C" int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,

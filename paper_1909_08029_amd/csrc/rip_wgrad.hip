@@ -346,9 +346,23 @@ __global__ __launch_bounds__(Tl::kThreads, RESIDENT) void wgrad_kernel(
     whole = rows > 0 ? (int)(rows / kTokens) : 0;
   }
   f32x16 acc[MN][MK] = {};
+  // A last step of fewer rows goes first: its loads are on their way together with
+  // the first whole steps'.
+  typename Tl::Regs tail;
+  if (whole < steps)
+    Tl::load_checked(p, dy, codes, exps, n0, k0, t0 + (int64_t)whole * kTokens, t1, tail);
+  typename Tl::Regs regs[kStages];
+  typename Tl::Frags f0, f1;
+  auto product = [&](typename Tl::Regs& r) {
+    Tl::store(r, sh[0]);
+    lds_barrier();
+    Tl::read(sh[0], 0, wn, wk, lane, f0);
+    Tl::multiply(f0, acc);
+    Tl::read(sh[0], 16, wn, wk, lane, f1);
+    Tl::multiply(f1, acc);
+    lds_barrier();
+  };
   if (whole > 0) {
-    typename Tl::Regs regs[kStages];
-    typename Tl::Frags f0, f1;
     const typename Tl::Offsets off = Tl::offsets(p, n0, k0);
     const int row_x = p.blocks * kCkptBlock;
     typename Tl::Rows rows = {(const char*)(dy + t0 * p.ld_dy), (const char*)(codes + t0 * row_x),
@@ -375,7 +389,10 @@ __global__ __launch_bounds__(Tl::kThreads, RESIDENT) void wgrad_kernel(
       half<Tl, 1>(f1, acc, sh[later(now, 1)], 0, wn, wk, lane, f0, r, to, load);
       lds_barrier();
     };
+#pragma unroll
     for (int i = 0; i < kStages; ++i) load(regs[i]);
+    if (whole < steps) product(tail);
+#pragma unroll
     for (int i = 0; i < 2; ++i) {
       Tl::store(regs[i], sh[i]);
       load(regs[i]);
@@ -394,17 +411,11 @@ __global__ __launch_bounds__(Tl::kThreads, RESIDENT) void wgrad_kernel(
       if (++s == whole) break;
     }
   }
-  for (int s = whole; s < steps; ++s) {
-    typename Tl::Regs r;
-    typename Tl::Frags f;
-    Tl::load_checked(p, dy, codes, exps, n0, k0, t0 + (int64_t)s * kTokens, t1, r);
-    Tl::store(r, sh[0]);
-    lds_barrier();
-    Tl::read(sh[0], 0, wn, wk, lane, f);
-    Tl::multiply(f, acc);
-    Tl::read(sh[0], 16, wn, wk, lane, f);
-    Tl::multiply(f, acc);
-    lds_barrier();
+  // Steps that cannot be loaded without looking (rows of a few elements, no whole
+  // step): one by one.
+  for (int s = whole + (whole > 0); s < steps; ++s) {
+    if (s > 0) Tl::load_checked(p, dy, codes, exps, n0, k0, t0 + (int64_t)s * kTokens, t1, tail);
+    product(tail);
   }
 #pragma unroll
   for (int i = 0; i < MN; ++i)
