@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kBlockThreads) void pack_kernel(Shape s, const type
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float f[kLane];
-  load_unit<DT>(x + p.row * ld, p.col, s.width, f);
+  load_unit<DT, true>(x + p.row * ld, p.col, s.width, f);
   store_ckpt(out, p, f);
 }
 
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(kBlockThreads) void gate_forward_kernel(
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float g[kLane], u[kLane];
-  load_unit<DT>(gate + p.row * ld_gate, p.col, s.width, g);
-  load_unit<DT>(up + p.row * ld_up, p.col, s.width, u);
+  load_unit<DT, true>(gate + p.row * ld_gate, p.col, s.width, g);
+  load_unit<DT, true>(up + p.row * ld_up, p.col, s.width, u);
   store_ckpt(gate8, p, g);
   store_ckpt(up8, p, u);
 #pragma unroll
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kBlockThreads) void gate_backward_kernel(
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float d[kLane], g[kLane], u[kLane];
-  load_unit<DT>(dh + p.row * ld_dh, p.col, s.width, d);
+  load_unit<DT, true>(dh + p.row * ld_dh, p.col, s.width, d);
   load_ckpt(gate8, p, g);
   load_ckpt(up8, p, u);
   float a[kLane], h[kLane];

@@ -22,32 +22,48 @@ namespace {
 constexpr int kWave = 64;
 constexpr int kLookupBlock = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kSortItems = 4;                          // tokens of a thread
+constexpr int kSortItems = 8;                          // tokens of a thread
 constexpr int kChunk = kSortThreads * kSortItems;      // tokens sorted by one workgroup
 constexpr int kMaxDigit = 8;                           // bits of a pass of the sort
+constexpr int kBatch = 4;                              // rows that a wave loads together
 constexpr int kColumns = kWave * kLane;                // columns of a wave
+constexpr int kMergeThreads = 256;
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;     // the memory-side cache
+
 constexpr int kFillBytes = 1 << 16;                    // bytes zeroed by a workgroup of the fill
 
-template <int TD, int OD>
+// A thread handles eight columns of ROWS consecutive tokens, whose rows it loads
+// together.
+template <int TD, int OD, int ROWS>
 __global__ __launch_bounds__(kLookupBlock) void lookup_kernel(
     const typename Elem<TD>::T* table, int64_t vocab, int width, int64_t ld, const void* ids,
-    int wide, uint32_t units, FastDiv per_row, float scale, typename Elem<OD>::T* out,
+    int wide, int64_t n, uint32_t units, FastDiv per_row, float scale, typename Elem<OD>::T* out,
     int64_t ld_out) {
   const uint32_t unit = blockIdx.x * kLookupBlock + threadIdx.x;
   if (unit >= units) return;
-  const uint32_t t = per_row.div(unit);
-  const int c = (int)(unit - t * per_row.d) * kLane;
-  const int64_t id = load_id(ids, wide, t);
-  float f[kLane];
-  if (id >= 0 && id < vocab) {
-    load_unit<TD>(table + id * ld, c, width, f);
+  const uint32_t group = per_row.div(unit);
+  const int c = (int)(unit - group * per_row.d) * kLane;
+  const int64_t t = (int64_t)group * ROWS;
+  float f[ROWS][kLane];
+  int64_t id[ROWS];
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) f[j] *= scale;
-  } else {
+  for (int r = 0; r < ROWS; ++r) id[r] = t + r < n ? load_id(ids, wide, t + r) : -1;
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) f[j] = 0.0f;
+  for (int r = 0; r < ROWS; ++r) {
+    if (id[r] >= 0 && id[r] < vocab) {
+      load_unit<TD>(table + id[r] * ld, c, width, f[r]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) f[r][j] = 0.0f;
+    }
   }
-  store_unit<OD>(out + (int64_t)t * ld_out, c, width, f);
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    if (t + r >= n) break;
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) f[r][j] *= id[r] >= 0 && id[r] < vocab ? scale : 1.0f;
+    store_unit<OD>(out + (t + r) * ld_out, c, width, f[r]);
+  }
 }
 
 // Sort of up to kChunk (id, position) pairs by id in one workgroup: passes over
@@ -65,7 +81,8 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-__device__ void sort_chunk(SortShared& sh, int passes, int bits) {
+// `items` of each thread, the first items * kSortThreads of the chunk, take part.
+__device__ void sort_chunk(SortShared& sh, int items, int passes, int bits) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int buckets = 1 << bits, cells = kSortWaves << bits;
   const uint64_t below = ((uint64_t)1 << lane) - 1;
@@ -76,7 +93,8 @@ __device__ void sort_chunk(SortShared& sh, int passes, int bits) {
     uint16_t pos[kSortItems];
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
-      const int i = (wave * kSortItems + r) * kWave + lane;
+      if (r >= items) break;
+      const int i = (wave * items + r) * kWave + lane;
       key[r] = sh.key[i];
       pos[r] = sh.pos[i];
       const uint32_t d = (key[r] >> (p * bits)) & (buckets - 1);
@@ -122,6 +140,7 @@ __device__ void sort_chunk(SortShared& sh, int passes, int bits) {
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortItems; ++r) {
+      if (r >= items) break;
       const uint32_t d = (key[r] >> (p * bits)) & (buckets - 1);
       const uint32_t to = sh.count[d * kSortWaves + wave] + rank[r];
       sh.key[to] = key[r];
@@ -131,85 +150,128 @@ __device__ void sort_chunk(SortShared& sh, int passes, int bits) {
   }
 }
 
-// Workgroups below `chunks` each sort kChunk tokens (ids outside the vocabulary
-// become `vocab` and go last); the others zero the gradient's rows meanwhile,
-// which takes longer than the sort for all but the smallest tables.
-template <int GD>
-__global__ __launch_bounds__(kSortThreads) void sort_fill_kernel(
-    const void* ids, int wide, int64_t n, uint32_t vocab, int passes, int bits, int chunks,
-    uint32_t* sorted_id, uint32_t* sorted_pos, typename Elem<GD>::T* grad, int width, int64_t ld,
-    int rows_per_block) {
-  __shared__ SortShared sh;
-  const int tid = threadIdx.x;
-  if ((int)blockIdx.x < chunks) {
-    const int64_t base = (int64_t)blockIdx.x * kChunk;
-    const int count = (int)(n - base < kChunk ? n - base : kChunk);
-    for (int i = tid; i < kChunk; i += kSortThreads) {
-      int64_t id = i < count ? load_id(ids, wide, base + i) : (int64_t)vocab;
-      if (id < 0 || id > (int64_t)vocab) id = vocab;
-      sh.key[i] = (uint32_t)id;
-      sh.pos[i] = (uint16_t)i;
-    }
-    __syncthreads();
-    sort_chunk(sh, passes, bits);
-    for (int i = tid; i < count; i += kSortThreads) {
-      sorted_id[base + i] = sh.key[i];
-      sorted_pos[base + i] = (uint32_t)base + sh.pos[i];
-    }
-    return;
+// Bytes [p, end) become zeros; both are even addresses.
+template <bool STREAM>
+__device__ __forceinline__ void zero_range(char* p, char* end, int thread, int threads) {
+  const u32x4_any zero = {0, 0, 0, 0};
+  char* body = (char*)(((uintptr_t)p + 15) & ~(uintptr_t)15);
+  body = body < end ? body : end;
+  for (char* q = p + 2 * thread; q < body; q += 2 * threads) *(uint16_t*)q = 0;
+  char* q = body + 16 * thread;
+  for (; q + 16 <= end; q += 16 * threads) {
+    if constexpr (STREAM)
+      store_stream((u32x4_any*)q, zero);
+    else
+      *(u32x4_any*)q = zero;
   }
-  const int64_t row0 = (int64_t)(blockIdx.x - chunks) * rows_per_block;
-  const int64_t row1 = row0 + rows_per_block < vocab ? row0 + rows_per_block : vocab;
-  const float zero[kLane] = {};
-  if (ld == width) {  // rows without gaps are one range
-    typename Elem<GD>::T* p = grad + row0 * ld;
-    const int64_t m = (row1 - row0) * (int64_t)width;
-    for (int64_t c = (int64_t)tid * kLane; c < m; c += (int64_t)kSortThreads * kLane) {
-      if (c + kLane <= m) {
-        Elem<GD>::store8(p + c, zero);
-      } else {
-        for (int64_t j = c; j < m; ++j) Elem<GD>::store(p + j, 0.0f);
-      }
-    }
-  } else {
-    for (int64_t r = row0; r < row1; ++r)
-      for (int c = tid * kLane; c < width; c += kSortThreads * kLane)
-        store_unit<GD>(grad + r * ld, c, width, zero);
-  }
+  if (q < end)
+    for (; q < end; q += 2) *(uint16_t*)q = 0;
 }
 
-// Number of entries of a sorted run that come before `id` (equal ones too with
-// `after`).
-__device__ __forceinline__ int rank_in(const uint32_t* run, int n, uint32_t id, bool after) {
-  int lo = 0;
-  for (int len = n; len > 0;) {
-    const int half = len / 2;
-    const uint32_t x = run[lo + half];
-    if (x < id || (after && x == id)) {
-      lo += half + 1;
-      len -= half + 1;
-    } else {
-      len = half;
+// Rows of the gradient that a launch zeroes beside its other work, a run of them to
+// a workgroup.
+struct Fill {
+  void* grad;
+  int64_t vocab, ld;
+  int width, rows;  // rows of a workgroup
+  int stream;       // past the caches
+  int64_t first;    // run of the launch's first such workgroup
+};
+template <int GD, int THREADS, bool STREAM>
+__device__ __forceinline__ void zero_rows(const Fill& z, int64_t run) {
+  const int64_t row0 = (z.first + run) * z.rows;
+  const int64_t row1 = row0 + z.rows < z.vocab ? row0 + z.rows : z.vocab;
+  constexpr int kSize = sizeof(typename Elem<GD>::T);
+  char* grad = static_cast<char*>(z.grad);
+  const int tid = threadIdx.x;
+  if (z.ld == z.width) {  // rows without gaps are one range
+    zero_range<STREAM>(grad + row0 * z.ld * kSize, grad + row1 * z.ld * kSize, tid, THREADS);
+  } else {  // a wave a row
+    for (int64_t r = row0 + tid / kWave; r < row1; r += THREADS / kWave) {
+      char* p = grad + r * z.ld * kSize;
+      zero_range<STREAM>(p, p + (int64_t)z.width * kSize, tid % kWave, kWave);
     }
   }
-  return lo;
+}
+template <int GD, int THREADS>
+__device__ __forceinline__ void zero_rows(const Fill& z, int64_t run) {
+  if (z.stream)
+    zero_rows<GD, THREADS, true>(z, run);
+  else
+    zero_rows<GD, THREADS, false>(z, run);
+}
+
+// Workgroups below `chunks` each sort kChunk tokens (ids outside the vocabulary
+// become `vocab` and go last); the others zero rows of the gradient meanwhile.
+template <int GD>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(
+    const void* ids, int wide, int64_t n, uint32_t vocab, int passes, int bits, int chunks,
+    uint32_t* sorted_id, uint32_t* sorted_pos, Fill fill) {
+  __shared__ SortShared sh;
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= chunks) {
+    zero_rows<GD, kSortThreads>(fill, blockIdx.x - chunks);
+    return;
+  }
+  const int64_t base = (int64_t)blockIdx.x * kChunk;
+  const int count = (int)(n - base < kChunk ? n - base : kChunk);
+  const int items = (count + kSortThreads - 1) / kSortThreads;
+  for (int i = tid; i < items * kSortThreads; i += kSortThreads) {
+    int64_t id = i < count ? load_id(ids, wide, base + i) : (int64_t)vocab;
+    if (id < 0 || id > (int64_t)vocab) id = vocab;
+    sh.key[i] = (uint32_t)id;
+    sh.pos[i] = (uint16_t)i;
+  }
+  __syncthreads();
+  sort_chunk(sh, items, passes, bits);
+  for (int i = tid; i < count; i += kSortThreads) {
+    sorted_id[base + i] = sh.key[i];
+    sorted_pos[base + i] = (uint32_t)base + sh.pos[i];
+  }
 }
 
 // The sorted chunks become one sorted list: an entry's place is its place in its
 // own chunk and its rank in every other (equal ids of earlier chunks go first).
-__global__ __launch_bounds__(256) void merge_kernel(const uint32_t* id_in, const uint32_t* pos_in,
-                                                    int64_t n, int chunks, uint32_t* id_out,
-                                                    uint32_t* pos_out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// Eight chunks are searched side by side, a halving of all of them at a time, as
+// the loads of one search wait for each other.  Workgroups from `merges` on zero
+// rows of the gradient.
+template <int GD>
+__global__ __launch_bounds__(kMergeThreads) void merge_kernel(
+    const uint32_t* id_in, const uint32_t* pos_in, int64_t n, int chunks, uint32_t* id_out,
+    uint32_t* pos_out, int merges, Fill fill) {
+  if ((int)blockIdx.x >= merges) {
+    zero_rows<GD, kMergeThreads>(fill, blockIdx.x - merges);
+    return;
+  }
+  constexpr int kSide = 8;
+  const int64_t i = (int64_t)blockIdx.x * kMergeThreads + threadIdx.x;
   if (i >= n) return;
   const int own = (int)(i / kChunk);
   const uint32_t id = id_in[i];
   int64_t at = i - (int64_t)own * kChunk;
-  for (int c = 0; c < chunks; ++c) {
-    if (c == own) continue;
-    const int64_t base = (int64_t)c * kChunk;
-    const int len = (int)(n - base < kChunk ? n - base : kChunk);
-    at += rank_in(id_in + base, len, id, c < own);
+  for (int c0 = 0; c0 < chunks; c0 += kSide) {
+    int rank[kSide];
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) rank[u] = 0;
+    // rank = entries below `id`, or up to it in earlier chunks: of 2 * half left
+    // to look at, the first half goes if its last entry does
+    for (int half = kChunk; half > 0; half /= 2) {
+      uint32_t x[kSide];
+      int last[kSide];
+#pragma unroll
+      for (int u = 0; u < kSide; ++u) {
+        last[u] = (c0 + u) * kChunk + rank[u] + half - 1;
+        x[u] = id_in[min(last[u], (int)n - 1)];
+      }
+#pragma unroll
+      for (int u = 0; u < kSide; ++u) {
+        const bool goes = x[u] < id || (x[u] == id && c0 + u < own);
+        rank[u] += goes && rank[u] + half <= kChunk && last[u] < n ? half : 0;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kSide; ++u)
+      if (c0 + u < chunks && c0 + u != own) at += rank[u];
   }
   id_out[at] = id;
   pos_out[at] = pos_in[i];
@@ -235,87 +297,135 @@ __device__ __forceinline__ void write_row(typename Elem<GD>::T* row, int c, int 
 // that begins here and goes on to slot 1.
 template <int DD, int GD>
 __global__ __launch_bounds__(kWave) void sum_kernel(
-    const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id, const uint32_t* pos,
-    int64_t n, uint32_t vocab, int per, float scale, typename Elem<GD>::T* grad, int width,
-    int64_t ld, int accumulate, float* partial) {
+    const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id_list,
+    const uint32_t* pos_list, int64_t n, uint32_t vocab, int per, float scale,
+    typename Elem<GD>::T* grad, int width, int64_t ld, int accumulate, float* partial) {
+  // the lists are not written while this runs: scalar loads
+  const RIP_CONST uint32_t* id = (const RIP_CONST uint32_t*)id_list;
+  const RIP_CONST uint32_t* pos = (const RIP_CONST uint32_t*)pos_list;
   const int64_t a = (int64_t)blockIdx.x * per;
   const int64_t b = a + per < n ? a + per : n;
   const int c = blockIdx.y * kColumns + threadIdx.x * kLane;
   if (id[a] >= vocab) return;  // only ids outside the vocabulary from here on
   float acc[kLane] = {};
   bool begins = a == 0 || id[a - 1] != id[a];
-  for (int64_t i = a; i < b; ++i) {
-    const uint32_t v = id[i];
-    if (v >= vocab) break;
-    float f[kLane] = {};
-    if (c < width) load_unit<DD>(dout + (int64_t)pos[i] * ld_dout, c, width, f);
+  for (int64_t i0 = a; i0 < b; i0 += kBatch) {
+    float f[kBatch][kLane];
+    uint32_t v[kBatch + 1];
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) acc[j] += f[j];
-    const bool ends = i + 1 >= n || id[i + 1] != v;
-    if (!ends && i + 1 < b) continue;
-    if (c < width) {
-      if (begins && ends) {
-        write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
-      } else {
-        float* p = partial + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * width;
-        store_unit<RIP_FP32>(p, c, width, acc);
-      }
+    for (int u = 0; u <= kBatch; ++u) v[u] = i0 + u < n ? id[i0 + u] : vocab;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      if (i0 + u < b && v[u] < vocab && c < width)
+        load_unit<DD, true>(dout + (int64_t)pos[i0 + u] * ld_dout, c, width, f[u]);
     }
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) acc[j] = 0.0f;
-    begins = true;
+    for (int u = 0; u < kBatch; ++u) {
+      if (i0 + u >= b || v[u] >= vocab) break;
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) acc[j] += f[u][j];
+      const bool ends = v[u + 1] != v[u];
+      if (!ends && i0 + u + 1 < b) continue;
+      if (c < width) {
+        if (begins && ends) {
+          write_row<GD>(grad + (int64_t)v[u] * ld, c, width, scale, accumulate, acc);
+        } else {
+          float* p = partial + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * width;
+          store_unit<RIP_FP32>(p, c, width, acc);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) acc[j] = 0.0f;
+      begins = true;
+    }
   }
 }
 
 constexpr int kJoinWaves = 8;
+constexpr int kShortRun = 16;  // partial sums that one wave adds
 
-// The workgroup of the wave in which a long run begins adds that run's partial
-// sums: its own slot 1 and slot 0 of the waves that the run passes through.
+// Runs that pass the end of a wave's entries: a workgroup looks at the ends of
+// kJoinWaves waves of the sum, one each of its own, and adds up the partial sums of
+// the runs that begin in those: slot 1 of the wave where a run begins and slot 0 of
+// those that it passes through.  A wave adds a short run alone; a long one is
+// shared by all waves of the workgroup.
 template <int GD>
 __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
     const uint32_t* id, int64_t n, uint32_t vocab, int per, int waves, const float* partial,
     float scale, typename Elem<GD>::T* grad, int width, int64_t ld, int accumulate) {
   __shared__ float part[kJoinWaves][kColumns];
-  const int64_t a = (int64_t)blockIdx.x * per;
-  const int64_t b = a + per;
-  if (b >= n) return;
-  const uint32_t v = id[b - 1];
-  if (v >= vocab || id[b] != v) return;       // the last run ends here
-  if (id[a] == v && a > 0 && id[a - 1] == v) return;  // it began in an earlier wave
+  __shared__ int run_last[kJoinWaves];
+  __shared__ uint32_t run_id[kJoinWaves];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  // last wave that the run reaches: the first whose own last entry differs
-  int last = blockIdx.x + 1;
-  for (;; last += kWave) {
-    const int w = last + lane;
-    const int64_t end = ((int64_t)w + 1) * per < n ? ((int64_t)w + 1) * per : n;
-    const bool on = w < waves - 1 && id[end - 1] == v && id[end] == v;
-    const uint64_t stop = ~__ballot(on);
-    if (stop) {
-      last += __ffsll((unsigned long long)stop) - 1;
-      break;
-    }
-  }
   const int c = blockIdx.y * kColumns + lane * kLane;
-  const int count = last - (int)blockIdx.x;  // partial sums after the first
-  const int share = (count + kJoinWaves - 1) / kJoinWaves;
-  float acc[kLane] = {}, f[kLane];
-  if (c < width) {
-    if (wave == 0) load_unit<RIP_FP32>(partial + ((int64_t)blockIdx.x * 2 + 1) * width, c, width, acc);
-    const int w1 = min(count, (wave + 1) * share);
-    for (int w = wave * share; w < w1; ++w) {
-      load_unit<RIP_FP32>(partial + ((int64_t)blockIdx.x + 1 + w) * 2 * width, c, width, f);
+  {
+    const int64_t own = (int64_t)blockIdx.x * kJoinWaves + wave, a = own * per, b = a + per;
+    int last = -1;  // last wave that the run reaches
+    uint32_t v = 0;
+    if (b < n) {
+      v = id[b - 1];
+      const bool goes_on = id[b] == v, began = id[a] != v || a == 0 || id[a - 1] != v;
+      if (v < vocab && goes_on && began) {
+        last = (int)own + 1;
+        for (;; last += kWave) {  // the first whose own last entry ends the run
+          const int w = last + lane;
+          const int64_t end = ((int64_t)w + 1) * per;
+          const bool on = w < waves - 1 && id[end - 1] == v && id[end] == v;
+          const uint64_t stop = ~__ballot(on);
+          if (stop) {
+            last += __ffsll((unsigned long long)stop) - 1;
+            break;
+          }
+        }
+      }
+    }
+    const int count = last - (int)own;
+    if (last >= 0 && count <= kShortRun) {
+      if (c < width) {
+        float acc[kLane], f[kLane];
+        load_unit<RIP_FP32>(partial + (own * 2 + 1) * width, c, width, acc);
+#pragma unroll 4
+        for (int w = 1; w <= count; ++w) {
+          load_unit<RIP_FP32>(partial + (own + w) * 2 * width, c, width, f);
 #pragma unroll
-      for (int j = 0; j < kLane; ++j) acc[j] += f[j];
+          for (int j = 0; j < kLane; ++j) acc[j] += f[j];
+        }
+        write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
+      }
+      last = -1;
+    }
+    if (lane == 0) {
+      run_last[wave] = last;
+      run_id[wave] = v;
     }
   }
-#pragma unroll
-  for (int j = 0; j < kLane; ++j) part[wave][lane * kLane + j] = acc[j];
   __syncthreads();
-  if (wave != 0 || c >= width) return;
-  for (int w = 1; w < kJoinWaves; ++w)
+  for (int r = 0; r < kJoinWaves; ++r) {
+    const int last = run_last[r], first = blockIdx.x * kJoinWaves + r;
+    if (last < 0) continue;
+    const int count = last - first;  // partial sums after the first
+    float acc[kLane] = {}, f[kLane];
+    if (c < width) {
+      if (wave == 0) load_unit<RIP_FP32>(partial + ((int64_t)first * 2 + 1) * width, c, width, acc);
+      const int w1 = (wave + 1) * count / kJoinWaves;
+#pragma unroll 4
+      for (int w = wave * count / kJoinWaves; w < w1; ++w) {
+        load_unit<RIP_FP32>(partial + ((int64_t)first + 1 + w) * 2 * width, c, width, f);
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) acc[j] += part[w][lane * kLane + j];
-  write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
+        for (int j = 0; j < kLane; ++j) acc[j] += f[j];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) part[wave][lane * kLane + j] = acc[j];
+    __syncthreads();
+    if (wave == 0 && c < width) {
+      for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+        for (int j = 0; j < kLane; ++j) acc[j] += part[w][lane * kLane + j];
+      write_row<GD>(grad + (int64_t)run_id[r] * ld, c, width, scale, accumulate, acc);
+    }
+    __syncthreads();
+  }
 }
 
 // Entries of the sorted list that a wave adds up.
@@ -340,6 +450,11 @@ GradPlan grad_plan(int64_t n, int64_t width) {
   // ids and positions, once more where chunks are merged, and the partial sums
   p.total = p.id_bytes * (p.chunks > 1 ? 4 : 2) + p.partial_bytes;
   return p;
+}
+
+template <int TD, int OD>
+const void* lookup_of(bool many) {
+  return many ? (const void*)lookup_kernel<TD, OD, 4> : (const void*)lookup_kernel<TD, OD, 1>;
 }
 
 int32_t check_ids(const void* ids, int32_t id_type, int64_t n) {
@@ -402,17 +517,18 @@ extern "C" int32_t rip_embed_lookup(const void* table, int32_t table_dtype, int6
   if (n_tokens * per_row >= (int64_t)1 << 31)
     return fail(RIP_E_UNSUPPORTED, "%lld tokens of width %lld are above the limit",
                 (long long)n_tokens, (long long)width);
-  uint32_t units = (uint32_t)(n_tokens * per_row);
+  // four rows to a thread where that leaves the card full
+  const bool many = n_tokens * per_row >= (int64_t)1 << 19;
+  uint32_t units = (uint32_t)(ceil_div(n_tokens, many ? 4 : 1) * per_row);
   FastDiv div = FastDiv::make((uint32_t)per_row);
   int w = (int)width, wide = id_type == RIP_INT64;
-  void* args[] = {&table, &vocab, &w,     &ld_table, &ids, &wide,
-                  &units, &div,   &scale, &out,      &ld_out};
-  const void* fn =
-      table_dtype == RIP_FP32
-          ? (out_dtype == RIP_FP32 ? (const void*)lookup_kernel<RIP_FP32, RIP_FP32>
-                                   : (const void*)lookup_kernel<RIP_FP32, RIP_BF16>)
-          : (out_dtype == RIP_FP32 ? (const void*)lookup_kernel<RIP_BF16, RIP_FP32>
-                                   : (const void*)lookup_kernel<RIP_BF16, RIP_BF16>);
+  void* args[] = {&table, &vocab, &w,   &ld_table, &ids, &wide, &n_tokens,
+                  &units, &div,   &scale, &out,    &ld_out};
+  const void* fn = table_dtype == RIP_FP32
+                       ? (out_dtype == RIP_FP32 ? lookup_of<RIP_FP32, RIP_FP32>(many)
+                                                : lookup_of<RIP_FP32, RIP_BF16>(many))
+                       : (out_dtype == RIP_FP32 ? lookup_of<RIP_BF16, RIP_FP32>(many)
+                                                : lookup_of<RIP_BF16, RIP_BF16>(many));
   return launch(fn, dim3((uint32_t)ceil_div(units, kLookupBlock)), dim3(kLookupBlock), args, 0,
                 stream, "rip_embed_lookup");
 }
@@ -466,23 +582,33 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
   int bits = (key_bits + passes - 1) / passes;
   int w = (int)width, wide = id_type == RIP_INT64;
   uint32_t v32 = (uint32_t)vocab;
-  int rows_per_block = (int)(kFillBytes / (width * elem_bytes(grad_dtype)));
-  if (rows_per_block < 1) rows_per_block = 1;
-  const int64_t fill = accumulate ? 0 : ceil_div(vocab, rows_per_block);
+  // Zeros that the memory-side cache holds stay there until the sums come (a table
+  // of 206 MB: 64 us against 72 past it); more go past it (537 MB: 281 against 290).
+  const bool stream_zeros = vocab * width * elem_bytes(grad_dtype) > kCacheBytes;
+  Fill fill{grad, vocab, ld_grad, w, (int)(kFillBytes / (width * elem_bytes(grad_dtype))),
+            stream_zeros, 0};
+  if (fill.rows < 1) fill.rows = 1;
+  // Runs of rows to zero, all beside the sort, or a third of them beside the merge.
+  const int64_t runs = accumulate ? 0 : ceil_div(vocab, fill.rows);
+  const int64_t later = p.chunks > 1 ? runs / 3 : 0;
   {
-    void* args[] = {&ids,  &wide,  &n_tokens, &v32, &passes,  &bits,          &p.chunks,
-                    &id_a, &pos_a, &grad,     &w,   &ld_grad, &rows_per_block};
-    const void* fn = grad_dtype == RIP_FP32 ? (const void*)sort_fill_kernel<RIP_FP32>
-                                            : (const void*)sort_fill_kernel<RIP_BF16>;
-    if ((rc = launch(fn, dim3((uint32_t)(p.chunks + fill)), dim3(kSortThreads), args, 0, stream,
-                     "rip_embed_grad: sort")))
+    void* args[] = {&ids,  &wide,     &n_tokens, &v32,   &passes,
+                    &bits, &p.chunks, &id_a,     &pos_a, &fill};
+    const void* fn = grad_dtype == RIP_FP32 ? (const void*)sort_kernel<RIP_FP32>
+                                            : (const void*)sort_kernel<RIP_BF16>;
+    if ((rc = launch(fn, dim3((uint32_t)(p.chunks + runs - later)), dim3(kSortThreads), args, 0,
+                     stream, "rip_embed_grad: sort")))
       return rc;
   }
   if (n_tokens == 0) return RIP_OK;
   if (p.chunks > 1) {
-    void* args[] = {&id_a, &pos_a, &n_tokens, &p.chunks, &id_b, &pos_b};
-    if ((rc = launch((const void*)merge_kernel, dim3((uint32_t)ceil_div(n_tokens, 256)), dim3(256),
-                     args, 0, stream, "rip_embed_grad: merge")))
+    int merges = (int)ceil_div(n_tokens, kMergeThreads);
+    fill.first = runs - later;
+    void* args[] = {&id_a, &pos_a, &n_tokens, &p.chunks, &id_b, &pos_b, &merges, &fill};
+    const void* fn = grad_dtype == RIP_FP32 ? (const void*)merge_kernel<RIP_FP32>
+                                            : (const void*)merge_kernel<RIP_BF16>;
+    if ((rc = launch(fn, dim3((uint32_t)(merges + later)), dim3(kMergeThreads), args, 0, stream,
+                     "rip_embed_grad: merge")))
       return rc;
   }
   const uint32_t columns = (uint32_t)ceil_div(width, kColumns);
@@ -504,6 +630,6 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
                   &scale, &grad,    &w,   &ld_grad, &accumulate};
   const void* fn = grad_dtype == RIP_FP32 ? (const void*)join_kernel<RIP_FP32>
                                           : (const void*)join_kernel<RIP_BF16>;
-  return launch(fn, dim3((uint32_t)p.waves, columns), dim3(kWave * kJoinWaves), args, 0, stream,
-                "rip_embed_grad: join");
+  return launch(fn, dim3((uint32_t)ceil_div(p.waves, kJoinWaves), columns), dim3(kWave * kJoinWaves),
+                args, 0, stream, "rip_embed_grad: join");
 }

@@ -8,6 +8,10 @@
 
 #include "rip_internal.h"
 
+// Address space of data that nothing writes while a kernel runs: wave-uniform reads
+// of it are scalar loads.
+#define RIP_CONST __attribute__((address_space(4)))
+
 namespace rip {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -16,6 +20,19 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // Sixteen bytes at any address that an element may have: rows of odd length
 // start anywhere, and gfx950 loads and stores 16 bytes at any alignment.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+// Sixteen bytes past the caches (non-temporal), for data of which a launch writes
+// or reads more than a cache holds, once: the gated unit of 16384 x 5504 bf16 took
+// 251 us without, 242 with such stores, 218 with such loads too; the policy loss
+// of 8192 x 131072 bf16 840 and 777 with such stores. Not for fp32, where a lane's
+// 32 bytes are two accesses and each covers half of every cache line: zeroing a
+// table's gradient took 1.7 times as long so.
+__device__ __forceinline__ void store_stream(u32x4_any* p, u32x4_any v) {
+  __builtin_nontemporal_store(v, p);
+}
+__device__ __forceinline__ u32x4 load_stream(const u32x4_any* p) {
+  return __builtin_nontemporal_load(p);
+}
 
 // Eight consecutive elements are what one lane handles of a row: 16 bytes of
 // bf16, 32 of fp32.
@@ -28,6 +45,7 @@ struct Elem<RIP_FP32> {
   typedef float T;
   static __device__ __forceinline__ float load(const T* p) { return *p; }
   static __device__ __forceinline__ void store(T* p, float x) { *p = x; }
+  template <bool STREAM = false>
   static __device__ __forceinline__ void load8(const T* p, float (&f)[kLane]) {
     const u32x4_any a = *(const u32x4_any*)p, b = *(const u32x4_any*)(p + 4);
 #pragma unroll
@@ -66,23 +84,25 @@ struct Elem<RIP_BF16> {
       f[2 * j + 1] = __uint_as_float(a[j] & 0xffff0000u);
     }
   }
+  template <bool STREAM = false>
   static __device__ __forceinline__ void load8(const T* p, float (&f)[kLane]) {
-    unpack8(*(const u32x4_any*)p, f);
+    const u32x4 a = STREAM ? load_stream((const u32x4_any*)p) : *(const u32x4_any*)p;
+    unpack8(a, f);
   }
   static __device__ __forceinline__ void store8(T* p, const float (&f)[kLane]) {
     u32x4_any a;
 #pragma unroll
     for (int j = 0; j < 4; ++j) a[j] = pack2(f[2 * j], f[2 * j + 1]);
-    *(u32x4_any*)p = a;
+    store_stream((u32x4_any*)p, a);
   }
 };
 
 // Elements c .. c+7 of a row of `width`; zero past its end, nothing read there.
-template <int DT>
+template <int DT, bool STREAM = false>
 __device__ __forceinline__ void load_unit(const typename Elem<DT>::T* row, int c, int width,
                                           float (&f)[kLane]) {
   if (c + kLane <= width) {
-    Elem<DT>::load8(row + c, f);
+    Elem<DT>::template load8<STREAM>(row + c, f);
   } else {
 #pragma unroll
     for (int j = 0; j < kLane; ++j) f[j] = c + j < width ? Elem<DT>::load(row + c + j) : 0.0f;
