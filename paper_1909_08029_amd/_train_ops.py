@@ -16,7 +16,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import RIP_BF16, RIP_FP32, _check, _stream_ptr, lib
+from . import RIP_BF16, RIP_FP32, _check, _raw_stream, _stream_ptr, lib
 
 _CODES = {torch.float32: RIP_FP32, torch.bfloat16: RIP_BF16}
 _IDS = {torch.int32: 0, torch.int64: 1}
@@ -52,30 +52,51 @@ def _declare():
 _declare()
 
 
-def _here(t, name: str):
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} must be on the current CUDA device, not {t.device}")
+# The checks below run on every call of a training loop or a decoding step, so they
+# ask each tensor for as little as possible and torch's bookkeeping only once.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _matrix(t, name: str):
+def _device() -> int:
+    """The current device; -2 (no tensor's) while CUDA is not in use."""
+    return _current_device() if torch.cuda.is_initialized() else -2
+
+
+def _stream(stream, dev: int):
+    """Raw stream of a call: torch's current one unless given."""
+    if stream is None and dev >= 0 and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream_ptr(stream)
+
+
+def _elsewhere(t, name: str):
+    raise ValueError(f"{name} must be on the current CUDA device, not {t.device}")
+
+
+def _matrix(t, name: str, dev: int):
     """(pointer, type, rows, width, row stride) of a tensor taken as rows."""
-    _here(t, name)
+    if t.get_device() != dev:
+        _elsewhere(t, name)
     code = _CODES.get(t.dtype)
     if code is None:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-    if t.dim() != 2:
-        if t.dim() < 2:
+    shape = t.shape
+    if len(shape) != 2:
+        if len(shape) < 2:
             raise ValueError(f"{name} must have at least two dimensions")
-        t = t.view(-1, t.shape[-1])
-    rows, width = t.shape
-    if rows and width > 1 and t.stride(1) != 1:
+        t = t.view(-1, shape[-1])
+        shape = t.shape
+    rows, width = shape
+    ld, dense = t.stride()
+    if dense != 1 and width > 1 and rows:
         raise ValueError(f"{name}: the last dimension must be dense")
-    return t.data_ptr(), code, rows, width, t.stride(0) if rows > 1 else width
+    return t.data_ptr(), code, rows, width, ld if rows > 1 else width
 
 
-def _ids(t, name: str):
+def _ids(t, name: str, dev: int):
     """(pointer, type, count) of a dense tensor of ids."""
-    _here(t, name)
+    if t.get_device() != dev:
+        _elsewhere(t, name)
     code = _IDS.get(t.dtype)
     if code is None:
         raise TypeError(f"{name}: ids are int32 or int64, not {t.dtype}")
@@ -84,36 +105,43 @@ def _ids(t, name: str):
     return t.data_ptr(), code, t.numel()
 
 
-def _floats(t, name: str, n: int):
+def _floats(t, name: str, n: int, dev: int):
     """Pointer of n dense fp32 values; None passes."""
     if t is None:
         return None
-    _here(t, name)
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+    if t.get_device() != dev:
+        _elsewhere(t, name)
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must hold {n} contiguous float32 values")
     return t.data_ptr()
 
 
-def _empty(shape, dtype, stream):
-    """A tensor of the pool of the stream that uses it."""
+def _empty(like, shape, dtype, stream):
+    """A tensor on the device of `like`, of the pool of the stream that uses it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device="cuda")
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _workspace(nbytes: int, stream):
+def _empty_like(like, stream):
+    """A dense tensor of the shape and dtype of `like`."""
+    if stream is None:
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(like, memory_format=torch.contiguous_format)
+
+
+def _workspace(nbytes: int, like, stream):
     """(tensor that keeps it, address) of a call's workspace."""
     if nbytes == 0:
         return None, None
-    t = _empty((nbytes,), torch.uint8, stream)
+    t = _empty(like, (nbytes,), torch.uint8, stream)
     return t, t.data_ptr()
 
 
-def _out(given, shape, dtype, name: str, stream):
-    if given is None:
-        return _empty(shape, dtype, stream)
-    if tuple(given.shape) != tuple(shape):
+def _shaped(given, shape, name: str):
+    if given.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(given.shape)}")
     return given
 
@@ -124,12 +152,19 @@ def _out(given, shape, dtype, name: str, stream):
 def rip_embed_lookup(table, ids, scale: float = 1.0, dtype=None, out=None, stream=None):
     """scale * table[ids], of ``dtype`` (default: the table's); rows of zeros for
     ids outside the table.  Returns a tensor of shape ids.shape + (width,)."""
-    tp, tc, vocab, width, ld = _matrix(table, "table")
-    ip, ic, n = _ids(ids, "ids")
-    out = _out(out, (*ids.shape, width), dtype or table.dtype, "out", stream)
-    op, oc, _, _, ld_out = _matrix(out if out.dim() > 1 else out.view(1, -1), "out")
-    _check(lib.rip_embed_lookup(tp, tc, vocab, width, ld, ip, ic, n, scale, op, oc, ld_out,
-                                _stream_ptr(stream)))
+    dev = _device()
+    tp, tc, vocab, width, ld = _matrix(table, "table", dev)
+    ip, ic, n = _ids(ids, "ids", dev)
+    shape = (*ids.shape, width)
+    if out is None:
+        out = _empty(table, shape, dtype or table.dtype, stream)
+    else:
+        _shaped(out, shape, "out")
+    op, oc, _, _, ld_out = _matrix(out if len(shape) > 1 else out.view(1, -1), "out", dev)
+    rc = lib.rip_embed_lookup(tp, tc, vocab, width, ld, ip, ic, n, scale, op, oc, ld_out,
+                              _stream(stream, dev))
+    if rc:
+        _check(rc)
     return out
 
 
@@ -137,15 +172,18 @@ def rip_embed_grad(dout, ids, grad, scale: float = 1.0, accumulate: bool = False
     """Gradient of rip_embed_lookup's table into ``grad`` (a replica's gradient
     segment, say): every row is written, or with ``accumulate`` the rows of the
     ids are added to.  Returns grad."""
-    dp, dc, rows, width, ld = _matrix(dout if dout.dim() > 1 else dout.view(1, -1), "dout")
-    ip, ic, n = _ids(ids, "ids")
-    gp, gc, vocab, width_g, ld_g = _matrix(grad, "grad")
+    dev = _device()
+    dp, dc, rows, width, ld = _matrix(dout if dout.dim() > 1 else dout.view(1, -1), "dout", dev)
+    ip, ic, n = _ids(ids, "ids", dev)
+    gp, gc, vocab, width_g, ld_g = _matrix(grad, "grad", dev)
     if rows != n or width != width_g:
         raise ValueError(f"dout is {rows} x {width} for {n} ids and a table of width {width_g}")
     nbytes = lib.rip_embed_grad_workspace(n, width)
-    _keep, ws = _workspace(nbytes, stream)
-    _check(lib.rip_embed_grad(dp, dc, ld, ip, ic, n, scale, gp, gc, vocab, width, ld_g,
-                              int(accumulate), ws, nbytes, _stream_ptr(stream)))
+    _keep, ws = _workspace(nbytes, grad, stream)
+    rc = lib.rip_embed_grad(dp, dc, ld, ip, ic, n, scale, gp, gc, vocab, width, ld_g,
+                            1 if accumulate else 0, ws, nbytes, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return grad
 
 
@@ -155,9 +193,10 @@ def rip_embed_grad(dout, ids, grad, scale: float = 1.0, accumulate: bool = False
 class Ckpt:
     """A matrix of activations kept in 8 bits (format: include/rip.h): ``codes``
     int8 [rows, 32 * blocks], ``exps`` uint8 [rows, blocks], blocks =
-    ceil(width / 32)."""
+    ceil(width / 32).  Made from such tensors, or by the calls below, which keep
+    both in one buffer."""
 
-    __slots__ = ("codes", "exps", "rows", "width")
+    __slots__ = ("rows", "width", "_codes", "_exps", "_buffer", "_at", "_ptrs", "_dev")
 
     def __init__(self, codes, exps, width: int):
         blocks = -(-width // BLOCK)
@@ -169,111 +208,178 @@ class Ckpt:
                              f"and uint8 exps [rows, {blocks}]")
         if not codes.is_contiguous() or not exps.is_contiguous():
             raise ValueError("codes and exps must be contiguous")
-        self.codes, self.exps, self.rows, self.width = codes, exps, rows, width
+        if codes.device != exps.device:
+            raise ValueError("codes and exps must be on one device")
+        self.rows, self.width, self._codes, self._exps = rows, width, codes, exps
+        self._buffer, self._at = None, None
+        self._ptrs, self._dev = (codes.data_ptr(), exps.data_ptr()), codes.get_device()
+
+    @classmethod
+    def _make(cls, like, rows: int, width: int, count: int, stream):
+        """`count` checkpoints in one buffer: all codes, then all exponents."""
+        units = rows * -(-width // BLOCK)
+        size = units * BLOCK
+        buf = _empty(like, (count * (size + units),), torch.uint8, stream)
+        base, dev, out = buf.data_ptr(), buf.get_device(), []
+        for i in range(count):
+            c = cls.__new__(cls)
+            c.rows, c.width, c._codes, c._exps, c._buffer, c._dev = rows, width, None, None, buf, dev
+            c._at = (i * size, count * size + i * units)
+            c._ptrs = (base + c._at[0], base + c._at[1]) if units else (None, None)
+            out.append(c)
+        return out
 
     @classmethod
     def empty(cls, rows: int, width: int, stream=None) -> "Ckpt":
-        blocks = -(-width // BLOCK)
-        return cls(_empty((rows, blocks * BLOCK), torch.int8, stream),
-                   _empty((rows, blocks), torch.uint8, stream), width)
+        """One of undefined contents on the current device."""
+        like = torch.empty(0, dtype=torch.uint8, device="cuda")
+        return cls._make(like, rows, width, 1, stream)[0]
 
-    def _ptrs(self, name: str):
-        _here(self.codes, name)
-        _here(self.exps, name)
-        return self.codes.data_ptr(), self.exps.data_ptr()
+    @property
+    def codes(self):
+        if self._codes is None:
+            blocks = -(-self.width // BLOCK)
+            part = self._buffer.narrow(0, self._at[0], self.rows * blocks * BLOCK)
+            self._codes = part.view(torch.int8).view(self.rows, blocks * BLOCK)
+        return self._codes
+
+    @property
+    def exps(self):
+        if self._exps is None:
+            blocks = -(-self.width // BLOCK)
+            part = self._buffer.narrow(0, self._at[1], self.rows * blocks)
+            self._exps = part.view(self.rows, blocks)
+        return self._exps
 
 
-def _ckpt_out(given: Optional[Ckpt], rows: int, width: int, name: str, stream) -> Ckpt:
-    if given is None:
-        return Ckpt.empty(rows, width, stream)
-    if (given.rows, given.width) != (rows, width):
-        raise ValueError(f"{name} must be a checkpoint of {rows} x {width}")
-    return given
+def _ckpt(c: Ckpt, rows: int, width: int, name: str, dev: int):
+    """Pointers of a checkpoint of these sizes."""
+    if c._dev != dev:
+        raise ValueError(f"{name} must be on the current CUDA device")
+    if c.rows != rows or c.width != width:
+        raise ValueError(f"{name} is a checkpoint of {c.rows} x {c.width}, not {rows} x {width}")
+    return c._ptrs
 
 
 def rip_ckpt_pack(x, out: Optional[Ckpt] = None, stream=None) -> Ckpt:
     """x kept in 8 bits."""
-    xp, xc, rows, width, ld = _matrix(x, "x")
-    out = _ckpt_out(out, rows, width, "out", stream)
-    _check(lib.rip_ckpt_pack(xp, xc, ld, rows, width, *out._ptrs("out"), _stream_ptr(stream)))
+    dev = _device()
+    xp, xc, rows, width, ld = _matrix(x, "x", dev)
+    if out is None:
+        out = Ckpt._make(x, rows, width, 1, stream)[0]
+    codes, exps = _ckpt(out, rows, width, "out", dev)
+    rc = lib.rip_ckpt_pack(xp, xc, ld, rows, width, codes, exps, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return out
 
 
 def rip_ckpt_unpack(ckpt: Ckpt, dtype=torch.bfloat16, out=None, stream=None):
     """The values that a checkpoint stands for."""
-    out = _out(out, (ckpt.rows, ckpt.width), dtype, "out", stream)
-    xp, xc, rows, width, ld = _matrix(out, "out")
-    _check(lib.rip_ckpt_unpack(*ckpt._ptrs("ckpt"), rows, width, xp, xc, ld, _stream_ptr(stream)))
+    dev = _device()
+    codes, exps = _ckpt(ckpt, ckpt.rows, ckpt.width, "ckpt", dev)
+    shape = (ckpt.rows, ckpt.width)
+    if out is None:
+        like = ckpt._codes if ckpt._buffer is None else ckpt._buffer
+        out = _empty(like, shape, dtype, stream)
+    else:
+        _shaped(out, shape, "out")
+    xp, xc, rows, width, ld = _matrix(out, "out", dev)
+    rc = lib.rip_ckpt_unpack(codes, exps, rows, width, xp, xc, ld, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return out
 
 
 def rip_gate_forward(gate, up, out=None, gate_ckpt: Optional[Ckpt] = None,
                      up_ckpt: Optional[Ckpt] = None, stream=None):
     """(silu(gate) * up, checkpoint of gate, checkpoint of up)."""
-    gp, gc, rows, width, ld_g = _matrix(gate, "gate")
-    up_, uc, rows_u, width_u, ld_u = _matrix(up, "up")
-    out = _out(out, gate.shape, gate.dtype, "out", stream)
-    hp, hc, _, _, ld_h = _matrix(out, "out")
-    if (rows, width, gc, gc) != (rows_u, width_u, uc, hc):
+    dev = _device()
+    gp, gc, rows, width, ld_g = _matrix(gate, "gate", dev)
+    up_, uc, rows_u, width_u, ld_u = _matrix(up, "up", dev)
+    if out is None:
+        out = _empty_like(gate, stream)
+        hp, hc, ld_h = out.data_ptr(), gc, width
+    else:
+        hp, hc, _, _, ld_h = _matrix(_shaped(out, gate.shape, "out"), "out", dev)
+    if rows != rows_u or width != width_u or gc != uc or gc != hc:
         raise ValueError("gate, up and out must have one shape and dtype")
-    g8 = _ckpt_out(gate_ckpt, rows, width, "gate_ckpt", stream)
-    u8 = _ckpt_out(up_ckpt, rows, width, "up_ckpt", stream)
-    _check(lib.rip_gate_forward(gp, ld_g, up_, ld_u, gc, rows, width, hp, ld_h,
-                                *g8._ptrs("gate_ckpt"), *u8._ptrs("up_ckpt"), _stream_ptr(stream)))
-    return out, g8, u8
+    if gate_ckpt is None and up_ckpt is None:
+        gate_ckpt, up_ckpt = Ckpt._make(gate, rows, width, 2, stream)
+    elif gate_ckpt is None or up_ckpt is None:
+        made = Ckpt._make(gate, rows, width, 1, stream)[0]
+        gate_ckpt, up_ckpt = gate_ckpt or made, up_ckpt or made
+    g_codes, g_exps = _ckpt(gate_ckpt, rows, width, "gate_ckpt", dev)
+    u_codes, u_exps = _ckpt(up_ckpt, rows, width, "up_ckpt", dev)
+    rc = lib.rip_gate_forward(gp, ld_g, up_, ld_u, gc, rows, width, hp, ld_h, g_codes, g_exps,
+                              u_codes, u_exps, _stream(stream, dev))
+    if rc:
+        _check(rc)
+    return out, gate_ckpt, up_ckpt
 
 
 def rip_gate_backward(dh, gate_ckpt: Ckpt, up_ckpt: Ckpt, dgate=None, dup=None, hidden=False,
                       stream=None):
     """(dgate, dup) from the checkpoints, and with ``hidden`` (True, or a Ckpt to
     fill) also a checkpoint of silu(gate) * up as the third value."""
-    dp, dc, rows, width, ld = _matrix(dh, "dh")
-    for c in (gate_ckpt, up_ckpt):
-        if (c.rows, c.width) != (rows, width):
-            raise ValueError(f"dh is {rows} x {width}, a checkpoint is {c.rows} x {c.width}")
-    dgate = _out(dgate, dh.shape, dh.dtype, "dgate", stream)
-    dup = _out(dup, dh.shape, dh.dtype, "dup", stream)
-    ap, ac, _, _, ld_a = _matrix(dgate, "dgate")
-    bp, bc, _, _, ld_b = _matrix(dup, "dup")
-    if (ac, bc) != (dc, dc):
+    dev = _device()
+    dp, dc, rows, width, ld = _matrix(dh, "dh", dev)
+    g_codes, g_exps = _ckpt(gate_ckpt, rows, width, "gate_ckpt", dev)
+    u_codes, u_exps = _ckpt(up_ckpt, rows, width, "up_ckpt", dev)
+    if dgate is None:
+        dgate = _empty_like(dh, stream)
+        ap, ac, ld_a = dgate.data_ptr(), dc, width
+    else:
+        ap, ac, _, _, ld_a = _matrix(_shaped(dgate, dh.shape, "dgate"), "dgate", dev)
+    if dup is None:
+        dup = _empty_like(dh, stream)
+        bp, bc, ld_b = dup.data_ptr(), dc, width
+    else:
+        bp, bc, _, _, ld_b = _matrix(_shaped(dup, dh.shape, "dup"), "dup", dev)
+    if ac != dc or bc != dc:
         raise ValueError("dh, dgate and dup must have one dtype")
-    h8 = None
+    h8, h_codes, h_exps = None, None, None
     if hidden is not False and hidden is not None:
-        h8 = _ckpt_out(None if hidden is True else hidden, rows, width, "hidden", stream)
-    _check(lib.rip_gate_backward(dp, ld, dc, *gate_ckpt._ptrs("gate_ckpt"),
-                                 *up_ckpt._ptrs("up_ckpt"), rows, width, ap, ld_a, bp, ld_b,
-                                 *((None, None) if h8 is None else h8._ptrs("hidden")),
-                                 _stream_ptr(stream)))
+        h8 = Ckpt._make(dh, rows, width, 1, stream)[0] if hidden is True else hidden
+        h_codes, h_exps = _ckpt(h8, rows, width, "hidden", dev)
+    rc = lib.rip_gate_backward(dp, ld, dc, g_codes, g_exps, u_codes, u_exps, rows, width, ap, ld_a,
+                               bp, ld_b, h_codes, h_exps, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return (dgate, dup) if h8 is None else (dgate, dup, h8)
 
 
 def rip_ckpt_wgrad(dy, ckpt: Ckpt, grad, accumulate: bool = False, stream=None):
     """dy^T x from the checkpoint of x, into ``grad`` [out_features, in_features]
     (added to it with ``accumulate``).  Returns grad."""
-    dp, dc, rows, n, ld = _matrix(dy, "dy")
-    gp, gc, n_g, k, ld_g = _matrix(grad, "grad")
-    if (rows, n, k) != (ckpt.rows, n_g, ckpt.width):
+    dev = _device()
+    dp, dc, rows, n, ld = _matrix(dy, "dy", dev)
+    gp, gc, n_g, k, ld_g = _matrix(grad, "grad", dev)
+    if rows != ckpt.rows or n != n_g or k != ckpt.width:
         raise ValueError(f"dy {rows} x {n}, checkpoint {ckpt.rows} x {ckpt.width} and grad "
                          f"{n_g} x {k} do not fit")
+    codes, exps = _ckpt(ckpt, rows, k, "ckpt", dev)
     nbytes = lib.rip_ckpt_wgrad_workspace(dc, rows, n, k)
-    _keep, ws = _workspace(nbytes, stream)
-    _check(lib.rip_ckpt_wgrad(dp, dc, ld, rows, n, *ckpt._ptrs("ckpt"), k, gp, gc, ld_g,
-                              int(accumulate), ws, nbytes, _stream_ptr(stream)))
+    _keep, ws = _workspace(nbytes, grad, stream)
+    rc = lib.rip_ckpt_wgrad(dp, dc, ld, rows, n, codes, exps, k, gp, gc, ld_g,
+                            1 if accumulate else 0, ws, nbytes, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return grad
 
 
 # ---------------------------------------------------------------------------
 # losses over the vocabulary
 # ---------------------------------------------------------------------------
-def _loss_args(logits, targets, grad):
-    lp, lc, n, vocab, ld = _matrix(logits, "logits")
-    tp, tc, m = _ids(targets, "targets")
+def _loss_args(logits, targets, grad, dev: int):
+    lp, lc, n, vocab, ld = _matrix(logits, "logits", dev)
+    tp, tc, m = _ids(targets, "targets", dev)
     if m != n:
         raise ValueError(f"{n} rows of logits for {m} targets")
     gp, ld_g = None, 0
     if grad is not None:
-        gp, gc, n_g, v_g, ld_g = _matrix(grad, "grad")
-        if (gc, n_g, v_g) != (lc, n, vocab):
+        gp, gc, n_g, v_g, ld_g = _matrix(grad, "grad", dev)
+        if gc != lc or n_g != n or v_g != vocab:
             raise ValueError("grad must have the logits' shape and dtype")
     return lp, lc, ld, n, vocab, tp, tc, gp, ld_g
 
@@ -287,19 +393,22 @@ def rip_pref_loss(logits, targets, seq_offsets, ref_logp, beta: float = 0.1,
     the gradient of the logits and may be the logits themselves; None computes the
     loss alone.  Returns (loss, log-probabilities of the sequences, of the
     tokens)."""
-    lp, lc, ld, n, vocab, tp, tc, gp, ld_g = _loss_args(logits, targets, grad)
-    op, oc, m = _ids(seq_offsets, "seq_offsets")
+    dev = _device()
+    lp, lc, ld, n, vocab, tp, tc, gp, ld_g = _loss_args(logits, targets, grad, dev)
+    op, oc, m = _ids(seq_offsets, "seq_offsets", dev)
     if oc != 0 or m < 3 or m % 2 == 0:
         raise ValueError("seq_offsets must hold 2 * pairs + 1 int32 values")
     pairs = m // 2
-    rp = _floats(ref_logp, "ref_logp", 2 * pairs)
-    out = _empty((1 + 2 * pairs + n,), torch.float32, stream)
+    rp = _floats(ref_logp, "ref_logp", 2 * pairs, dev)
+    out = _empty(logits, (1 + 2 * pairs + n,), torch.float32, stream)
     base = out.data_ptr()
     nbytes = lib.rip_pref_loss_workspace(n, vocab, pairs)
-    _keep, ws = _workspace(nbytes, stream)
-    _check(lib.rip_pref_loss(lp, lc, ld, n, vocab, tp, tc, op, pairs, rp, beta, smoothing,
-                             grad_scale, base, base + 4, base + 4 + 8 * pairs, gp, ld_g, ws,
-                             nbytes, _stream_ptr(stream)))
+    _keep, ws = _workspace(nbytes, logits, stream)
+    rc = lib.rip_pref_loss(lp, lc, ld, n, vocab, tp, tc, op, pairs, rp, beta, smoothing,
+                           grad_scale, base, base + 4, base + 4 + 8 * pairs, gp, ld_g, ws,
+                           nbytes, _stream(stream, dev))
+    if rc:
+        _check(rc)
     return out[0], out[1:1 + 2 * pairs], out[1 + 2 * pairs:]
 
 
@@ -309,16 +418,19 @@ def rip_policy_loss(logits, targets, old_logp, advantage, weight=None, ref_logp=
     """Clipped policy loss with a KL term against ``ref_logp`` (see include/rip.h);
     ``grad`` as in rip_pref_loss.  Returns (loss, log-probabilities of the
     tokens)."""
-    lp, lc, ld, n, vocab, tp, tc, gp, ld_g = _loss_args(logits, targets, grad)
+    dev = _device()
+    lp, lc, ld, n, vocab, tp, tc, gp, ld_g = _loss_args(logits, targets, grad, dev)
     if old_logp is None or advantage is None:
         raise ValueError("old_logp and advantage are needed")
-    old, adv = _floats(old_logp, "old_logp", n), _floats(advantage, "advantage", n)
-    w, ref = _floats(weight, "weight", n), _floats(ref_logp, "ref_logp", n)
-    out = _empty((1 + n,), torch.float32, stream)
+    old, adv = _floats(old_logp, "old_logp", n, dev), _floats(advantage, "advantage", n, dev)
+    w, ref = _floats(weight, "weight", n, dev), _floats(ref_logp, "ref_logp", n, dev)
+    out = _empty(logits, (1 + n,), torch.float32, stream)
     base = out.data_ptr()
     nbytes = lib.rip_policy_loss_workspace(n, vocab)
-    _keep, ws = _workspace(nbytes, stream)
-    _check(lib.rip_policy_loss(lp, lc, ld, n, vocab, tp, tc, old, adv, w, ref, clip_low, clip_high,
-                               kl, grad_scale, base, base + 4, gp, ld_g, ws, nbytes,
-                               _stream_ptr(stream)))
+    _keep, ws = _workspace(nbytes, logits, stream)
+    rc = lib.rip_policy_loss(lp, lc, ld, n, vocab, tp, tc, old, adv, w, ref, clip_low, clip_high,
+                             kl, grad_scale, base, base + 4, gp, ld_g, ws, nbytes,
+                             _stream(stream, dev))
+    if rc:
+        _check(rc)
     return out[0], out[1:]
