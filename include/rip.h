@@ -366,7 +366,8 @@ int32_t rip_set_blocks_per_cu(int32_t blocks_per_cu);
  *    written.  Indexes into it are 64-bit.
  *  - Arithmetic and every sum are fp32 (or wider); a result is rounded to bf16
  *    once, to nearest even.  Nothing is added atomically: a call's result is the
- *    same bits every time.
+ *    same bits every time for the same sizes, strides and alignment (a loss adds
+ *    a row's exponentials in an order that follows the sixteen-byte boundaries).
  *  - Token ids and targets are RIP_INT32 or RIP_INT64 device arrays.
  *  - `workspace` is device memory of at least the bytes that the call's
  *    _workspace function returns for the same sizes (0 = none needed; sizes that

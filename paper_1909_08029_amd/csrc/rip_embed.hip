@@ -25,6 +25,7 @@ constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortItems = 8;                          // tokens of a thread
 constexpr int kChunk = kSortThreads * kSortItems;      // tokens sorted by one workgroup
 constexpr int kMaxDigit = 8;                           // bits of a pass of the sort
+constexpr int kMaxEntries = 32;                        // of the sorted list to a wave, below kWave
 constexpr int kBatch = 4;                              // rows that a wave loads together
 constexpr int kColumns = kWave * kLane;                // columns of a wave
 constexpr int kMergeThreads = 256;
@@ -32,9 +33,41 @@ constexpr int64_t kCacheBytes = (int64_t)256 << 20;     // the memory-side cache
 
 constexpr int kFillBytes = 1 << 16;                    // bytes zeroed by a workgroup of the fill
 
+// A lane's columns: eight from `at` on, of which it owns those from skip on.  The
+// last lane of a row whose width is no multiple of eight moves back so that its
+// eight lie in the row: no load then needs a second look at the width.  NARROW rows,
+// of fewer than eight columns, are taken element by element.
+struct Columns {
+  int at, skip, width;
+  bool on;
+};
+__device__ __forceinline__ Columns columns_of(int c, int width) {
+  const int at = min(c, max(width - kLane, 0));
+  return {at, c - at, width, c < width};
+}
+template <int DT, bool NARROW, bool STREAM = false>
+__device__ __forceinline__ void load_columns(const typename Elem<DT>::T* row, const Columns& k,
+                                             float (&f)[kLane]) {
+  if constexpr (NARROW)
+    load_unit<DT>(row, 0, k.width, f);
+  else
+    Elem<DT>::template load8<STREAM>(row + k.at, f);
+}
+template <int DT>
+__device__ __forceinline__ void store_columns(typename Elem<DT>::T* row, const Columns& k,
+                                              const float (&f)[kLane]) {
+  if (k.skip == 0 && k.width >= kLane) {
+    Elem<DT>::store8(row + k.at, f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j)
+      if (j >= k.skip && k.at + j < k.width) Elem<DT>::store(row + k.at + j, f[j]);
+  }
+}
+
 // A thread handles eight columns of ROWS consecutive tokens, whose rows it loads
 // together.
-template <int TD, int OD, int ROWS>
+template <int TD, int OD, int ROWS, bool NARROW>
 __global__ __launch_bounds__(kLookupBlock) void lookup_kernel(
     const typename Elem<TD>::T* table, int64_t vocab, int width, int64_t ld, const void* ids,
     int wide, int64_t n, uint32_t units, FastDiv per_row, float scale, typename Elem<OD>::T* out,
@@ -42,27 +75,22 @@ __global__ __launch_bounds__(kLookupBlock) void lookup_kernel(
   const uint32_t unit = blockIdx.x * kLookupBlock + threadIdx.x;
   if (unit >= units) return;
   const uint32_t group = per_row.div(unit);
-  const int c = (int)(unit - group * per_row.d) * kLane;
+  const Columns k = columns_of((int)(unit - group * per_row.d) * kLane, width);
   const int64_t t = (int64_t)group * ROWS;
   float f[ROWS][kLane];
-  int64_t id[ROWS];
+  bool live[ROWS];
 #pragma unroll
-  for (int r = 0; r < ROWS; ++r) id[r] = t + r < n ? load_id(ids, wide, t + r) : -1;
-#pragma unroll
-  for (int r = 0; r < ROWS; ++r) {
-    if (id[r] >= 0 && id[r] < vocab) {
-      load_unit<TD>(table + id[r] * ld, c, width, f[r]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kLane; ++j) f[r][j] = 0.0f;
-    }
+  for (int r = 0; r < ROWS; ++r) {  // every row is loaded, row 0 for ids outside the table
+    const int64_t id = load_id(ids, wide, t + r < n ? t + r : n - 1);
+    live[r] = id >= 0 && id < vocab;
+    load_columns<TD, NARROW>(table + (live[r] ? id : 0) * ld, k, f[r]);
   }
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     if (t + r >= n) break;
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) f[r][j] *= id[r] >= 0 && id[r] < vocab ? scale : 1.0f;
-    store_unit<OD>(out + (t + r) * ld_out, c, width, f[r]);
+    for (int j = 0; j < kLane; ++j) f[r][j] = live[r] ? f[r][j] * scale : 0.0f;
+    store_columns<OD>(out + (t + r) * ld_out, k, f[r]);
   }
 }
 
@@ -277,62 +305,70 @@ __global__ __launch_bounds__(kMergeThreads) void merge_kernel(
   pos_out[at] = pos_in[i];
 }
 
-template <int GD>
-__device__ __forceinline__ void write_row(typename Elem<GD>::T* row, int c, int width, float scale,
+template <int GD, bool NARROW>
+__device__ __forceinline__ void write_row(typename Elem<GD>::T* row, const Columns& k, float scale,
                                           int accumulate, const float (&acc)[kLane]) {
   float f[kLane];
   if (accumulate) {
-    load_unit<GD>(row, c, width, f);
+    load_columns<GD, NARROW>(row, k, f);
 #pragma unroll
     for (int j = 0; j < kLane; ++j) f[j] = f[j] + scale * acc[j];
   } else {
 #pragma unroll
     for (int j = 0; j < kLane; ++j) f[j] = scale * acc[j];
   }
-  store_unit<GD>(row, c, width, f);
+  store_columns<GD>(row, k, f);
+}
+
+// Partial sums of a wave's two slots, a lane's eight columns in a row.
+__device__ __forceinline__ float* partial_at(float* partial, int64_t wave, int slot, int lanes,
+                                             int lane) {
+  return partial + ((wave * 2 + slot) * lanes + lane) * kLane;
 }
 
 // One wave: entries [a, b) of the sorted list, 512 columns.  Partial sums of a
 // run that began before `a` go to slot 0 of the wave's share, those of a run
 // that begins here and goes on to slot 1.
-template <int DD, int GD>
+template <int DD, int GD, bool NARROW>
 __global__ __launch_bounds__(kWave) void sum_kernel(
-    const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id_list,
-    const uint32_t* pos_list, int64_t n, uint32_t vocab, int per, float scale,
-    typename Elem<GD>::T* grad, int width, int64_t ld, int accumulate, float* partial) {
-  // the lists are not written while this runs: scalar loads
-  const RIP_CONST uint32_t* id = (const RIP_CONST uint32_t*)id_list;
-  const RIP_CONST uint32_t* pos = (const RIP_CONST uint32_t*)pos_list;
+    const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id, const uint32_t* pos,
+    int64_t n, uint32_t vocab, int per, float scale, typename Elem<GD>::T* grad, int width,
+    int64_t ld, int accumulate, float* partial) {
   const int64_t a = (int64_t)blockIdx.x * per;
-  const int64_t b = a + per < n ? a + per : n;
-  const int c = blockIdx.y * kColumns + threadIdx.x * kLane;
-  if (id[a] >= vocab) return;  // only ids outside the vocabulary from here on
+  const int count = (int)(a + per < n ? per : n - a), lane = threadIdx.x;
+  const int c = blockIdx.y * kColumns + lane * kLane, lanes = (width + kLane - 1) / kLane;
+  const Columns k = columns_of(c, width);
+  // the wave's entries and the one after them, an entry a lane
+  const int64_t mine = a + lane < n ? a + lane : n - 1;
+  const uint32_t my_id = a + lane < n ? id[mine] : vocab, my_pos = pos[mine];
+  const uint32_t before = id[a > 0 ? a - 1 : 0];
+  const uint32_t head = __builtin_amdgcn_readfirstlane(my_id);
+  if (head >= vocab) return;  // only ids outside the vocabulary from here on
   float acc[kLane] = {};
-  bool begins = a == 0 || id[a - 1] != id[a];
-  for (int64_t i0 = a; i0 < b; i0 += kBatch) {
+  bool begins = a == 0 || before != head;
+  for (int i0 = 0; i0 < count; i0 += kBatch) {
     float f[kBatch][kLane];
     uint32_t v[kBatch + 1];
 #pragma unroll
-    for (int u = 0; u <= kBatch; ++u) v[u] = i0 + u < n ? id[i0 + u] : vocab;
+    for (int u = 0; u <= kBatch; ++u) v[u] = __builtin_amdgcn_readlane(my_id, i0 + u);
+    // all of them are loaded, by all lanes, and not all are used
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (i0 + u < b && v[u] < vocab && c < width)
-        load_unit<DD, true>(dout + (int64_t)pos[i0 + u] * ld_dout, c, width, f[u]);
+      const int64_t t = (uint32_t)__builtin_amdgcn_readlane(my_pos, min(i0 + u, count - 1));
+      load_columns<DD, NARROW, true>(dout + t * ld_dout, k, f[u]);
     }
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
-      if (i0 + u >= b || v[u] >= vocab) break;
+      if (i0 + u >= count || v[u] >= vocab) break;
 #pragma unroll
       for (int j = 0; j < kLane; ++j) acc[j] += f[u][j];
       const bool ends = v[u + 1] != v[u];
-      if (!ends && i0 + u + 1 < b) continue;
-      if (c < width) {
-        if (begins && ends) {
-          write_row<GD>(grad + (int64_t)v[u] * ld, c, width, scale, accumulate, acc);
-        } else {
-          float* p = partial + ((int64_t)blockIdx.x * 2 + (begins ? 1 : 0)) * width;
-          store_unit<RIP_FP32>(p, c, width, acc);
-        }
+      if (!ends && i0 + u + 1 < count) continue;
+      if (k.on) {
+        if (begins && ends)
+          write_row<GD, NARROW>(grad + (int64_t)v[u] * ld, k, scale, accumulate, acc);
+        else
+          Elem<RIP_FP32>::store8(partial_at(partial, blockIdx.x, begins ? 1 : 0, lanes, c / kLane), acc);
       }
 #pragma unroll
       for (int j = 0; j < kLane; ++j) acc[j] = 0.0f;
@@ -349,15 +385,16 @@ constexpr int kShortRun = 16;  // partial sums that one wave adds
 // the runs that begin in those: slot 1 of the wave where a run begins and slot 0 of
 // those that it passes through.  A wave adds a short run alone; a long one is
 // shared by all waves of the workgroup.
-template <int GD>
+template <int GD, bool NARROW>
 __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
-    const uint32_t* id, int64_t n, uint32_t vocab, int per, int waves, const float* partial,
+    const uint32_t* id, int64_t n, uint32_t vocab, int per, int waves, float* partial,
     float scale, typename Elem<GD>::T* grad, int width, int64_t ld, int accumulate) {
   __shared__ float part[kJoinWaves][kColumns];
   __shared__ int run_last[kJoinWaves];
   __shared__ uint32_t run_id[kJoinWaves];
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int c = blockIdx.y * kColumns + lane * kLane;
+  const int c = blockIdx.y * kColumns + lane * kLane, lanes = (width + kLane - 1) / kLane;
+  const Columns k = columns_of(c, width);
   {
     const int64_t own = (int64_t)blockIdx.x * kJoinWaves + wave, a = own * per, b = a + per;
     int last = -1;  // last wave that the run reaches
@@ -381,16 +418,16 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
     }
     const int count = last - (int)own;
     if (last >= 0 && count <= kShortRun) {
-      if (c < width) {
+      if (k.on) {
         float acc[kLane], f[kLane];
-        load_unit<RIP_FP32>(partial + (own * 2 + 1) * width, c, width, acc);
-#pragma unroll 4
+        Elem<RIP_FP32>::load8(partial_at(partial, own, 1, lanes, c / kLane), acc);
+#pragma unroll 8
         for (int w = 1; w <= count; ++w) {
-          load_unit<RIP_FP32>(partial + (own + w) * 2 * width, c, width, f);
+          Elem<RIP_FP32>::load8(partial_at(partial, own + w, 0, lanes, c / kLane), f);
 #pragma unroll
           for (int j = 0; j < kLane; ++j) acc[j] += f[j];
         }
-        write_row<GD>(grad + (int64_t)v * ld, c, width, scale, accumulate, acc);
+        write_row<GD, NARROW>(grad + (int64_t)v * ld, k, scale, accumulate, acc);
       }
       last = -1;
     }
@@ -405,12 +442,12 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
     if (last < 0) continue;
     const int count = last - first;  // partial sums after the first
     float acc[kLane] = {}, f[kLane];
-    if (c < width) {
-      if (wave == 0) load_unit<RIP_FP32>(partial + ((int64_t)first * 2 + 1) * width, c, width, acc);
+    if (k.on) {
+      if (wave == 0) Elem<RIP_FP32>::load8(partial_at(partial, first, 1, lanes, c / kLane), acc);
       const int w1 = (wave + 1) * count / kJoinWaves;
-#pragma unroll 4
+#pragma unroll 8
       for (int w = wave * count / kJoinWaves; w < w1; ++w) {
-        load_unit<RIP_FP32>(partial + ((int64_t)first + 1 + w) * 2 * width, c, width, f);
+        Elem<RIP_FP32>::load8(partial_at(partial, (int64_t)first + 1 + w, 0, lanes, c / kLane), f);
 #pragma unroll
         for (int j = 0; j < kLane; ++j) acc[j] += f[j];
       }
@@ -418,11 +455,11 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
 #pragma unroll
     for (int j = 0; j < kLane; ++j) part[wave][lane * kLane + j] = acc[j];
     __syncthreads();
-    if (wave == 0 && c < width) {
+    if (wave == 0 && k.on) {
       for (int w = 1; w < kJoinWaves; ++w)
 #pragma unroll
         for (int j = 0; j < kLane; ++j) acc[j] += part[w][lane * kLane + j];
-      write_row<GD>(grad + (int64_t)run_id[r] * ld, c, width, scale, accumulate, acc);
+      write_row<GD, NARROW>(grad + (int64_t)run_id[r] * ld, k, scale, accumulate, acc);
     }
     __syncthreads();
   }
@@ -432,7 +469,7 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
 int entries_per_wave(int64_t n, int64_t width) {
   const int64_t columns = ceil_div(width, kColumns);
   int per = 4;
-  while (per < 32 && ceil_div(n, 2 * per) * columns >= 4096) per *= 2;
+  while (per < kMaxEntries && ceil_div(n, 2 * per) * columns >= 2048) per *= 2;
   return per;
 }
 
@@ -446,15 +483,21 @@ GradPlan grad_plan(int64_t n, int64_t width) {
   p.waves = (int)ceil_div(n, p.per);
   p.chunks = (int)ceil_div(n, kChunk);
   p.id_bytes = ceil_div(n * 4, 256) * 256;
-  p.partial_bytes = (int64_t)p.waves * 2 * width * 4;
+  p.partial_bytes = (int64_t)p.waves * 2 * ceil_div(width, kLane) * kLane * 4;
   // ids and positions, once more where chunks are merged, and the partial sums
   p.total = p.id_bytes * (p.chunks > 1 ? 4 : 2) + p.partial_bytes;
   return p;
 }
 
 template <int TD, int OD>
-const void* lookup_of(bool many) {
-  return many ? (const void*)lookup_kernel<TD, OD, 4> : (const void*)lookup_kernel<TD, OD, 1>;
+const void* lookup_of(bool many, bool narrow) {
+  return narrow ? (const void*)lookup_kernel<TD, OD, 1, true>
+         : many ? (const void*)lookup_kernel<TD, OD, 4, false>
+                : (const void*)lookup_kernel<TD, OD, 1, false>;
+}
+template <int DD, int GD>
+const void* sum_of(bool narrow) {
+  return narrow ? (const void*)sum_kernel<DD, GD, true> : (const void*)sum_kernel<DD, GD, false>;
 }
 
 int32_t check_ids(const void* ids, int32_t id_type, int64_t n) {
@@ -518,17 +561,17 @@ extern "C" int32_t rip_embed_lookup(const void* table, int32_t table_dtype, int6
     return fail(RIP_E_UNSUPPORTED, "%lld tokens of width %lld are above the limit",
                 (long long)n_tokens, (long long)width);
   // four rows to a thread where that leaves the card full
-  const bool many = n_tokens * per_row >= (int64_t)1 << 19;
+  const bool narrow = width < kLane, many = !narrow && n_tokens * per_row >= (int64_t)1 << 19;
   uint32_t units = (uint32_t)(ceil_div(n_tokens, many ? 4 : 1) * per_row);
   FastDiv div = FastDiv::make((uint32_t)per_row);
   int w = (int)width, wide = id_type == RIP_INT64;
   void* args[] = {&table, &vocab, &w,   &ld_table, &ids, &wide, &n_tokens,
                   &units, &div,   &scale, &out,    &ld_out};
   const void* fn = table_dtype == RIP_FP32
-                       ? (out_dtype == RIP_FP32 ? lookup_of<RIP_FP32, RIP_FP32>(many)
-                                                : lookup_of<RIP_FP32, RIP_BF16>(many))
-                       : (out_dtype == RIP_FP32 ? lookup_of<RIP_BF16, RIP_FP32>(many)
-                                                : lookup_of<RIP_BF16, RIP_BF16>(many));
+                       ? (out_dtype == RIP_FP32 ? lookup_of<RIP_FP32, RIP_FP32>(many, narrow)
+                                                : lookup_of<RIP_FP32, RIP_BF16>(many, narrow))
+                       : (out_dtype == RIP_FP32 ? lookup_of<RIP_BF16, RIP_FP32>(many, narrow)
+                                                : lookup_of<RIP_BF16, RIP_BF16>(many, narrow));
   return launch(fn, dim3((uint32_t)ceil_div(units, kLookupBlock)), dim3(kLookupBlock), args, 0,
                 stream, "rip_embed_lookup");
 }
@@ -612,15 +655,16 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
       return rc;
   }
   const uint32_t columns = (uint32_t)ceil_div(width, kColumns);
+  const bool narrow = width < kLane;
   {
     void* args[] = {&dout,  &ld_dout, &id_b, &pos_b,   &n_tokens,   &v32,    &p.per,
                     &scale, &grad,    &w,    &ld_grad, &accumulate, &partial};
     const void* fn =
         dout_dtype == RIP_FP32
-            ? (grad_dtype == RIP_FP32 ? (const void*)sum_kernel<RIP_FP32, RIP_FP32>
-                                      : (const void*)sum_kernel<RIP_FP32, RIP_BF16>)
-            : (grad_dtype == RIP_FP32 ? (const void*)sum_kernel<RIP_BF16, RIP_FP32>
-                                      : (const void*)sum_kernel<RIP_BF16, RIP_BF16>);
+            ? (grad_dtype == RIP_FP32 ? sum_of<RIP_FP32, RIP_FP32>(narrow)
+                                      : sum_of<RIP_FP32, RIP_BF16>(narrow))
+            : (grad_dtype == RIP_FP32 ? sum_of<RIP_BF16, RIP_FP32>(narrow)
+                                      : sum_of<RIP_BF16, RIP_BF16>(narrow));
     if ((rc = launch(fn, dim3((uint32_t)p.waves, columns), dim3(kWave), args, 0, stream,
                      "rip_embed_grad: sum")))
       return rc;
@@ -628,8 +672,10 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
   if (p.waves < 2) return RIP_OK;
   void* args[] = {&id_b, &n_tokens, &v32, &p.per,   &p.waves,   &partial,
                   &scale, &grad,    &w,   &ld_grad, &accumulate};
-  const void* fn = grad_dtype == RIP_FP32 ? (const void*)join_kernel<RIP_FP32>
-                                          : (const void*)join_kernel<RIP_BF16>;
+  const void* fn = grad_dtype == RIP_FP32 ? (narrow ? (const void*)join_kernel<RIP_FP32, true>
+                                                    : (const void*)join_kernel<RIP_FP32, false>)
+                                          : (narrow ? (const void*)join_kernel<RIP_BF16, true>
+                                                    : (const void*)join_kernel<RIP_BF16, false>);
   return launch(fn, dim3((uint32_t)ceil_div(p.waves, kJoinWaves), columns), dim3(kWave * kJoinWaves),
                 args, 0, stream, "rip_embed_grad: join");
 }

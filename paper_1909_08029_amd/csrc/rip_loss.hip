@@ -25,8 +25,9 @@ namespace {
 constexpr int kWave = 64;
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kStep = kThreads * kLane;  // elements of a workgroup's round
-constexpr int kRowThreads = 512;         // of the policy loss's one-launch form
-constexpr int kHold = 8;                 // units of a row that a lane of it keeps in registers
+constexpr int kTotalThreads = 1024;      // of the launch that adds the tokens' losses
+constexpr int kHold = 8;                 // units of a row that a lane of the policy loss's
+                                         // one-launch form keeps in registers
 constexpr float kLowest = -3.402823466e38f;
 
 // A row's largest logit and sum of e^(x - top).  sum == 0 only where every
@@ -76,6 +77,43 @@ __device__ __forceinline__ bool counts(const Rows& r, int64_t t, int64_t* target
   return *target >= 0 && *target < r.vocab;
 }
 
+// Columns [begin, end) of a row as a workgroup walks them: units of eight that
+// begin at sixteen-byte boundaries (rows of an odd vocabulary begin anywhere, and
+// sixteen bytes across a boundary take twice as long: statistics of 5461 rows of
+// 50257 bf16 150 us, 110 so), and fewer than a unit before and after them.
+struct Walk {
+  int begin, first, units, rest, end;  // units from `first` to `rest`
+};
+template <typename T>
+__device__ __forceinline__ Walk walk(const T* row, int begin, int end) {
+  const int off = (int)((16 - ((uintptr_t)(row + begin) & 15)) & 15) / (int)sizeof(T);
+  Walk w;
+  w.begin = begin;
+  w.end = end;
+  w.first = min(begin + off, end);
+  w.units = (end - w.first) / kLane;
+  w.rest = w.first + w.units * kLane;
+  return w;
+}
+// The columns before the units (edge 0) or after them (edge 1), as a unit filled
+// up with -inf.
+template <int DT>
+__device__ __forceinline__ void load_edge(const typename Elem<DT>::T* row, const Walk& w, int edge,
+                                          float (&f)[kLane]) {
+  const int a = edge ? w.rest : w.begin, b = edge ? w.end : w.first;
+#pragma unroll
+  for (int j = 0; j < kLane; ++j)
+    f[j] = a + j < b ? Elem<DT>::load(row + a + j) : -__builtin_huge_valf();
+}
+template <int DT>
+__device__ __forceinline__ void store_edge(typename Elem<DT>::T* row, const Walk& w, int edge,
+                                           const float (&f)[kLane]) {
+  const int a = edge ? w.rest : w.begin, b = edge ? w.end : w.first;
+#pragma unroll
+  for (int j = 0; j < kLane; ++j)
+    if (a + j < b) Elem<DT>::store(row + a + j, f[j]);
+}
+
 // What the grad launch needs of a token: gradient[v] = scale * e^(x[v] - top),
 // plus coef at the target.
 struct Token {
@@ -98,24 +136,24 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
   if (!counts(r, t, &target)) return;
   const int end = min(r.vocab, (split + 1) * r.columns);
   const typename Elem<DT>::T* row = logits + t * r.ld;
+  const Walk w = walk(row, split * r.columns, end);
+  const typename Elem<DT>::T* unit = row + w.first;
   Stat s{kLowest, 0.0f};
-  int c = split * r.columns + threadIdx.x * kLane;
-  for (; c + 3 * kStep + kLane <= end; c += 4 * kStep) {
+  int u = threadIdx.x;
+  for (; u + 3 * kThreads < w.units; u += 4 * kThreads) {
     float f[4][kLane];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) Elem<DT>::load8(row + c + u * kStep, f[u]);
+    for (int i = 0; i < 4; ++i) Elem<DT>::load8(unit + (u + i * kThreads) * kLane, f[i]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) add8(s, f[u]);
+    for (int i = 0; i < 4; ++i) add8(s, f[i]);
   }
-  for (; c < end; c += kStep) {
-    float f[kLane];
-    if (c + kLane <= end) {
-      Elem<DT>::load8(row + c, f);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kLane; ++j)
-        f[j] = c + j < end ? Elem<DT>::load(row + c + j) : -__builtin_huge_valf();
-    }
+  float f[kLane];
+  for (; u < w.units; u += kThreads) {
+    Elem<DT>::load8(unit + u * kLane, f);
+    add8(s, f);
+  }
+  if (threadIdx.x < 2) {
+    load_edge<DT>(row, w, threadIdx.x, f);
     add8(s, f);
   }
   s = join_block(s, shared);
@@ -140,6 +178,7 @@ __device__ __forceinline__ Stat row_stat(const Rows& r, const Stat* stat, int64_
   return s;
 }
 
+template <int WAVES = kWaves>
 __device__ __forceinline__ double sum_block(double x, double* shared) {
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) x += __shfl_xor(x, o);
@@ -147,7 +186,7 @@ __device__ __forceinline__ double sum_block(double x, double* shared) {
   if (threadIdx.x % kWave == 0) shared[threadIdx.x / kWave] = x;
   __syncthreads();
   double s = shared[0];
-  for (int w = 1; w < kWaves; ++w) s += shared[w];
+  for (int w = 1; w < WAVES; ++w) s += shared[w];
   return s;
 }
 
@@ -261,6 +300,79 @@ __global__ __launch_bounds__(kThreads) void tokens_kernel(Rows r,
   if (threadIdx.x == 0) part_loss[blockIdx.x] = loss;
 }
 
+// The loss: the sum of `parts` numbers, by one workgroup.
+template <int THREADS>
+__device__ __forceinline__ void total_loss(const double* part, int parts, float* loss,
+                                           double* shared) {
+  double sum = 0.0;
+  for (int i = threadIdx.x; i < parts; i += 8 * THREADS) {
+    double v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = i + u * THREADS < parts ? part[i + u * THREADS] : 0.0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += v[u];
+  }
+  sum = sum_block<THREADS / kWave>(sum, shared);
+  if (threadIdx.x == 0) *loss = (float)sum;
+}
+__global__ __launch_bounds__(kTotalThreads) void total_kernel(const double* part, int parts,
+                                                              float* loss) {
+  __shared__ double shared[kTotalThreads / kWave];
+  total_loss<kTotalThreads>(part, parts, loss, shared);
+}
+
+// Gradient of eight logits from column c on.
+__device__ __forceinline__ void grad8(const Token& k, int c, float (&f)[kLane]) {
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    f[j] = k.scale * exp_acc(f[j] - k.top);
+    if (c + j == k.target) f[j] += k.coef;
+  }
+}
+// A part of a row's gradient by `threads` threads; zeros without a look at the
+// logits where the token does not count.
+template <int DT>
+__device__ __forceinline__ void row_grad(const typename Elem<DT>::T* row, const Walk& w,
+                                         const Token& k, typename Elem<DT>::T* out, int thread,
+                                         int threads) {
+  float f[kLane] = {};
+  if (k.coef == 0.0f) {
+    for (int u = thread; u < w.units; u += threads) Elem<DT>::store8(out + w.first + u * kLane, f);
+    if (thread < 2) store_edge<DT>(out, w, thread, f);
+    return;
+  }
+  for (int u = thread; u < w.units; u += threads) {
+    const int c = w.first + u * kLane;
+    Elem<DT>::load8(row + c, f);
+    grad8(k, c, f);
+    Elem<DT>::store8(out + c, f);
+  }
+  if (thread < 2) {
+    load_edge<DT>(row, w, thread, f);
+    grad8(k, thread ? w.rest : w.begin, f);
+    store_edge<DT>(out, w, thread, f);
+  }
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
+                                                        const typename Elem<DT>::T* logits,
+                                                        const Token* token,
+                                                        typename Elem<DT>::T* grad, int64_t ld_grad,
+                                                        const double* part, int parts,
+                                                        float* loss) {
+  __shared__ double shared[kWaves];
+  if (blockIdx.x == 0) total_loss<kThreads>(part, parts, loss, shared);
+  // from the last row back: those that were read last are still in the caches
+  const uint32_t from_end = gridDim.x - 1 - blockIdx.x;
+  const int64_t t = from_end / r.splits;
+  const int split = from_end - (uint32_t)t * r.splits;
+  const int end = min(r.vocab, (split + 1) * r.columns);
+  const typename Elem<DT>::T* row = logits + t * r.ld;
+  row_grad<DT>(row, walk(row, split * r.columns, end), token[t], grad + t * ld_grad, threadIdx.x,
+               kThreads);
+}
+
 // A lane's eight elements as they lie in memory.
 template <int DT>
 struct Unit;
@@ -283,144 +395,87 @@ struct Unit<RIP_FP32> {
 // The policy loss of one token in one workgroup, gradient and all: coef needs
 // nothing beyond the token's own row.  The first kHold units of a lane stay in
 // registers between the two passes; the rest is read again, last first, mostly
-// from the caches: 8192 rows of 131072 bf16 took 1031 us in three launches.
-template <int DT>
-__global__ __launch_bounds__(kRowThreads) void policy_row_kernel(
+// from the caches (8192 rows of 131072 bf16: 1031 us in three launches, 780 so).
+template <int DT, int THREADS>
+__global__ __launch_bounds__(THREADS) void policy_row_kernel(
     Rows r, const typename Elem<DT>::T* logits, Policy p, float* logp, double* part,
     typename Elem<DT>::T* grad, int64_t ld_grad) {
-  constexpr int kRound = kRowThreads * kLane;
-  __shared__ Stat shared[kRowThreads / kWave];
+  __shared__ Stat shared[THREADS / kWave];
   const int64_t t = blockIdx.x;
-  const int first = threadIdx.x * kLane, vocab = r.vocab;
+  const int tid = threadIdx.x;
   const typename Elem<DT>::T* row = logits + t * r.ld;
-  typename Elem<DT>::T* out = grad + t * ld_grad;
-  float f[kLane], lp = 0.0f, coef = 0.0f;
+  const Walk w = walk(row, 0, r.vocab);
+  const typename Elem<DT>::T* unit = row + w.first;
+  float f[kLane], edge[kLane], lp = 0.0f, coef = 0.0f;
   Stat s{kLowest, 0.0f};
   int64_t target;
   double loss = 0.0;
   Unit<DT> held[kHold];
-  const bool on = counts(r, t, &target);
-  const int whole = vocab - kLane;  // a unit from a column up to here is whole
-  if (on) {
+  if (counts(r, t, &target)) {
 #pragma unroll
-    for (int u = 0; u < kHold; ++u)
-      if (first + u * kRound <= whole) held[u].load(row + first + u * kRound);
+    for (int i = 0; i < kHold; ++i)
+      if (tid + i * THREADS < w.units) held[i].load(unit + (tid + i * THREADS) * kLane);
+    if (tid < 2) load_edge<DT>(row, w, tid, edge);
+    const float hit = Elem<DT>::load(row + target);
 #pragma unroll
-    for (int u = 0; u < kHold; ++u)
-      if (first + u * kRound <= whole) {
-        held[u].get(f);
+    for (int i = 0; i < kHold; ++i)
+      if (tid + i * THREADS < w.units) {
+        held[i].get(f);
         add8(s, f);
       }
-    int c = first + kHold * kRound;
-    for (; c + 3 * kRound <= whole; c += 4 * kRound) {
+    if (tid < 2) add8(s, edge);
+    int u = tid + kHold * THREADS;
+    for (; u + 3 * THREADS < w.units; u += 4 * THREADS) {
       Unit<DT> next[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) next[u].load(row + c + u * kRound);
+      for (int i = 0; i < 4; ++i) next[i].load(unit + (u + i * THREADS) * kLane);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        next[u].get(f);
+      for (int i = 0; i < 4; ++i) {
+        next[i].get(f);
         add8(s, f);
       }
     }
-    for (; c <= whole; c += kRound) {
-      Elem<DT>::load8(row + c, f);
+    for (; u < w.units; u += THREADS) {
+      Elem<DT>::load8(unit + u * kLane, f);
       add8(s, f);
     }
-    // the last columns, fewer than a unit: one lane has them
-    const int rest = vocab / kLane * kLane;
-    if (rest < vocab && rest / kLane % kRowThreads == (int)threadIdx.x) {
-#pragma unroll
-      for (int j = 0; j < kLane; ++j)
-        f[j] = rest + j < vocab ? Elem<DT>::load(row + rest + j) : -__builtin_huge_valf();
-      add8(s, f);
-    }
-    s = join_block<kRowThreads / kWave>(s, shared);
+    s = join_block<THREADS / kWave>(s, shared);
     if (s.sum != 0.0f) {
-      lp = Elem<DT>::load(row + target) - s.top - logf(s.sum);
+      lp = hit - s.top - logf(s.sum);
       loss = policy_token(p, t, r.n, lp, &coef);
     }
   }
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     part[t] = loss;
     if (logp) logp[t] = lp;
   }
   if (!grad) return;
-  __syncthreads();  // in place, the target's logit has been read by now
-  if (coef == 0.0f) {
-    const float zero[kLane] = {};
-    for (int c = first; c < vocab; c += kRound) store_unit<DT>(out, c, vocab, zero);
-    return;
-  }
-  const float scale = -coef / s.sum;
-  const int at = (int)target;
-  auto finish = [&](int c) {
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      f[j] = scale * exp_acc(f[j] - s.top);
-      if (c + j == at) f[j] += coef;
-    }
-    store_unit<DT>(out, c, vocab, f);
-  };
-  int c = first + (vocab - 1 - first) / kRound * kRound;
-  if (first < vocab)
-    for (; c >= first + kHold * kRound || (c > whole && c >= first); c -= kRound) {
-      load_unit<DT>(row, c, vocab, f);
-      finish(c);
-    }
-#pragma unroll
-  for (int u = kHold - 1; u >= 0; --u)
-    if (first + u * kRound <= whole) {
-      held[u].get(f);
-      finish(first + u * kRound);
-    }
-}
-
-// The loss: the sum of `parts` numbers, by one workgroup.
-__device__ __forceinline__ void total_loss(const double* part, int parts, float* loss,
-                                           double* shared) {
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < parts; i += kThreads) sum += part[i];
-  sum = sum_block(sum, shared);
-  if (threadIdx.x == 0) *loss = (float)sum;
-}
-__global__ __launch_bounds__(kThreads) void total_kernel(const double* part, int parts,
-                                                         float* loss) {
-  __shared__ double shared[kWaves];
-  total_loss(part, parts, loss, shared);
-}
-
-template <int DT>
-__global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
-                                                        const typename Elem<DT>::T* logits,
-                                                        const Token* token,
-                                                        typename Elem<DT>::T* grad, int64_t ld_grad,
-                                                        const double* part, int parts,
-                                                        float* loss) {
-  __shared__ double shared[kWaves];
-  if (blockIdx.x == 0) total_loss(part, parts, loss, shared);
-  // from the last row back: those that were read last are still in the caches
-  const uint32_t from_end = gridDim.x - 1 - blockIdx.x;
-  const int64_t t = from_end / r.splits;
-  const int split = from_end - (uint32_t)t * r.splits;
-  const int end = min(r.vocab, (split + 1) * r.columns);
-  const typename Elem<DT>::T* row = logits + t * r.ld;
   typename Elem<DT>::T* out = grad + t * ld_grad;
-  const Token k = token[t];
-  int c = split * r.columns + threadIdx.x * kLane;
-  if (k.coef == 0.0f) {
-    const float zero[kLane] = {};
-    for (; c < end; c += kStep) store_unit<DT>(out, c, end, zero);
+  const Token k = {s.top, -coef / s.sum, coef, (int)target};
+  if (coef == 0.0f) {
+    row_grad<DT>(row, w, k, out, tid, THREADS);
     return;
   }
-  for (; c < end; c += kStep) {
-    float f[kLane];
-    load_unit<DT>(row, c, end, f);
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      f[j] = k.scale * exp_acc(f[j] - k.top);
-      if (c + j == k.target) f[j] += k.coef;
+  // in place: each lane overwrites what it alone reads, but for the target's
+  // logit, which every lane has read before the join
+  if (w.units > tid)
+    for (int u = tid + (w.units - 1 - tid) / THREADS * THREADS; u >= tid + kHold * THREADS; u -= THREADS) {
+      const int c = w.first + u * kLane;
+      Elem<DT>::load8(row + c, f);
+      grad8(k, c, f);
+      Elem<DT>::store8(out + c, f);
     }
-    store_unit<DT>(out, c, end, f);
+#pragma unroll
+  for (int i = kHold - 1; i >= 0; --i)
+    if (tid + i * THREADS < w.units) {
+      const int c = w.first + (tid + i * THREADS) * kLane;
+      held[i].get(f);
+      grad8(k, c, f);
+      Elem<DT>::store8(out + c, f);
+    }
+  if (tid < 2) {
+    grad8(k, tid ? w.rest : w.begin, edge);
+    store_edge<DT>(out, w, tid, edge);
   }
 }
 
@@ -460,8 +515,16 @@ int join_lanes(const Rows& r) {
   return lanes;
 }
 // The policy loss takes its one-launch form where the rows fill the card or are
-// short: a workgroup a row.  (512 rows of 32768: see the table of measurements.)
-bool one_launch(const Rows& r) { return r.n >= 512 || (r.n > 0 && r.vocab <= kHold * kRowThreads * kLane); }
+// short: a workgroup a row, of one wave, four or eight, so that a lane has a few
+// units of a short row to itself.
+bool one_launch(const Rows& r) { return r.n >= 512 || (r.n > 0 && r.vocab <= 1 << 14); }
+template <int DT>
+const void* row_kernel(const Rows& r, int* threads) {
+  *threads = r.vocab <= 1 << 11 ? 64 : r.vocab <= 1 << 14 ? 256 : 512;
+  return *threads == 64    ? (const void*)policy_row_kernel<DT, 64>
+         : *threads == 256 ? (const void*)policy_row_kernel<DT, 256>
+                           : (const void*)policy_row_kernel<DT, 512>;
+}
 int64_t policy_parts(const Rows& r) { return one_launch(r) ? r.n : ceil_div(r.n * join_lanes(r), kThreads); }
 
 int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t ld, int64_t n,
@@ -512,7 +575,7 @@ int32_t run_grad(Rows& r, const void* logits, Work& w, void* grad, int64_t ld_gr
                  float* loss, void* stream) {
   if (!grad || r.n == 0) {
     void* args[] = {&w.part, &parts, &loss};
-    return launch((const void*)total_kernel, dim3(1), dim3(kThreads), args, 0, stream,
+    return launch((const void*)total_kernel, dim3(1), dim3(kTotalThreads), args, 0, stream,
                   "loss: total");
   }
   void* args[] = {&r, &logits, &w.token, &grad, &ld_grad, &w.part, &parts, &loss};
@@ -544,11 +607,13 @@ int32_t run_policy(Rows r, const void* logits, Policy p, float* loss, float* log
   int32_t rc;
   if (one_launch(r)) {
     void* args[] = {&r, &logits, &p, &logp, &w.part, &grad, &ld_grad};
-    if ((rc = launch((const void*)policy_row_kernel<DT>, dim3((uint32_t)r.n), dim3(kRowThreads),
-                     args, 0, stream, "rip_policy_loss: rows")))
+    int threads;
+    const void* fn = row_kernel<DT>(r, &threads);
+    if ((rc = launch(fn, dim3((uint32_t)r.n), dim3(threads), args, 0, stream,
+                     "rip_policy_loss: rows")))
       return rc;
     void* total[] = {&w.part, &parts, &loss};
-    return launch((const void*)total_kernel, dim3(1), dim3(kThreads), total, 0, stream,
+    return launch((const void*)total_kernel, dim3(1), dim3(kTotalThreads), total, 0, stream,
                   "rip_policy_loss: total");
   }
   if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;

@@ -8,10 +8,6 @@
 
 #include "rip_internal.h"
 
-// Address space of data that nothing writes while a kernel runs: wave-uniform reads
-// of it are scalar loads.
-#define RIP_CONST __attribute__((address_space(4)))
-
 namespace rip {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));

@@ -94,12 +94,9 @@ def test_pref_loss(shape, dtype):
         assert ref.guards_intact(grad, buf)
         alone = rip.rip_pref_loss(x, t, od, rd, beta, smoothing)
         assert torch.equal(alone[0], loss) and torch.equal(alone[1], got_seq)
-        own = x.clone()
-        if own.stride() == grad.stride():
-            rip.rip_pref_loss(own, t, od, rd, beta, smoothing, grad=own, grad_scale=scale)
-            assert torch.equal(own, grad)
-            rip.rip_pref_loss(x, t, od, rd, beta, smoothing, grad=own, grad_scale=scale)
-            assert torch.equal(own, grad)
+        own, _ = ref.device_matrix(xh, dtype, pad, offset)   # in place, laid out alike
+        rip.rip_pref_loss(own, t, od, rd, beta, smoothing, grad=own, grad_scale=scale)
+        assert torch.equal(own, grad)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
@@ -147,7 +144,7 @@ def test_policy_loss(shape, dtype):
         again = torch.full_like(grad, 5.0)
         loss2, _ = rip.rip_policy_loss(x, t, cuda(old), cuda(adv), grad=again, **args)
         assert torch.equal(again, grad) and torch.equal(loss2, loss)
-        own = x.clone()
+        own, _ = ref.device_matrix(xh, dtype, pad, offset)   # in place, laid out alike
         rip.rip_policy_loss(own, t, cuda(old), cuda(adv), grad=own, **args)
         assert torch.equal(own, grad)
 
