@@ -421,7 +421,7 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
       if (k.on) {
         float acc[kLane], f[kLane];
         Elem<RIP_FP32>::load8(partial_at(partial, own, 1, lanes, c / kLane), acc);
-#pragma unroll 8
+#pragma unroll 4
         for (int w = 1; w <= count; ++w) {
           Elem<RIP_FP32>::load8(partial_at(partial, own + w, 0, lanes, c / kLane), f);
 #pragma unroll
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
     if (k.on) {
       if (wave == 0) Elem<RIP_FP32>::load8(partial_at(partial, first, 1, lanes, c / kLane), acc);
       const int w1 = (wave + 1) * count / kJoinWaves;
-#pragma unroll 8
+#pragma unroll 4
       for (int w = wave * count / kJoinWaves; w < w1; ++w) {
         Elem<RIP_FP32>::load8(partial_at(partial, (int64_t)first + 1 + w, 0, lanes, c / kLane), f);
 #pragma unroll
@@ -462,6 +462,66 @@ __global__ __launch_bounds__(kWave* kJoinWaves) void join_kernel(
       write_row<GD, NARROW>(grad + (int64_t)run_id[r] * ld, k, scale, accumulate, acc);
     }
     __syncthreads();
+  }
+}
+
+// The gradient of up to kFewTokens tokens in one launch, without a sort: each
+// workgroup has a run of the table's rows, and each wave has all ids in registers,
+// two to a lane, and finds a row's tokens with two ballots.  (40 tokens, a table of
+// 50257 x 512 fp32: 21 us through the sort, 14.5 so.)
+constexpr int kFewTokens = 2 * kWave, kFewThreads = 256, kFewBatch = 8;
+template <int DD, int GD, bool NARROW>
+__global__ __launch_bounds__(kFewThreads) void few_kernel(
+    const typename Elem<DD>::T* dout, int64_t ld_dout, const void* ids, int wide, int n,
+    float scale, int accumulate, Fill fill) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, width = fill.width;
+  const int64_t id0 = lane < n ? load_id(ids, wide, lane) : -1;
+  const int64_t id1 = lane + kWave < n ? load_id(ids, wide, lane + kWave) : -1;
+  const int64_t row0 = (int64_t)blockIdx.x * fill.rows;
+  const int64_t row1 = row0 + fill.rows < fill.vocab ? row0 + fill.rows : fill.vocab;
+  if (!__ballot((id0 >= row0 && id0 < row1) || (id1 >= row0 && id1 < row1))) {
+    if (!accumulate) zero_rows<GD, kFewThreads>(fill, blockIdx.x);
+    return;
+  }
+  typename Elem<GD>::T* grad = static_cast<typename Elem<GD>::T*>(fill.grad);
+  // a wave takes 512 columns of a row at a time
+  const int parts = (width + kColumns - 1) / kColumns, units = (int)(row1 - row0) * parts;
+  for (int unit = wave; unit < units; unit += kFewThreads / kWave) {
+    const int64_t r = row0 + unit / parts;
+    const int c0 = unit % parts * kColumns, c = c0 + lane * kLane;
+    uint64_t in0 = __ballot(id0 == r), in1 = __ballot(id1 == r);
+    typename Elem<GD>::T* row = grad + r * fill.ld;
+    if (!(in0 | in1)) {
+      if (!accumulate)
+        zero_range<false>((char*)(row + c0), (char*)(row + min(c0 + kColumns, width)), lane, kWave);
+      continue;
+    }
+    const Columns k = columns_of(c, width);
+    float acc[kLane] = {};
+    while (in0 | in1) {  // kFewBatch of the row's tokens at a time, ascending
+      float f[kFewBatch][kLane];
+      int64_t t = 0;
+      int got = 0;
+#pragma unroll
+      for (int u = 0; u < kFewBatch; ++u) {
+        if (in0) {
+          t = __ffsll((unsigned long long)in0) - 1;
+          in0 &= in0 - 1;
+          got = u + 1;
+        } else if (in1) {
+          t = kWave + __ffsll((unsigned long long)in1) - 1;
+          in1 &= in1 - 1;
+          got = u + 1;
+        }
+        load_columns<DD, NARROW>(dout + t * ld_dout, k, f[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kFewBatch; ++u)
+#pragma unroll
+        for (int j = 0; j < kLane; ++j)
+          if (u < got) acc[j] += f[u][j];
+    }
+    if (k.on) write_row<GD, NARROW>(row, k, scale, accumulate, acc);
   }
 }
 
@@ -498,6 +558,11 @@ const void* lookup_of(bool many, bool narrow) {
 template <int DD, int GD>
 const void* sum_of(bool narrow) {
   return narrow ? (const void*)sum_kernel<DD, GD, true> : (const void*)sum_kernel<DD, GD, false>;
+}
+
+template <int DD, int GD>
+const void* few_of(bool narrow) {
+  return narrow ? (const void*)few_kernel<DD, GD, true> : (const void*)few_kernel<DD, GD, false>;
 }
 
 int32_t check_ids(const void* ids, int32_t id_type, int64_t n) {
@@ -577,7 +642,7 @@ extern "C" int32_t rip_embed_lookup(const void* table, int32_t table_dtype, int6
 }
 
 extern "C" int64_t rip_embed_grad_workspace(int64_t n_tokens, int64_t width) {
-  if (n_tokens < 1 || n_tokens > RIP_MAX_TOKENS || width < 1 || width > RIP_MAX_WIDTH) return 0;
+  if (n_tokens <= kFewTokens || n_tokens > RIP_MAX_TOKENS || width < 1 || width > RIP_MAX_WIDTH) return 0;
   return grad_plan(n_tokens, width).total;
 }
 
@@ -610,6 +675,28 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
   }
   if (n_tokens == 0 && accumulate) return RIP_OK;
 
+  int w = (int)width, wide = id_type == RIP_INT64;
+  const bool narrow = width < kLane;
+  // Zeros that the memory-side cache holds stay there until the sums come (a table
+  // of 206 MB: 64 us against 72 past it); more go past it (537 MB: 281 against 290).
+  const bool stream_zeros = vocab * width * elem_bytes(grad_dtype) > kCacheBytes;
+  Fill fill{grad, vocab, ld_grad, w, (int)(kFillBytes / (width * elem_bytes(grad_dtype))),
+            stream_zeros, 0};
+  if (fill.rows < 1) fill.rows = 1;
+  if (n_tokens <= kFewTokens) {
+    int n = (int)n_tokens;
+    const int64_t spread = ceil_div(vocab, 1024);  // rows of a workgroup that leave the card full
+    if (fill.rows > spread) fill.rows = (int)spread;
+    void* args[] = {&dout, &ld_dout, &ids, &wide, &n, &scale, &accumulate, &fill};
+    const void* fn = dout_dtype == RIP_FP32
+                         ? (grad_dtype == RIP_FP32 ? few_of<RIP_FP32, RIP_FP32>(narrow)
+                                                   : few_of<RIP_FP32, RIP_BF16>(narrow))
+                         : (grad_dtype == RIP_FP32 ? few_of<RIP_BF16, RIP_FP32>(narrow)
+                                                   : few_of<RIP_BF16, RIP_BF16>(narrow));
+    return launch(fn, dim3((uint32_t)ceil_div(vocab, fill.rows)), dim3(kFewThreads), args, 0,
+                  stream, "rip_embed_grad: few");
+  }
+
   GradPlan p = grad_plan(n_tokens, width);
   char* ws = static_cast<char*>(workspace);
   uint32_t* id_a = (uint32_t*)ws;
@@ -623,14 +710,7 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
   while (((int64_t)1 << key_bits) <= vocab) ++key_bits;
   int passes = (key_bits + kMaxDigit - 1) / kMaxDigit;
   int bits = (key_bits + passes - 1) / passes;
-  int w = (int)width, wide = id_type == RIP_INT64;
   uint32_t v32 = (uint32_t)vocab;
-  // Zeros that the memory-side cache holds stay there until the sums come (a table
-  // of 206 MB: 64 us against 72 past it); more go past it (537 MB: 281 against 290).
-  const bool stream_zeros = vocab * width * elem_bytes(grad_dtype) > kCacheBytes;
-  Fill fill{grad, vocab, ld_grad, w, (int)(kFillBytes / (width * elem_bytes(grad_dtype))),
-            stream_zeros, 0};
-  if (fill.rows < 1) fill.rows = 1;
   // Runs of rows to zero, all beside the sort, or a third of them beside the merge.
   const int64_t runs = accumulate ? 0 : ceil_div(vocab, fill.rows);
   const int64_t later = p.chunks > 1 ? runs / 3 : 0;
@@ -643,7 +723,6 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
                      stream, "rip_embed_grad: sort")))
       return rc;
   }
-  if (n_tokens == 0) return RIP_OK;
   if (p.chunks > 1) {
     int merges = (int)ceil_div(n_tokens, kMergeThreads);
     fill.first = runs - later;
@@ -655,7 +734,6 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
       return rc;
   }
   const uint32_t columns = (uint32_t)ceil_div(width, kColumns);
-  const bool narrow = width < kLane;
   {
     void* args[] = {&dout,  &ld_dout, &id_b, &pos_b,   &n_tokens,   &v32,    &p.per,
                     &scale, &grad,    &w,    &ld_grad, &accumulate, &partial};

@@ -20,7 +20,7 @@ def call(fn, defaults, **change):
 
 LOOKUP = dict(table=A, tt=0, vocab=100, width=16, ld=16, ids=B, idt=1, n=8, scale=1.0, out=C,
               ot=1, ld_out=16, stream=None)
-GRAD = dict(dout=A, dt=0, ld=16, ids=B, idt=0, n=8, scale=1.0, grad=C, gt=0, vocab=100, width=16,
+GRAD = dict(dout=A, dt=0, ld=16, ids=B, idt=0, n=800, scale=1.0, grad=C, gt=0, vocab=100, width=16,
             ld_g=16, acc=0, ws=W, nbytes=BIG, stream=None)
 PACK = dict(x=A, dt=1, ld=40, rows=8, width=40, codes=B, exps=C, stream=None)
 UNPACK = dict(codes=B, exps=C, rows=8, width=40, x=A, dt=1, ld=40, stream=None)
@@ -139,14 +139,14 @@ def test_refused_before_any_launch(fn, defaults, change, code):
 def test_workspace_sizes():
     lib = rip.lib
     assert lib.rip_embed_grad_workspace(0, 16) == 0
-    assert lib.rip_embed_grad_workspace(1, 16) > 0
+    assert lib.rip_embed_grad_workspace(1, 16) == 0        # few tokens are not sorted
     assert lib.rip_embed_grad_workspace(-1, 16) == 0 == lib.rip_embed_grad_workspace(1, 0)
     assert lib.rip_pref_loss_workspace(0, 10, 1) > 0
     assert lib.rip_policy_loss_workspace(0, 10) > 0
     assert lib.rip_pref_loss_workspace(-1, 10, 1) == 0
     assert lib.rip_ckpt_wgrad_workspace(0, 0, 4, 4) == 0
     assert lib.rip_ckpt_wgrad_workspace(9, 100, 4, 4) == 0
-    for n in (1, 63, 4096, 4097, 100_000, 1 << 23):
+    for n in (1000, 4096, 4097, 100_000, 1 << 23):
         for width in (1, 512, 513, 5000):
             assert lib.rip_embed_grad_workspace(n, width) >= 8 * n
     # a small gradient summed over many tokens is split, a large one is not
