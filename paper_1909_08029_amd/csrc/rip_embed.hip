@@ -26,6 +26,7 @@ constexpr int kSortItems = 8;                          // tokens of a thread
 constexpr int kChunk = kSortThreads * kSortItems;      // tokens sorted by one workgroup
 constexpr int kMaxDigit = 8;                           // bits of a pass of the sort
 constexpr int kMaxEntries = 32;                        // of the sorted list to a wave, below kWave
+constexpr int kSumWaves = 4;                            // that share a row's columns in a workgroup
 constexpr int kBatch = 4;                              // rows that a wave loads together
 constexpr int kColumns = kWave * kLane;                // columns of a wave
 constexpr int kMergeThreads = 256;
@@ -330,13 +331,13 @@ __device__ __forceinline__ float* partial_at(float* partial, int64_t wave, int s
 // run that began before `a` go to slot 0 of the wave's share, those of a run
 // that begins here and goes on to slot 1.
 template <int DD, int GD, bool NARROW>
-__global__ __launch_bounds__(kWave) void sum_kernel(
+__global__ __launch_bounds__(kWave* kSumWaves) void sum_kernel(
     const typename Elem<DD>::T* dout, int64_t ld_dout, const uint32_t* id, const uint32_t* pos,
     int64_t n, uint32_t vocab, int per, float scale, typename Elem<GD>::T* grad, int width,
     int64_t ld, int accumulate, float* partial) {
   const int64_t a = (int64_t)blockIdx.x * per;
-  const int count = (int)(a + per < n ? per : n - a), lane = threadIdx.x;
-  const int c = blockIdx.y * kColumns + lane * kLane, lanes = (width + kLane - 1) / kLane;
+  const int count = (int)(a + per < n ? per : n - a), lane = threadIdx.x % kWave;
+  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * kLane, lanes = (width + kLane - 1) / kLane;
   const Columns k = columns_of(c, width);
   // the wave's entries and the one after them, an entry a lane
   const int64_t mine = a + lane < n ? a + lane : n - 1;
@@ -743,8 +744,9 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
                                       : sum_of<RIP_FP32, RIP_BF16>(narrow))
             : (grad_dtype == RIP_FP32 ? sum_of<RIP_BF16, RIP_FP32>(narrow)
                                       : sum_of<RIP_BF16, RIP_BF16>(narrow));
-    if ((rc = launch(fn, dim3((uint32_t)p.waves, columns), dim3(kWave), args, 0, stream,
-                     "rip_embed_grad: sum")))
+    const uint32_t side = columns < kSumWaves ? columns : kSumWaves;
+    if ((rc = launch(fn, dim3((uint32_t)p.waves, (columns + side - 1) / side), dim3(kWave * side),
+                     args, 0, stream, "rip_embed_grad: sum")))
       return rc;
   }
   if (p.waves < 2) return RIP_OK;
