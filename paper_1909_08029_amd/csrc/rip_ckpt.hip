@@ -83,7 +83,7 @@ __global__ __launch_bounds__(kBlockThreads) void pack_kernel(Shape s, const type
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float f[kLane];
-  load_unit<DT, true>(x + p.row * ld, p.col, s.width, f);
+  load_unit<DT>(x + p.row * ld, p.col, s.width, f);
   store_ckpt(out, p, f);
 }
 
@@ -99,7 +99,8 @@ __global__ __launch_bounds__(kBlockThreads) void unpack_kernel(Shape s, Ckpt in,
   store_unit<DT>(x + p.row * ld, p.col, s.width, f);
 }
 
-template <int DT>
+// STREAM: the inputs are read past the caches.
+template <int DT, bool STREAM>
 __global__ __launch_bounds__(kBlockThreads) void gate_forward_kernel(
     Shape s, const typename Elem<DT>::T* gate, int64_t ld_gate, const typename Elem<DT>::T* up,
     int64_t ld_up, typename Elem<DT>::T* h, int64_t ld_h, Ckpt gate8, Ckpt up8) {
@@ -107,8 +108,8 @@ __global__ __launch_bounds__(kBlockThreads) void gate_forward_kernel(
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float g[kLane], u[kLane];
-  load_unit<DT, true>(gate + p.row * ld_gate, p.col, s.width, g);
-  load_unit<DT, true>(up + p.row * ld_up, p.col, s.width, u);
+  load_unit<DT, STREAM>(gate + p.row * ld_gate, p.col, s.width, g);
+  load_unit<DT, STREAM>(up + p.row * ld_up, p.col, s.width, u);
   store_ckpt(gate8, p, g);
   store_ckpt(up8, p, u);
 #pragma unroll
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(kBlockThreads) void gate_forward_kernel(
   store_unit<DT>(h + p.row * ld_h, p.col, s.width, g);
 }
 
-template <int DT, bool AGAIN>
+template <int DT, bool AGAIN, bool STREAM>
 __global__ __launch_bounds__(kBlockThreads) void gate_backward_kernel(
     Shape s, const typename Elem<DT>::T* dh, int64_t ld_dh, Ckpt gate8, Ckpt up8,
     typename Elem<DT>::T* dgate, int64_t ld_dgate, typename Elem<DT>::T* dup, int64_t ld_dup,
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(kBlockThreads) void gate_backward_kernel(
   if (unit >= s.units) return;
   const Place p = place(s, unit);
   float d[kLane], g[kLane], u[kLane];
-  load_unit<DT, true>(dh + p.row * ld_dh, p.col, s.width, d);
+  load_unit<DT, STREAM>(dh + p.row * ld_dh, p.col, s.width, d);
   load_ckpt(gate8, p, g);
   load_ckpt(up8, p, u);
   float a[kLane], h[kLane];
@@ -155,6 +156,13 @@ int32_t make_shape(int64_t rows, int64_t width, Shape* out) {
   out->width = (int)width;
   out->blocks = (int)blocks;
   return RIP_OK;
+}
+
+// Inputs that the memory-side cache cannot hold are read past it (16384 x 5504 bf16
+// forward 113 us against 119, backward 107 against 117); smaller ones may lie in it
+// from the launch that made them (8192 x 1024: 13 against 15 past it).
+bool stream_inputs(int32_t dtype, int64_t rows, int64_t width, int inputs) {
+  return dtype == RIP_BF16 && rows * width * elem_bytes(dtype) * inputs > kCacheBytes;
 }
 
 int64_t code_bytes(const Shape& s) { return (int64_t)s.units * kLane; }
@@ -284,9 +292,11 @@ extern "C" int32_t rip_gate_forward(const void* gate, int64_t ld_gate, const voi
   if ((rc = b.check())) return rc;
   Ckpt g8{gate_codes, gate_exps}, u8{up_codes, up_exps};
   void* args[] = {&s, &gate, &ld_gate, &up, &ld_up, &h, &ld_h, &g8, &u8};
-  return run(dtype == RIP_FP32 ? (const void*)gate_forward_kernel<RIP_FP32>
-                               : (const void*)gate_forward_kernel<RIP_BF16>,
-             s, args, stream, "rip_gate_forward");
+  const void* fn = dtype == RIP_FP32 ? (const void*)gate_forward_kernel<RIP_FP32, false>
+                   : stream_inputs(dtype, rows, width, 2)
+                       ? (const void*)gate_forward_kernel<RIP_BF16, true>
+                       : (const void*)gate_forward_kernel<RIP_BF16, false>;
+  return run(fn, s, args, stream, "rip_gate_forward");
 }
 
 extern "C" int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtype,
@@ -324,9 +334,15 @@ extern "C" int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtyp
   Ckpt u8{const_cast<int8_t*>(up_codes), const_cast<uint8_t*>(up_exps)};
   Ckpt h8{h_codes, h_exps};
   void* args[] = {&s, &dh, &ld_dh, &g8, &u8, &dgate, &ld_dgate, &dup, &ld_dup, &h8};
-  const void* fn = dtype == RIP_FP32 ? (again ? (const void*)gate_backward_kernel<RIP_FP32, true>
-                                              : (const void*)gate_backward_kernel<RIP_FP32, false>)
-                                     : (again ? (const void*)gate_backward_kernel<RIP_BF16, true>
-                                              : (const void*)gate_backward_kernel<RIP_BF16, false>);
+  const void* fn;
+  if (dtype == RIP_FP32)
+    fn = again ? (const void*)gate_backward_kernel<RIP_FP32, true, false>
+               : (const void*)gate_backward_kernel<RIP_FP32, false, false>;
+  else if (stream_inputs(dtype, rows, width, 2))  // dh, and as many bytes of checkpoints
+    fn = again ? (const void*)gate_backward_kernel<RIP_BF16, true, true>
+               : (const void*)gate_backward_kernel<RIP_BF16, false, true>;
+  else
+    fn = again ? (const void*)gate_backward_kernel<RIP_BF16, true, false>
+               : (const void*)gate_backward_kernel<RIP_BF16, false, false>;
   return run(fn, s, args, stream, "rip_gate_backward");
 }

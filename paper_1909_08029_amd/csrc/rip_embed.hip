@@ -30,7 +30,6 @@ constexpr int kSumWaves = 4;                            // that share a row's co
 constexpr int kBatch = 4;                              // rows that a wave loads together
 constexpr int kColumns = kWave * kLane;                // columns of a wave
 constexpr int kMergeThreads = 256;
-constexpr int64_t kCacheBytes = (int64_t)256 << 20;     // the memory-side cache
 
 constexpr int kFillBytes = 1 << 16;                    // bytes zeroed by a workgroup of the fill
 

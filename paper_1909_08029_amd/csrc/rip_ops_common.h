@@ -17,6 +17,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // start anywhere, and gfx950 loads and stores 16 bytes at any alignment.
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
+constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // what the memory-side cache holds
+
 // Sixteen bytes past the caches (non-temporal), for data of which a launch writes
 // or reads more than a cache holds, once: the gated unit of 16384 x 5504 bf16 took
 // 251 us without, 242 with such stores, 218 with such loads too; the policy loss
