@@ -24,7 +24,13 @@ namespace {
 
 constexpr int kWave = 64;
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kStep = kThreads * kLane;  // elements of a workgroup's round
+// A lane's unit of a row here is sixteen bytes, so that every access of a wave is
+// one range whatever the type (fp32 units of 32 bytes, in two accesses of half
+// lines: 829 rows of 73856 123 us, 97 so).
+template <int DT>
+constexpr int kUnit = DT == RIP_BF16 ? 8 : 4;  // elements
+constexpr int kStep = kThreads * 8;            // columns of a workgroup that a row is split for
+constexpr int kPairThreads = 1024;       // of a pair's workgroup
 constexpr int kTotalThreads = 1024;      // of the launch that adds the tokens' losses
 constexpr int kHold = 8;                 // units of a row that a lane of the policy loss's
                                          // one-launch form keeps in registers
@@ -42,13 +48,14 @@ __device__ __forceinline__ Stat join(Stat a, Stat b) {
   const float top = fmaxf(a.top, b.top);
   return {top, a.sum * exp_fast(a.top - top) + b.sum * exp_fast(b.top - top)};
 }
-__device__ __forceinline__ void add8(Stat& s, const float (&f)[kLane]) {
-  float top = fmaxf(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])),
-                    fmaxf(fmaxf(f[4], f[5]), fmaxf(f[6], f[7])));
-  top = fmaxf(top, s.top);
+template <int N>
+__device__ __forceinline__ void add(Stat& s, const float (&f)[N]) {
+  float top = s.top;
+#pragma unroll
+  for (int j = 0; j < N; ++j) top = fmaxf(top, f[j]);
   float sum = s.sum * exp_fast(s.top - top);
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) sum += exp_fast(f[j] - top);
+  for (int j = 0; j < N; ++j) sum += exp_fast(f[j] - top);
   s = {top, sum};
 }
 // The workgroup's joined pair, in every thread.
@@ -68,7 +75,7 @@ struct Rows {
   int64_t n, ld;
   int vocab;
   int splits;   // workgroups of a row
-  int columns;  // of a workgroup, a multiple of kLane
+  int columns;  // of a workgroup, a multiple of eight
   const void* targets;
   int wide;
 };
@@ -77,40 +84,72 @@ __device__ __forceinline__ bool counts(const Rows& r, int64_t t, int64_t* target
   return *target >= 0 && *target < r.vocab;
 }
 
-// Columns [begin, end) of a row as a workgroup walks them: units of eight that
+// A lane's unit as it lies in memory.
+template <int DT>
+struct Unit {
+  u32x4_any a;
+  __device__ __forceinline__ void load(const typename Elem<DT>::T* p) { a = *(const u32x4_any*)p; }
+  __device__ __forceinline__ void get(float (&f)[kUnit<DT>]) const {
+    if constexpr (DT == RIP_BF16) {
+      Elem<RIP_BF16>::unpack8(a, f);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(a[j]);
+    }
+  }
+};
+template <int DT>
+__device__ __forceinline__ void load_elems(const typename Elem<DT>::T* p, float (&f)[kUnit<DT>]) {
+  Unit<DT> u;
+  u.load(p);
+  u.get(f);
+}
+template <int DT>
+__device__ __forceinline__ void store_elems(typename Elem<DT>::T* p, const float (&f)[kUnit<DT>]) {
+  if constexpr (DT == RIP_BF16) {
+    Elem<RIP_BF16>::store8(p, f);
+  } else {
+    u32x4_any a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(f[j]);
+    store_stream((u32x4_any*)p, a);
+  }
+}
+
+// Columns [begin, end) of a row as a workgroup walks them: units that
 // begin at sixteen-byte boundaries (rows of an odd vocabulary begin anywhere, and
 // sixteen bytes across a boundary take twice as long: statistics of 5461 rows of
 // 50257 bf16 150 us, 110 so), and fewer than a unit before and after them.
 struct Walk {
   int begin, first, units, rest, end;  // units from `first` to `rest`
 };
-template <typename T>
-__device__ __forceinline__ Walk walk(const T* row, int begin, int end) {
-  const int off = (int)((16 - ((uintptr_t)(row + begin) & 15)) & 15) / (int)sizeof(T);
+template <int DT>
+__device__ __forceinline__ Walk walk(const typename Elem<DT>::T* row, int begin, int end) {
+  const int off = (int)(-(uintptr_t)(row + begin) & 15) / (int)sizeof(typename Elem<DT>::T);
   Walk w;
   w.begin = begin;
   w.end = end;
   w.first = min(begin + off, end);
-  w.units = (end - w.first) / kLane;
-  w.rest = w.first + w.units * kLane;
+  w.units = (end - w.first) / kUnit<DT>;
+  w.rest = w.first + w.units * kUnit<DT>;
   return w;
 }
 // The columns before the units (edge 0) or after them (edge 1), as a unit filled
 // up with -inf.
 template <int DT>
 __device__ __forceinline__ void load_edge(const typename Elem<DT>::T* row, const Walk& w, int edge,
-                                          float (&f)[kLane]) {
+                                          float (&f)[kUnit<DT>]) {
   const int a = edge ? w.rest : w.begin, b = edge ? w.end : w.first;
 #pragma unroll
-  for (int j = 0; j < kLane; ++j)
+  for (int j = 0; j < kUnit<DT>; ++j)
     f[j] = a + j < b ? Elem<DT>::load(row + a + j) : -__builtin_huge_valf();
 }
 template <int DT>
 __device__ __forceinline__ void store_edge(typename Elem<DT>::T* row, const Walk& w, int edge,
-                                           const float (&f)[kLane]) {
+                                           const float (&f)[kUnit<DT>]) {
   const int a = edge ? w.rest : w.begin, b = edge ? w.end : w.first;
 #pragma unroll
-  for (int j = 0; j < kLane; ++j)
+  for (int j = 0; j < kUnit<DT>; ++j)
     if (a + j < b) Elem<DT>::store(row + a + j, f[j]);
 }
 
@@ -136,25 +175,26 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
   if (!counts(r, t, &target)) return;
   const int end = min(r.vocab, (split + 1) * r.columns);
   const typename Elem<DT>::T* row = logits + t * r.ld;
-  const Walk w = walk(row, split * r.columns, end);
+  const Walk w = walk<DT>(row, split * r.columns, end);
   const typename Elem<DT>::T* unit = row + w.first;
   Stat s{kLowest, 0.0f};
   int u = threadIdx.x;
-  for (; u + 3 * kThreads < w.units; u += 4 * kThreads) {
-    float f[4][kLane];
+  constexpr int kAhead = 32 / kUnit<DT>;
+  for (; u + (kAhead - 1) * kThreads < w.units; u += kAhead * kThreads) {
+    float f[kAhead][kUnit<DT>];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) Elem<DT>::load8(unit + (u + i * kThreads) * kLane, f[i]);
+    for (int i = 0; i < kAhead; ++i) load_elems<DT>(unit + (u + i * kThreads) * kUnit<DT>, f[i]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) add8(s, f[i]);
+    for (int i = 0; i < kAhead; ++i) add(s, f[i]);
   }
-  float f[kLane];
+  float f[kUnit<DT>];
   for (; u < w.units; u += kThreads) {
-    Elem<DT>::load8(unit + u * kLane, f);
-    add8(s, f);
+    load_elems<DT>(unit + u * kUnit<DT>, f);
+    add(s, f);
   }
   if (threadIdx.x < 2) {
     load_edge<DT>(row, w, threadIdx.x, f);
-    add8(s, f);
+    add(s, f);
   }
   s = join_block(s, shared);
   if (threadIdx.x == 0) stat[blockIdx.x] = s;
@@ -198,11 +238,12 @@ __device__ __forceinline__ float log_sigmoid(float z) {
 // over a sequence are held in 64 bits: they run to thousands while the loss
 // depends on differences of a few.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void pairs_kernel(
+__global__ __launch_bounds__(kPairThreads) void pairs_kernel(
     Rows r, const typename Elem<DT>::T* logits, const Stat* stat, const int32_t* offsets, int pairs,
     const float* ref, float beta, float smoothing, float grad_scale, int lanes, float* seq_logp,
     Token* token, float* logp, double* pair_loss) {
-  __shared__ double shared[kWaves];
+  __shared__ double shared[2][kPairThreads / kWave];
+  const double refs[2] = {ref[2 * blockIdx.x], ref[2 * blockIdx.x + 1]};
   int64_t at[3];
   for (int i = 0; i < 3; ++i) {  // within the tokens and ascending, whatever the offsets say
     int64_t o = offsets[2 * blockIdx.x + i];
@@ -210,7 +251,7 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(
     at[i] = i && o < at[i - 1] ? at[i - 1] : o;
   }
   const bool lead = (threadIdx.x & (lanes - 1)) == 0;
-  const int64_t begin = at[0] + threadIdx.x / lanes, round = kThreads / lanes;
+  const int64_t begin = at[0] + threadIdx.x / lanes, round = kPairThreads / lanes;
   double sum[2] = {0.0, 0.0};
   Token mine = {0.0f, 0.0f, 0.0f, -1};  // of the first round, kept in registers
   for (int64_t t = begin; t < at[2]; t += round) {
@@ -229,8 +270,8 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(
   }
   double margin[2];
   for (int q = 0; q < 2; ++q) {
-    const double all = sum_block(sum[q], shared);
-    margin[q] = all - (double)ref[2 * blockIdx.x + q];
+    const double all = sum_block<kPairThreads / kWave>(sum[q], shared[q]);
+    margin[q] = all - refs[q];
     if (threadIdx.x == 0) seq_logp[2 * blockIdx.x + q] = (float)all;
   }
   const float z = (float)((double)beta * (margin[0] - margin[1]));
@@ -321,19 +362,19 @@ __global__ __launch_bounds__(kTotalThreads) void total_kernel(const double* part
   total_loss<kTotalThreads>(part, parts, loss, shared);
 }
 
-// Gradient of eight logits from column c on.  The short exponential's error, |x|
+// Gradient of a unit from column c on.  The short exponential's error, |x|
 // 2^-24, is far below what rounding to bf16 leaves.
 template <int DT>
-__device__ __forceinline__ void grad8(const Token& k, int c, float (&f)[kLane]) {
+__device__ __forceinline__ void grad_unit(const Token& k, int c, float (&f)[kUnit<DT>]) {
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) {
+  for (int j = 0; j < kUnit<DT>; ++j) {
     const float x = f[j] - k.top;
     f[j] = k.scale * (DT == RIP_BF16 ? exp_fast(x) : exp_acc(x));
   }
   const int hit = k.target - c;
-  if (hit >= 0 && hit < kLane) {
+  if (hit >= 0 && hit < kUnit<DT>) {
 #pragma unroll
-    for (int j = 0; j < kLane; ++j)
+    for (int j = 0; j < kUnit<DT>; ++j)
       if (j == hit) f[j] += k.coef;
   }
 }
@@ -343,21 +384,21 @@ template <int DT>
 __device__ __forceinline__ void row_grad(const typename Elem<DT>::T* row, const Walk& w,
                                          const Token& k, typename Elem<DT>::T* out, int thread,
                                          int threads) {
-  float f[kLane] = {};
+  float f[kUnit<DT>] = {};
   if (k.coef == 0.0f) {
-    for (int u = thread; u < w.units; u += threads) Elem<DT>::store8(out + w.first + u * kLane, f);
+    for (int u = thread; u < w.units; u += threads) store_elems<DT>(out + w.first + u * kUnit<DT>, f);
     if (thread < 2) store_edge<DT>(out, w, thread, f);
     return;
   }
   for (int u = thread; u < w.units; u += threads) {
-    const int c = w.first + u * kLane;
-    Elem<DT>::load8(row + c, f);
-    grad8<DT>(k, c, f);
-    Elem<DT>::store8(out + c, f);
+    const int c = w.first + u * kUnit<DT>;
+    load_elems<DT>(row + c, f);
+    grad_unit<DT>(k, c, f);
+    store_elems<DT>(out + c, f);
   }
   if (thread < 2) {
     load_edge<DT>(row, w, thread, f);
-    grad8<DT>(k, thread ? w.rest : w.begin, f);
+    grad_unit<DT>(k, thread ? w.rest : w.begin, f);
     store_edge<DT>(out, w, thread, f);
   }
 }
@@ -377,28 +418,9 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
   const int split = from_end - (uint32_t)t * r.splits;
   const int end = min(r.vocab, (split + 1) * r.columns);
   const typename Elem<DT>::T* row = logits + t * r.ld;
-  row_grad<DT>(row, walk(row, split * r.columns, end), token[t], grad + t * ld_grad, threadIdx.x,
+  row_grad<DT>(row, walk<DT>(row, split * r.columns, end), token[t], grad + t * ld_grad, threadIdx.x,
                kThreads);
 }
-
-// A lane's eight elements as they lie in memory.
-template <int DT>
-struct Unit;
-template <>
-struct Unit<RIP_BF16> {
-  u32x4_any a;
-  __device__ __forceinline__ void load(const uint16_t* p) { a = *(const u32x4_any*)p; }
-  __device__ __forceinline__ void get(float (&f)[kLane]) const { Elem<RIP_BF16>::unpack8(a, f); }
-};
-template <>
-struct Unit<RIP_FP32> {
-  float v[kLane];
-  __device__ __forceinline__ void load(const float* p) { Elem<RIP_FP32>::load8(p, v); }
-  __device__ __forceinline__ void get(float (&f)[kLane]) const {
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) f[j] = v[j];
-  }
-};
 
 // The policy loss of one token in one workgroup, gradient and all: coef needs
 // nothing beyond the token's own row.  The first kHold units of a lane stay in
@@ -412,9 +434,9 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x;
   const typename Elem<DT>::T* row = logits + t * r.ld;
-  const Walk w = walk(row, 0, r.vocab);
+  const Walk w = walk<DT>(row, 0, r.vocab);
   const typename Elem<DT>::T* unit = row + w.first;
-  float f[kLane], edge[kLane], lp = 0.0f, coef = 0.0f;
+  float f[kUnit<DT>], edge[kUnit<DT>], lp = 0.0f, coef = 0.0f;
   Stat s{kLowest, 0.0f};
   int64_t target;
   double loss = 0.0;
@@ -422,30 +444,30 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(
   if (counts(r, t, &target)) {
 #pragma unroll
     for (int i = 0; i < kHold; ++i)
-      if (tid + i * THREADS < w.units) held[i].load(unit + (tid + i * THREADS) * kLane);
+      if (tid + i * THREADS < w.units) held[i].load(unit + (tid + i * THREADS) * kUnit<DT>);
     if (tid < 2) load_edge<DT>(row, w, tid, edge);
     const float hit = Elem<DT>::load(row + target);
 #pragma unroll
     for (int i = 0; i < kHold; ++i)
       if (tid + i * THREADS < w.units) {
         held[i].get(f);
-        add8(s, f);
+        add(s, f);
       }
-    if (tid < 2) add8(s, edge);
+    if (tid < 2) add(s, edge);
     int u = tid + kHold * THREADS;
     for (; u + 3 * THREADS < w.units; u += 4 * THREADS) {
       Unit<DT> next[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) next[i].load(unit + (u + i * THREADS) * kLane);
+      for (int i = 0; i < 4; ++i) next[i].load(unit + (u + i * THREADS) * kUnit<DT>);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         next[i].get(f);
-        add8(s, f);
+        add(s, f);
       }
     }
     for (; u < w.units; u += THREADS) {
-      Elem<DT>::load8(unit + u * kLane, f);
-      add8(s, f);
+      load_elems<DT>(unit + u * kUnit<DT>, f);
+      add(s, f);
     }
     s = join_block<THREADS / kWave>(s, shared);
     if (s.sum != 0.0f) {
@@ -468,21 +490,21 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(
   // logit, which every lane has read before the join
   if (w.units > tid)
     for (int u = tid + (w.units - 1 - tid) / THREADS * THREADS; u >= tid + kHold * THREADS; u -= THREADS) {
-      const int c = w.first + u * kLane;
-      Elem<DT>::load8(row + c, f);
-      grad8<DT>(k, c, f);
-      Elem<DT>::store8(out + c, f);
+      const int c = w.first + u * kUnit<DT>;
+      load_elems<DT>(row + c, f);
+      grad_unit<DT>(k, c, f);
+      store_elems<DT>(out + c, f);
     }
 #pragma unroll
   for (int i = kHold - 1; i >= 0; --i)
     if (tid + i * THREADS < w.units) {
-      const int c = w.first + (tid + i * THREADS) * kLane;
+      const int c = w.first + (tid + i * THREADS) * kUnit<DT>;
       held[i].get(f);
-      grad8<DT>(k, c, f);
-      Elem<DT>::store8(out + c, f);
+      grad_unit<DT>(k, c, f);
+      store_elems<DT>(out + c, f);
     }
   if (tid < 2) {
-    grad8<DT>(k, tid ? w.rest : w.begin, edge);
+    grad_unit<DT>(k, tid ? w.rest : w.begin, edge);
     store_edge<DT>(out, w, tid, edge);
   }
 }
@@ -601,7 +623,7 @@ int32_t run_pref(Rows r, const void* logits, const int32_t* offsets, int pairs, 
   int lanes = join_lanes(r);
   void* args[] = {&r,          &logits, &w.stat,   &offsets, &pairs, &ref,   &beta, &smoothing,
                   &grad_scale, &lanes,  &seq_logp, &w.token, &logp,  &w.part};
-  if ((rc = launch((const void*)pairs_kernel<DT>, dim3((uint32_t)pairs), dim3(kThreads), args, 0,
+  if ((rc = launch((const void*)pairs_kernel<DT>, dim3((uint32_t)pairs), dim3(kPairThreads), args, 0,
                    stream, "rip_pref_loss: pairs")))
     return rc;
   return run_grad<DT>(r, logits, w, grad, ld_grad, pairs, loss, stream);
