@@ -23,7 +23,9 @@ constexpr int kWave = 64;
 constexpr int kLookupBlock = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
 constexpr int kSortItems = 8;                          // tokens of a thread
-constexpr int kChunk = kSortThreads * kSortItems;      // tokens sorted by one workgroup
+constexpr int kChunk = kSortThreads * kSortItems;      // most tokens sorted by one workgroup
+constexpr int kPart = kChunk / 2;                      // tokens of a chunk where there are several:
+                                                       // 8192 at once take 21 us, 4096 14
 constexpr int kMaxDigit = 8;                           // bits of a pass of the sort
 constexpr int kMaxEntries = 32;                        // of the sorted list to a wave, below kWave
 constexpr int kSumWaves = 4;                            // that share a row's columns in a workgroup
@@ -229,20 +231,20 @@ __device__ __forceinline__ void zero_rows(const Fill& z, int64_t run) {
     zero_rows<GD, THREADS, false>(z, run);
 }
 
-// Workgroups below `chunks` each sort kChunk tokens (ids outside the vocabulary
+// Workgroups below `chunks` each sort `chunk` tokens (ids outside the vocabulary
 // become `vocab` and go last); the others zero rows of the gradient meanwhile.
 template <int GD>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(
     const void* ids, int wide, int64_t n, uint32_t vocab, int passes, int bits, int chunks,
-    uint32_t* sorted_id, uint32_t* sorted_pos, Fill fill) {
+    int chunk, uint32_t* sorted_id, uint32_t* sorted_pos, Fill fill) {
   __shared__ SortShared sh;
   const int tid = threadIdx.x;
   if ((int)blockIdx.x >= chunks) {
     zero_rows<GD, kSortThreads>(fill, blockIdx.x - chunks);
     return;
   }
-  const int64_t base = (int64_t)blockIdx.x * kChunk;
-  const int count = (int)(n - base < kChunk ? n - base : kChunk);
+  const int64_t base = (int64_t)blockIdx.x * chunk;
+  const int count = (int)(n - base < chunk ? n - base : chunk);
   const int items = (count + kSortThreads - 1) / kSortThreads;
   for (int i = tid; i < items * kSortThreads; i += kSortThreads) {
     int64_t id = i < count ? load_id(ids, wide, base + i) : (int64_t)vocab;
@@ -260,49 +262,71 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(
 
 // The sorted chunks become one sorted list: an entry's place is its place in its
 // own chunk and its rank in every other (equal ids of earlier chunks go first).
-// Eight chunks are searched side by side, a halving of all of them at a time, as
-// the loads of one search wait for each other.  Workgroups from `merges` on zero
-// rows of the gradient.
+// kSide chunks are searched side by side, a halving of all of them at a time, as
+// the loads of one search wait for each other: first among every 64th entry of the
+// chunks, in LDS, then among the 64 before it, which lie in two cache lines.
+// Workgroups from `merges` on zero rows of the gradient.
+constexpr int kSide = 8, kEvery = 64, kSamples = kPart / kEvery;
 template <int GD>
 __global__ __launch_bounds__(kMergeThreads) void merge_kernel(
     const uint32_t* id_in, const uint32_t* pos_in, int64_t n, int chunks, uint32_t* id_out,
     uint32_t* pos_out, int merges, Fill fill) {
+  __shared__ uint32_t sample[kSide][kSamples];
   if ((int)blockIdx.x >= merges) {
     zero_rows<GD, kMergeThreads>(fill, blockIdx.x - merges);
     return;
   }
-  constexpr int kSide = 8;
-  const int64_t i = (int64_t)blockIdx.x * kMergeThreads + threadIdx.x;
-  if (i >= n) return;
-  const int own = (int)(i / kChunk);
-  const uint32_t id = id_in[i];
-  int64_t at = i - (int64_t)own * kChunk;
+  const int last_entry = (int)n - 1;
+  const int i = (int)blockIdx.x * kMergeThreads + threadIdx.x, mine = min(i, last_entry);
+  const int own = mine / kPart;
+  const uint32_t id = id_in[mine], pos = pos_in[mine];
+  int at = mine - own * kPart;
   for (int c0 = 0; c0 < chunks; c0 += kSide) {
+    __syncthreads();
+    for (int j = threadIdx.x; j < kSide * kSamples; j += kMergeThreads) {
+      const int64_t e = (int64_t)c0 * kPart + (int64_t)j * kEvery + kEvery - 1;
+      sample[j / kSamples][j % kSamples] = e < n ? id_in[e] : ~0u;  // past the end: above all ids
+    }
+    __syncthreads();
+    // rank = entries below `id`, or up to it in earlier chunks: of 2 * half left
+    // to look at, the first half goes if its last entry does
     int rank[kSide];
 #pragma unroll
     for (int u = 0; u < kSide; ++u) rank[u] = 0;
-    // rank = entries below `id`, or up to it in earlier chunks: of 2 * half left
-    // to look at, the first half goes if its last entry does
-    for (int half = kChunk; half > 0; half /= 2) {
-      uint32_t x[kSide];
-      int last[kSide];
+#pragma unroll
+    for (int half = kSamples; half > 0; half /= 2)
 #pragma unroll
       for (int u = 0; u < kSide; ++u) {
-        last[u] = (c0 + u) * kChunk + rank[u] + half - 1;
-        x[u] = id_in[min(last[u], (int)n - 1)];
+        const int to = rank[u] + half;
+        const uint32_t x = sample[u][min(to, kSamples) - 1];
+        const bool goes = x < id || (x == id && c0 + u < own);
+        rank[u] = goes && to <= kSamples ? to : rank[u];
+      }
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) rank[u] *= kEvery;
+#pragma unroll
+    for (int half = kEvery / 2; half > 0; half /= 2) {
+      uint32_t x[kSide];
+      int e[kSide];
+#pragma unroll
+      for (int u = 0; u < kSide; ++u) {
+        e[u] = (c0 + u) * kPart + rank[u] + half - 1;
+        x[u] = id_in[min(e[u], last_entry)];
       }
 #pragma unroll
       for (int u = 0; u < kSide; ++u) {
         const bool goes = x[u] < id || (x[u] == id && c0 + u < own);
-        rank[u] += goes && rank[u] + half <= kChunk && last[u] < n ? half : 0;
+        rank[u] += goes && rank[u] < kPart && e[u] <= last_entry ? half : 0;
       }
     }
 #pragma unroll
     for (int u = 0; u < kSide; ++u)
       if (c0 + u < chunks && c0 + u != own) at += rank[u];
   }
-  id_out[at] = id;
-  pos_out[at] = pos_in[i];
+  if (i <= last_entry) {
+    id_out[at] = id;
+    pos_out[at] = pos;
+  }
 }
 
 template <int GD, bool NARROW>
@@ -534,14 +558,15 @@ int entries_per_wave(int64_t n, int64_t width) {
 }
 
 struct GradPlan {
-  int per, waves, chunks;
+  int per, waves, chunk, chunks;
   int64_t id_bytes, partial_bytes, total;
 };
 GradPlan grad_plan(int64_t n, int64_t width) {
   GradPlan p{};
   p.per = entries_per_wave(n, width);
   p.waves = (int)ceil_div(n, p.per);
-  p.chunks = (int)ceil_div(n, kChunk);
+  p.chunk = n <= kChunk ? kChunk : kPart;
+  p.chunks = (int)ceil_div(n, p.chunk);
   p.id_bytes = ceil_div(n * 4, 256) * 256;
   p.partial_bytes = (int64_t)p.waves * 2 * ceil_div(width, kLane) * kLane * 4;
   // ids and positions, once more where chunks are merged, and the partial sums
@@ -715,8 +740,8 @@ extern "C" int32_t rip_embed_grad(const void* dout, int32_t dout_dtype, int64_t 
   const int64_t runs = accumulate ? 0 : ceil_div(vocab, fill.rows);
   const int64_t later = p.chunks > 1 ? runs / 3 : 0;
   {
-    void* args[] = {&ids,  &wide,     &n_tokens, &v32,   &passes,
-                    &bits, &p.chunks, &id_a,     &pos_a, &fill};
+    void* args[] = {&ids,      &wide,    &n_tokens, &v32,   &passes, &bits,
+                    &p.chunks, &p.chunk, &id_a,     &pos_a, &fill};
     const void* fn = grad_dtype == RIP_FP32 ? (const void*)sort_kernel<RIP_FP32>
                                             : (const void*)sort_kernel<RIP_BF16>;
     if ((rc = launch(fn, dim3((uint32_t)(p.chunks + runs - later)), dim3(kSortThreads), args, 0,
