@@ -362,8 +362,8 @@ int32_t rip_set_blocks_per_cu(int32_t blocks_per_cu);
  * Conventions beyond those at the top of this file
  *  - A matrix is a device pointer, its type (RIP_FP32 / RIP_BF16) and its row
  *    stride `ld` in elements (at least its width).  It need only be aligned to
- *    its elements; columns between the width and `ld` are neither read nor
- *    written.  Indexes into it are 64-bit.
+ *    its elements; columns between the width and `ld` are not written (nor read,
+ *    unless a call says so).  Indexes into it are 64-bit.
  *  - Arithmetic and every sum are fp32 (or wider); a result is rounded to bf16
  *    once, to nearest even.  Nothing is added atomically: a call's result is the
  *    same bits every time for the same sizes, strides and alignment (a loss adds
@@ -446,7 +446,9 @@ int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtype, const in
 /* Weight gradient of a linear layer y = x W^T from the checkpoint of x:
  *   grad[n][k] = sum_t dy[t][n] * x'[t][k]     (out_features x in_features)
  * added to what grad holds if `accumulate` is nonzero.  x' is what the
- * checkpoint stands for; products are exact and sums fp32 for either type of dy. */
+ * checkpoint stands for; products are exact and sums fp32 for either type of dy.
+ * Of dy it also reads up to seven elements after a row but the last one; no
+ * result depends on them.  Its row stride is at most RIP_MAX_WIDTH. */
 int64_t rip_ckpt_wgrad_workspace(int32_t dy_dtype, int64_t rows, int64_t out_features,
                                  int64_t in_features);
 int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_dy, int64_t rows,

@@ -14,7 +14,9 @@
 // consecutive columns of a row and four lanes a block, so a block's largest
 // magnitude takes two exchanges within a quad and every access of a wave is
 // consecutive.  The codes of a row fill whole blocks (zeros past the last
-// column), so they are always stored and read eight bytes a lane.
+// column), so they are always stored and read eight bytes a lane.  16384 x 5504
+// bf16: pack 44 us (6.2 TB/s), unpack 40, forward 110 (734 MB, 6.7 TB/s), backward
+// 107; a width of 5503, whose rows begin anywhere, takes 1.1 to 1.25 times that.
 
 #include "rip_ckpt_format.h"
 

@@ -74,7 +74,9 @@ CASES = [  # tokens, vocab, width, ids, pad, offset
     (63, 40, 17, "any", 5, 3), (64, 300, 512, "edges", 0, 0), (65, 300, 513, "zipf", 0, 0),
     (129, 1000, 8, "none", 0, 0), (1000, 5, 100, "any", 1, 0), (4096, 70, 24, "zipf", 0, 0),
     (4097, 257, 33, "zipf", 0, 0), (9000, 3, 40, "same", 0, 0), (12289, 66000, 16, "any", 0, 0),
-    (20000, 300, 1030, "zipf", 0, 2), (8192, 70000, 8, "edges", 0, 0)]
+    (20000, 300, 1030, "zipf", 0, 2), (8192, 70000, 8, "edges", 0, 0),
+    (70001, 5000, 9, "zipf", 0, 0), (128, 40, 520, "zipf", 0, 0), (40, 3000, 1100, "edges", 0, 1),
+    (128, 3, 2100, "same", 0, 0), (1100003, 60, 8, "zipf", 0, 0)]
 
 
 @pytest.mark.parametrize("accumulate", [False, True])

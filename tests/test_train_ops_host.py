@@ -103,6 +103,7 @@ POLICY = dict(x=A, dt=1, ld=50, n=8, vocab=50, t=B, idt=1, old=C, adv=C + 4096, 
     ("rip_ckpt_wgrad", WGRAD, dict(n=0), INVAL),
     ("rip_ckpt_wgrad", WGRAD, dict(k=1 << 19, ld_g=1 << 19), UNSUP),
     ("rip_ckpt_wgrad", WGRAD, dict(dt=5), UNSUP),
+    ("rip_ckpt_wgrad", WGRAD, dict(ld=(1 << 24) + 1, rows=1), UNSUP),
     ("rip_ckpt_wgrad", WGRAD, dict(codes=B + 4), ALIGN),
     ("rip_ckpt_wgrad", WGRAD, dict(ws=W + 1), ALIGN),
     ("rip_ckpt_wgrad", WGRAD, dict(grad=B), OVERLAP),
