@@ -10,11 +10,12 @@
 //                  and, if asked for, h' = gate' * s * up' packed anew: the
 //                  checkpoint of the next layer's input, which need not be kept
 //
-// Each is one pass over its data, bound by memory.  A lane handles eight
-// consecutive columns of a row and four lanes a block, so a block's largest
-// magnitude takes two exchanges within a quad and every access of a wave is
-// consecutive.  The codes of a row fill whole blocks (zeros past the last
-// column), so they are always stored and read eight bytes a lane.  16384 x 5504
+// Each is one pass over its data, bound by memory.  A lane handles sixteen bytes of
+// a row, eight columns of bf16 or four of fp32, so that every access of a wave is
+// one range (fp32 with eight columns a lane: 116 us for the backward pass of 8192 x
+// 5504, 94 so), and four or eight lanes a block, whose largest magnitude takes
+// two or three exchanges between them.  The codes of a row fill whole blocks
+// (zeros past the last column), so they are always stored and read whole.  16384 x 5504
 // bf16: pack 44 us (6.2 TB/s), unpack 40, forward 110 (734 MB, 6.7 TB/s), backward
 // 107; a width of 5503, whose rows begin anywhere, takes 1.1 to 1.25 times that.
 
@@ -25,14 +26,50 @@ namespace {
 
 constexpr int kBlockThreads = 256;
 
-// A row's blocks as the kernels index them: `units` lanes of eight columns in
-// all, 4 * blocks to a row.
+template <int DT>
+constexpr int kCols = DT == RIP_BF16 ? 8 : 4;  // columns of a lane
+template <int DT>
+constexpr int kLanes = kCkptBlock / kCols<DT>;  // lanes of a block
+
+// A matrix's blocks as the kernels index them: a lane each for its units.
 struct Shape {
   uint32_t units;
   FastDiv per_row;
   int width;
-  int blocks;
+  uint32_t blocks;  // of all rows
 };
+
+// Columns c .. c + kCols - 1 of a row; zero past its end, nothing read there.
+template <int DT, bool STREAM = false>
+__device__ __forceinline__ void load_cols(const typename Elem<DT>::T* row, int c, int width,
+                                          float (&f)[kCols<DT>]) {
+  if constexpr (DT == RIP_BF16) {
+    load_unit<DT, STREAM>(row, c, width, f);
+  } else if (c + 4 <= width) {
+    const u32x4 a = STREAM ? load_stream((const u32x4_any*)(row + c)) : *(const u32x4_any*)(row + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = __uint_as_float(a[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = c + j < width ? row[c + j] : 0.0f;
+  }
+}
+template <int DT>
+__device__ __forceinline__ void store_cols(typename Elem<DT>::T* row, int c, int width,
+                                           const float (&f)[kCols<DT>]) {
+  if constexpr (DT == RIP_BF16) {
+    store_unit<DT>(row, c, width, f);
+  } else if (c + 4 <= width) {
+    u32x4_any a;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[j] = __float_as_uint(f[j]);
+    store_stream((u32x4_any*)(row + c), a);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (c + j < width) row[c + j] = f[j];
+  }
+}
 
 struct Ckpt {
   int8_t* codes;
@@ -46,25 +83,39 @@ struct Place {
   int64_t exp;   // index of its block's exponent
   bool lead;   // first lane of the block
 };
+template <int DT>
 __device__ __forceinline__ Place place(const Shape& s, uint32_t unit) {
   Place p;
   const uint32_t row = s.per_row.div(unit), in = unit - row * s.per_row.d;
   p.row = row;
-  p.col = (int)in * kLane;
-  p.code = (int64_t)unit * kLane;
-  p.exp = unit / kCkptLanes;
-  p.lead = in % kCkptLanes == 0;
+  p.col = (int)in * kCols<DT>;
+  p.code = (int64_t)unit * kCols<DT>;
+  p.exp = unit / kLanes<DT>;
+  p.lead = in % kLanes<DT> == 0;
   return p;
 }
 
-__device__ __forceinline__ void store_ckpt(const Ckpt& c, const Place& p, const float (&x)[kLane]) {
-  uint2 codes;
-  const uint32_t e = ckpt_pack(x, codes);
-  *(uint2*)(c.codes + p.code) = codes;
+template <int DT>
+__device__ __forceinline__ void store_ckpt(const Ckpt& c, const Place& p,
+                                           const float (&x)[kCols<DT>]) {
+  uint32_t codes[kCols<DT> / 4];
+  const uint32_t e = ckpt_pack<kCols<DT>>(x, codes);
+  if constexpr (DT == RIP_BF16)
+    *(uint2*)(c.codes + p.code) = make_uint2(codes[0], codes[1]);
+  else
+    *(uint32_t*)(c.codes + p.code) = codes[0];
   if (p.lead) c.exps[p.exp] = (uint8_t)e;
 }
-__device__ __forceinline__ void load_ckpt(const Ckpt& c, const Place& p, float (&x)[kLane]) {
-  ckpt_unpack(*(const uint2*)(c.codes + p.code), c.exps[p.exp], x);
+template <int DT>
+__device__ __forceinline__ void load_ckpt(const Ckpt& c, const Place& p, float (&x)[kCols<DT>]) {
+  uint32_t codes[kCols<DT> / 4];
+  if constexpr (DT == RIP_BF16) {
+    const uint2 v = *(const uint2*)(c.codes + p.code);
+    codes[0] = v.x, codes[1] = v.y;
+  } else {
+    codes[0] = *(const uint32_t*)(c.codes + p.code);
+  }
+  ckpt_unpack<kCols<DT>>(codes, c.exps[p.exp], x);
 }
 
 // 1 / (1 + e^-x), from e^-|x|, which neither overflows nor loses the small
@@ -76,17 +127,17 @@ __device__ __forceinline__ float sigmoid(float x) {
   return x < 0.0f ? e * y : y;
 }
 
-// The four lanes of a block take every branch together: units is a multiple of
-// four and so is the number of lanes past it.
+// The lanes of a block take every branch together: units are whole blocks, and so
+// are the lanes past them.
 template <int DT>
 __global__ __launch_bounds__(kBlockThreads) void pack_kernel(Shape s, const typename Elem<DT>::T* x,
                                                              int64_t ld, Ckpt out) {
   const uint32_t unit = blockIdx.x * kBlockThreads + threadIdx.x;
   if (unit >= s.units) return;
-  const Place p = place(s, unit);
-  float f[kLane];
-  load_unit<DT>(x + p.row * ld, p.col, s.width, f);
-  store_ckpt(out, p, f);
+  const Place p = place<DT>(s, unit);
+  float f[kCols<DT>];
+  load_cols<DT>(x + p.row * ld, p.col, s.width, f);
+  store_ckpt<DT>(out, p, f);
 }
 
 template <int DT>
@@ -95,10 +146,10 @@ __global__ __launch_bounds__(kBlockThreads) void unpack_kernel(Shape s, Ckpt in,
                                                                int64_t ld) {
   const uint32_t unit = blockIdx.x * kBlockThreads + threadIdx.x;
   if (unit >= s.units) return;
-  const Place p = place(s, unit);
-  float f[kLane];
-  load_ckpt(in, p, f);
-  store_unit<DT>(x + p.row * ld, p.col, s.width, f);
+  const Place p = place<DT>(s, unit);
+  float f[kCols<DT>];
+  load_ckpt<DT>(in, p, f);
+  store_cols<DT>(x + p.row * ld, p.col, s.width, f);
 }
 
 // STREAM: the inputs are read past the caches.
@@ -108,15 +159,15 @@ __global__ __launch_bounds__(kBlockThreads) void gate_forward_kernel(
     int64_t ld_up, typename Elem<DT>::T* h, int64_t ld_h, Ckpt gate8, Ckpt up8) {
   const uint32_t unit = blockIdx.x * kBlockThreads + threadIdx.x;
   if (unit >= s.units) return;
-  const Place p = place(s, unit);
-  float g[kLane], u[kLane];
-  load_unit<DT, STREAM>(gate + p.row * ld_gate, p.col, s.width, g);
-  load_unit<DT, STREAM>(up + p.row * ld_up, p.col, s.width, u);
-  store_ckpt(gate8, p, g);
-  store_ckpt(up8, p, u);
+  const Place p = place<DT>(s, unit);
+  float g[kCols<DT>], u[kCols<DT>];
+  load_cols<DT, STREAM>(gate + p.row * ld_gate, p.col, s.width, g);
+  load_cols<DT, STREAM>(up + p.row * ld_up, p.col, s.width, u);
+  store_ckpt<DT>(gate8, p, g);
+  store_ckpt<DT>(up8, p, u);
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) g[j] = g[j] * sigmoid(g[j]) * u[j];
-  store_unit<DT>(h + p.row * ld_h, p.col, s.width, g);
+  for (int j = 0; j < kCols<DT>; ++j) g[j] = g[j] * sigmoid(g[j]) * u[j];
+  store_cols<DT>(h + p.row * ld_h, p.col, s.width, g);
 }
 
 template <int DT, bool AGAIN, bool STREAM>
@@ -126,49 +177,59 @@ __global__ __launch_bounds__(kBlockThreads) void gate_backward_kernel(
     Ckpt h8) {
   const uint32_t unit = blockIdx.x * kBlockThreads + threadIdx.x;
   if (unit >= s.units) return;
-  const Place p = place(s, unit);
-  float d[kLane], g[kLane], u[kLane];
-  load_unit<DT, STREAM>(dh + p.row * ld_dh, p.col, s.width, d);
-  load_ckpt(gate8, p, g);
-  load_ckpt(up8, p, u);
-  float a[kLane], h[kLane];
+  const Place p = place<DT>(s, unit);
+  float d[kCols<DT>], g[kCols<DT>], u[kCols<DT>];
+  load_cols<DT, STREAM>(dh + p.row * ld_dh, p.col, s.width, d);
+  load_ckpt<DT>(gate8, p, g);
+  load_ckpt<DT>(up8, p, u);
+  float a[kCols<DT>], h[kCols<DT>];
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) {
+  for (int j = 0; j < kCols<DT>; ++j) {
     const float sg = sigmoid(g[j]);
     const float silu = g[j] * sg;
     a[j] = d[j] * u[j] * (sg * (1.0f + g[j] * (1.0f - sg)));
     h[j] = silu * u[j];
     d[j] *= silu;
   }
-  store_unit<DT>(dgate + p.row * ld_dgate, p.col, s.width, a);
-  store_unit<DT>(dup + p.row * ld_dup, p.col, s.width, d);
-  if (AGAIN) store_ckpt(h8, p, h);
+  store_cols<DT>(dgate + p.row * ld_dgate, p.col, s.width, a);
+  store_cols<DT>(dup + p.row * ld_dup, p.col, s.width, d);
+  if (AGAIN) store_ckpt<DT>(h8, p, h);
 }
 
-int32_t make_shape(int64_t rows, int64_t width, Shape* out) {
+int32_t make_shape(int32_t dtype, int64_t rows, int64_t width, Shape* out) {
+  if (!known_dtype(dtype)) return fail(RIP_E_UNSUPPORTED, "unknown dtype %d", dtype);
   if (rows < 0 || width < 1)
     return fail(RIP_E_INVAL, "%lld rows of width %lld", (long long)rows, (long long)width);
   const int64_t blocks = ceil_div(width, kCkptBlock);
+  const int lanes = dtype == RIP_BF16 ? kLanes<RIP_BF16> : kLanes<RIP_FP32>;
   if (rows > RIP_MAX_TOKENS || width > RIP_MAX_WIDTH ||
-      rows * blocks * kCkptLanes >= (int64_t)1 << 31)
+      rows * blocks * kLanes<RIP_FP32> >= (int64_t)1 << 31)
     return fail(RIP_E_UNSUPPORTED, "%lld rows of width %lld are above the limit", (long long)rows,
                 (long long)width);
-  out->units = (uint32_t)(rows * blocks * kCkptLanes);
-  out->per_row = FastDiv::make((uint32_t)(blocks * kCkptLanes));
+  out->units = (uint32_t)(rows * blocks * lanes);
+  out->per_row = FastDiv::make((uint32_t)(blocks * lanes));
   out->width = (int)width;
-  out->blocks = (int)blocks;
+  out->blocks = (uint32_t)(rows * blocks);
   return RIP_OK;
+}
+
+template <int DT>
+const void* backward_of(bool again, bool past) {
+  return again ? (past ? (const void*)gate_backward_kernel<DT, true, true>
+                       : (const void*)gate_backward_kernel<DT, true, false>)
+               : (past ? (const void*)gate_backward_kernel<DT, false, true>
+                       : (const void*)gate_backward_kernel<DT, false, false>);
 }
 
 // Inputs that the memory-side cache cannot hold are read past it (16384 x 5504 bf16
 // forward 113 us against 119, backward 107 against 117); smaller ones may lie in it
 // from the launch that made them (8192 x 1024: 13 against 15 past it).
 bool stream_inputs(int32_t dtype, int64_t rows, int64_t width, int inputs) {
-  return dtype == RIP_BF16 && rows * width * elem_bytes(dtype) * inputs > kCacheBytes;
+  return rows * width * elem_bytes(dtype) * inputs > kCacheBytes;
 }
 
-int64_t code_bytes(const Shape& s) { return (int64_t)s.units * kLane; }
-int64_t exp_bytes(const Shape& s) { return s.units / kCkptLanes; }
+int64_t code_bytes(const Shape& s) { return (int64_t)s.blocks * kCkptBlock; }
+int64_t exp_bytes(const Shape& s) { return s.blocks; }
 
 // The buffers of a call; those that are written share no element with any
 // other, except an output that is exactly one of the inputs (each element is
@@ -233,7 +294,7 @@ extern "C" int32_t rip_ckpt_pack(const void* x, int32_t dtype, int64_t ld, int64
   clear_error();
   int32_t rc;
   Shape s;
-  if ((rc = make_shape(rows, width, &s)) || (rc = check_matrix(x, "x", dtype, rows, width, ld)) ||
+  if ((rc = make_shape(dtype, rows, width, &s)) || (rc = check_matrix(x, "x", dtype, rows, width, ld)) ||
       (rc = check_ckpt(codes, exps, "out", s)))
     return rc;
   Buffers b;
@@ -254,7 +315,7 @@ extern "C" int32_t rip_ckpt_unpack(const int8_t* codes, const uint8_t* exps, int
   clear_error();
   int32_t rc;
   Shape s;
-  if ((rc = make_shape(rows, width, &s)) || (rc = check_matrix(x, "x", dtype, rows, width, ld)) ||
+  if ((rc = make_shape(dtype, rows, width, &s)) || (rc = check_matrix(x, "x", dtype, rows, width, ld)) ||
       (rc = check_ckpt(codes, exps, "in", s)))
     return rc;
   Buffers b;
@@ -276,7 +337,7 @@ extern "C" int32_t rip_gate_forward(const void* gate, int64_t ld_gate, const voi
   clear_error();
   int32_t rc;
   Shape s;
-  if ((rc = make_shape(rows, width, &s)) ||
+  if ((rc = make_shape(dtype, rows, width, &s)) ||
       (rc = check_matrix(gate, "gate", dtype, rows, width, ld_gate)) ||
       (rc = check_matrix(up, "up", dtype, rows, width, ld_up)) ||
       (rc = check_matrix(h, "h", dtype, rows, width, ld_h)) ||
@@ -294,10 +355,11 @@ extern "C" int32_t rip_gate_forward(const void* gate, int64_t ld_gate, const voi
   if ((rc = b.check())) return rc;
   Ckpt g8{gate_codes, gate_exps}, u8{up_codes, up_exps};
   void* args[] = {&s, &gate, &ld_gate, &up, &ld_up, &h, &ld_h, &g8, &u8};
-  const void* fn = dtype == RIP_FP32 ? (const void*)gate_forward_kernel<RIP_FP32, false>
-                   : stream_inputs(dtype, rows, width, 2)
-                       ? (const void*)gate_forward_kernel<RIP_BF16, true>
-                       : (const void*)gate_forward_kernel<RIP_BF16, false>;
+  const bool past = stream_inputs(dtype, rows, width, 2);
+  const void* fn = dtype == RIP_FP32 ? (past ? (const void*)gate_forward_kernel<RIP_FP32, true>
+                                             : (const void*)gate_forward_kernel<RIP_FP32, false>)
+                                     : (past ? (const void*)gate_forward_kernel<RIP_BF16, true>
+                                             : (const void*)gate_forward_kernel<RIP_BF16, false>);
   return run(fn, s, args, stream, "rip_gate_forward");
 }
 
@@ -310,7 +372,7 @@ extern "C" int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtyp
   clear_error();
   int32_t rc;
   Shape s;
-  if ((rc = make_shape(rows, width, &s)) ||
+  if ((rc = make_shape(dtype, rows, width, &s)) ||
       (rc = check_matrix(dh, "dh", dtype, rows, width, ld_dh)) ||
       (rc = check_matrix(dgate, "dgate", dtype, rows, width, ld_dgate)) ||
       (rc = check_matrix(dup, "dup", dtype, rows, width, ld_dup)) ||
@@ -336,15 +398,8 @@ extern "C" int32_t rip_gate_backward(const void* dh, int64_t ld_dh, int32_t dtyp
   Ckpt u8{const_cast<int8_t*>(up_codes), const_cast<uint8_t*>(up_exps)};
   Ckpt h8{h_codes, h_exps};
   void* args[] = {&s, &dh, &ld_dh, &g8, &u8, &dgate, &ld_dgate, &dup, &ld_dup, &h8};
-  const void* fn;
-  if (dtype == RIP_FP32)
-    fn = again ? (const void*)gate_backward_kernel<RIP_FP32, true, false>
-               : (const void*)gate_backward_kernel<RIP_FP32, false, false>;
-  else if (stream_inputs(dtype, rows, width, 2))  // dh, and as many bytes of checkpoints
-    fn = again ? (const void*)gate_backward_kernel<RIP_BF16, true, true>
-               : (const void*)gate_backward_kernel<RIP_BF16, false, true>;
-  else
-    fn = again ? (const void*)gate_backward_kernel<RIP_BF16, true, false>
-               : (const void*)gate_backward_kernel<RIP_BF16, false, false>;
+  const bool past = stream_inputs(dtype, rows, width, 2);  // dh, and at most as much again
+  const void* fn = dtype == RIP_FP32 ? backward_of<RIP_FP32>(again, past)
+                                     : backward_of<RIP_BF16>(again, past);
   return run(fn, s, args, stream, "rip_gate_backward");
 }

@@ -16,7 +16,6 @@
 namespace rip {
 
 constexpr int kCkptBlock = 32;                 // columns of a block
-constexpr int kCkptLanes = kCkptBlock / kLane; // lanes that hold a block
 constexpr uint32_t kCkptMax = 121 + 127;       // largest exponent byte of a finite block
 constexpr uint32_t kCkptNan = 255;             // exponent byte of a block with an inf or NaN
 
@@ -28,29 +27,30 @@ __device__ __forceinline__ uint32_t ckpt_exponent(uint32_t top) {
   return top >= 0x7f800000u ? kCkptNan : (uint32_t)max(1, min(e, (int)kCkptMax));
 }
 
-// Exponent byte and codes (8 bytes) of the lane's eight values; the four lanes
+// Exponent byte and codes (four to a word) of the lane's N values; the 32 / N lanes
 // of a block are consecutive and all active.
-__device__ __forceinline__ uint32_t ckpt_pack(const float (&x)[kLane], uint2& codes) {
+template <int N>
+__device__ __forceinline__ uint32_t ckpt_pack(const float (&x)[N], uint32_t (&codes)[N / 4]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-  top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-  top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+  for (int j = 0; j < N; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 1; o < kCkptBlock / N; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o));
   const uint32_t e = ckpt_exponent(top);
   // x / 2^e + 1.5 * 2^23, rounded once to nearest even: its low byte is q
   const float inv = e == kCkptNan ? 0.0f : __uint_as_float((254 - e) << 23);
-  uint32_t q[kLane];
+  uint32_t q[N];
 #pragma unroll
-  for (int j = 0; j < kLane; ++j)
+  for (int j = 0; j < N; ++j)
     q[j] = __float_as_uint(__builtin_fmaf(x[j], inv, 12582912.0f)) & 0xff;
   if (e == kCkptMax) {  // the one step that a magnitude may exceed
 #pragma unroll
-    for (int j = 0; j < kLane; ++j)
+    for (int j = 0; j < N; ++j)
       q[j] = (uint32_t)(int)fminf(fmaxf(rintf(x[j] * inv), -127.0f), 127.0f) & 0xff;
   }
-  codes.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
-  codes.y = q[4] | q[5] << 8 | q[6] << 16 | q[7] << 24;
-  if (e == kCkptNan) codes.x = codes.y = 0;
+#pragma unroll
+  for (int j = 0; j < N; j += 4)
+    codes[j / 4] = e == kCkptNan ? 0 : q[j] | q[j + 1] << 8 | q[j + 2] << 16 | q[j + 3] << 24;
   return e;
 }
 
@@ -65,10 +65,12 @@ __device__ __forceinline__ float widen(uint32_t w, int j) {
   return (float)((int)(w << (24 - 8 * j)) >> 24);
 }
 
-__device__ __forceinline__ void ckpt_unpack(uint2 codes, uint32_t e, float (&x)[kLane]) {
+template <int N>
+__device__ __forceinline__ void ckpt_unpack(const uint32_t (&codes)[N / 4], uint32_t e,
+                                            float (&x)[N]) {
   const float step = ckpt_step(e);
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) x[j] = widen(j < 4 ? codes.x : codes.y, j % 4) * step;
+  for (int j = 0; j < N; ++j) x[j] = widen(codes[j / 4], j % 4) * step;
 }
 
 }  // namespace rip

@@ -222,7 +222,8 @@ struct Tile {
       const int u = unit<kXAll>(i / 2), row = u / (kK / kCodes);
       const int c = u % (kK / kCodes) * kCodes + i % 2 * kLane;
       float x[kLane];
-      ckpt_unpack(make_uint2(r.x[i / 2][i % 2 * 2], r.x[i / 2][i % 2 * 2 + 1]), r.e[i / 2], x);
+      const uint32_t codes[2] = {r.x[i / 2][i % 2 * 2], r.x[i / 2][i % 2 * 2 + 1]};
+      ckpt_unpack<kLane>(codes, r.e[i / 2], x);
       u32x4 v;  // the values' low halves are zeros
 #pragma unroll
       for (int j = 0; j < 4; ++j)
