@@ -294,28 +294,14 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Half of a step: the products of the operands in `f`, and beside every MK matrix
 // instructions (each keeps its unit busy for 32 cycles) a share of the reads of the
-// next operands and of the writes of a later step, spread between them.
-template <int MFMA, int READS, int VALU, int WRITES, int LOADS, int I = 0>
-__device__ __forceinline__ void interleave() {
-  if constexpr (I < MFMA) {
-    constexpr int kRead = (I + 1) * READS / MFMA - I * READS / MFMA;
-    constexpr int kValu = (I + 1) * VALU / MFMA - I * VALU / MFMA;
-    constexpr int kWrite = (I + 1) * WRITES / MFMA - I * WRITES / MFMA;
-    constexpr int kLoad = (I + 1) * LOADS / MFMA - I * LOADS / MFMA;
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    if constexpr (kRead > 0) __builtin_amdgcn_sched_group_barrier(0x100, kRead, 0);
-    if constexpr (kLoad > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoad, 0);
-    if constexpr (kValu > 0) __builtin_amdgcn_sched_group_barrier(0x002, kValu, 0);
-    if constexpr (kWrite > 0) __builtin_amdgcn_sched_group_barrier(0x200, kWrite, 0);
-    interleave<MFMA, READS, VALU, WRITES, LOADS, I + 1>();
-  }
-}
+// next operands and of the writes of a later step.  The compiler orders what lies
+// between two sched_barriers, and may not gather all reads or all products.
 template <typename Tl, int HALF, int C = 0, typename Load>
 __device__ __forceinline__ void half(const typename Tl::Frags& f, f32x16 (&acc)[Tl::MN][Tl::MK],
                                      const typename Tl::Shared& from, int at, int wn, int wk,
                                      int lane, typename Tl::Frags& next, typename Tl::Regs& regs,
                                      typename Tl::Shared& to, Load& load) {
-  constexpr int MN = Tl::MN, MK = Tl::MK, kRows = Tl::kParts * MN, kLast = 2 * kRows - 1;
+  constexpr int MN = Tl::MN, kRows = Tl::kParts * MN, kLast = 2 * kRows - 1;
   if constexpr (C < kRows) {
     constexpr int r0 = C * Tl::kOperands / kRows, r1 = (C + 1) * Tl::kOperands / kRows;
     constexpr int g = HALF * kRows + C;  // the last one starts the loads instead of writing
@@ -326,8 +312,6 @@ __device__ __forceinline__ void half(const typename Tl::Frags& f, f32x16 (&acc)[
     else
       load(regs);
     Tl::multiply(f, C / MN, C % MN, acc);
-    interleave<MK, 2 * (r1 - r0), 22 * (i1 - i0), i1 - i0,
-               g < kLast ? 0 : 2 * Tl::kXUnits + Tl::kYUnits * Tl::kYRegs>();
     __builtin_amdgcn_sched_barrier(0);
     half<Tl, HALF, C + 1>(f, acc, from, at, wn, wk, lane, next, regs, to, load);
   }
@@ -558,6 +542,10 @@ int32_t run(Product& p, const Plan& plan, const void* dy, const int8_t* codes, c
                 args2, 0, stream, "rip_ckpt_wgrad: reduce");
 }
 
+int64_t part_bytes(const Plan& plan, int64_t n) {
+  return plan.splits > 1 ? plan.splits * n * plan.part_k * 4 : 0;
+}
+
 bool sizes_ok(int64_t tokens, int64_t n, int64_t k) {
   return tokens >= 0 && tokens <= RIP_MAX_TOKENS && n >= 1 && n <= RIP_MAX_FEATURES && k >= 1 &&
          k <= RIP_MAX_FEATURES;
@@ -571,8 +559,7 @@ using namespace rip;
 extern "C" int64_t rip_ckpt_wgrad_workspace(int32_t dy_dtype, int64_t rows,
                                             int64_t out_features, int64_t in_features) {
   if (!known_dtype(dy_dtype) || !sizes_ok(rows, out_features, in_features)) return 0;
-  const Plan plan = make_plan(dy_dtype, rows, out_features, in_features);
-  return plan.splits > 1 ? plan.splits * out_features * plan.part_k * 4 : 0;
+  return part_bytes(make_plan(dy_dtype, rows, out_features, in_features), out_features);
 }
 
 extern "C" int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_dy, int64_t rows,
@@ -597,7 +584,8 @@ extern "C" int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_d
   if (ld_dy > RIP_MAX_WIDTH)
     return fail(RIP_E_UNSUPPORTED, "rip_ckpt_wgrad: row stride %lld of dy is above the limit",
                 (long long)ld_dy);
-  const int64_t need = rip_ckpt_wgrad_workspace(dy_dtype, rows, out_features, in_features);
+  const Plan plan = make_plan(dy_dtype, rows, out_features, in_features);
+  const int64_t need = part_bytes(plan, out_features);
   if (need && (!workspace || workspace_bytes < need))
     return fail(RIP_E_INVAL, "rip_ckpt_wgrad: workspace of %lld bytes, %lld needed",
                 (long long)workspace_bytes, (long long)need);
@@ -613,7 +601,6 @@ extern "C" int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_d
       overlap(workspace, need, exps, rows * blocks))
     return fail(RIP_E_OVERLAP, "rip_ckpt_wgrad: grad or workspace overlaps another buffer");
   if (rows == 0 && accumulate) return RIP_OK;
-  const Plan plan = make_plan(dy_dtype, rows, out_features, in_features);
   Product p{rows,
             ld_dy,
             ld_grad,
