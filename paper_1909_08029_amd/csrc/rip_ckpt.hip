@@ -16,8 +16,8 @@
 // 5504, 94 so), and four or eight lanes a block, whose largest magnitude takes
 // two or three exchanges between them.  The codes of a row fill whole blocks
 // (zeros past the last column), so they are always stored and read whole.  16384 x 5504
-// bf16: pack 44 us (6.2 TB/s), unpack 40, forward 110 (734 MB, 6.7 TB/s), backward
-// 107; a width of 5503, whose rows begin anywhere, takes 1.1 to 1.25 times that.
+// bf16: pack 44 us (6.2 TB/s), unpack 40, forward 112 (734 MB, 6.6 TB/s), backward
+// 109; a width of 5503, whose rows begin anywhere, takes 1.1 to 1.25 times that.
 
 #include "rip_ckpt_format.h"
 

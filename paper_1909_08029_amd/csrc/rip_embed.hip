@@ -6,9 +6,9 @@
 // Both are bound by memory: the lookup reads and writes a row a token, the
 // gradient reads a row a token and writes the whole table's gradient (P-Reduce
 // reads every element of it).  65536 tokens, a table of 131072 x 2048, all bf16:
-// the lookup takes 59 us (350 MB, 5.9 TB/s), the gradient 185: sort and two thirds
-// of the zeros 68, merge and the other third 33 (537 MB, 5.3 TB/s), sums 72 (350
-// MB, 4.9 TB/s), joins 12.
+// the lookup takes 59 us (350 MB, 5.9 TB/s), the gradient 187: sort and two thirds
+// of the zeros 68, merge and the other third 37 (537 MB, 5.1 TB/s), sums 70 (350
+// MB, 5.0 TB/s), joins 12.
 //
 // The gradient runs over the tokens sorted by id, a fixed number of them to a
 // wave, however often an id occurs: a frequent id is shared by many waves

@@ -17,7 +17,7 @@
 //
 // Bound by memory: the preference loss reads the logits twice (coef needs the whole
 // pair) and writes the gradient once, 8192 x 50257 bf16, two thirds of it counted:
-// stats 92 us (549 MB, 6.0 TB/s), pairs 7, grad 277 (1372 MB, 5.0 TB/s).  The policy
+// stats 90 us (549 MB, 6.1 TB/s), pairs 7, grad 277 (1372 MB, 5.0 TB/s).  The policy
 // loss needs no more than the row, which one workgroup takes through all three
 // steps: 8192 x 131072 bf16, three quarters counted, 722 us (3.76 GB, 5.2 TB/s).
 
@@ -430,7 +430,8 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows r,
 // The policy loss of one token in one workgroup, gradient and all: coef needs
 // nothing beyond the token's own row.  The first kHold units of a lane stay in
 // registers between the two passes; the rest is read again, last first, mostly
-// from the caches (8192 rows of 131072 bf16: 1031 us in three launches, 780 so before either streamed its stores).
+// from the caches (8192 rows of 131072 bf16, neither with streaming stores: 1031 us in
+// three launches, 780 so; 722 with them).
 template <int DT, int THREADS>
 __global__ __launch_bounds__(THREADS) void policy_row_kernel(
     Rows r, const typename Elem<DT>::T* logits, Policy p, float* logp, double* part,

@@ -22,9 +22,9 @@ constexpr int64_t kCacheBytes = (int64_t)256 << 20;  // what the memory-side cac
 // Sixteen bytes past the caches (non-temporal), for data of which a launch writes
 // or reads more than a cache holds, once: the gated unit of 16384 x 5504 bf16 took
 // 251 us without, 242 with such stores, 218 with such loads too; the policy loss
-// of 8192 x 131072 bf16 840 and 777 with such stores. Not for fp32, where a lane's
-// 32 bytes are two accesses and each covers half of every cache line: zeroing a
-// table's gradient took 1.7 times as long so.
+// of 8192 x 131072 bf16 840 and 777 with such stores.  Not where a lane's 32 bytes are
+// two accesses and each covers half of every cache line (eight fp32 columns): an
+// embedding and its gradient in fp32 took 1.7 times as long so.
 __device__ __forceinline__ void store_stream(u32x4_any* p, u32x4_any v) {
   __builtin_nontemporal_store(v, p);
 }
