@@ -487,9 +487,12 @@ int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_t
  *   loss_t = -min(r * advantage, c * advantage) + kl * (e^d - d - 1),  d = ref_logp - logp
  *   loss = sum over the counted t of weight[t] * loss_t
  * The derivative by logp of the first term is -r * advantage where r * advantage
- * <= c * advantage, else 0.  old_logp, advantage, weight and ref_logp are fp32
- * [n_tokens]; weight NULL stands for 1 / n_tokens, ref_logp may be NULL if kl is
- * 0.  0 <= clip_low <= 1, clip_high >= 0.  Outputs as above. */
+ * <= c * advantage, else 0.  An advantage of 0 makes the first term and its
+ * derivative 0 also where r is beyond fp32.  A token of weight 0 adds nothing to the
+ * loss and its row of grad is zeros, whatever its other numbers are.  old_logp,
+ * advantage, weight and ref_logp are fp32 [n_tokens]; weight NULL stands for
+ * 1 / n_tokens, ref_logp may be NULL if kl is 0.  0 <= clip_low <= 1, clip_high >= 0.
+ * Outputs as above. */
 int64_t rip_policy_loss_workspace(int64_t n_tokens, int64_t vocab);
 int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,
                         int64_t vocab, const void* targets, int32_t id_type, const float* old_logp,

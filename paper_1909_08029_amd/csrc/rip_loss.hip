@@ -304,21 +304,31 @@ struct Policy {
   float low, high, kl, grad_scale;
 };
 
+// x * a where x may be a number that left fp32: nothing if a is 0, as for any
+// number that did not.
+__device__ __forceinline__ float times(float x, float a) {
+  return a == 0.0f && __builtin_isinf(x) ? 0.0f : x * a;
+}
+
 // A counted token's loss and its derivative by logp.  ratio * A is flat where
-// the clipped value is the smaller one; a NaN stays on the other branch.
+// the clipped value is the smaller one; a NaN stays on the other branch.  The ratio
+// passes fp32 where logp - old_logp is above 88 (a low value in old_logp that marks
+// tokens to be left out, say), which no weight or advantage of 0 may turn into NaN.
 __device__ __forceinline__ float policy_token(const Policy& p, int64_t t, int64_t n, float lp,
                                               float* coef) {
   const float a = p.advantage[t], w = p.weight ? p.weight[t] : 1.0f / (float)n;
+  *coef = 0.0f;
+  if (w == 0.0f) return 0.0f;
   const float ratio = expf(lp - p.old_logp[t]);
-  const float bound = fminf(fmaxf(ratio, p.low), p.high) * a;
-  const bool flat = ratio * a > bound;
-  float loss = flat ? -bound : -(ratio * a), slope = flat ? 0.0f : -(ratio * a);
+  const float gain = times(ratio, a), bound = times(fminf(fmaxf(ratio, p.low), p.high), a);
+  const bool flat = gain > bound;
+  float loss = flat ? -bound : -gain, slope = flat ? 0.0f : -gain;
   if (p.ref_logp) {
     const float d = p.ref_logp[t] - lp, e = expf(d);
     loss += p.kl * (e - d - 1.0f);
     slope += p.kl * (1.0f - e);
   }
-  *coef = w * slope * p.grad_scale;
+  *coef = times(w * slope, p.grad_scale);
   return w * loss;
 }
 
