@@ -460,8 +460,9 @@ int32_t rip_ckpt_wgrad(const void* dy, int32_t dy_dtype, int64_t ld_dy, int64_t 
  *   logits   [n_tokens][vocab]; targets[t] is the token that row t predicts
  *   seq_offsets [2 * n_pairs + 1] int32 on the device, ascending: sequence q is
  *            the tokens seq_offsets[q] .. seq_offsets[q+1]-1; 2p is the chosen
- *            and 2p+1 the rejected one of pair p.  Offsets outside 0..n_tokens or
- *            out of order are cut to fit.
+ *            and 2p+1 the rejected one of pair p.  Offsets that are not so are cut
+ *            to fit: to 0 .. n_tokens, and one below an earlier offset (of any
+ *            pair) to the largest of those, so that no token is in two sequences.
  *   ref_logp [2 * n_pairs] log-probabilities of the sequences under the reference
  * A token counts unless its target lies outside 0 .. vocab-1 (prompt, padding),
  * it belongs to no sequence, or every logit of its row is -inf.  With

@@ -10,7 +10,8 @@
 //
 //   1. stats   a row's largest logit and the sum of e^(x - largest), in one pass
 //              (each lane keeps a running pair); few rows are split over several
-//              workgroups, whose pairs the next launch joins
+//              workgroups, whose pairs the next launch joins; beside them the
+//              preference loss's offsets are put in order
 //   2. pairs / tokens   log-probabilities, the loss and coef
 //   3. grad    one pass over the logits, writing the gradient; rows that do not
 //              count are written as zeros without being read
@@ -164,13 +165,60 @@ struct Token {
   int target;
 };
 
+// The preference loss's offsets as its pairs take them: within the tokens, and none
+// below an earlier one, of whichever pair, so that no two sequences share a token.
+// That needs all earlier offsets: one workgroup makes the running maximum, beside
+// those that read the logits.
+struct Cut {
+  const int32_t* offsets;  // as the caller gave them
+  int32_t* cut;
+  int count;               // 0: no sequences
+};
+__device__ __forceinline__ void cut_offsets(const Cut& c, int64_t n) {
+  constexpr int kEach = 8;  // consecutive offsets of a thread in a round
+  __shared__ int32_t tops[2][kWaves];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int32_t before = 0;       // the maximum of the rounds before
+  for (int i0 = 0, round = 0; i0 < c.count; i0 += kThreads * kEach, ++round) {
+    const int i = i0 + (int)threadIdx.x * kEach;
+    int32_t o[kEach], top = 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) o[u] = i + u < c.count ? c.offsets[i + u] : 0;
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) top = o[u] = max(top, min(o[u], (int32_t)n));
+    for (int s = 1; s < kWave; s <<= 1) {
+      const int32_t up = __shfl_up(top, s);
+      if (lane >= s) top = max(top, up);
+    }
+    int32_t mine = __shfl_up(top, 1);  // of the lanes below
+    mine = lane ? max(mine, before) : before;
+    if (lane == kWave - 1) tops[round % 2][wave] = top;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) {
+      const int32_t x = tops[round % 2][w];
+      mine = w < wave ? max(mine, x) : mine;
+      before = max(before, x);
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u)
+      if (i + u < c.count) c.cut[i + u] = max(o[u], mine);
+  }
+}
+
 template <int DT>
 __global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
                                                          const typename Elem<DT>::T* logits,
-                                                         Stat* stat, Token* token, float* logp) {
+                                                         Stat* stat, Token* token, float* logp,
+                                                         Cut c) {
   __shared__ Stat shared[kWaves];
-  const int64_t t = blockIdx.x / r.splits;
-  const int split = blockIdx.x - (uint32_t)t * r.splits;
+  const uint32_t first = c.count > 0;  // a workgroup before those of the rows
+  if (blockIdx.x < first) {
+    cut_offsets(c, r.n);
+    return;
+  }
+  const uint32_t at = blockIdx.x - first;
+  const int64_t t = at / r.splits;
+  const int split = at - (uint32_t)t * r.splits;
   if (split == 0 && threadIdx.x == 0) {  // stands for tokens that do not count
     token[t] = {0.0f, 0.0f, 0.0f, -1};
     if (logp) logp[t] = 0.0f;
@@ -201,7 +249,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows r,
     add(s, f);
   }
   s = join_block(s, shared);
-  if (threadIdx.x == 0) stat[blockIdx.x] = s;
+  if (threadIdx.x == 0) stat[at] = s;
 }
 
 // log-probability of a counted token's target; false where the row has no
@@ -243,17 +291,13 @@ __device__ __forceinline__ float log_sigmoid(float z) {
 // depends on differences of a few.
 template <int DT>
 __global__ __launch_bounds__(kPairThreads) void pairs_kernel(
-    Rows r, const typename Elem<DT>::T* logits, const Stat* stat, const int32_t* offsets, int pairs,
+    Rows r, const typename Elem<DT>::T* logits, const Stat* stat, const int32_t* cut, int pairs,
     const float* ref, float beta, float smoothing, float grad_scale, int lanes, float* seq_logp,
     Token* token, float* logp, double* pair_loss) {
   __shared__ double shared[2][kPairThreads / kWave];
   const double refs[2] = {ref[2 * blockIdx.x], ref[2 * blockIdx.x + 1]};
-  int64_t at[3];
-  for (int i = 0; i < 3; ++i) {  // within the tokens and ascending, whatever the offsets say
-    int64_t o = offsets[2 * blockIdx.x + i];
-    o = o < 0 ? 0 : o > r.n ? r.n : o;
-    at[i] = i && o < at[i - 1] ? at[i - 1] : o;
-  }
+  // the pair's tokens, no other pair's
+  const int64_t at[3] = {cut[2 * blockIdx.x], cut[2 * blockIdx.x + 1], cut[2 * blockIdx.x + 2]};
   const bool lead = (threadIdx.x & (lanes - 1)) == 0;
   const int64_t begin = at[0] + threadIdx.x / lanes, round = kPairThreads / lanes;
   double chosen = 0.0, rejected = 0.0;
@@ -541,9 +585,10 @@ struct Work {
   Stat* stat;
   Token* token;
   double* part;
+  int32_t* cut;
   int64_t bytes;
 };
-Work make_work(const Rows& r, int64_t parts, void* workspace) {
+Work make_work(const Rows& r, int64_t parts, int64_t offsets, void* workspace) {
   char* p = static_cast<char*>(workspace);
   Work w{};
   w.stat = (Stat*)p;
@@ -551,7 +596,9 @@ Work make_work(const Rows& r, int64_t parts, void* workspace) {
   w.token = (Token*)(p + at);
   at += ceil_div(r.n * (int64_t)sizeof(Token), 256) * 256;
   w.part = (double*)(p + at);
-  w.bytes = at + (parts + 1) * (int64_t)sizeof(double);
+  at += (parts + 1) * (int64_t)sizeof(double);
+  w.cut = (int32_t*)(p + at);
+  w.bytes = at + offsets * (int64_t)sizeof(int32_t);
   return w;
 }
 // Threads that join the splits of a row.
@@ -613,11 +660,12 @@ int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t 
 }
 
 template <int DT>
-int32_t run_stats(Rows& r, const void* logits, Work& w, float* logp, void* stream) {
-  if (r.n == 0) return RIP_OK;
-  void* args[] = {&r, &logits, &w.stat, &w.token, &logp};
-  return launch((const void*)stats_kernel<DT>, dim3((uint32_t)(r.n * r.splits)), dim3(kThreads),
-                args, 0, stream, "loss: stats");
+int32_t run_stats(Rows& r, const void* logits, Work& w, float* logp, Cut c, void* stream) {
+  const int64_t groups = r.n * r.splits + (c.count > 0);
+  if (groups == 0) return RIP_OK;
+  void* args[] = {&r, &logits, &w.stat, &w.token, &logp, &c};
+  return launch((const void*)stats_kernel<DT>, dim3((uint32_t)groups), dim3(kThreads), args, 0,
+                stream, "loss: stats");
 }
 template <int DT>
 int32_t run_grad(Rows& r, const void* logits, Work& w, void* grad, int64_t ld_grad, int parts,
@@ -636,11 +684,11 @@ template <int DT>
 int32_t run_pref(Rows r, const void* logits, const int32_t* offsets, int pairs, const float* ref,
                  float beta, float smoothing, float grad_scale, float* loss, float* seq_logp,
                  float* logp, void* grad, int64_t ld_grad, void* workspace, void* stream) {
-  Work w = make_work(r, pairs, workspace);
+  Work w = make_work(r, pairs, 2 * (int64_t)pairs + 1, workspace);
   int32_t rc;
-  if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
+  if ((rc = run_stats<DT>(r, logits, w, logp, Cut{offsets, w.cut, 2 * pairs + 1}, stream))) return rc;
   int lanes = join_lanes(r);
-  void* args[] = {&r,          &logits, &w.stat,   &offsets, &pairs, &ref,   &beta, &smoothing,
+  void* args[] = {&r,          &logits, &w.stat,   &w.cut,   &pairs, &ref,   &beta, &smoothing,
                   &grad_scale, &lanes,  &seq_logp, &w.token, &logp,  &w.part};
   if ((rc = launch((const void*)pairs_kernel<DT>, dim3((uint32_t)pairs), dim3(kPairThreads), args, 0,
                    stream, "rip_pref_loss: pairs")))
@@ -652,7 +700,7 @@ template <int DT>
 int32_t run_policy(Rows r, const void* logits, Policy p, float* loss, float* logp, void* grad,
                    int64_t ld_grad, void* workspace, void* stream) {
   int parts = (int)policy_parts(r);
-  Work w = make_work(r, parts, workspace);
+  Work w = make_work(r, parts, 0, workspace);
   int32_t rc;
   if (one_launch(r)) {
     void* args[] = {&r, &logits, &p, &logp, &w.part, &grad, &ld_grad};
@@ -665,7 +713,7 @@ int32_t run_policy(Rows r, const void* logits, Policy p, float* loss, float* log
     return launch((const void*)total_kernel, dim3(1), dim3(kTotalThreads), total, 0, stream,
                   "rip_policy_loss: total");
   }
-  if ((rc = run_stats<DT>(r, logits, w, logp, stream))) return rc;
+  if ((rc = run_stats<DT>(r, logits, w, logp, Cut{}, stream))) return rc;
   if (r.n) {
     int lanes = join_lanes(r);
     void* args[] = {&r, &logits, &w.stat, &p, &lanes, &w.token, &logp, &w.part};
@@ -685,12 +733,14 @@ extern "C" int64_t rip_pref_loss_workspace(int64_t n_tokens, int64_t vocab, int3
   if (n_tokens < 0 || n_tokens > RIP_MAX_TOKENS || vocab < 1 || vocab > RIP_MAX_WIDTH ||
       n_pairs < 0 || n_pairs > RIP_MAX_PAIRS)
     return 0;
-  return make_work(make_rows(n_tokens, vocab, vocab, nullptr, 0), n_pairs, nullptr).bytes;
+  return make_work(make_rows(n_tokens, vocab, vocab, nullptr, 0), n_pairs, 2 * (int64_t)n_pairs + 1,
+                   nullptr)
+      .bytes;
 }
 extern "C" int64_t rip_policy_loss_workspace(int64_t n_tokens, int64_t vocab) {
   if (n_tokens < 0 || n_tokens > RIP_MAX_TOKENS || vocab < 1 || vocab > RIP_MAX_WIDTH) return 0;
   const Rows r = make_rows(n_tokens, vocab, vocab, nullptr, 0);
-  return make_work(r, policy_parts(r), nullptr).bytes;
+  return make_work(r, policy_parts(r), 0, nullptr).bytes;
 }
 
 extern "C" int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n_tokens,

@@ -68,3 +68,64 @@ def test_ratios_beyond_fp32(form, dtype, kl):
     check_grad(ref.host(grad), want, targets, rel[:, None], dtype)
     nothing = (kind >= 2) | ((kind == 1) & (kl == 0))
     assert (ref.host(grad)[nothing] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("tokens,vocab", [(12, 50), (3000, 40), (150, 40000), (40, 1031)])
+def test_offsets_out_of_order_across_pairs(tokens, vocab, dtype):
+    """A token belongs to one sequence at most, whatever the offsets: the same bits as
+    with the offsets' running maximum within the tokens.  Sequences of one round of
+    a workgroup's threads and of several, thousands of pairs, and no tokens."""
+    import torch
+    import paper_1909_08029_amd as rip
+    rng = np.random.default_rng(tokens)
+    x = torch.from_numpy(rng.standard_normal((tokens, vocab)) * 2).to(dtype).cuda()
+    t = torch.from_numpy(rng.integers(0, vocab, tokens)).cuda()
+    third = tokens // 3
+    wild = [[0, tokens, third, tokens // 2, tokens], [third, 0, tokens, -7, 2 * tokens],
+            [tokens, 0, third, tokens, tokens], [0, third, 2 * third, third, tokens],
+            rng.integers(-tokens, 2 * tokens, 9).tolist(), [-2 ** 31, 2 ** 31 - 1, 0, 0, third],
+            [0] * 5, (np.sort(rng.integers(0, tokens + 1, 6001)) - rng.integers(0, 5, 6001)).tolist()]
+    for o in wild:
+        fit = np.maximum.accumulate(np.clip(o, 0, tokens))
+        r = torch.from_numpy(rng.standard_normal(len(o) - 1).astype(np.float32)).cuda()
+        out = []
+        for offsets in (o, fit):
+            grad = torch.full_like(x, 5.0)
+            od = torch.from_numpy(np.asarray(offsets, np.int32)).cuda()
+            got = rip.rip_pref_loss(x, t, od, r, 0.3, 0.1, grad=grad)
+            assert torch.equal(od.cpu(), torch.from_numpy(np.asarray(offsets, np.int32)))
+            out.append([a.clone() for a in (*got, grad)])
+        for a, b in zip(*out):
+            assert torch.equal(a, b)
+        inside = np.zeros(tokens, bool)
+        inside[fit[0]:fit[-1]] = True
+        assert (ref.host(out[0][2])[~inside] == 0).all() and (ref.host(out[0][2])[inside] < 0).all()
+    od = torch.from_numpy(np.array([3, -1, 2, 0, 9], np.int32)).cuda()
+    r = torch.tensor([1.0, 2.0, 0.5, 0.25], device="cuda")
+    loss, seq, logp = rip.rip_pref_loss(x[:0], t[:0], od, r, 0.5)
+    want = np.mean(np.log1p(np.exp(-0.5 * np.array([1.0, -0.25]))))
+    assert abs(float(loss) - want) < 1e-6 and (seq == 0).all() and logp.numel() == 0
+
+
+def test_offsets_in_order_against_the_plain_form():
+    """Backward offsets with the running maximum as the plain form takes them."""
+    import torch
+    import paper_1909_08029_amd as rip
+    rng = np.random.default_rng(11)
+    x, t, xh, targets, logp = policy_inputs(rng, 90, 333, F32)
+    offsets = np.array([0, 40, 20, 30, 60, 50, 90])
+    fit = np.maximum.accumulate(offsets)
+    r = rng.standard_normal(6).astype(np.float32) - 100
+    beta = float(np.float32(0.2))
+    want = ref.pref_loss(xh, targets, fit, r.astype(np.float64), beta, 0.0)
+    grad = torch.empty_like(x)
+    loss, seq, got = rip.rip_pref_loss(x, t, torch.from_numpy(offsets.astype(np.int32)).cuda(),
+                                       torch.from_numpy(r).cuda(), beta, grad=grad)
+    d = delta(xh, 333)
+    ref.close(ref.host(got), want["logp"], d + 2.0 ** -23 * np.abs(want["logp"]), "logp")
+    count = np.diff(fit) * d
+    ref.close(ref.host(seq), want["seq"], count + 2.0 ** -23 * np.abs(want["seq"]), "seq")
+    dz = beta * 2 * count.sum()
+    ref.close(ref.host(loss), want["loss"], dz + 2.0 ** -20 * (1 + abs(want["loss"])), "loss")
+    check_grad(ref.host(grad), want, targets, dz + 2.0 ** -20, F32)
