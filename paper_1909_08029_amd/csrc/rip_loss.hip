@@ -354,23 +354,41 @@ __device__ __forceinline__ float times(float x, float a) {
   return a == 0.0f && __builtin_isinf(x) ? 0.0f : x * a;
 }
 
+// e^d - d - 1, given m = e^d - 1, within 2^-21 of it: near 0, where policies begin and
+// the terms cancel, by its series (as m - d in fp32 it is 0 or off by percents
+// below d = 1e-3).
+__device__ __forceinline__ float exp_rest(float d, float m) {
+  if (fabsf(d) < 0.5f) {  // the next term is below 2^-24 of the sum
+    float s = 1.0f / 40320;
+    s = __builtin_fmaf(s, d, 1.0f / 5040);
+    s = __builtin_fmaf(s, d, 1.0f / 720);
+    s = __builtin_fmaf(s, d, 1.0f / 120);
+    s = __builtin_fmaf(s, d, 1.0f / 24);
+    s = __builtin_fmaf(s, d, 1.0f / 6);
+    return d * d * __builtin_fmaf(s, d, 0.5f);
+  }
+  return __builtin_isinf(m) ? m : m - d;
+}
+
 // A counted token's loss and its derivative by logp.  ratio * A is flat where
 // the clipped value is the smaller one; a NaN stays on the other branch.  The ratio
 // passes fp32 where logp - old_logp is above 88 (a low value in old_logp that marks
-// tokens to be left out, say), which no weight or advantage of 0 may turn into NaN.
-__device__ __forceinline__ float policy_token(const Policy& p, int64_t t, int64_t n, float lp,
-                                              float* coef) {
+// tokens to be left out, say), which no weight or advantage of 0 may turn into NaN.  The KL
+// term is added in 64 bits, as the batch is: it may be far smaller than the first.
+__device__ __forceinline__ double policy_token(const Policy& p, int64_t t, int64_t n, float lp,
+                                               float* coef) {
   const float a = p.advantage[t], w = p.weight ? p.weight[t] : 1.0f / (float)n;
   *coef = 0.0f;
-  if (w == 0.0f) return 0.0f;
+  if (w == 0.0f) return 0.0;
   const float ratio = expf(lp - p.old_logp[t]);
   const float gain = times(ratio, a), bound = times(fminf(fmaxf(ratio, p.low), p.high), a);
   const bool flat = gain > bound;
-  float loss = flat ? -bound : -gain, slope = flat ? 0.0f : -gain;
+  double loss = flat ? -bound : -gain;
+  float slope = flat ? 0.0f : -gain;
   if (p.ref_logp) {
-    const float d = p.ref_logp[t] - lp, e = expf(d);
-    loss += p.kl * (e - d - 1.0f);
-    slope += p.kl * (1.0f - e);
+    const float d = p.ref_logp[t] - lp, m = expm1f(d);
+    loss += (double)p.kl * exp_rest(d, m);
+    slope -= p.kl * m;
   }
   *coef = times(w * slope, p.grad_scale);
   return w * loss;

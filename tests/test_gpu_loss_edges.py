@@ -129,3 +129,53 @@ def test_offsets_in_order_against_the_plain_form():
     dz = beta * 2 * count.sum()
     ref.close(ref.host(loss), want["loss"], dz + 2.0 ** -20 * (1 + abs(want["loss"])), "loss")
     check_grad(ref.host(grad), want, targets, dz + 2.0 ** -20, F32)
+
+
+@pytest.mark.parametrize("scale", [1e-4, 3e-4, 1e-3, 1e-2, 0.3, 2.0])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("form", FORMS, ids=str)
+def test_kl_near_its_zero(form, dtype, scale):
+    """A policy close to its reference: K = e^d - d - 1 is about d^2 / 2.  Without the
+    first term the loss is kl * sum of w K; K has a relative error of 2^-20 and that of
+    logp (delta, and its rounding), which K's derivative and half its square carry on."""
+    import torch
+    import paper_1909_08029_amd as rip
+    tokens, vocab = form
+    rng = np.random.default_rng(tokens + vocab)
+    x, t, xh, targets, logp = policy_inputs(rng, tokens, vocab, dtype)
+    refp = (logp + scale * rng.choice([-1, 1], tokens) * (1 + rng.random(tokens))).astype(np.float32)
+    w = (rng.random(tokens) + 0.1).astype(np.float32)
+    zero = np.zeros(tokens, np.float32)
+    old = logp.astype(np.float32)
+    kl = float(np.float32(0.05))
+    want = ref.policy_loss(xh, targets, old.astype(np.float64), zero.astype(np.float64),
+                           w.astype(np.float64), refp.astype(np.float64), 0.2, 0.2, 0.0)
+    d = refp.astype(np.float64) - want["logp"]
+    k, slope = np.where(want["counted"], np.expm1(d) - d, 0), np.where(want["counted"], -np.expm1(d), 0)
+    k = np.where(want["counted"] & (np.abs(d) < 0.05), d * d * (1 / 2 + d * (1 / 6 + d * (1 / 24 + d / 120))), k)
+    cuda = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    grad = torch.empty_like(x)
+    loss, _ = rip.rip_policy_loss(x, t, cuda(old), cuda(zero), cuda(w), cuda(refp), 0.2, 0.2, kl, grad=grad)
+    off = delta(xh, vocab) + 2.0 ** -23 * np.abs(want["logp"])
+    tol = kl * w * (2.0 ** -20 * k + off * np.abs(slope) + off ** 2 * np.exp(d))
+    loss64 = (kl * w * k)[want["counted"]].sum()
+    ref.close(ref.host(loss), loss64, tol[want["counted"]].sum() + 2.0 ** -24 * loss64, "loss")
+    want["coef"] = kl * w * slope
+    rel = np.where(want["counted"], off * np.exp(d) / np.maximum(np.abs(slope), 1e-30) + 2.0 ** -20, 0)
+    want["grad"] = ref.logits_grad(want["coef"], want["counted"], want["soft"], targets)
+    check_grad(ref.host(grad), want, targets, rel[:, None], dtype)
+
+
+def test_kl_beside_a_large_first_term():
+    """A KL term of 5e-9 a token is not lost beside a first term of 1: it moves the
+    sum over tokens whose first terms cancel."""
+    import torch
+    import paper_1909_08029_amd as rip
+    x = torch.zeros(64, 32, device="cuda")
+    t = torch.zeros(64, dtype=torch.int64, device="cuda")
+    lp = rip.rip_policy_loss(x, t, torch.zeros(64, device="cuda"), torch.zeros(64, device="cuda"))[1]
+    adv = torch.tensor([1.0, -1.0], device="cuda").repeat(32)
+    refp = lp + 1e-4
+    k = torch.expm1((refp - lp).double()) - (refp - lp).double()
+    loss, _ = rip.rip_policy_loss(x, t, lp, adv, torch.ones(64, device="cuda"), refp, kl=1.0)
+    assert abs(float(loss) - float(k.sum())) <= 2.0 ** -20 * float(k.sum())
