@@ -374,7 +374,8 @@ int32_t rip_set_blocks_per_cu(int32_t blocks_per_cu);
  *    the call itself refuses also give 0), 16-byte aligned, free again when the
  *    stream has passed the call.  It need not be cleared.
  *  - A buffer that a call writes must not overlap any other of its buffers,
- *    except where a call says that it may be the same matrix.
+ *    except where a call says that it may be the same matrix.  Arrays of 32-bit
+ *    numbers (offsets, log-probabilities, weights, a loss) are 4-byte aligned.
  *  - Empty inputs (no tokens) are no error; their pointers may be NULL.
  *  - All calls are only kernel launches on `stream` (no allocation, copy, memset
  *    or wait), so they may be captured into a HIP graph.

@@ -641,10 +641,18 @@ const void* row_kernel(const Rows& r, int* threads) {
 }
 int64_t policy_parts(const Rows& r) { return one_launch(r) ? r.n : ceil_div(r.n * join_lanes(r), kThreads); }
 
+// An array of 32-bit numbers that a loss reads or writes; NULL where it has none.
+struct Small {
+  const void* p;
+  int64_t count;
+  const char* what;
+  bool written;
+};
+template <int SMALL>
 int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t ld, int64_t n,
                    int64_t vocab, const void* targets, int32_t id_type, const void* loss,
                    const void* grad, int64_t ld_grad, const void* workspace,
-                   int64_t workspace_bytes, int64_t need) {
+                   int64_t workspace_bytes, int64_t need, const Small (&small)[SMALL]) {
   int32_t rc;
   if (vocab < 1) return fail(RIP_E_INVAL, "%s: vocab %lld < 1", name, (long long)vocab);
   if (vocab > RIP_MAX_WIDTH || n > RIP_MAX_TOKENS)
@@ -664,17 +672,19 @@ int32_t check_loss(const char* name, const void* logits, int32_t dtype, int64_t 
                 (long long)workspace_bytes, (long long)need);
   if (reinterpret_cast<uintptr_t>(workspace) % 16)
     return fail(RIP_E_ALIGN, "%s: workspace = %p is not 16-byte aligned", name, workspace);
-  const int64_t ls = span(dtype, n, vocab, ld);
-  if (grad) {
-    const int64_t gs = span(dtype, n, vocab, ld_grad);
-    if (overlap(grad, gs, logits, ls) && !(grad == logits && ld == ld_grad))
-      return fail(RIP_E_OVERLAP, "%s: grad overlaps logits without being the same matrix", name);
-    if (overlap(grad, gs, targets, n * id_bytes) || overlap(grad, gs, workspace, need))
-      return fail(RIP_E_OVERLAP, "%s: grad overlaps targets or workspace", name);
-  }
-  if (overlap(workspace, need, logits, ls) || overlap(workspace, need, targets, n * id_bytes))
-    return fail(RIP_E_OVERLAP, "%s: workspace overlaps logits or targets", name);
-  return RIP_OK;
+  for (const Small& s : small)
+    if (reinterpret_cast<uintptr_t>(s.p) % 4)
+      return fail(RIP_E_ALIGN, "%s: %s = %p is not 4-byte aligned", name, s.what, s.p);
+  // the gradient may be the logits' own matrix
+  const bool in_place = grad && grad == logits && ld_grad == ld;
+  Range list[4 + SMALL] = {
+      {logits, span(dtype, n, vocab, ld), "logits", in_place},
+      {grad, grad && !in_place ? span(dtype, n, vocab, ld_grad) : 0, "grad", true},
+      {targets, n * id_bytes, "targets", false},
+      {workspace, need, "workspace", true}};
+  for (int i = 0; i < SMALL; ++i)
+    list[4 + i] = {small[i].p, small[i].p ? small[i].count * 4 : 0, small[i].what, small[i].written};
+  return check_apart(name, list, 4 + SMALL);
 }
 
 template <int DT>
@@ -775,7 +785,12 @@ extern "C" int32_t rip_pref_loss(const void* logits, int32_t dtype, int64_t ld, 
   int32_t rc;
   if ((rc = check_loss("rip_pref_loss", logits, dtype, ld, n_tokens, vocab, targets, id_type, loss,
                        grad, ld_grad, workspace, workspace_bytes,
-                       rip_pref_loss_workspace(n_tokens, vocab, n_pairs))))
+                       rip_pref_loss_workspace(n_tokens, vocab, n_pairs),
+                       {{seq_offsets, 2 * (int64_t)n_pairs + 1, "seq_offsets", false},
+                        {ref_logp, 2 * (int64_t)n_pairs, "ref_logp", false},
+                        {loss, 1, "loss", true},
+                        {seq_logp, 2 * (int64_t)n_pairs, "seq_logp", true},
+                        {logp, n_tokens, "logp", true}})))
     return rc;
   if (!seq_offsets || !ref_logp || !seq_logp)
     return fail(RIP_E_INVAL, "rip_pref_loss: seq_offsets, ref_logp or seq_logp is NULL");
@@ -804,7 +819,13 @@ extern "C" int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld
   if (n_tokens < 0) return fail(RIP_E_INVAL, "rip_policy_loss: n_tokens %lld < 0", (long long)n_tokens);
   if ((rc = check_loss("rip_policy_loss", logits, dtype, ld, n_tokens, vocab, targets, id_type,
                        loss, grad, ld_grad, workspace, workspace_bytes,
-                       rip_policy_loss_workspace(n_tokens, vocab))))
+                       rip_policy_loss_workspace(n_tokens, vocab),
+                       {{old_logp, n_tokens, "old_logp", false},
+                        {advantage, n_tokens, "advantage", false},
+                        {weight, n_tokens, "weight", false},
+                        {ref_logp, n_tokens, "ref_logp", false},
+                        {loss, 1, "loss", true},
+                        {logp, n_tokens, "logp", true}})))
     return rc;
   if (n_tokens && (!old_logp || !advantage))
     return fail(RIP_E_INVAL, "rip_policy_loss: old_logp or advantage is NULL");

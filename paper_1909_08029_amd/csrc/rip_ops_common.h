@@ -171,6 +171,22 @@ inline bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return na > 0 && nb > 0 && x < y + (uintptr_t)nb && y < x + (uintptr_t)na;
 }
+// One of a call's buffers; RIP_E_OVERLAP where one that is written shares a byte with
+// another.
+struct Range {
+  const void* p;
+  int64_t bytes;
+  const char* what;
+  bool written;
+};
+inline int32_t check_apart(const char* name, const Range* list, int count) {
+  for (int i = 0; i < count; ++i)
+    for (int j = 0; j < i; ++j)
+      if ((list[i].written || list[j].written) &&
+          overlap(list[i].p, list[i].bytes, list[j].p, list[j].bytes))
+        return fail(RIP_E_OVERLAP, "%s: %s overlaps %s", name, list[i].what, list[j].what);
+  return RIP_OK;
+}
 // Bytes from a matrix's first element to the end of its last.
 inline int64_t span(int32_t dtype, int64_t rows, int64_t width, int64_t ld) {
   return rows < 1 || width < 1 ? 0 : ((rows - 1) * ld + width) * elem_bytes(dtype);
