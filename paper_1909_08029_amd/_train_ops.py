@@ -8,6 +8,12 @@ dimensions are taken as rows of their last one.  Work is enqueued on `stream`
 among them, are allocated for that stream; the caller makes sure that the inputs
 are ready there and keeps them until the stream has passed the call, as with any
 tensor used on a second stream.
+
+The calls stand outside automatic differentiation, as a backward pass written by
+hand does: a tensor that requires grad is taken as its values, and nothing that a
+call returns requires grad.  A tensor that a call writes counts as modified in
+place, so that autograd refuses a later backward pass that would have needed what
+it held before (logits under their own gradient, say).
 """
 from __future__ import annotations
 
@@ -50,6 +56,10 @@ def _declare():
 
 
 _declare()
+
+
+# Marks a caller's tensor as modified in place (0.3 us).
+_wrote = torch.autograd.graph.increment_version
 
 
 # The checks below run on every call of a training loop or a decoding step, so they
@@ -156,15 +166,18 @@ def rip_embed_lookup(table, ids, scale: float = 1.0, dtype=None, out=None, strea
     tp, tc, vocab, width, ld = _matrix(table, "table", dev)
     ip, ic, n = _ids(ids, "ids", dev)
     shape = (*ids.shape, width)
-    if out is None:
-        out = _empty(table, shape, dtype or table.dtype, stream)
-    else:
+    given = out is not None
+    if given:
         _shaped(out, shape, "out")
+    else:
+        out = _empty(table, shape, dtype or table.dtype, stream)
     op, oc, _, _, ld_out = _matrix(out if len(shape) > 1 else out.view(1, -1), "out", dev)
     rc = lib.rip_embed_lookup(tp, tc, vocab, width, ld, ip, ic, n, scale, op, oc, ld_out,
                               _stream(stream, dev))
     if rc:
         _check(rc)
+    if given:
+        _wrote(out)
     return out
 
 
@@ -184,6 +197,7 @@ def rip_embed_grad(dout, ids, grad, scale: float = 1.0, accumulate: bool = False
                             1 if accumulate else 0, ws, nbytes, _stream(stream, dev))
     if rc:
         _check(rc)
+    _wrote(grad)
     return grad
 
 
@@ -279,15 +293,18 @@ def rip_ckpt_unpack(ckpt: Ckpt, dtype=torch.bfloat16, out=None, stream=None):
     dev = _device()
     codes, exps = _ckpt(ckpt, ckpt.rows, ckpt.width, "ckpt", dev)
     shape = (ckpt.rows, ckpt.width)
-    if out is None:
+    given = out is not None
+    if given:
+        _shaped(out, shape, "out")
+    else:
         like = ckpt._codes if ckpt._buffer is None else ckpt._buffer
         out = _empty(like, shape, dtype, stream)
-    else:
-        _shaped(out, shape, "out")
     xp, xc, rows, width, ld = _matrix(out, "out", dev)
     rc = lib.rip_ckpt_unpack(codes, exps, rows, width, xp, xc, ld, _stream(stream, dev))
     if rc:
         _check(rc)
+    if given:
+        _wrote(out)
     return out
 
 
@@ -297,11 +314,12 @@ def rip_gate_forward(gate, up, out=None, gate_ckpt: Optional[Ckpt] = None,
     dev = _device()
     gp, gc, rows, width, ld_g = _matrix(gate, "gate", dev)
     up_, uc, rows_u, width_u, ld_u = _matrix(up, "up", dev)
-    if out is None:
+    given = out is not None
+    if given:
+        hp, hc, _, _, ld_h = _matrix(_shaped(out, gate.shape, "out"), "out", dev)
+    else:
         out = _empty_like(gate, stream)
         hp, hc, ld_h = out.data_ptr(), gc, width
-    else:
-        hp, hc, _, _, ld_h = _matrix(_shaped(out, gate.shape, "out"), "out", dev)
     if rows != rows_u or width != width_u or gc != uc or gc != hc:
         raise ValueError("gate, up and out must have one shape and dtype")
     if gate_ckpt is None and up_ckpt is None:
@@ -315,6 +333,8 @@ def rip_gate_forward(gate, up, out=None, gate_ckpt: Optional[Ckpt] = None,
                               u_codes, u_exps, _stream(stream, dev))
     if rc:
         _check(rc)
+    if given:
+        _wrote(out)
     return out, gate_ckpt, up_ckpt
 
 
@@ -326,6 +346,7 @@ def rip_gate_backward(dh, gate_ckpt: Ckpt, up_ckpt: Ckpt, dgate=None, dup=None, 
     dp, dc, rows, width, ld = _matrix(dh, "dh", dev)
     g_codes, g_exps = _ckpt(gate_ckpt, rows, width, "gate_ckpt", dev)
     u_codes, u_exps = _ckpt(up_ckpt, rows, width, "up_ckpt", dev)
+    given = [t for t in (dgate, dup) if t is not None]
     if dgate is None:
         dgate = _empty_like(dh, stream)
         ap, ac, ld_a = dgate.data_ptr(), dc, width
@@ -346,6 +367,8 @@ def rip_gate_backward(dh, gate_ckpt: Ckpt, up_ckpt: Ckpt, dgate=None, dup=None, 
                                bp, ld_b, h_codes, h_exps, _stream(stream, dev))
     if rc:
         _check(rc)
+    for t in given:
+        _wrote(t)
     return (dgate, dup) if h8 is None else (dgate, dup, h8)
 
 
@@ -365,6 +388,7 @@ def rip_ckpt_wgrad(dy, ckpt: Ckpt, grad, accumulate: bool = False, stream=None):
                             1 if accumulate else 0, ws, nbytes, _stream(stream, dev))
     if rc:
         _check(rc)
+    _wrote(grad)
     return grad
 
 
@@ -409,6 +433,8 @@ def rip_pref_loss(logits, targets, seq_offsets, ref_logp, beta: float = 0.1,
                            nbytes, _stream(stream, dev))
     if rc:
         _check(rc)
+    if grad is not None:
+        _wrote(grad)
     return out[0], out[1:1 + 2 * pairs], out[1 + 2 * pairs:]
 
 
@@ -433,4 +459,6 @@ def rip_policy_loss(logits, targets, old_logp, advantage, weight=None, ref_logp=
                              _stream(stream, dev))
     if rc:
         _check(rc)
+    if grad is not None:
+        _wrote(grad)
     return out[0], out[1:]
