@@ -45,6 +45,8 @@
 extern "C" {
 #endif
 
+/* Changes where a declaration below changes what it was; a function that is only
+ * added leaves it, as a caller built without that function still runs. */
 #define RIP_ABI_VERSION 2
 
 /* status codes */

@@ -22,7 +22,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from . import RIP_BF16, RIP_FP32, _check, _raw_stream, _stream_ptr, lib
+from . import LIB_PATH, RIP_BF16, RIP_FP32, _check, _raw_stream, _stream_ptr, lib
 
 _CODES = {torch.float32: RIP_FP32, torch.bfloat16: RIP_BF16}
 _IDS = {torch.int32: 0, torch.int64: 1}
@@ -51,7 +51,10 @@ def _declare():
                                   i64, p, i64, p]),
     }
     for name, (res, args) in sigs.items():
-        fn = getattr(lib, name)
+        fn = getattr(lib, name, None)
+        if fn is None:
+            raise ImportError(f"{LIB_PATH} (ABI version {lib.rip_abi_version()}) is older than this "
+                              f"package: it has no {name}; run __graft_entry__.build()")
         fn.restype, fn.argtypes = res, args
 
 
