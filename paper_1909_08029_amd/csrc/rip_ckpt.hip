@@ -187,7 +187,8 @@ __global__ __launch_bounds__(kBlockThreads) void gate_backward_kernel(
   for (int j = 0; j < kCols<DT>; ++j) {
     const float sg = sigmoid(g[j]);
     const float silu = g[j] * sg;
-    a[j] = d[j] * u[j] * (sg * (1.0f + g[j] * (1.0f - sg)));
+    // dh and up' meet last: their product alone may pass fp32 where dgate does not
+    a[j] = d[j] * (sg * (1.0f + g[j] * (1.0f - sg))) * u[j];
     h[j] = silu * u[j];
     d[j] *= silu;
   }
