@@ -13,6 +13,8 @@ namespace rip {
 int32_t fail(int32_t code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
 
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 // Number of workers of a scheduler.
 int32_t sched_workers(const rip_sched* s);
 

@@ -150,7 +150,6 @@ struct FastDiv {
   }
 };
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int elem_bytes(int32_t dtype) { return dtype == RIP_BF16 ? 2 : 4; }
 inline bool known_dtype(int32_t dtype) { return dtype == RIP_FP32 || dtype == RIP_BF16; }
 
