@@ -10,10 +10,11 @@
 // what the fp32 matrix instructions reach.  Sums are fp32.
 //
 // Bound by the matrix units where the product is large: 16384 tokens, 5504 x 2048,
-// bf16, take 351 to 400 us with the card's clock, the pack of x (20 us) included (920
+// bf16, take 351 to 400 us by card and clock, the pack of x (20 us) included (920
 // to 1050 TFLOP/s; a product of the same sizes without codes to widen takes the
 // vendor's library 416); 8192 x 2048 x 2048 fp32 200 us (345 TFLOP/s, 1030 of bf16
-// products).  Few tokens are bound by the latency of their loads, narrow layers by
+// products).  Small products are bound by the steps of the smallest tile, which leaves
+// most of the card idle (257 x 383 x 1000 fp32: 24 workgroups, 14.3 us), narrow layers by
 // that and by the parts' way to memory.
 //
 // A workgroup of four or eight waves computes a tile of grad and goes over its tokens in
