@@ -346,7 +346,7 @@ def _plain_adamw(s):
     case = s["case"]
     decay = 1 - LR * DECAY
     rate, root = LR / (1 - BETA1 ** STEP), 1 / math.sqrt(1 - BETA2 ** STEP)
-    g = s["grad"].float().mul_(GRAD_SCALE)
+    g = s["grad"].float() * GRAD_SCALE
     m, v = s["m"], s["v"]
     if case["bits"] == 8:
         m = _value_m(m.view(-1, BLOCK), s["m_exps"].view(-1)).view(g.shape)
