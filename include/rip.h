@@ -505,6 +505,95 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
                         float* logp, void* grad, int64_t ld_grad, void* workspace,
                         int64_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * AdamW (decoupled weight decay) as a replica's local update, in place of the
+ * SGD of rip_local_step: a handle holds the moments of registered replicas, one
+ * launch updates every segment of the workers listed, and rip_preduce without an
+ * sgd then averages their groups.
+ *
+ * Arithmetic (fp32, this order, no fused multiply-add; constants are computed in
+ * 64 bits and rounded):
+ *   g = grad_scale * grad
+ *   m = beta1 * m + (1 - beta1) * g
+ *   v = beta2 * v + ((1 - beta2) * g) * g
+ *   w = w * decay - (rate * m) / (sqrt(v) * root + eps)
+ *   decay = 1 - lr * weight_decay, rate = lr / (1 - beta1^step),
+ *   root = 1 / sqrt(1 - beta2^step)
+ * bf16 storage is rounded to nearest even once, when stored.
+ *
+ * Moments of RIP_STATE_FP32: m and v [numel] fp32 for each segment.
+ * Moments of RIP_STATE_8BIT: for each segment, in blocks of 32 elements (the last
+ * one may be short; its other codes are 0),
+ *   m [32 * blocks] int8 and m_exps [blocks] uint8: a checkpoint of one row
+ *     (rip_ckpt_pack): code q stands for q * 2^(exp - 127);
+ *   v [32 * blocks] uint8 and v_exps [blocks] uint8: with c = 16 x + y, 0 <= y < 16,
+ *     a code stands for f(c) * 2^(exp - 127), f = y if x = 0, else
+ *     (16 + y) * 2^(x - 1); the exponent is the smallest (>= -126) for which the
+ *     block's largest value is at most f(255) = 31 * 2^14.
+ * All zeros stand for zeros.  A step updates w from the moments before they are
+ * rounded.  A value between two codes takes the upper one if r / 2^16 reaches what
+ * is missing to it (m: q = floor(x / 2^e + r / 2^16); v alike within its exponent),
+ * where r are the low (m) or high (v) 16 bits of a 32-bit hash, so that the mean is
+ * kept; a positive v has a code above 0.  A block with an infinity or a NaN has exp
+ * 255 and codes 0 and stands for NaN throughout.  The hash of element i of a segment is the 32-bit
+ * finalizer of MurmurHash3 over (i mod 2^32) ^ (k + (i / 2^32) * 0x9E3779B9), k the
+ * low 32 bits of the seed folded with step, replica and segment by SplitMix64 (as
+ * the keys of the scheduler).
+ * ---------------------------------------------------------------------- */
+enum { RIP_STATE_FP32 = 0, RIP_STATE_8BIT = 1 };
+
+typedef struct rip_adamw {
+  double lr, beta1, beta2;  /* 0 <= beta < 1 */
+  double eps;               /* > 0 (in fp32) */
+  double weight_decay;
+  double grad_scale;        /* multiplies every gradient (1 = none) */
+  uint64_t seed;            /* of the random roundings */
+} rip_adamw;
+
+/* What changes from step to step. */
+typedef struct rip_adamw_scalars {
+  float decay, rate, root, grad_scale;
+  uint32_t key[2];          /* seed folded with step: low, high */
+} rip_adamw_scalars;
+
+typedef struct rip_adamw_state rip_adamw_state; /* opaque, library-owned */
+
+/* Registers n_replicas x n_segments segments of parameters and gradients (the
+ * layout of rip_replicas_create) with their moments of `format`.  m_exps and v_exps
+ * may be NULL for RIP_STATE_FP32.  Pointers of zero-length segments may be NULL.
+ * Codes are 16-byte aligned, everything else to its elements.  Buffers that a step
+ * writes (all but grad) must overlap no other; every buffer must be memory of the
+ * current device and lie inside its allocation.  The handle copies its tables to
+ * device memory (one allocation), and calls with it need its device current.
+ * Errors: RIP_E_INVAL, RIP_E_ALIGN, RIP_E_OVERLAP, RIP_E_UNSUPPORTED (dtype,
+ * format, more than RIP_MAX_REPLICAS replicas, above 2^35 elements in one),
+ * RIP_E_NOMEM, RIP_E_HIP. */
+int32_t rip_adamw_state_create(int32_t n_replicas, int32_t n_segments, int32_t dtype,
+                               const int64_t* seg_numel, void* const* param, void* const* grad,
+                               int32_t format, void* const* m, void* const* v,
+                               void* const* m_exps, void* const* v_exps, rip_adamw_state** out);
+void rip_adamw_state_destroy(rip_adamw_state* s); /* NULL is a no-op */
+
+/* The scalars of step `step` (1, 2, ...). */
+int32_t rip_adamw_scalars_at(const rip_adamw* cfg, int64_t step, rip_adamw_scalars* out);
+
+/* Step `step` of the n_active workers listed (distinct ids), in one launch.
+ * `scalars` NULL: those of cfg and step; else they are read from this device memory
+ * (4-byte aligned) when the launch runs, so that a captured graph can be replayed for
+ * later steps and a gradient's clipping factor need not come to the host; beta1,
+ * beta2 and eps are cfg's either way.  May be captured into a HIP graph.
+ * Errors: RIP_E_INVAL (also: a scalar out of its range, another device current),
+ * RIP_E_ALIGN, RIP_E_HIP. */
+int32_t rip_adamw_step(const rip_adamw_state* s, const int32_t* active, int32_t n_active,
+                       const rip_adamw* cfg, int64_t step, const rip_adamw_scalars* scalars,
+                       void* stream);
+
+/* The values that 8-bit moments stand for (exact in bf16): m and v are
+ * [n_replicas][rip_adamw_packed(s)] of `dtype`, a replica's segments one after
+ * another, each in whole blocks of 32 (zeros behind its end), in one launch. */
+int64_t rip_adamw_packed(const rip_adamw_state* s);
+int32_t rip_adamw_moments(const rip_adamw_state* s, int32_t dtype, void* m, void* v, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -386,3 +386,6 @@ def rip_last_launch_count() -> int:
 from ._train_ops import (  # noqa: E402,F401
     Ckpt, rip_ckpt_pack, rip_ckpt_unpack, rip_ckpt_wgrad, rip_embed_grad, rip_embed_lookup,
     rip_gate_backward, rip_gate_forward, rip_policy_loss, rip_pref_loss)
+
+# AdamW as the local update
+from ._adamw import AdamwState, rip_adamw_scalars, rip_adamw_step  # noqa: E402,F401

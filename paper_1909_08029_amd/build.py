@@ -42,7 +42,7 @@ def build_librip(out: str = LIBRIP, extra=()):
     csrc = os.path.join(PKG, "csrc")
     srcs = [os.path.join(csrc, f) for f in ("rip_api.hip", "rip_kernels.hip", "rip_sched.cpp",
                                             "rip_embed.hip", "rip_ckpt.hip", "rip_wgrad.hip",
-                                            "rip_loss.hip")]
+                                            "rip_loss.hip", "rip_adamw.hip")]
     tmp = out + ".tmp"
     _run([HIPCC, *COMMON, *extra, "-I", os.path.join(ROOT, "include"), "-I", csrc,
           "-x", "hip", *srcs, "-o", tmp])

@@ -15,6 +15,25 @@ void clear_error();
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// A kind of registered buffers: p[r*S + s] is segment s of replica r, numel[s]
+// elements of esize bytes (p NULL: there are none).
+struct BufferKind {
+  void* const* p;
+  const char* what;
+  bool written;
+  const int64_t* numel;
+  int esize;
+};
+// Every non-empty segment must be memory of `device` that a kernel can address
+// (device or managed memory, not a host pointer) and must lie inside the
+// allocation that holds its first byte, and the written ones must overlap no
+// other.  Those that are only read may overlap each other (several replicas may
+// read one gradient).
+int32_t check_buffers(const BufferKind* kinds, int count, int32_t n, int32_t S, int device);
+// No non-empty segment's pointer is NULL.
+int32_t check_nonnull(void* const* p, const char* what, int32_t n, int32_t S,
+                      const int64_t* numel);
+
 // Number of workers of a scheduler.
 int32_t sched_workers(const rip_sched* s);
 

@@ -17,22 +17,18 @@
 #include <vector>
 
 #include "rip_internal.h"
+#include "rip_splitmix.h"
 
 namespace {
 
-constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ULL;
+using rip::kGamma;
+using rip::mix;
+
 constexpr int kSchedTag = 3;
 constexpr int kMaxStaticAttempts = 1000;
 
-// SplitMix64 output function (Steele, Lea & Flood, OOPSLA 2014).
-inline uint64_t mix(uint64_t z) {
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ULL;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBULL;
-  return z ^ (z >> 31);
-}
-
 inline uint64_t fold(uint64_t k, std::initializer_list<uint64_t> comps) {
-  for (uint64_t c : comps) k = mix(k + kGamma * (c + 1));
+  for (uint64_t c : comps) k = rip::fold(k, c);
   return k;
 }
 
