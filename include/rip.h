@@ -506,6 +506,83 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
                         int64_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Attention of packed sequences with an optional learned relative position bias,
+ * and its backward pass (conventions: as for the operators above)
+ *
+ *   q, out, dout, dq  [q_tokens][heads * head_dim], head h at columns h * head_dim
+ *   k, v, dk, dv      [k_tokens][kv_heads * head_dim]; head h of q reads head
+ *                     h / (heads / kv_heads)
+ * Sequence s has the queries q_offsets[s] .. q_offsets[s+1]-1 and the keys
+ * k_offsets[s] .. k_offsets[s+1]-1 (int32, on the device; k_offsets NULL: as
+ * q_offsets).  Offsets out of order are cut to fit as in rip_pref_loss.  With L_q
+ * queries and L_k keys, query i stands at position i + L_k - L_q (its sequence's
+ * queries are the last of its keys) and sees every key j of its sequence, or with
+ * `causal` those with j <= i + L_k - L_q.
+ *   x_ij   = scale * q_i . k_j + bias[row of (j - position of i)][h]
+ *   lse_i  = log sum_j e^x_ij,  p_ij = e^(x_ij - lse_i),  out_i = sum_j p_ij v_j
+ * A bias below -65536 (-inf, a type's lowest value) hides its keys.  A query that sees no
+ * key has out 0 and lse -inf and adds to no gradient; so have tokens that belong to no
+ * sequence.  Every row of an output is written.  What a sequence's tokens hold reaches
+ * no other sequence; within one, an infinity or a NaN may reach any of its rows.
+ *
+ * Products are taken of the inputs as they are and of p and ds rounded to the
+ * inputs' type; sums, scores and statistics are fp32.
+ *
+ * The bias.  Distances j - position fall into n_intervals intervals: those below
+ * starts[0], from starts[0] to starts[1] - 1, ..., from starts[n_intervals - 2] on
+ * (strictly ascending); interval b reads row rows[b] of the table [buckets][heads].
+ * Several intervals may share a row. */
+#define RIP_MAX_HEADS 256
+#define RIP_MAX_HEAD_DIM 256
+#define RIP_MAX_SEQUENCES (1 << 20)
+#define RIP_MAX_INTERVALS 128
+#define RIP_MAX_BIAS_SPAN 2048   /* last start - first start + 2 */
+
+typedef struct rip_rel_buckets {
+  int32_t n_intervals;      /* 1 .. RIP_MAX_INTERVALS */
+  const int32_t* starts;    /* host [n_intervals - 1] */
+  const int32_t* rows;      /* host [n_intervals], 0 .. buckets - 1 */
+} rip_rel_buckets;
+
+typedef struct rip_attn {
+  int32_t dtype;            /* of q, k, v, out and their gradients */
+  int32_t heads, kv_heads, head_dim;
+  int64_t q_tokens, k_tokens;
+  const int32_t* q_offsets; /* device [n_sequences + 1] */
+  const int32_t* k_offsets; /* device, or NULL: the queries' */
+  int32_t n_sequences;
+  int32_t causal;
+  float scale;              /* > 0 */
+  const void* bias;         /* device [buckets][heads], or NULL: none */
+  int32_t bias_dtype;
+  int64_t ld_bias;
+  int32_t buckets;
+  const rip_rel_buckets* rel;
+} rip_attn;
+
+/* out, and unless NULL lse [heads][q_tokens] (fp32) and low [q_tokens][heads *
+ * head_dim]: the rounding error of a bf16 out, itself rounded to bf16 (fp32: not
+ * written).  The backward pass takes its row sums from out + low, to 16 bits; without
+ * low its gradients, the bias's above all, hold the 8 bits that out has. */
+int64_t rip_attn_forward_workspace(const rip_attn* a);
+int32_t rip_attn_forward(const rip_attn* a, const void* q, int64_t ld_q, const void* k,
+                         int64_t ld_k, const void* v, int64_t ld_v, void* out, int64_t ld_out,
+                         float* lse, void* low, int64_t ld_low, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/* dq, dk and dv from dout and what the forward pass gave (low may be NULL), and with a
+ * bias, unless dbias is NULL, its gradient dbias [buckets][heads] of dbias_dtype (rows
+ * of no interval: zeros), added to what it holds if `accumulate` is nonzero. */
+int64_t rip_attn_backward_workspace(const rip_attn* a);
+int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t ld_q, const void* k,
+                          int64_t ld_k, const void* v, int64_t ld_v, const void* out,
+                          int64_t ld_out, const float* lse, const void* low, int64_t ld_low,
+                          const void* dout, int64_t ld_dout, void* dq, int64_t ld_dq, void* dk,
+                          int64_t ld_dk, void* dv, int64_t ld_dv, void* dbias,
+                          int32_t dbias_dtype, int64_t ld_dbias, int32_t accumulate,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * AdamW (decoupled weight decay) as a replica's local update, in place of the
  * SGD of rip_local_step: a handle holds the moments of registered replicas, one
  * launch updates every segment of the workers listed, and rip_preduce without an

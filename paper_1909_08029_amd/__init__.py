@@ -389,3 +389,6 @@ from ._train_ops import (  # noqa: E402,F401
 
 # AdamW as the local update
 from ._adamw import AdamwState, rip_adamw_scalars, rip_adamw_step  # noqa: E402,F401
+
+# attention with a relative position bias
+from ._attn import Kept, RelBuckets, rip_attn_backward, rip_attn_forward  # noqa: E402,F401

@@ -11,6 +11,8 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -38,14 +40,25 @@ def _run(cmd):
         raise subprocess.CalledProcessError(res.returncode, cmd)
 
 
+SOURCES = ("rip_api.hip", "rip_kernels.hip", "rip_sched.cpp", "rip_embed.hip", "rip_ckpt.hip",
+           "rip_wgrad.hip", "rip_loss.hip", "rip_adamw.hip", "rip_attn.hip",
+           "rip_attn_forward.hip", "rip_attn_backward.hip")
+
+
 def build_librip(out: str = LIBRIP, extra=()):
+    """Compiles the sources side by side (the attention kernels' variants take a minute
+    or two), then links them."""
     csrc = os.path.join(PKG, "csrc")
-    srcs = [os.path.join(csrc, f) for f in ("rip_api.hip", "rip_kernels.hip", "rip_sched.cpp",
-                                            "rip_embed.hip", "rip_ckpt.hip", "rip_wgrad.hip",
-                                            "rip_loss.hip", "rip_adamw.hip")]
+    flags = [f for f in COMMON if f != "-shared"]
     tmp = out + ".tmp"
-    _run([HIPCC, *COMMON, *extra, "-I", os.path.join(ROOT, "include"), "-I", csrc,
-          "-x", "hip", *srcs, "-o", tmp])
+    with tempfile.TemporaryDirectory() as folder:
+        objects = [os.path.join(folder, f + ".o") for f in SOURCES]
+        commands = [[HIPCC, *flags, *extra, "-I", os.path.join(ROOT, "include"), "-I", csrc,
+                     "-x", "hip", "-c", os.path.join(csrc, f), "-o", o]
+                    for f, o in zip(SOURCES, objects)]
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(_run, reversed(commands)))  # the longest first
+        _run([HIPCC, f"--offload-arch={ARCH}", "-shared", *extra, *objects, "-o", tmp])
     os.replace(tmp, out)
 
 

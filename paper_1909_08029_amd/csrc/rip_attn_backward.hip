@@ -1,0 +1,524 @@
+// Attention's backward pass (gfx950), which computes the probabilities again from the
+// scores and the rows' log-sums:
+//
+//   p_ij = e^(x_ij - lse_i),  ds_ij = p_ij (dout_i . v_j - delta_i),  delta_i = dout_i . out_i
+//   dq_i = scale sum_j ds_ij k_j;  dk_j = scale sum_i ds_ij q_i;  dv_j = sum_i p_ij dout_i
+//
+// Two kernels, each with the sum that it accumulates in registers: one over the keys
+// for 32 queries to a wave (dq, delta and the bias's gradient), one over the queries
+// for 32 keys to a wave (dk and dv, over all heads that share them).  Seven products
+// where one kernel would take five, but no sum is added atomically or goes through
+// memory.
+#include "rip_attn_tile.h"
+
+namespace rip {
+namespace attn {
+namespace {
+
+template <int DT, int D>
+constexpr int kStep = DT == RIP_BF16 && D <= 128 ? 64 : 32;  // keys (queries) of a tile
+
+// A row's log-sum in the log2 domain; +inf, so that every exponential is 0, for a
+// query that sees no key.
+__device__ __forceinline__ float reference(float lse) {
+  return lse == -kInf ? kInf : lse * kLog2e;
+}
+
+// Elements of LDS behind the bias's values: sums by distance, and a block, per wave.
+constexpr int kBlockPitch = 33;
+__device__ __host__ constexpr int sums_size(int lut_size) { return lut_size + 2 * 62; }
+
+// Adds a block's ds (32 keys x 32 queries as the matrix instructions leave them, the
+// first at distance `rel`) to the sums by distance: through LDS, a lane to a
+// diagonal.  Only this wave touches its sums, so their order is fixed.
+__device__ __forceinline__ void add_diagonals(const f32x16& ds, int rel, int first, float* sums,
+                                              float* block, int lane) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) block[block_row(r, lane / 32) * kBlockPitch + lane % 32] = ds[r];
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  const int off = lane - 31;  // key - query within the block
+  float sum = 0.0f;
+  if (lane < 63) {
+#pragma unroll
+    for (int n = 0; n < 32; ++n) {
+      const int key = n + off;
+      sum += key >= 0 && key < 32 ? block[key * kBlockPitch + n] : 0.0f;
+    }
+    sums[rel + off - first + 62] += sum;
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <int DT, int D, bool BIAS, bool SPLIT>
+__global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) void dq_kernel(
+    Backward f) {
+  typedef typename Elem<DT>::T T;
+  typedef Tile<DT, D> Tl;
+  constexpr int KT = kStep<DT, D>, KB = KT / 32, QT = kRows * kWaves;
+  __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
+  extern __shared__ __align__(16) float lut[];
+  const Args& p = f.a;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
+
+  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
+  const int hz = place / per_head, rest = place - hz * per_head, split = SPLIT ? rest / p.slots : 0;
+  const int slot = p.slots - 1 - (SPLIT ? rest - split * p.slots : rest);
+  const Place at = find<QT>(p, p.q, p.k, slot, p.pack);
+  const int lq = at.here.end - at.here.begin, lk = at.other.end - at.other.begin, shift = lk - lq;
+  const int rows = lq * p.pack, w0 = at.tile * QT;
+  const int head0 = hz * p.pack, kv = head0 / p.group;
+  // sums by distance of each wave, then a block of each
+  const int pitch = BIAS ? sums_size(p.lut_size) : 0;
+  float* const sums = lut + p.lut_size;
+  float* const mine = sums + wave * pitch;
+  float* const block = sums + kWaves * pitch + wave * 32 * kBlockPitch;
+  const int intervals = BIAS ? f.buckets->n : 0;
+  float* const bias_part =
+      BIAS ? f.bias_part + ((int64_t)hz * p.slots * p.splits + slot * p.splits + split) * intervals
+           : nullptr;
+  if (w0 >= rows) {
+    if (BIAS)
+      for (int b = threadIdx.x; b < intervals; b += 64 * kWaves) bias_part[b] = 0.0f;
+    return;
+  }
+
+  const int wq = w0 + wave * kRows, w = min(wq + lane % 32, rows - 1);
+  const int i = p.by_pack.div(w), head = head0 + w - i * p.pack, pos = i + shift;
+  const bool valid = wq + lane % 32 < rows;
+  const int64_t token = at.here.begin + i;
+  const int limit = p.causal ? min(lk, pos + 1) : lk;
+  const int least = __builtin_amdgcn_readlane(limit, 0), most = __builtin_amdgcn_readlane(limit, 31);
+  int keys = lk;
+  if (p.causal) keys = max(0, min(lk, (int)p.by_pack.div(min(w0 + QT, rows) - 1) + shift + 1));
+  int t = 0, end = keys;
+  if (SPLIT) {
+    const int share = (((keys + KT - 1) / KT + p.splits - 1) / p.splits) * KT;
+    t = min(keys, split * share), end = min(keys, t + share);
+  }
+  Bias bias{lut, p.lut_first, p.lut_size};
+  float below = 0.0f, above = 0.0f;  // ds of blocks all in the first (last) interval
+  if (BIAS) {
+    load_lut(p, head0, lut);
+    for (int x = lane; x < pitch; x += 64) mine[x] = 0.0f;
+  }
+
+  Frag<DT> q[D / 16], dout[D / 16];
+  load_row<DT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
+  load_row<DT, D>((const T*)f.dout.p + token * f.dout.ld + (int64_t)head * p.dim, valid, half, p.dim,
+                  dout);
+  // delta in fp32 from out and what its rounding left
+  float delta = 0.0f;
+  {
+    const T* out = (const T*)f.out.p + token * f.out.ld + (int64_t)head * p.dim;
+    const T* low = f.low.p ? (const T*)f.low.p + token * f.low.ld + (int64_t)head * p.dim : nullptr;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      const int col = 16 * c + 8 * half;
+      float x[kLane] = {}, y[kLane] = {}, z[kLane];
+      if (valid && col < p.dim) {
+        load_unit<DT>(out, col, p.dim, x);
+        if (DT == RIP_BF16 && low) load_unit<DT>(low, col, p.dim, y);
+      }
+      dout[c].get(z);
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) delta = __builtin_fmaf(z[j], x[j] + y[j], delta);
+    }
+    delta = add_halves(delta);
+  }
+  const int64_t row = (int64_t)head * p.q.tokens + token;
+  const float ref = valid ? reference(f.lse[row]) : kInf;
+  if (valid && half == 0 && split == 0) f.delta[row] = delta;
+  const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
+  const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
+  auto k_row = [&](int r) { return k0 + r * f.k.ld; };
+  auto v_row = [&](int r) { return v0 + r * f.v.ld; };
+
+  f32x16 dq[D / 32] = {};
+  Stage<DT, D, KT, 64 * kWaves> ks, vs;
+  if (t < end) {
+    ks.load(k_row, t, end, p.dim);
+    vs.load(v_row, t, end, p.dim);
+  }
+  for (; t < end; t += KT) {
+    ks.store(k_tile);
+    vs.store(v_tile);
+    lds_barrier();
+    if (t + KT < end) {
+      ks.load(k_row, t + KT, end, p.dim);
+      vs.load(v_row, t + KT, end, p.dim);
+    }
+    if (wq < rows && t < most) {
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          s = mma(Tl::row(k_tile, b * 32 + lane % 32, c, half), q[c], s);
+          dp = mma(Tl::row(v_tile, b * 32 + lane % 32, c, half), dout[c], dp);
+        }
+        const int key = t + b * 32;
+        int side = 0;
+        if (BIAS) {
+          side = bias.uniform(key - __builtin_amdgcn_readlane(pos, 31),
+                              key + 31 - __builtin_amdgcn_readlane(pos, 0));
+          add_bias(s, p.scale2, bias, side, [&](int r) { return key + block_row(r, half) - pos; });
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = BIAS ? s[r] - ref : __builtin_fmaf(s[r], p.scale2, -ref);
+          s[r] = __builtin_amdgcn_exp2f(x);
+        }
+        if (key + 32 > least || key + 32 > end) {
+          const int cut = min(limit, end) - key;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = block_row(r, half) < cut ? s[r] : 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+        if (BIAS) {
+          if (side) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += s[r];
+            if (side < 0)
+              below += sum;
+            else
+              above += sum;
+          } else {
+            // (queries behind the last have zeros, whatever their diagonal)
+            add_diagonals(s, key - (wq + shift), p.lut_first, mine, block, lane);
+          }
+        }
+        // ds rounded to bf16 (half a step of 2^-8, as dq is) for the product
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag<DT> e;
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = s[8 * u + j];
+          e.set(x);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c)
+            dq[c] = mma(Tl::column(k_tile, b * 32 + 16 * u, c, lane), e, dq[c]);
+        }
+      }
+    }
+    lds_barrier();
+  }
+  if (valid) {
+    T* to = (T*)f.dq.p + token * f.dq.ld + (int64_t)head * p.dim;
+    float* part = SPLIT ? f.part + (((int64_t)split * p.q.tokens + token) * p.heads + head) * p.dim
+                        : nullptr;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = dq[c][r + j] * p.scale;
+        if (SPLIT)
+          store4<RIP_FP32>(part, c * 32 + block_row(r, half), p.dim, x);
+        else
+          store4<DT>(to, c * 32 + block_row(r, half), p.dim, x);
+      }
+  }
+  if constexpr (BIAS) {
+    // sums of an interval's distances over the waves, a wave to an interval
+    __syncthreads();
+#pragma unroll
+    for (int o = 32; o >= 1; o /= 2) below += __shfl_xor(below, o), above += __shfl_xor(above, o);
+    if (lane == 0) block[0] = below, block[1] = above;
+    __syncthreads();
+    const float* const blocks = sums + kWaves * pitch;
+    const int x0 = p.lut_first - 62;  // distance of the first sum
+    for (int b = wave; b < intervals; b += kWaves) {
+      const int from = b == 0 ? x0 : f.buckets->start[b - 1];
+      const int to = b == intervals - 1 ? x0 + pitch : f.buckets->start[b];
+      float sum = 0.0f;
+      for (int x = from + lane; x < to; x += 64)
+#pragma unroll
+        for (int s = 0; s < kWaves; ++s) sum += sums[s * pitch + x - x0];
+      if (lane < kWaves) {
+        if (b == 0) sum += blocks[lane * 32 * kBlockPitch];
+        if (b == intervals - 1) sum += blocks[lane * 32 * kBlockPitch + 1];
+      }
+#pragma unroll
+      for (int o = 32; o >= 1; o /= 2) sum += __shfl_xor(sum, o);
+      if (lane == 0) bias_part[b] = sum;
+    }
+  }
+}
+
+// dk (DK) and dv (DV) of 32 keys to a wave.
+template <int DT, int D, bool BIAS, bool SPLIT, bool DK, bool DV>
+__global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
+  typedef typename Elem<DT>::T T;
+  typedef Tile<DT, D> Tl;
+  constexpr int QT = kStep<DT, D>, QB = QT / 32, KT = kRows * kWaves;
+  __shared__ __align__(128) T q_tile[QT * Tl::kPitch], do_tile[QT * Tl::kPitch];
+  __shared__ __align__(16) float refs[QT], deltas[QT];
+  extern __shared__ __align__(16) float lut[];
+  const Args& p = f.a;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
+
+  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
+  const int kv = place / per_head, rest = place - kv * per_head, split = SPLIT ? rest / p.slots : 0;
+  // the first keys of a causal sequence have the most queries
+  const Place at = find<KT>(p, p.k, p.q, SPLIT ? rest - split * p.slots : rest, 1);
+  const int lk = at.here.end - at.here.begin, lq = at.other.end - at.other.begin, shift = lk - lq;
+  const int j0 = at.tile * KT;
+  if (j0 >= lk) return;
+  const int jw = j0 + wave * kRows, j = min(jw + lane % 32, lk - 1);
+  const bool valid = jw + lane % 32 < lk;
+  const int64_t token = at.here.begin + j;
+  // queries from `first` on see the key
+  const int first = p.causal ? j - shift : -1;
+  const int first_last = __builtin_amdgcn_readlane(first, 31);
+  const int first_wave = __builtin_amdgcn_readlane(first, 0);
+  const int start = p.causal ? max(0, j0 - shift) / QT * QT : 0;  // of the workgroup
+  const int tiles = lq > start ? (lq - start + QT - 1) / QT : 0, steps = tiles * p.group;
+  int n = 0, end = steps;  // (head, tile), tile fastest
+  if (SPLIT) {
+    const int share = (steps + p.splits - 1) / p.splits;
+    n = min(steps, split * share), end = min(steps, n + share);
+  }
+  Bias bias{lut, p.lut_first, p.lut_size};
+
+  Frag<DT> k[D / 16], v[DK ? D / 16 : 1];
+  load_row<DT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
+  if constexpr (DK)
+    load_row<DT, D>((const T*)f.v.p + token * f.v.ld + (int64_t)kv * p.dim, valid, half, p.dim, v);
+  f32x16 dk[DK ? D / 32 : 1] = {}, dv[DV ? D / 32 : 1] = {};
+
+  const T* q0 = (const T*)f.q.p + at.other.begin * f.q.ld + (int64_t)kv * p.group * p.dim;
+  const T* do0 = (const T*)f.dout.p + at.other.begin * f.dout.ld + (int64_t)kv * p.group * p.dim;
+  Stage<DT, D, QT, 64 * kWaves> qs, ds;
+  float ref = kInf, del = 0.0f;  // of query threadIdx.x of the tile
+  auto load = [&](int step) {
+    const int g = step / tiles, i0 = start + (step - g * tiles) * QT;
+    qs.load([&](int r) { return q0 + r * f.q.ld + (int64_t)g * p.dim; }, i0, lq, p.dim);
+    ds.load([&](int r) { return do0 + r * f.dout.ld + (int64_t)g * p.dim; }, i0, lq, p.dim);
+    const int i = i0 + threadIdx.x;
+    ref = kInf, del = 0.0f;
+    if (threadIdx.x < QT && i < lq) {
+      const int64_t row = ((int64_t)kv * p.group + g) * p.q.tokens + at.other.begin + i;
+      ref = reference(f.lse[row]);
+      if (DK) del = f.delta[row];
+    }
+  };
+  if (n < end) load(n);
+  int lut_head = -1;
+  for (; n < end; ++n) {
+    const int g = n / tiles, i0 = start + (n - g * tiles) * QT;
+    qs.store(q_tile);
+    ds.store(do_tile);
+    if (threadIdx.x < QT) refs[threadIdx.x] = ref, deltas[threadIdx.x] = del;
+    if (BIAS && lut_head != g) {
+      load_lut(p, kv * p.group + g, lut);
+      lut_head = g;
+    }
+    lds_barrier();
+    if (n + 1 < end) load(n + 1);
+    if (jw < lk && i0 + QT > first_wave) {
+#pragma unroll
+      for (int b = 0; b < QB; ++b) {
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          s = mma(Tl::row(q_tile, b * 32 + lane % 32, c, half), k[c], s);
+          if constexpr (DK) dp = mma(Tl::row(do_tile, b * 32 + lane % 32, c, half), v[c], dp);
+        }
+        const int ib = i0 + b * 32;
+        if (BIAS)
+          add_bias(s, p.scale2, bias,
+                   bias.uniform(__builtin_amdgcn_readlane(j, 0) - (ib + 31 + shift),
+                                __builtin_amdgcn_readlane(j, 31) - (ib + shift)),
+                   [&](int r) { return j - (ib + block_row(r, half) + shift); });
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x4 ref4 = *(const f32x4*)&refs[b * 32 + block_row(r, half)];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float y = BIAS ? s[r + x] - ref4[x] : __builtin_fmaf(s[r + x], p.scale2, -ref4[x]);
+            s[r + x] = __builtin_amdgcn_exp2f(y);
+          }
+        }
+        if (ib < first_last) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = ib + block_row(r, half) < first ? 0.0f : s[r];
+        }
+        if constexpr (DK) {
+#pragma unroll
+          for (int r = 0; r < 16; r += 4) {
+            const f32x4 del4 = *(const f32x4*)&deltas[b * 32 + block_row(r, half)];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) dp[r + x] = s[r + x] * (dp[r + x] - del4[x]);
+          }
+        }
+        // p and ds rounded to bf16 (half a step of 2^-8, as dv and dk are)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag<DT> e, de;
+          float x[8], y[8];
+#pragma unroll
+          for (int z = 0; z < 8; ++z) x[z] = s[8 * u + z], y[z] = dp[8 * u + z];
+          e.set(x);
+          de.set(y);
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            if constexpr (DV) dv[c] = mma(Tl::column(do_tile, b * 32 + 16 * u, c, lane), e, dv[c]);
+            if constexpr (DK) dk[c] = mma(Tl::column(q_tile, b * 32 + 16 * u, c, lane), de, dk[c]);
+          }
+        }
+      }
+    }
+    lds_barrier();
+  }
+  if (!valid) return;
+  const int kv_heads = p.heads / p.group;
+  const int64_t row = ((int64_t)split * p.k.tokens + token) * kv_heads + kv;
+  const int64_t all = (int64_t)p.splits * p.k.tokens * kv_heads;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) {
+      const int col = c * 32 + block_row(r, half);
+      float x[4];
+      if constexpr (DK) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = dk[c][r + z] * p.scale;
+        if (SPLIT)
+          store4<RIP_FP32>(f.part + row * p.dim, col, p.dim, x);
+        else
+          store4<DT>((T*)f.dk.p + token * f.dk.ld + (int64_t)kv * p.dim, col, p.dim, x);
+      }
+      if constexpr (DV) {
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = dv[c][r + z];
+        if (SPLIT)
+          store4<RIP_FP32>(f.part + (all + row) * p.dim, col, p.dim, x);
+        else
+          store4<DT>((T*)f.dv.p + token * f.dv.ld + (int64_t)kv * p.dim, col, p.dim, x);
+      }
+    }
+}
+
+// The splits' parts of `tokens` rows of `width` added in order.
+template <int DT>
+__global__ __launch_bounds__(256) void add_kernel(const float* part, int splits, int64_t tokens,
+                                                  int width, typename Elem<DT>::T* to, int64_t ld) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = tokens * width;
+  if (i >= all) return;
+  float sum = 0.0f;
+  for (int s = 0; s < splits; ++s) sum += part[s * all + i];
+  const int64_t row = i / width;
+  Elem<DT>::store(to + row * ld + (i - row * width), sum);
+}
+
+// The bias's gradient: a workgroup adds the parts of one row of the table and one head.
+template <int DT>
+__global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buckets* buckets,
+                                                   int64_t parts, typename Elem<DT>::T* grad,
+                                                   int64_t ld, int accumulate) {
+  __shared__ float sums[4];
+  const int row = blockIdx.x, head = blockIdx.y, n = parts ? buckets->n : 0;
+  float sum = 0.0f;
+  for (int b = 0; b < n; ++b) {
+    if (buckets->row[b] != row) continue;
+    for (int64_t x = threadIdx.x; x < parts; x += 256) sum += part[(head * parts + x) * n + b];
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o /= 2) sum += __shfl_xor(sum, o);
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum;
+  __syncthreads();
+  if (threadIdx.x) return;
+  sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  typename Elem<DT>::T* g = grad + (int64_t)row * ld + head;
+  Elem<DT>::store(g, accumulate ? Elem<DT>::load(g) + sum : sum);
+}
+
+template <int DT, int D>
+const void* dq_of(bool bias, bool split) {
+  return bias ? (split ? (const void*)dq_kernel<DT, D, true, true> : (const void*)dq_kernel<DT, D, true, false>)
+              : (split ? (const void*)dq_kernel<DT, D, false, true> : (const void*)dq_kernel<DT, D, false, false>);
+}
+template <int DT, int D, bool DK, bool DV>
+const void* dkv_of(bool bias, bool split) {
+  return bias ? (split ? (const void*)dkv_kernel<DT, D, true, true, DK, DV>
+                       : (const void*)dkv_kernel<DT, D, true, false, DK, DV>)
+              : (split ? (const void*)dkv_kernel<DT, D, false, true, DK, DV>
+                       : (const void*)dkv_kernel<DT, D, false, false, DK, DV>);
+}
+template <int DT>
+int32_t add(const float* part, int splits, int64_t tokens, int width, Heads to, void* stream) {
+  void* args[] = {&part, &splits, &tokens, &width, &to.p, &to.ld};
+  return launch((const void*)add_kernel<DT>, dim3((uint32_t)ceil_div(tokens * width, 256)), dim3(256),
+                args, 0, stream, "rip_attn_backward: add");
+}
+
+template <int DT>
+int32_t run(Backward& f, const Args& over_q, const Args& over_k, int width, void* stream) {
+  int32_t rc;
+  const bool bias = over_q.lut;
+  {
+    f.a = over_q;
+    const bool split = f.a.splits > 1;
+    const void* fn = width == 64    ? dq_of<DT, 64>(bias, split)
+                     : width == 128 ? dq_of<DT, 128>(bias, split)
+                                    : dq_of<DT, 256>(bias, split);
+    const size_t lds =
+        bias ? 4 * (f.a.lut_size + kWaves * (sums_size(f.a.lut_size) + 32 * kBlockPitch)) : 0;
+    void* args[] = {&f};
+    if ((rc = launch(fn, dim3((uint32_t)f.a.slots * f.a.splits, (uint32_t)(f.a.heads / f.a.pack)),
+                     dim3(64 * kWaves), args, lds, stream, "rip_attn_backward: queries")))
+      return rc;
+    if (split && (rc = add<DT>(f.part, f.a.splits, f.a.q.tokens, f.a.heads * f.a.dim, f.dq, stream)))
+      return rc;
+  }
+  f.a = over_k;
+  const int kv_heads = f.a.heads / f.a.group;
+  const bool split = f.a.splits > 1;
+  const dim3 grid((uint32_t)f.a.slots * f.a.splits, (uint32_t)kv_heads);
+  const size_t lds = bias ? 4 * f.a.lut_size : 0;
+  void* args[] = {&f};
+  const char* what = "rip_attn_backward: keys";
+  if (DT == RIP_FP32 && width == 256) {
+    // dk and dv with the operands of both do not fit the registers: one after the other
+    if ((rc = launch(dkv_of<RIP_FP32, 256, false, true>(bias, split), grid, dim3(64 * kWaves), args, lds,
+                     stream, what)) ||
+        (rc = launch(dkv_of<RIP_FP32, 256, true, false>(bias, split), grid, dim3(64 * kWaves), args, lds,
+                     stream, what)))
+      return rc;
+  } else {
+    const void* fn = width == 64    ? dkv_of<DT, 64, true, true>(bias, split)
+                     : width == 128 ? dkv_of<DT, 128, true, true>(bias, split)
+                                    : dkv_of<RIP_BF16, 256, true, true>(bias, split);
+    if ((rc = launch(fn, grid, dim3(64 * kWaves), args, lds, stream, what))) return rc;
+  }
+  if (!split) return RIP_OK;
+  const int cols = kv_heads * f.a.dim;
+  if ((rc = add<DT>(f.part, f.a.splits, f.a.k.tokens, cols, f.dk, stream))) return rc;
+  return add<DT>(f.part + (int64_t)f.a.splits * f.a.k.tokens * cols, f.a.splits, f.a.k.tokens, cols,
+                 f.dv, stream);
+}
+
+}  // namespace
+
+int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype, int width,
+                     void* stream) {
+  return dtype == RIP_BF16 ? run<RIP_BF16>(f, over_q, over_k, width, stream)
+                           : run<RIP_FP32>(f, over_q, over_k, width, stream);
+}
+
+int32_t run_bias_grad(const Backward& f, int64_t parts, int32_t buckets, int32_t heads, int32_t dtype,
+                      void* grad, int64_t ld, int32_t accumulate, void* stream) {
+  void* args[] = {(void*)&f.bias_part, (void*)&f.buckets, &parts, &grad, &ld, &accumulate};
+  return launch(dtype == RIP_BF16 ? (const void*)bias_kernel<RIP_BF16> : (const void*)bias_kernel<RIP_FP32>,
+                dim3((uint32_t)buckets, (uint32_t)heads), dim3(256), args, 0, stream,
+                "rip_attn_backward: bias");
+}
+
+}  // namespace attn
+}  // namespace rip

@@ -1,0 +1,276 @@
+// Attention's forward pass (gfx950): out_i = sum_j softmax_j(x_ij) v_j in one pass over
+// the keys, with the running maximum and sum of each query's scores.
+//
+// A wave takes 32 queries (a query and a head of it where heads share k and v) whose
+// operands stay in registers, and goes over the keys in tiles that the workgroup
+// shares in LDS.  Scores are computed as keys x queries: a lane holds one query's
+// scores, so the maximum and sum need one exchange with the lane 32 away, and the
+// exponentials are the operand of the product with v as they lie.  A maximum that
+// grows by less than a factor of 64 (in e^x) stays the reference, which
+// leaves the sums within fp32's range and saves rescaling them.
+#include "rip_attn_tile.h"
+
+namespace rip {
+namespace attn {
+namespace {
+
+template <int DT, int D>
+constexpr int kKeys = DT == RIP_BF16 && D <= 128 ? 64 : 32;  // keys of a tile
+
+// Without a bias, with one, and with one whose gradient will be wanted: that sums ds
+// in fp32, and its row sums delta come from out, which must not hold the rounding of
+// the exponentials then.  They enter the product as two bf16 numbers (16 bits).
+enum { kPlain, kBias, kExact };
+
+constexpr float kSlack = 6.0f;  // growth of a maximum (log2) that needs no rescaling
+
+template <int DT, int D, int WAVES, int MODE, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) void forward_kernel(
+    Forward f) {
+  typedef typename Elem<DT>::T T;
+  typedef Tile<DT, D> Tl;
+  constexpr int KT = kKeys<DT, D>, KB = KT / 32, QT = kRows * WAVES;
+  constexpr bool BIAS = MODE != kPlain, EXACT = MODE == kExact;
+  __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
+  extern __shared__ __align__(16) float lut[];
+  const Args& p = f.a;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
+
+  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
+  const int hz = place / per_head, rest = place - hz * per_head, split = SPLIT ? rest / p.slots : 0;
+  // the last tiles of a causal sequence have the most keys and go first
+  const Place at = find<QT>(p, p.q, p.k, p.slots - 1 - (SPLIT ? rest - split * p.slots : rest), p.pack);
+  const int lq = at.here.end - at.here.begin, lk = at.other.end - at.other.begin, shift = lk - lq;
+  const int rows = lq * p.pack, w0 = at.tile * QT;
+  if (w0 >= rows) return;
+  const int head0 = hz * p.pack, kv = head0 / p.group;
+
+  const int wq = w0 + wave * kRows, w = min(wq + lane % 32, rows - 1);
+  const int i = p.by_pack.div(w), head = head0 + w - i * p.pack, pos = i + shift;
+  const bool valid = wq + lane % 32 < rows;
+  const int64_t token = at.here.begin + i;
+  const int limit = p.causal ? min(lk, pos + 1) : lk;  // keys below it are seen
+  const int least = __builtin_amdgcn_readlane(limit, 0), most = __builtin_amdgcn_readlane(limit, 31);
+  int keys = lk;  // that the workgroup goes over
+  if (p.causal) keys = max(0, min(lk, (int)p.by_pack.div(min(w0 + QT, rows) - 1) + shift + 1));
+  int t = 0, end = keys;
+  if (SPLIT) {
+    const int share = (((keys + KT - 1) / KT + p.splits - 1) / p.splits) * KT;
+    t = min(keys, split * share), end = min(keys, t + share);
+  }
+  Bias bias{lut, p.lut_first, p.lut_size};
+  if (BIAS) load_lut(p, head0, lut);
+
+  Frag<DT> q[D / 16];
+  load_row<DT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
+  const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
+  const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
+  auto k_row = [&](int r) { return k0 + r * f.k.ld; };
+  auto v_row = [&](int r) { return v0 + r * f.v.ld; };
+
+  f32x16 o[D / 32] = {};
+  float m = -kInf, l = 0.0f;  // reference (log2); the sum of this half's keys
+  Stage<DT, D, KT, 64 * WAVES> ks, vs;
+  if (t < end) {
+    ks.load(k_row, t, end, p.dim);
+    vs.load(v_row, t, end, p.dim);
+  }
+  for (; t < end; t += KT) {
+    ks.store(k_tile);
+    vs.store(v_tile);
+    lds_barrier();
+    if (t + KT < end) {
+      ks.load(k_row, t + KT, end, p.dim);
+      vs.load(v_row, t + KT, end, p.dim);
+    }
+    if (wq < rows && t < most) {
+      f32x16 s[KB] = {};
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+          s[b] = mma(Tl::row(k_tile, b * 32 + lane % 32, c, half), q[c], s[b]);
+      if (BIAS) {
+        const int first = __builtin_amdgcn_readlane(pos, 0), last = __builtin_amdgcn_readlane(pos, 31);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+          const int key = t + b * 32;
+          add_bias(s[b], p.scale2, bias, bias.uniform(key - last, key + 31 - first),
+                   [&](int r) { return key + block_row(r, half) - pos; });
+        }
+      }
+      if (t + KT > least || t + KT > end) {
+        const int cut = min(limit, end) - t;
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s[b][r] = b * 32 + block_row(r, half) < cut ? s[b][r] : -kInf;
+      }
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[b][r]);
+      top = max_halves(BIAS ? top : top * p.scale2);
+      if (__any(top > m + kSlack)) {
+        const float next = fmaxf(m, top), scale = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
+        m = next;
+        l *= scale;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[c][r] *= scale;
+      }
+      const float ref = m == -kInf ? 0.0f : m;  // no key seen so far: every exponential is 0
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = BIAS ? s[b][r] - ref : __builtin_fmaf(s[b][r], p.scale2, -ref);
+          s[b][r] = __builtin_amdgcn_exp2f(x);
+          l += s[b][r];
+        }
+      // e^x rounded to bf16 (half a step of 2^-8, as out is; their sum is not) so that
+      // the product runs at bf16's rate
+#pragma unroll
+      for (int b = 0; b < KB; ++b)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag<DT> e;
+          float x[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) x[j] = s[b][8 * u + j];
+          e.set(x);
+          Frag<DT> rest;
+          if constexpr (EXACT) {
+            float y[8];
+            e.get(y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] -= y[j];
+            rest.set(x);
+          }
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            const Frag<DT> v = Tl::column(v_tile, b * 32 + 16 * u, c, lane);
+            o[c] = mma(v, e, o[c]);
+            if constexpr (EXACT) o[c] = mma(v, rest, o[c]);
+          }
+        }
+    }
+    lds_barrier();
+  }
+  if (!valid) return;
+  l = add_halves(l);
+  if constexpr (SPLIT) {
+    const int64_t row = ((int64_t)split * p.heads + head) * p.q.tokens + token;
+    const int64_t all = (int64_t)p.splits * p.heads * p.q.tokens;
+    float* to = f.part + row * p.dim;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float x[4] = {o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
+        store4<RIP_FP32>(to, c * 32 + block_row(r, half), p.dim, x);
+      }
+    if (half == 0) {
+      f.part[all * p.dim + row] = m;
+      f.part[all * (p.dim + 1) + row] = l;
+    }
+  } else {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    T* out = (T*)f.out.p + token * f.out.ld + (int64_t)head * p.dim;
+    T* low = f.low.p ? (T*)f.low.p + token * f.low.ld + (int64_t)head * p.dim : nullptr;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = o[c][r + j] * inv;
+        store4<DT>(out, c * 32 + block_row(r, half), p.dim, x);
+        if (DT == RIP_BF16 && low) {
+#pragma unroll
+          for (int j = 0; j < 4; j += 2) {
+            const uint32_t b = Elem<RIP_BF16>::pack2(x[j], x[j + 1]);
+            x[j] -= __uint_as_float(b << 16), x[j + 1] -= __uint_as_float(b & 0xffff0000u);
+          }
+          store4<DT>(low, c * 32 + block_row(r, half), p.dim, x);
+        }
+      }
+    if (f.lse && half == 0)
+      f.lse[(int64_t)head * p.q.tokens + token] = l == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// The splits of a query joined: a wave for each query and head.
+template <int DT>
+__global__ __launch_bounds__(256) void join_kernel(Forward f) {
+  typedef typename Elem<DT>::T T;
+  const Args& p = f.a;
+  const int lane = threadIdx.x % 64;
+  const int64_t all = (int64_t)p.heads * p.q.tokens, row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+  if (row >= all) return;
+  const float* ms = f.part + all * p.splits * p.dim;
+  const float* ls = ms + all * p.splits;
+  float m = -kInf;
+  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ms[s * all + row]);
+  const float ref = m == -kInf ? 0.0f : m;
+  float l = 0.0f;
+  for (int s = 0; s < p.splits; ++s)
+    l += ls[s * all + row] * __builtin_amdgcn_exp2f(ms[s * all + row] - ref);
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int64_t head = row / p.q.tokens, token = row - head * p.q.tokens;
+  for (int c = lane; c < p.dim; c += 64) {
+    float x = 0.0f;
+    for (int s = 0; s < p.splits; ++s)
+      x += f.part[(s * all + row) * p.dim + c] * __builtin_amdgcn_exp2f(ms[s * all + row] - ref);
+    x *= inv;
+    Elem<DT>::store((T*)f.out.p + token * f.out.ld + head * p.dim + c, x);
+    if (DT == RIP_BF16 && f.low.p) {
+      const uint32_t b = Elem<RIP_BF16>::pack2(x, x) << 16;
+      Elem<DT>::store((T*)f.low.p + token * f.low.ld + head * p.dim + c, x - __uint_as_float(b));
+    }
+  }
+  if (f.lse && lane == 0) f.lse[row] = l == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <int DT, int D, int WAVES, int MODE>
+const void* variant(bool split) {
+  return split ? (const void*)forward_kernel<DT, D, WAVES, MODE, true>
+               : (const void*)forward_kernel<DT, D, WAVES, MODE, false>;
+}
+template <int DT, int D, int WAVES>
+const void* variant(int mode, bool split) {
+  if (DT == RIP_BF16 && mode == kExact) return variant<RIP_BF16, D, WAVES, kExact>(split);
+  return mode == kPlain ? variant<DT, D, WAVES, kPlain>(split) : variant<DT, D, WAVES, kBias>(split);
+}
+template <int DT>
+const void* kernel_of(int width, int waves, int mode, bool split) {
+  const bool one = waves == 1;
+  switch (width) {
+    case 64: return one ? variant<DT, 64, 1>(mode, split) : variant<DT, 64, kWaves>(mode, split);
+    case 128: return one ? variant<DT, 128, 1>(mode, split) : variant<DT, 128, kWaves>(mode, split);
+    default: return one ? variant<DT, 256, 1>(mode, split) : variant<DT, 256, kWaves>(mode, split);
+  }
+}
+
+}  // namespace
+
+int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* stream) {
+  const Args& p = f.a;
+  void* args[] = {&f};
+  const bool split = p.splits > 1;
+  const int mode = !p.lut ? kPlain : f.low.p ? kExact : kBias;
+  const void* fn = dtype == RIP_BF16 ? kernel_of<RIP_BF16>(width, waves, mode, split)
+                                     : kernel_of<RIP_FP32>(width, waves, mode, split);
+  int32_t rc = launch(fn, dim3((uint32_t)p.slots * p.splits, (uint32_t)(p.heads / p.pack)),
+                      dim3(64 * waves), args, p.lut ? p.lut_size * 4 : 0, stream, "rip_attn_forward");
+  if (rc || !split) return rc;
+  return launch(dtype == RIP_BF16 ? (const void*)join_kernel<RIP_BF16> : (const void*)join_kernel<RIP_FP32>,
+                dim3((uint32_t)ceil_div((int64_t)p.heads * p.q.tokens, 4)), dim3(256), args, 0, stream,
+                "rip_attn_forward: join");
+}
+
+}  // namespace attn
+}  // namespace rip

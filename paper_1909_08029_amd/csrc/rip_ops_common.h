@@ -1,5 +1,5 @@
 // Device and host helpers shared by the operators that fill gradient buffers
-// (rip_embed.hip, rip_ckpt.hip, rip_wgrad.hip, rip_loss.hip).
+// (rip_embed.hip, rip_ckpt.hip, rip_wgrad.hip, rip_loss.hip, rip_attn*.hip).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -190,5 +190,46 @@ inline int32_t check_apart(const char* name, const Range* list, int count) {
 inline int64_t span(int32_t dtype, int64_t rows, int64_t width, int64_t ld) {
   return rows < 1 || width < 1 ? 0 : ((rows - 1) * ld + width) * elem_bytes(dtype);
 }
+
+// The buffers of a call; those that are written share no element with any
+// other, except (with `in_place`) an output that is exactly one of the inputs (each
+// element is read by the lane that writes it, before it does).  Two matrices may lie
+// side by side in the rows of one buffer (gate and up of one projection).
+struct Buffers {
+  struct One {
+    const void* p;
+    int64_t bytes, pitch, row;  // from first to last byte, between rows, of a row
+    const char* what;
+    bool written, matrix;
+  } list[16];
+  int n = 0;
+  bool in_place = true;
+  void matrix(const void* p, int32_t dtype, int64_t rows, int64_t width, int64_t ld,
+              const char* what, bool written) {
+    list[n++] = {p, span(dtype, rows, width, ld), ld * elem_bytes(dtype), width * elem_bytes(dtype),
+                 what, written, true};
+  }
+  void range(const void* p, int64_t bytes, const char* what, bool written) {
+    list[n++] = {p, bytes, bytes, bytes, what, written, false};
+  }
+  static bool side_by_side(const One& a, const One& b) {
+    if (!a.matrix || !b.matrix || a.pitch != b.pitch) return false;
+    const intptr_t gap = reinterpret_cast<intptr_t>(b.p) - reinterpret_cast<intptr_t>(a.p);
+    const int64_t off = ((gap % a.pitch) + a.pitch) % a.pitch;
+    return off >= a.row && off + b.row <= a.pitch;
+  }
+  int32_t check() const {
+    for (int i = 0; i < n; ++i)
+      for (int j = 0; j < i; ++j) {
+        const One &a = list[i], &b = list[j];
+        if (!a.written && !b.written) continue;
+        if (!overlap(a.p, a.bytes, b.p, b.bytes) || side_by_side(a, b)) continue;
+        if (in_place && a.written != b.written && a.matrix && b.matrix && a.p == b.p && a.pitch == b.pitch)
+          continue;
+        return fail(RIP_E_OVERLAP, "%s overlaps %s", a.what, b.what);
+      }
+    return RIP_OK;
+  }
+};
 
 }  // namespace rip
