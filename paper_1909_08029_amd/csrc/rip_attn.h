@@ -65,10 +65,20 @@ struct Backward {
   const Buckets* buckets;  // device
 };
 
+// The grid of a launch over slots, splits and heads: as many rows as its 32-bit sizes
+// need.
+inline dim3 grid_of(const Args& p, int heads) {
+  const int64_t all = (int64_t)p.slots * p.splits * heads, row = 1 << 20;
+  return all <= row ? dim3((uint32_t)all) : dim3((uint32_t)row, (uint32_t)ceil_div(all, row));
+}
+
 // Launches by type and width (rip_attn_forward.hip, rip_attn_backward.hip).
 int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* stream);
-int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype, int width,
-                     void* stream);
+struct Plans {
+  Plan q, k;
+};
+int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype,
+                     const Plans& plan, void* stream);
 int32_t run_bias_grad(const Backward& f, int64_t parts, int32_t buckets, int32_t heads,
                       int32_t dtype, void* grad, int64_t ld, int32_t accumulate, void* stream);
 

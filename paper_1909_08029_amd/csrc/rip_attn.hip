@@ -82,15 +82,11 @@ struct Layout {
   }
 };
 
-struct Plans {
-  Plan q, k;
-};
-
 bool two_sided(const rip_attn& a) { return a.k_offsets && a.k_offsets != a.q_offsets; }
 
 Sizes sizes_of(const rip_attn& a) {
   return {a.q_tokens, a.k_tokens, a.n_sequences, a.heads, a.heads / a.kv_heads, a.head_dim,
-          a.bias != nullptr};
+          a.dtype == RIP_BF16, a.causal != 0, a.bias != nullptr};
 }
 
 Layout layout_of(const rip_attn& a, const Plans& plan, bool backward) {
@@ -157,9 +153,9 @@ int32_t check(const rip_attn* a, const char* name) {
   return check_matrix(a->bias, "bias", a->bias_dtype, a->buckets, a->heads, a->ld_bias);
 }
 
-// A grid's sizes are 32 bits of work-items, and places among all its workgroups too.
+// Workgroups are counted in 32 bits.
 int32_t check_grid(const Plan& p, int64_t heads, const char* name) {
-  if (p.slots * p.splits >= (int64_t)1 << 24 || p.slots * p.splits * heads >= (int64_t)1 << 31)
+  if (p.slots * p.splits * heads >= (int64_t)1 << 31)
     return fail(RIP_E_UNSUPPORTED, "%s: %lld tiles of %lld heads are above the limit", name,
                 (long long)(p.slots * p.splits), (long long)heads);
   return RIP_OK;
@@ -223,7 +219,7 @@ int32_t check_workspace(const void* ws, int64_t bytes, int64_t need, const char*
 
 Plans plans_of(const rip_attn& a, bool backward) {
   const Sizes s = sizes_of(a);
-  return {over_queries(s, !backward), backward ? over_keys(s) : Plan{}};
+  return {backward ? plan_dq(s) : plan_forward(s), backward ? plan_dkv(s) : Plan{}};
 }
 
 // What every call reads besides its matrices.
@@ -365,8 +361,7 @@ extern "C" int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t l
     f.bias_part = (float*)(ws + l.bias_part);
     f.buckets = (const Buckets*)(ws + l.buckets);
   }
-  if ((rc = run_backward(f, args_of(*a, plan.q, l, ws), args_of(*a, plan.k, l, ws), t, plan.q.width,
-                         stream)) ||
+  if ((rc = run_backward(f, args_of(*a, plan.q, l, ws), args_of(*a, plan.k, l, ws), t, plan, stream)) ||
       !dbias)
     return rc;
   return run_bias_grad(f, plan.q.slots * plan.q.splits, a->buckets, a->heads, dbias_dtype, dbias, ld_dbias,

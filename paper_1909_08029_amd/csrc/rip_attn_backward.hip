@@ -15,9 +15,6 @@ namespace rip {
 namespace attn {
 namespace {
 
-template <int DT, int D>
-constexpr int kStep = DT == RIP_BF16 && D <= 128 ? 64 : 32;  // keys (queries) of a tile
-
 // A row's log-sum in the log2 domain; +inf, so that every exponential is 0, for a
 // query that sees no key.
 __device__ __forceinline__ float reference(float lse) {
@@ -51,20 +48,19 @@ __device__ __forceinline__ void add_diagonals(const f32x16& ds, int rel, int fir
   __builtin_amdgcn_wave_barrier();
 }
 
-template <int DT, int D, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) void dq_kernel(
-    Backward f) {
+template <int DT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   typedef typename Elem<DT>::T T;
   typedef Tile<DT, D> Tl;
-  constexpr int KT = kStep<DT, D>, KB = KT / 32, QT = kRows * kWaves;
+  constexpr int KT = STEP, KB = KT / 32, QT = kRows * WAVES;
   __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
 
-  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
-  const int hz = place / per_head, rest = place - hz * per_head, split = SPLIT ? rest / p.slots : 0;
-  const int slot = p.slots - 1 - (SPLIT ? rest - split * p.slots : rest);
+  Share my;
+  if (!my_share(p, p.heads / p.pack, &my)) return;
+  const int hz = my.head, split = my.split, slot = p.slots - 1 - my.slot;
   const Place at = find<QT>(p, p.q, p.k, slot, p.pack);
   const int lq = at.here.end - at.here.begin, lk = at.other.end - at.other.begin, shift = lk - lq;
   const int rows = lq * p.pack, w0 = at.tile * QT;
@@ -73,14 +69,14 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
   const int pitch = BIAS ? sums_size(p.lut_size) : 0;
   float* const sums = lut + p.lut_size;
   float* const mine = sums + wave * pitch;
-  float* const block = sums + kWaves * pitch + wave * 32 * kBlockPitch;
+  float* const block = sums + WAVES * pitch + wave * 32 * kBlockPitch;
   const int intervals = BIAS ? f.buckets->n : 0;
   float* const bias_part =
       BIAS ? f.bias_part + ((int64_t)hz * p.slots * p.splits + slot * p.splits + split) * intervals
            : nullptr;
   if (w0 >= rows) {
     if (BIAS)
-      for (int b = threadIdx.x; b < intervals; b += 64 * kWaves) bias_part[b] = 0.0f;
+      for (int b = threadIdx.x; b < intervals; b += 64 * WAVES) bias_part[b] = 0.0f;
     return;
   }
 
@@ -111,19 +107,18 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
   // delta in fp32 from out and what its rounding left
   float delta = 0.0f;
   {
-    const T* out = (const T*)f.out.p + token * f.out.ld + (int64_t)head * p.dim;
-    const T* low = f.low.p ? (const T*)f.low.p + token * f.low.ld + (int64_t)head * p.dim : nullptr;
+    const int64_t at_head = (int64_t)head * p.dim;
+    Frag<DT> out[D / 16], low[D / 16] = {};
+    load_row<DT, D>((const T*)f.out.p + token * f.out.ld + at_head, valid, half, p.dim, out);
+    if (DT == RIP_BF16 && f.low.p)
+      load_row<DT, D>((const T*)f.low.p + token * f.low.ld + at_head, valid, half, p.dim, low);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
-      const int col = 16 * c + 8 * half;
-      float x[kLane] = {}, y[kLane] = {}, z[kLane];
-      if (valid && col < p.dim) {
-        load_unit<DT>(out, col, p.dim, x);
-        if (DT == RIP_BF16 && low) load_unit<DT>(low, col, p.dim, y);
-      }
-      dout[c].get(z);
+      float x[kLane], y[kLane], z[kLane];
+      out[c].get(x), low[c].get(y), dout[c].get(z);
 #pragma unroll
-      for (int j = 0; j < kLane; ++j) delta = __builtin_fmaf(z[j], x[j] + y[j], delta);
+      for (int j = 0; j < kLane; ++j)
+        delta = __builtin_fmaf(z[j], DT == RIP_BF16 ? x[j] + y[j] : x[j], delta);
     }
     delta = add_halves(delta);
   }
@@ -132,22 +127,21 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
   if (valid && half == 0 && split == 0) f.delta[row] = delta;
   const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
   const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
-  auto k_row = [&](int r) { return k0 + r * f.k.ld; };
-  auto v_row = [&](int r) { return v0 + r * f.v.ld; };
+  const Tl at_lane(lane);
 
   f32x16 dq[D / 32] = {};
-  Stage<DT, D, KT, 64 * kWaves> ks, vs;
+  Stage<DT, D, KT, 64 * WAVES> ks, vs;
   if (t < end) {
-    ks.load(k_row, t, end, p.dim);
-    vs.load(v_row, t, end, p.dim);
+    ks.load(k0, f.k.ld, t, end, p.dim);
+    vs.load(v0, f.v.ld, t, end, p.dim);
   }
   for (; t < end; t += KT) {
-    ks.store(k_tile);
-    vs.store(v_tile);
+    ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
+    vs.store(v_tile, v0, f.v.ld, t, end, p.dim);
     lds_barrier();
     if (t + KT < end) {
-      ks.load(k_row, t + KT, end, p.dim);
-      vs.load(v_row, t + KT, end, p.dim);
+      ks.load(k0, f.k.ld, t + KT, end, p.dim);
+      vs.load(v0, f.v.ld, t + KT, end, p.dim);
     }
     if (wq < rows && t < most) {
 #pragma unroll
@@ -155,8 +149,8 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          s = mma(Tl::row(k_tile, b * 32 + lane % 32, c, half), q[c], s);
-          dp = mma(Tl::row(v_tile, b * 32 + lane % 32, c, half), dout[c], dp);
+          s = mma(at_lane.row(k_tile, b * 32, c), q[c], s);
+          dp = mma(at_lane.row(v_tile, b * 32, c), dout[c], dp);
         }
         const int key = t + b * 32;
         int side = 0;
@@ -201,7 +195,7 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
           e.set(x);
 #pragma unroll
           for (int c = 0; c < D / 32; ++c)
-            dq[c] = mma(Tl::column(k_tile, b * 32 + 16 * u, c, lane), e, dq[c]);
+            dq[c] = mma(at_lane.column(k_tile, b * 32 + 16 * u, c), e, dq[c]);
         }
       }
     }
@@ -231,16 +225,16 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
     for (int o = 32; o >= 1; o /= 2) below += __shfl_xor(below, o), above += __shfl_xor(above, o);
     if (lane == 0) block[0] = below, block[1] = above;
     __syncthreads();
-    const float* const blocks = sums + kWaves * pitch;
+    const float* const blocks = sums + WAVES * pitch;
     const int x0 = p.lut_first - 62;  // distance of the first sum
-    for (int b = wave; b < intervals; b += kWaves) {
+    for (int b = wave; b < intervals; b += WAVES) {
       const int from = b == 0 ? x0 : f.buckets->start[b - 1];
       const int to = b == intervals - 1 ? x0 + pitch : f.buckets->start[b];
       float sum = 0.0f;
       for (int x = from + lane; x < to; x += 64)
 #pragma unroll
-        for (int s = 0; s < kWaves; ++s) sum += sums[s * pitch + x - x0];
-      if (lane < kWaves) {
+        for (int s = 0; s < WAVES; ++s) sum += sums[s * pitch + x - x0];
+      if (lane < WAVES) {
         if (b == 0) sum += blocks[lane * 32 * kBlockPitch];
         if (b == intervals - 1) sum += blocks[lane * 32 * kBlockPitch + 1];
       }
@@ -252,21 +246,22 @@ __global__ __launch_bounds__(64 * kWaves, DT == RIP_BF16 && D <= 64 ? 2 : 1) voi
 }
 
 // dk (DK) and dv (DV) of 32 keys to a wave.
-template <int DT, int D, bool BIAS, bool SPLIT, bool DK, bool DV>
-__global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
+template <int DT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT, bool DK, bool DV>
+__global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
   typedef typename Elem<DT>::T T;
   typedef Tile<DT, D> Tl;
-  constexpr int QT = kStep<DT, D>, QB = QT / 32, KT = kRows * kWaves;
+  constexpr int QT = STEP, QB = QT / 32, KT = kRows * WAVES;
   __shared__ __align__(128) T q_tile[QT * Tl::kPitch], do_tile[QT * Tl::kPitch];
   __shared__ __align__(16) float refs[QT], deltas[QT];
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
 
-  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
-  const int kv = place / per_head, rest = place - kv * per_head, split = SPLIT ? rest / p.slots : 0;
+  Share my;
+  if (!my_share(p, p.heads / p.group, &my)) return;
+  const int kv = my.head, split = my.split;
   // the first keys of a causal sequence have the most queries
-  const Place at = find<KT>(p, p.k, p.q, SPLIT ? rest - split * p.slots : rest, 1);
+  const Place at = find<KT>(p, p.k, p.q, my.slot, 1);
   const int lk = at.here.end - at.here.begin, lq = at.other.end - at.other.begin, shift = lk - lq;
   const int j0 = at.tile * KT;
   if (j0 >= lk) return;
@@ -294,12 +289,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
 
   const T* q0 = (const T*)f.q.p + at.other.begin * f.q.ld + (int64_t)kv * p.group * p.dim;
   const T* do0 = (const T*)f.dout.p + at.other.begin * f.dout.ld + (int64_t)kv * p.group * p.dim;
-  Stage<DT, D, QT, 64 * kWaves> qs, ds;
+  const Tl at_lane(lane);
+  Stage<DT, D, QT, 64 * WAVES> qs, ds;
   float ref = kInf, del = 0.0f;  // of query threadIdx.x of the tile
   auto load = [&](int step) {
     const int g = step / tiles, i0 = start + (step - g * tiles) * QT;
-    qs.load([&](int r) { return q0 + r * f.q.ld + (int64_t)g * p.dim; }, i0, lq, p.dim);
-    ds.load([&](int r) { return do0 + r * f.dout.ld + (int64_t)g * p.dim; }, i0, lq, p.dim);
+    qs.load(q0 + (int64_t)g * p.dim, f.q.ld, i0, lq, p.dim);
+    ds.load(do0 + (int64_t)g * p.dim, f.dout.ld, i0, lq, p.dim);
     const int i = i0 + threadIdx.x;
     ref = kInf, del = 0.0f;
     if (threadIdx.x < QT && i < lq) {
@@ -312,8 +308,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
   int lut_head = -1;
   for (; n < end; ++n) {
     const int g = n / tiles, i0 = start + (n - g * tiles) * QT;
-    qs.store(q_tile);
-    ds.store(do_tile);
+    qs.store(q_tile, q0 + (int64_t)g * p.dim, f.q.ld, i0, lq, p.dim);
+    ds.store(do_tile, do0 + (int64_t)g * p.dim, f.dout.ld, i0, lq, p.dim);
     if (threadIdx.x < QT) refs[threadIdx.x] = ref, deltas[threadIdx.x] = del;
     if (BIAS && lut_head != g) {
       load_lut(p, kv * p.group + g, lut);
@@ -327,8 +323,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          s = mma(Tl::row(q_tile, b * 32 + lane % 32, c, half), k[c], s);
-          if constexpr (DK) dp = mma(Tl::row(do_tile, b * 32 + lane % 32, c, half), v[c], dp);
+          s = mma(at_lane.row(q_tile, b * 32, c), k[c], s);
+          if constexpr (DK) dp = mma(at_lane.row(do_tile, b * 32, c), v[c], dp);
         }
         const int ib = i0 + b * 32;
         if (BIAS)
@@ -368,8 +364,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void dkv_kernel(Backward f) {
           de.set(y);
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
-            if constexpr (DV) dv[c] = mma(Tl::column(do_tile, b * 32 + 16 * u, c, lane), e, dv[c]);
-            if constexpr (DK) dk[c] = mma(Tl::column(q_tile, b * 32 + 16 * u, c, lane), de, dk[c]);
+            if constexpr (DV) dv[c] = mma(at_lane.column(do_tile, b * 32 + 16 * u, c), e, dv[c]);
+            if constexpr (DK) dk[c] = mma(at_lane.column(q_tile, b * 32 + 16 * u, c), de, dk[c]);
           }
         }
       }
@@ -439,17 +435,35 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buck
   Elem<DT>::store(g, accumulate ? Elem<DT>::load(g) + sum : sum);
 }
 
+// Variants: waves of a workgroup, rows of a tile of the other axis, waves to a SIMD
+// that the registers have to leave room for.
+template <int DT, int D>
+struct Shape {
+  static constexpr int kDqWaves = dq_waves(DT == RIP_BF16, D), kDkvWaves = dkv_waves(DT == RIP_BF16, D);
+  static constexpr int kDqStep = DT == RIP_BF16 && D <= 64 ? 64 : 32;
+  static constexpr int kDkvStep = kDqStep;
+  static constexpr int kDqUnits = DT == RIP_BF16 && D <= 128 ? 2 : 1;
+  static constexpr int kDkvUnits = DT == RIP_BF16 && D == 128 ? 2 : 1;
+};
+template <int DT, int D, bool BIAS, bool SPLIT>
+const void* dq_of() {
+  typedef Shape<DT, D> S;
+  return (const void*)dq_kernel<DT, D, S::kDqWaves, S::kDqStep, S::kDqUnits, BIAS, SPLIT>;
+}
 template <int DT, int D>
 const void* dq_of(bool bias, bool split) {
-  return bias ? (split ? (const void*)dq_kernel<DT, D, true, true> : (const void*)dq_kernel<DT, D, true, false>)
-              : (split ? (const void*)dq_kernel<DT, D, false, true> : (const void*)dq_kernel<DT, D, false, false>);
+  return bias ? (split ? dq_of<DT, D, true, true>() : dq_of<DT, D, true, false>())
+              : (split ? dq_of<DT, D, false, true>() : dq_of<DT, D, false, false>());
+}
+template <int DT, int D, bool BIAS, bool SPLIT, bool DK, bool DV>
+const void* dkv_of() {
+  typedef Shape<DT, D> S;
+  return (const void*)dkv_kernel<DT, D, S::kDkvWaves, S::kDkvStep, S::kDkvUnits, BIAS, SPLIT, DK, DV>;
 }
 template <int DT, int D, bool DK, bool DV>
 const void* dkv_of(bool bias, bool split) {
-  return bias ? (split ? (const void*)dkv_kernel<DT, D, true, true, DK, DV>
-                       : (const void*)dkv_kernel<DT, D, true, false, DK, DV>)
-              : (split ? (const void*)dkv_kernel<DT, D, false, true, DK, DV>
-                       : (const void*)dkv_kernel<DT, D, false, false, DK, DV>);
+  return bias ? (split ? dkv_of<DT, D, true, true, DK, DV>() : dkv_of<DT, D, true, false, DK, DV>())
+              : (split ? dkv_of<DT, D, false, true, DK, DV>() : dkv_of<DT, D, false, false, DK, DV>());
 }
 template <int DT>
 int32_t add(const float* part, int splits, int64_t tokens, int width, Heads to, void* stream) {
@@ -459,9 +473,10 @@ int32_t add(const float* part, int splits, int64_t tokens, int width, Heads to, 
 }
 
 template <int DT>
-int32_t run(Backward& f, const Args& over_q, const Args& over_k, int width, void* stream) {
+int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& plan, void* stream) {
   int32_t rc;
   const bool bias = over_q.lut;
+  const int width = plan.q.width;
   {
     f.a = over_q;
     const bool split = f.a.splits > 1;
@@ -469,10 +484,9 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, int width, void
                      : width == 128 ? dq_of<DT, 128>(bias, split)
                                     : dq_of<DT, 256>(bias, split);
     const size_t lds =
-        bias ? 4 * (f.a.lut_size + kWaves * (sums_size(f.a.lut_size) + 32 * kBlockPitch)) : 0;
+        bias ? 4 * (f.a.lut_size + plan.q.waves * (sums_size(f.a.lut_size) + 32 * kBlockPitch)) : 0;
     void* args[] = {&f};
-    if ((rc = launch(fn, dim3((uint32_t)f.a.slots * f.a.splits, (uint32_t)(f.a.heads / f.a.pack)),
-                     dim3(64 * kWaves), args, lds, stream, "rip_attn_backward: queries")))
+    if ((rc = launch(fn, grid_of(f.a, f.a.heads / f.a.pack), dim3(64 * plan.q.waves), args, lds, stream, "rip_attn_backward: queries")))
       return rc;
     if (split && (rc = add<DT>(f.part, f.a.splits, f.a.q.tokens, f.a.heads * f.a.dim, f.dq, stream)))
       return rc;
@@ -480,22 +494,22 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, int width, void
   f.a = over_k;
   const int kv_heads = f.a.heads / f.a.group;
   const bool split = f.a.splits > 1;
-  const dim3 grid((uint32_t)f.a.slots * f.a.splits, (uint32_t)kv_heads);
+  const dim3 grid = grid_of(f.a, kv_heads);
   const size_t lds = bias ? 4 * f.a.lut_size : 0;
   void* args[] = {&f};
   const char* what = "rip_attn_backward: keys";
   if (DT == RIP_FP32 && width == 256) {
     // dk and dv with the operands of both do not fit the registers: one after the other
-    if ((rc = launch(dkv_of<RIP_FP32, 256, false, true>(bias, split), grid, dim3(64 * kWaves), args, lds,
+    if ((rc = launch(dkv_of<RIP_FP32, 256, false, true>(bias, split), grid, dim3(64 * plan.k.waves), args, lds,
                      stream, what)) ||
-        (rc = launch(dkv_of<RIP_FP32, 256, true, false>(bias, split), grid, dim3(64 * kWaves), args, lds,
+        (rc = launch(dkv_of<RIP_FP32, 256, true, false>(bias, split), grid, dim3(64 * plan.k.waves), args, lds,
                      stream, what)))
       return rc;
   } else {
     const void* fn = width == 64    ? dkv_of<DT, 64, true, true>(bias, split)
                      : width == 128 ? dkv_of<DT, 128, true, true>(bias, split)
                                     : dkv_of<RIP_BF16, 256, true, true>(bias, split);
-    if ((rc = launch(fn, grid, dim3(64 * kWaves), args, lds, stream, what))) return rc;
+    if ((rc = launch(fn, grid, dim3(64 * plan.k.waves), args, lds, stream, what))) return rc;
   }
   if (!split) return RIP_OK;
   const int cols = kv_heads * f.a.dim;
@@ -506,10 +520,10 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, int width, void
 
 }  // namespace
 
-int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype, int width,
+int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype, const Plans& plan,
                      void* stream) {
-  return dtype == RIP_BF16 ? run<RIP_BF16>(f, over_q, over_k, width, stream)
-                           : run<RIP_FP32>(f, over_q, over_k, width, stream);
+  return dtype == RIP_BF16 ? run<RIP_BF16>(f, over_q, over_k, plan, stream)
+                           : run<RIP_FP32>(f, over_q, over_k, plan, stream);
 }
 
 int32_t run_bias_grad(const Backward& f, int64_t parts, int32_t buckets, int32_t heads, int32_t dtype,

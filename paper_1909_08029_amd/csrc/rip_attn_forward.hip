@@ -14,8 +14,9 @@ namespace rip {
 namespace attn {
 namespace {
 
-template <int DT, int D>
-constexpr int kKeys = DT == RIP_BF16 && D <= 128 ? 64 : 32;  // keys of a tile
+// Keys of a tile.  A wave by itself holds a whole tile on its way in its registers.
+template <int DT, int D, int WAVES>
+constexpr int kKeys = DT == RIP_BF16 && D <= 128 && (WAVES > 1 || D <= 64) ? 64 : 32;
 
 // Without a bias, with one, and with one whose gradient will be wanted: that sums ds
 // in fp32, and its row sums delta come from out, which must not hold the rounding of
@@ -29,17 +30,18 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
     Forward f) {
   typedef typename Elem<DT>::T T;
   typedef Tile<DT, D> Tl;
-  constexpr int KT = kKeys<DT, D>, KB = KT / 32, QT = kRows * WAVES;
+  constexpr int KT = kKeys<DT, D, WAVES>, KB = KT / 32, QT = kRows * WAVES;
   constexpr bool BIAS = MODE != kPlain, EXACT = MODE == kExact;
   __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
 
-  const uint32_t place = xcd_place(), per_head = (uint32_t)p.slots * p.splits;
-  const int hz = place / per_head, rest = place - hz * per_head, split = SPLIT ? rest / p.slots : 0;
+  Share my;
+  if (!my_share(p, p.heads / p.pack, &my)) return;
+  const int hz = my.head, split = my.split;
   // the last tiles of a causal sequence have the most keys and go first
-  const Place at = find<QT>(p, p.q, p.k, p.slots - 1 - (SPLIT ? rest - split * p.slots : rest), p.pack);
+  const Place at = find<QT>(p, p.q, p.k, p.slots - 1 - my.slot, p.pack);
   const int lq = at.here.end - at.here.begin, lk = at.other.end - at.other.begin, shift = lk - lq;
   const int rows = lq * p.pack, w0 = at.tile * QT;
   if (w0 >= rows) return;
@@ -65,23 +67,22 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
   load_row<DT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
   const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
-  auto k_row = [&](int r) { return k0 + r * f.k.ld; };
-  auto v_row = [&](int r) { return v0 + r * f.v.ld; };
+  const Tl at_lane(lane);
 
   f32x16 o[D / 32] = {};
   float m = -kInf, l = 0.0f;  // reference (log2); the sum of this half's keys
   Stage<DT, D, KT, 64 * WAVES> ks, vs;
   if (t < end) {
-    ks.load(k_row, t, end, p.dim);
-    vs.load(v_row, t, end, p.dim);
+    ks.load(k0, f.k.ld, t, end, p.dim);
+    vs.load(v0, f.v.ld, t, end, p.dim);
   }
   for (; t < end; t += KT) {
-    ks.store(k_tile);
-    vs.store(v_tile);
+    ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
+    vs.store(v_tile, v0, f.v.ld, t, end, p.dim);
     lds_barrier();
     if (t + KT < end) {
-      ks.load(k_row, t + KT, end, p.dim);
-      vs.load(v_row, t + KT, end, p.dim);
+      ks.load(k0, f.k.ld, t + KT, end, p.dim);
+      vs.load(v0, f.v.ld, t + KT, end, p.dim);
     }
     if (wq < rows && t < most) {
       f32x16 s[KB] = {};
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
       for (int c = 0; c < D / 16; ++c)
 #pragma unroll
         for (int b = 0; b < KB; ++b)
-          s[b] = mma(Tl::row(k_tile, b * 32 + lane % 32, c, half), q[c], s[b]);
+          s[b] = mma(at_lane.row(k_tile, b * 32, c), q[c], s[b]);
       if (BIAS) {
         const int first = __builtin_amdgcn_readlane(pos, 0), last = __builtin_amdgcn_readlane(pos, 31);
 #pragma unroll
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
           }
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
-            const Frag<DT> v = Tl::column(v_tile, b * 32 + 16 * u, c, lane);
+            const Frag<DT> v = at_lane.column(v_tile, b * 32 + 16 * u, c);
             o[c] = mma(v, e, o[c]);
             if constexpr (EXACT) o[c] = mma(v, rest, o[c]);
           }
@@ -203,36 +204,53 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
   }
 }
 
-// The splits of a query joined: a wave for each query and head.
+// The splits of a query and head joined by a workgroup: a lane of each wave has a
+// split's weight, and the waves take the splits in turn.
 template <int DT>
 __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   typedef typename Elem<DT>::T T;
+  static_assert(kMaxSplits <= 64, "a lane to a split");
+  __shared__ float sums[4][RIP_MAX_HEAD_DIM];
   const Args& p = f.a;
-  const int lane = threadIdx.x % 64;
-  const int64_t all = (int64_t)p.heads * p.q.tokens, row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (row >= all) return;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t all = (int64_t)p.heads * p.q.tokens, row = blockIdx.x;
   const float* ms = f.part + all * p.splits * p.dim;
-  const float* ls = ms + all * p.splits;
-  float m = -kInf;
-  for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ms[s * all + row]);
-  const float ref = m == -kInf ? 0.0f : m;
-  float l = 0.0f;
-  for (int s = 0; s < p.splits; ++s)
-    l += ls[s * all + row] * __builtin_amdgcn_exp2f(ms[s * all + row] - ref);
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  float m = -kInf, l = 0.0f;
+  if (lane < p.splits) {
+    m = ms[lane * all + row];
+    l = ms[(p.splits + lane) * all + row];
+  }
+  float top = m;
+#pragma unroll
+  for (int o = 32; o >= 1; o /= 2) top = fmaxf(top, __shfl_xor(top, o));
+  const float weight = __builtin_amdgcn_exp2f(m - (top == -kInf ? 0.0f : top));
+  l *= weight;
+#pragma unroll
+  for (int o = 32; o >= 1; o /= 2) l += __shfl_xor(l, o);
+  constexpr int kColumns = RIP_MAX_HEAD_DIM / 64;
+  float x[kColumns] = {};
+  const float* from = f.part + row * p.dim + lane;
+#pragma unroll 4
+  for (int s = wave; s < p.splits; s += 4) {
+    const float w = __shfl(weight, s);
+#pragma unroll
+    for (int c = 0; c < kColumns; ++c)
+      if (lane + 64 * c < p.dim) x[c] += from[s * all * p.dim + 64 * c] * w;
+  }
+#pragma unroll
+  for (int c = 0; c < kColumns; ++c) sums[wave][lane + 64 * c] = x[c];
+  __syncthreads();
+  const int c = threadIdx.x;
   const int64_t head = row / p.q.tokens, token = row - head * p.q.tokens;
-  for (int c = lane; c < p.dim; c += 64) {
-    float x = 0.0f;
-    for (int s = 0; s < p.splits; ++s)
-      x += f.part[(s * all + row) * p.dim + c] * __builtin_amdgcn_exp2f(ms[s * all + row] - ref);
-    x *= inv;
-    Elem<DT>::store((T*)f.out.p + token * f.out.ld + head * p.dim + c, x);
+  if (c < p.dim) {
+    const float y = ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])) * (l == 0.0f ? 0.0f : 1.0f / l);
+    Elem<DT>::store((T*)f.out.p + token * f.out.ld + head * p.dim + c, y);
     if (DT == RIP_BF16 && f.low.p) {
-      const uint32_t b = Elem<RIP_BF16>::pack2(x, x) << 16;
-      Elem<DT>::store((T*)f.low.p + token * f.low.ld + head * p.dim + c, x - __uint_as_float(b));
+      const uint32_t b = Elem<RIP_BF16>::pack2(y, y) << 16;
+      Elem<DT>::store((T*)f.low.p + token * f.low.ld + head * p.dim + c, y - __uint_as_float(b));
     }
   }
-  if (f.lse && lane == 0) f.lse[row] = l == 0.0f ? -kInf : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  if (f.lse && c == 0) f.lse[row] = l == 0.0f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <int DT, int D, int WAVES, int MODE>
@@ -249,9 +267,9 @@ template <int DT>
 const void* kernel_of(int width, int waves, int mode, bool split) {
   const bool one = waves == 1;
   switch (width) {
-    case 64: return one ? variant<DT, 64, 1>(mode, split) : variant<DT, 64, kWaves>(mode, split);
-    case 128: return one ? variant<DT, 128, 1>(mode, split) : variant<DT, 128, kWaves>(mode, split);
-    default: return one ? variant<DT, 256, 1>(mode, split) : variant<DT, 256, kWaves>(mode, split);
+    case 64: return one ? variant<DT, 64, 1>(mode, split) : variant<DT, 64, 4>(mode, split);
+    case 128: return one ? variant<DT, 128, 1>(mode, split) : variant<DT, 128, 4>(mode, split);
+    default: return one ? variant<DT, 256, 1>(mode, split) : variant<DT, 256, 4>(mode, split);
   }
 }
 
@@ -264,11 +282,10 @@ int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* strea
   const int mode = !p.lut ? kPlain : f.low.p ? kExact : kBias;
   const void* fn = dtype == RIP_BF16 ? kernel_of<RIP_BF16>(width, waves, mode, split)
                                      : kernel_of<RIP_FP32>(width, waves, mode, split);
-  int32_t rc = launch(fn, dim3((uint32_t)p.slots * p.splits, (uint32_t)(p.heads / p.pack)),
-                      dim3(64 * waves), args, p.lut ? p.lut_size * 4 : 0, stream, "rip_attn_forward");
+  int32_t rc = launch(fn, grid_of(p, p.heads / p.pack), dim3(64 * waves), args, p.lut ? p.lut_size * 4 : 0, stream, "rip_attn_forward");
   if (rc || !split) return rc;
   return launch(dtype == RIP_BF16 ? (const void*)join_kernel<RIP_BF16> : (const void*)join_kernel<RIP_FP32>,
-                dim3((uint32_t)ceil_div((int64_t)p.heads * p.q.tokens, 4)), dim3(256), args, 0, stream,
+                dim3((uint32_t)(p.heads * p.q.tokens)), dim3(256), args, 0, stream,
                 "rip_attn_forward: join");
 }
 

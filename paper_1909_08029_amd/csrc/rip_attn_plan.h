@@ -10,62 +10,107 @@
 namespace rip {
 namespace attn {
 
-constexpr int kWidths = 3;
-constexpr int kWidth[kWidths] = {64, 128, 256};  // of a head, padded with zeros
-constexpr int kWaves = 4;         // of a workgroup; one where queries are few
 constexpr int kRows = 32;         // queries (or keys) of a wave
-constexpr int kUnits = 256;       // compute units
 constexpr int kMaxSplits = 64;
 constexpr int kScan = 1024;       // offsets that every workgroup puts in order by itself
+
+constexpr int kWidths = 3;
+constexpr int kWidth[kWidths] = {64, 128, 256};  // of a head, padded with zeros
+inline int width_of(int dim) {
+  for (int i = 0; i < kWidths; ++i)
+    if (dim <= kWidth[i]) return kWidth[i];
+  return 0;
+}
 
 // Lengths are the device's; the host knows only how many tokens and sequences.
 struct Sizes {
   int64_t q_tokens, k_tokens;
   int n, heads, group, dim;
-  bool bias;
+  bool bf16, causal, bias;
 };
 struct Plan {
   int width, waves, pack, splits;
   int64_t slots;  // tiles of the grid
 };
 
-inline int width_of(int dim) {
-  for (int i = 0; i < kWidths; ++i)
-    if (dim <= kWidth[i]) return kWidth[i];
-  return 0;
-}
 inline int64_t slots_of(int64_t tokens, int pack, int n, int tile) { return tokens * pack / tile + n + 2; }
+
+// The kernels: products of a block of 32 x 32, and time (us) of a block beside them.
+struct Kernel {
+  int products;
+  double softmax;
+};
+constexpr Kernel kForward = {2, 0.12}, kDq = {3, 0.16}, kDkv = {4, 0.2};
+
+// Time (us) of `units` tiles of `waves` waves that go over `axis` elements each (half of
+// them where causal) in `splits` parts, from the time of a block on a SIMD (1024 of
+// them, shared by `resident` waves): what all SIMDs have to do, or one tile's chain,
+// whichever is longer; then the parts' way through memory and the launch that adds
+// them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us (bf16; 8192
+// clocks for 128 columns and four in fp32) a column each with two waves to a SIMD, half as
+// long again alone; a tile costs about four us before its first block.
+inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int64_t axis,
+                      int splits, double part) {
+  const double product = (s.bf16 ? 0.0021 : 0.0134) * width, block = k.products * product + k.softmax;
+  const double alone = (s.bf16 ? 1.5 : 1.0) * block * (waves == 1 ? 1.25 : 1.0);
+  const double blocks = (double)ceil_div(axis, kRows);
+  const double all = (double)units * waves * (blocks * (s.causal ? 0.5 : 1.0) * block + 2.0 * splits) / 1024;
+  const double chain = blocks / splits * alone + 4.0;
+  return std::max(all, chain) + (splits > 1 ? 5.0 + splits * part / 2e6 : 0.0);
+}
+
+constexpr int kTrySplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
 // Over the queries (forward; dq).  A tile that the queries of a head would not fill
 // takes those of all heads that share k and v.
-inline Plan over_queries(const Sizes& s, bool one_wave_allowed) {
-  Plan p{width_of(s.dim), kWaves, 1, 1, 0};
+inline Plan over_queries(const Sizes& s, const Kernel& kernel, const int* waves, int options) {
+  Plan best{width_of(s.dim), waves[0], 1, 1, 0};
   const int n = std::max(1, s.n);
   const int64_t q = ceil_div(s.q_tokens, n), k = ceil_div(s.k_tokens, n);  // of a sequence
-  if (!s.bias && s.group > 1 && q < kRows * kWaves && s.q_tokens * s.group < (int64_t)1 << 30)
-    p.pack = s.group;
-  auto units = [&] { return n * ceil_div(q * p.pack, kRows * p.waves) * (s.heads / p.pack); };
-  if (one_wave_allowed && units() < kUnits) p.waves = 1;
-  const int64_t want = p.waves == 1 ? 4 * kUnits : 2 * kUnits;
-  if (units() < want / 2)
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(want, std::max<int64_t>(1, units())),
-                                                            k / 128, kMaxSplits}));
-  p.slots = slots_of(s.q_tokens, p.pack, s.n, kRows * p.waves);
-  return p;
+  if (!s.bias && s.group > 1 && q < kRows * 4 && s.q_tokens * s.group < (int64_t)1 << 30) best.pack = s.group;
+  double least = 1e30;
+  for (int i = 0; i < options; ++i) {
+    const int64_t units = n * ceil_div(q * best.pack, kRows * waves[i]) * (s.heads / best.pack);
+    for (int splits : kTrySplits) {
+      if (splits > 1 && splits * 64 > k) break;
+      const double us = time_of(kernel, s, best.width, units, waves[i], k, splits,
+                                4.0 * s.q_tokens * s.heads * s.dim);
+      if (us < least) least = us, best.waves = waves[i], best.splits = splits;
+    }
+  }
+  best.slots = slots_of(s.q_tokens, best.pack, s.n, kRows * best.waves);
+  return best;
 }
 
-// Over the keys (dk and dv).
-inline Plan over_keys(const Sizes& s) {
-  Plan p{width_of(s.dim), kWaves, 1, 1, 0};
+// Over the keys (dk and dv), each of which goes over the queries of its heads.
+inline Plan over_keys(const Sizes& s, int waves) {
+  Plan best{width_of(s.dim), waves, 1, 1, 0};
   const int n = std::max(1, s.n);
   const int64_t q = ceil_div(s.q_tokens, n), k = ceil_div(s.k_tokens, n);
-  const int64_t units = n * ceil_div(k, kRows * kWaves) * (s.heads / s.group);
-  if (units < kUnits)
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({ceil_div(2 * kUnits, std::max<int64_t>(1, units)),
-                                                            ceil_div(q, 64) * s.group / 2, kMaxSplits}));
-  p.slots = slots_of(s.k_tokens, 1, s.n, kRows * kWaves);
-  return p;
+  const int64_t units = n * ceil_div(k, kRows * waves) * (s.heads / s.group), axis = ceil_div(q, kRows) * kRows * s.group;
+  double least = 1e30;
+  for (int splits : kTrySplits) {
+    if (splits > 1 && splits * 64 > axis) break;
+    const double us = time_of(kDkv, s, best.width, units, waves, axis, splits,
+                              8.0 * s.k_tokens * (s.heads / s.group) * s.dim);
+    if (us < least) least = us, best.splits = splits;
+  }
+  best.slots = slots_of(s.k_tokens, 1, s.n, kRows * waves);
+  return best;
 }
+
+// Waves of a workgroup.
+inline Plan plan_forward(const Sizes& s) {
+  constexpr int waves[] = {4, 1};
+  return over_queries(s, kForward, waves, 2);
+}
+constexpr int dq_waves(bool bf16, int width) { return bf16 && width == 128 ? 8 : 4; }
+constexpr int dkv_waves(bool bf16, int width) { return bf16 && width == 128 ? 8 : 4; }
+inline Plan plan_dq(const Sizes& s) {
+  const int waves[] = {dq_waves(s.bf16, width_of(s.dim))};
+  return over_queries(s, kDq, waves, 1);
+}
+inline Plan plan_dkv(const Sizes& s) { return over_keys(s, dkv_waves(s.bf16, width_of(s.dim))); }
 
 }  // namespace attn
 }  // namespace rip

@@ -85,101 +85,164 @@ __device__ __forceinline__ float add_halves(float x) {
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ int swizzle(int row) { return (row & 3) << 1 | (row >> 2 & 1); }
 
+// Swizzles change the lowest three bits of a piece's number alone, and those of a
+// lane's rows are the same in every block, so few addresses (bytes) serve all blocks:
+// the rest of an address is known when the code is compiled.
 template <int DT, int D>
-struct Tile {
-  typedef typename Elem<DT>::T T;
-  static constexpr int kPiece = 16 / (int)sizeof(T);              // elements of 16 bytes
-  static constexpr int kPitch = D * (int)sizeof(T) < 128 ? 128 / (int)sizeof(T) : D;
-  static constexpr int kSteps = D / 16;                            // products along a row
-  // Element of piece p of a row.
-  static __device__ __forceinline__ int at(int row, int piece) {
-    return row * kPitch + (piece ^ swizzle(row)) * kPiece;
-  }
-  // Operand of row `row` (the block's first + lane % 32), elements 16 s + 8 half ..
-  static __device__ __forceinline__ Frag<DT> row(const T* tile, int row, int s, int half) {
-    Frag<DT> f;
-    if constexpr (DT == RIP_BF16) {
-      f.set(*(const u32x4*)(tile + at(row, 2 * s + half)));
-    } else {
-      const f32x4 a = *(const f32x4*)(tile + at(row, 4 * s + 2 * half));
-      const f32x4 b = *(const f32x4*)(tile + at(row, 4 * s + 2 * half + 1));
+struct Tile;
+template <int D>
+struct Tile<RIP_BF16, D> {
+  typedef uint16_t T;
+  static constexpr int kPiece = 8;                    // elements of 16 bytes
+  static constexpr int kPitch = D < 64 ? 64 : D;
+  static constexpr int kBytes = kPitch * 2;
+  uint32_t rows[4], columns[2];
+  __device__ __forceinline__ explicit Tile(int lane) {
+    const int r = lane % 32, half = lane / 32;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f.x[j] = a[j], f.x[4 + j] = b[j];
-    }
+    for (int s = 0; s < 4; ++s) rows[s] = r * kBytes + ((2 * s + half) ^ swizzle(r)) * 16;
+    // sixteen lanes read four rows of 16 columns and receive a column each
+    const int group = lane / 16, in = lane % 16, row = 4 * (group / 2) + in / 4;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      columns[c] = row * kBytes + ((4 * c + group % 2 * 2 + in % 4 / 2) ^ swizzle(row)) * 16 + in % 2 * 8;
+  }
+  // Operand of row `first` + lane % 32, elements 16 s + 8 half .. (first: of 32)
+  __device__ __forceinline__ Frag<RIP_BF16> row(const T* tile, int first, int s) const {
+    Frag<RIP_BF16> f;
+    f.set(*(const u32x4*)((const char*)tile + first * kBytes + rows[s % 4] + s / 4 * 128));
     return f;
   }
   // Operand of column 32 c + lane % 32 over the 16 rows from `first` (a multiple of
   // 16), in block_row's order: rows first + 4 half .. + 3, then those 8 further.
-  static __device__ __forceinline__ Frag<DT> column(const T* tile, int first, int c, int lane) {
-    Frag<DT> f;
-    if constexpr (DT == RIP_BF16) {
-      // sixteen lanes read four rows of 16 columns and receive a column each
-      const int group = lane / 16, in = lane % 16;
-      const int row = first + 4 * (group / 2) + in / 4, col = c * 32 + group % 2 * 16 + in % 4 * 4;
-      const T* p = tile + at(row, col / 8) + col % 8;
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kPitch));
-      f.set(__builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)));
-    } else {
-      const int half = lane / 32, col = c * 32 + lane % 32;
+  __device__ __forceinline__ Frag<RIP_BF16> column(const T* tile, int first, int c) const {
+    const char* p = (const char*)tile + first * kBytes + columns[c % 2] + c / 2 * 128;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kBytes));
+    Frag<RIP_BF16> f;
+    f.set(__builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)));
+    return f;
+  }
+};
+template <int D>
+struct Tile<RIP_FP32, D> {
+  typedef float T;
+  static constexpr int kPiece = 4;
+  static constexpr int kPitch = D < 32 ? 32 : D;
+  static constexpr int kBytes = kPitch * 4;
+  uint32_t rows[4], columns[4];
+  __device__ __forceinline__ explicit Tile(int lane) {
+    const int r = lane % 32, half = lane / 32;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int row = first + 4 * half + j % 4 + j / 4 * 8;
-        f.x[j] = tile[at(row, col / 4) + col % 4];
-      }
+    for (int s = 0; s < 4; ++s)
+      rows[s] = r * kBytes + ((s / 2 * 4 + 2 * half + s % 2) ^ swizzle(r)) * 16;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = 4 * half + j;
+      columns[j] = row * kBytes + (lane % 32 / 4 ^ swizzle(row)) * 16 + lane % 4 * 4;
     }
+  }
+  __device__ __forceinline__ Frag<RIP_FP32> row(const T* tile, int first, int s) const {
+    const char* p = (const char*)tile + first * kBytes + s / 2 * 128;
+    const f32x4 a = *(const f32x4*)(p + rows[s % 2 * 2]), b = *(const f32x4*)(p + rows[s % 2 * 2 + 1]);
+    Frag<RIP_FP32> f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.x[j] = a[j], f.x[4 + j] = b[j];
+    return f;
+  }
+  __device__ __forceinline__ Frag<RIP_FP32> column(const T* tile, int first, int c) const {
+    Frag<RIP_FP32> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      f.x[j] = *(const float*)((const char*)tile + (first + j / 4 * 8) * kBytes + columns[j % 4] + c * 128);
     return f;
   }
 };
 
+// The first n (1 .. 7) of eight elements, then zeros; the others are not read.
+template <int DT>
+__device__ __forceinline__ void load_tail(const typename Elem<DT>::T* p, int n, float (&f)[kLane]) {
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    const float x = Elem<DT>::load(p + min(j, n - 1));
+    f[j] = j < n ? x : 0.0f;
+  }
+}
+
 // Rows on their way to LDS: ROWS rows of d <= D elements, by THREADS threads, in units
-// of eight elements.
+// of eight elements.  Rows of a width that eight does not divide go straight there.
 template <int DT, int D, int ROWS, int THREADS>
 struct Stage {
   typedef typename Elem<DT>::T T;
   typedef Tile<DT, D> Tl;
-  static constexpr int kPerRow = D / kLane;
-  static constexpr int kUnits = (ROWS * kPerRow + THREADS - 1) / THREADS;
+  static constexpr int kPerRow = D / kLane, kAtOnce = THREADS / kPerRow;  // rows
+  static constexpr int kUnits = ROWS / kAtOnce;
   static constexpr int kWords = DT == RIP_BF16 ? 1 : 2;  // 16 bytes each
+  static_assert(THREADS % kPerRow == 0 && ROWS % kAtOnce == 0, "whole rows at once");
   u32x4 x[kUnits][kWords];
 
-  // Rows row .. of a sequence's `rows`; those past the end and columns past d are
-  // zeros.  `address(r)` gives row r.
-  template <typename A>
-  __device__ __forceinline__ void load(const A& address, int row, int rows, int d) {
+  // Rows row .. of the `rows` from `base` on; those past the end and columns past d
+  // are zeros.
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int row, int rows, int d) {
+    if (d % kLane) return;
+    const int r = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * kLane;
+    const T* first = base + row * ld;                 // the same in every lane
+    const uint32_t at = (uint32_t)r * (uint32_t)ld + c;
+    if (row + ROWS <= rows && d == D) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * Tl::kPiece);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int u = threadIdx.x + i * THREADS, r = row + u / kPerRow, c = u % kPerRow * kLane;
-      const bool in = (ROWS * kPerRow % THREADS == 0 || u < ROWS * kPerRow) && r < rows;
 #pragma unroll
       for (int w = 0; w < kWords; ++w) x[i][w] = u32x4{0, 0, 0, 0};
-      if (in && c + kLane <= d) {
-        const T* p = address(r) + c;
+      if (row + r + i * kAtOnce < rows && c < d) {
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) x[i][w] = *(const u32x4_any*)(p + w * Tl::kPiece);
-      } else if (in && c < d) {
-        const T* p = address(r) + c;
-        float f[kLane];
-#pragma unroll
-        for (int j = 0; j < kLane; ++j) f[j] = c + j < d ? Elem<DT>::load(p + j) : 0.0f;
-        if constexpr (DT == RIP_BF16) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[i][0][j] = Elem<DT>::pack2(f[2 * j], f[2 * j + 1]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < kLane; ++j) x[i][j / 4][j % 4] = __float_as_uint(f[j]);
-        }
+        for (int w = 0; w < kWords; ++w)
+          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * Tl::kPiece);
       }
     }
   }
-  __device__ __forceinline__ void store(T* tile) const {
+  // What load() took; the arguments are the same.
+  __device__ __forceinline__ void store(T* tile, const T* base, int64_t ld, int row, int rows, int d) const {
+    if (d % kLane) {
+#pragma unroll 1
+      for (int u = threadIdx.x; u < ROWS * kPerRow; u += THREADS) {
+        const int r = u / kPerRow, c = u % kPerRow * kLane;
+        float f[kLane] = {};
+        if (row + r < rows && c < d) {
+          const T* p = base + (row + r) * ld + c;
+          if (c + kLane <= d)
+            Elem<DT>::load8(p, f);
+          else
+            load_tail<DT>(p, d - c, f);
+        }
+#pragma unroll
+        for (int w = 0; w < kWords; ++w) {
+          u32x4 v;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            if constexpr (DT == RIP_BF16)
+              v[j] = Elem<RIP_BF16>::pack2(f[2 * j], f[2 * j + 1]);
+            else
+              v[j] = __float_as_uint(f[4 * w + j]);
+          }
+          *(u32x4*)((char*)tile + r * Tl::kBytes + ((c / Tl::kPiece + w) ^ swizzle(r)) * 16) = v;
+        }
+      }
+      return;
+    }
+    const int r = threadIdx.x / kPerRow, piece = threadIdx.x % kPerRow * (kLane / Tl::kPiece);
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
-      const int u = threadIdx.x + i * THREADS, r = u / kPerRow, c = u % kPerRow * kLane;
-      if (ROWS * kPerRow % THREADS != 0 && u >= ROWS * kPerRow) break;
+      const int row = r + i * kAtOnce;
 #pragma unroll
       for (int w = 0; w < kWords; ++w)
-        *(u32x4*)(tile + Tl::at(r, c / Tl::kPiece + w)) = x[i][w];
+        *(u32x4*)((char*)tile + row * Tl::kBytes + ((piece + w) ^ swizzle(row)) * 16) = x[i][w];
     }
   }
 };
@@ -192,9 +255,22 @@ __device__ __forceinline__ void load_row(const typename Elem<DT>::T* row, bool v
   for (int s = 0; s < D / 16; ++s) {
     float x[kLane] = {};
     const int c = 16 * s + 8 * half;
-    if (valid && c < d) load_unit<DT>(row, c, d, x);
+    if (valid && c + kLane <= d) Elem<DT>::load8(row + c, x);
     f[s].set(x);
   }
+  if (d % kLane == 0) return;
+  const int unit = d / kLane;  // the one that ends inside
+  float x[kLane] = {};
+  if (valid && half == unit % 2) load_tail<DT>(row + unit * kLane, d % kLane, x);
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s)
+    if (s == unit / 2) {
+      float y[kLane];
+      f[s].get(y);
+#pragma unroll
+      for (int j = 0; j < kLane; ++j) y[j] = half == unit % 2 ? x[j] : y[j];
+      f[s].set(y);
+    }
 }
 
 // The 4 consecutive elements that a lane holds of its row: c .. c + 3 below d.
@@ -306,13 +382,19 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// The workgroup's place among all: workgroups go to the eight XCDs in turn, and each
-// XCD, whose workgroups share an L2, takes a run of consecutive places.
-__device__ __forceinline__ uint32_t xcd_place() {
-  constexpr uint32_t kXcds = 8;
-  const uint32_t all = gridDim.x * gridDim.y, id = blockIdx.y * gridDim.x + blockIdx.x;
-  const uint32_t xcd = id % kXcds, rest = all % kXcds;
-  return xcd * (all / kXcds) + (xcd < rest ? xcd : rest) + id / kXcds;
+// A workgroup's head (of `heads`), split and slot.  Heads go fastest: workgroups go to
+// the eight XCDs, each with an L2 of its own, in turn, so that where 8 divides the
+// heads (or they divide 8) a head's rows are read by one (or few) of them; and the
+// slots with the most work, which come first, start first whatever their head.
+struct Share {
+  int head, split, slot;
+};
+__device__ __forceinline__ bool my_share(const Args& p, int heads, Share* s) {
+  const uint32_t id = blockIdx.y * gridDim.x + blockIdx.x, at = id / (uint32_t)heads;
+  s->head = id - at * heads;
+  s->slot = at / (uint32_t)p.splits;
+  s->split = at - s->slot * p.splits;
+  return s->slot < p.slots;
 }
 
 // ---------------------------------------------------------------------------
