@@ -48,18 +48,16 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(Prepare p) {
     return;
   }
   const int head = blockIdx.x - p.cleans, n = p.buckets.n;
-  float* lut = p.lut + (int64_t)head * p.lut_size;
-  for (int b = 0; b < n; ++b) {
-    const int64_t at = p.buckets.row[b] * p.ld_bias + head;
+  const int first = n > 1 ? p.buckets.start[0] - 1 : 0;
+  for (int i = threadIdx.x; i < p.lut_size; i += kThreads) {
+    int row = p.buckets.row[0];
+    for (int b = 1; b < n; ++b) row = first + i >= p.buckets.start[b - 1] ? p.buckets.row[b] : row;
+    const int64_t at = row * p.ld_bias + head;
     const float x = p.bias_bf16 ? Elem<RIP_BF16>::load((const uint16_t*)p.bias + at)
                                 : ((const float*)p.bias)[at];
-    const int first = n > 1 ? p.buckets.start[0] - 1 : 0;
-    const int from = b == 0 ? 0 : p.buckets.start[b - 1] - first;
-    const int to = b == n - 1 ? p.lut_size : p.buckets.start[b] - first;
     // masks of a type's lowest value too: the log-sum of a row of such scores would not
     // hold what tells them apart
-    const float y = x < kHides ? -__builtin_inff() : x * 1.44269504f;
-    for (int i = from + threadIdx.x; i < to; i += kThreads) lut[i] = y;
+    p.lut[(int64_t)head * p.lut_size + i] = x < kHides ? -__builtin_inff() : x * 1.44269504f;
   }
   if (head == 0 && p.buckets_out)
     for (int i = threadIdx.x; i < (int)(sizeof(Buckets) / 4); i += kThreads)

@@ -21,39 +21,43 @@ __device__ __forceinline__ float reference(float lse) {
   return lse == -kInf ? kInf : lse * kLog2e;
 }
 
-// Elements of LDS behind the bias's values: sums by distance, and a block, per wave.
-constexpr int kBlockPitch = 33;
+// Behind the bias's values in LDS: sums by distance of each wave, and a block of each.
+// A block's element of key k and query n lies in row (k - n) mod 64, column n; the
+// places that no element takes are zeros from the start.  Rows of 36 numbers: a lane's
+// writes and the reads of 16 bytes fall into different banks.
+constexpr int kBlockPitch = 36, kBlockFloats = 64 * kBlockPitch;
 __device__ __host__ constexpr int sums_size(int lut_size) { return lut_size + 2 * 62; }
 
 // Adds a block's ds (32 keys x 32 queries as the matrix instructions leave them, the
-// first at distance `rel`) to the sums by distance: through LDS, a lane to a
-// diagonal.  Only this wave touches its sums, so their order is fixed.
+// first at distance `rel`) to the sums by distance, a lane to a diagonal.  Only this
+// wave touches its sums, so their order is fixed.
 __device__ __forceinline__ void add_diagonals(const f32x16& ds, int rel, int first, float* sums,
                                               float* block, int lane) {
+  const int n = lane % 32;
 #pragma unroll
-  for (int r = 0; r < 16; ++r) block[block_row(r, lane / 32) * kBlockPitch + lane % 32] = ds[r];
+  for (int r = 0; r < 16; ++r)
+    block[((block_row(r, lane / 32) - n) & 63) * kBlockPitch + n] = ds[r];
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
   const int off = lane - 31;  // key - query within the block
-  float sum = 0.0f;
   if (lane < 63) {
+    const f32x4* row = (const f32x4*)(block + (off & 63) * kBlockPitch);
+    f32x4 sum = row[0];
 #pragma unroll
-    for (int n = 0; n < 32; ++n) {
-      const int key = n + off;
-      sum += key >= 0 && key < 32 ? block[key * kBlockPitch + n] : 0.0f;
-    }
-    sums[rel + off - first + 62] += sum;
+    for (int i = 1; i < 8; ++i) sum += row[i];
+    sums[rel + off - first + 62] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
   }
   __builtin_amdgcn_wave_barrier();
 }
 
-template <int DT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT>
+template <int NT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT>
 __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
-  typedef typename Elem<DT>::T T;
-  typedef Tile<DT, D> Tl;
+  constexpr int DT = storage(NT);
+  typedef Tile<NT, D> Tl;
+  typedef typename Tl::T T;
   constexpr int KT = STEP, KB = KT / 32, QT = kRows * WAVES;
-  __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
+  __shared__ typename Tl::template Store<KT> k_tile, v_tile;
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
@@ -67,9 +71,9 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   const int head0 = hz * p.pack, kv = head0 / p.group;
   // sums by distance of each wave, then a block of each
   const int pitch = BIAS ? sums_size(p.lut_size) : 0;
-  float* const sums = lut + p.lut_size;
+  float* const sums = lut + lut_floats(p.lut_size);
   float* const mine = sums + wave * pitch;
-  float* const block = sums + WAVES * pitch + wave * 32 * kBlockPitch;
+  float* const block = sums + WAVES * pitch + wave * kBlockFloats;
   const int intervals = BIAS ? f.buckets->n : 0;
   float* const bias_part =
       BIAS ? f.bias_part + ((int64_t)hz * p.slots * p.splits + slot * p.splits + split) * intervals
@@ -93,25 +97,26 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
     const int share = (((keys + KT - 1) / KT + p.splits - 1) / p.splits) * KT;
     t = min(keys, split * share), end = min(keys, t + share);
   }
-  Bias bias{lut, p.lut_first, p.lut_size};
+  const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
   float below = 0.0f, above = 0.0f;  // ds of blocks all in the first (last) interval
   if (BIAS) {
     load_lut(p, head0, lut);
     for (int x = lane; x < pitch; x += 64) mine[x] = 0.0f;
+    for (int x = lane; x < kBlockFloats; x += 64) block[x] = 0.0f;
   }
 
-  Frag<DT> q[D / 16], dout[D / 16];
-  load_row<DT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
-  load_row<DT, D>((const T*)f.dout.p + token * f.dout.ld + (int64_t)head * p.dim, valid, half, p.dim,
+  Frag<NT> q[D / 16], dout[D / 16];
+  load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
+  load_row<NT, D>((const T*)f.dout.p + token * f.dout.ld + (int64_t)head * p.dim, valid, half, p.dim,
                   dout);
   // delta in fp32 from out and what its rounding left
   float delta = 0.0f;
   {
     const int64_t at_head = (int64_t)head * p.dim;
-    Frag<DT> out[D / 16], low[D / 16] = {};
-    load_row<DT, D>((const T*)f.out.p + token * f.out.ld + at_head, valid, half, p.dim, out);
+    Frag<NT> out[D / 16], low[D / 16] = {};
+    load_row<NT, D>((const T*)f.out.p + token * f.out.ld + at_head, valid, half, p.dim, out);
     if (DT == RIP_BF16 && f.low.p)
-      load_row<DT, D>((const T*)f.low.p + token * f.low.ld + at_head, valid, half, p.dim, low);
+      load_row<NT, D>((const T*)f.low.p + token * f.low.ld + at_head, valid, half, p.dim, low);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) {
       float x[kLane], y[kLane], z[kLane];
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   const Tl at_lane(lane);
 
   f32x16 dq[D / 32] = {};
-  Stage<DT, D, KT, 64 * WAVES> ks, vs;
+  Stage<NT, D, KT, 64 * WAVES> ks, vs;
   if (t < end) {
     ks.load(k0, f.k.ld, t, end, p.dim);
     vs.load(v0, f.v.ld, t, end, p.dim);
@@ -147,17 +152,34 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
         f32x16 s = {}, dp = {};
+        struct Rows {
+          Frag<NT> k, v;
+        } rows[2];
+        auto read = [&](int c, Rows& r) {
+          r.k = at_lane.row(k_tile, b * 32, c);
+          r.v = at_lane.row(v_tile, b * 32, c);
+        };
+        read(0, rows[0]);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          s = mma(at_lane.row(k_tile, b * 32, c), q[c], s);
-          dp = mma(at_lane.row(v_tile, b * 32, c), dout[c], dp);
+          const Rows& r = rows[c % 2];
+          if (c + 1 < D / 16) read(c + 1, rows[(c + 1) % 2]);
+          s = mma(r.k, q[c], s);
+          dp = mma(r.v, dout[c], dp);
+          group_end();
         }
+        constexpr int kAhead = 2;  // columns on their way
+        Frag<NT> columns[kAhead];
+        auto read_column = [&](int x) {
+          columns[x % kAhead] = at_lane.column(k_tile, b * 32 + 16 * (x / (D / 32)), x % (D / 32));
+        };
+        read_column(0);
         const int key = t + b * 32;
         int side = 0;
         if (BIAS) {
           side = bias.uniform(key - __builtin_amdgcn_readlane(pos, 31),
                               key + 31 - __builtin_amdgcn_readlane(pos, 0));
-          add_bias(s, p.scale2, bias, side, [&](int r) { return key + block_row(r, half) - pos; });
+          add_bias<1>(s, p.scale2, bias, side, key + 4 * half - pos);
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -186,16 +208,22 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
           }
         }
         // ds rounded to bf16 (half a step of 2^-8, as dq is) for the product
+        Frag<NT> e[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          Frag<DT> e;
           float x[8];
 #pragma unroll
           for (int j = 0; j < 8; ++j) x[j] = s[8 * u + j];
-          e.set(x);
+          e[u].set(x);
+        }
+        read_column(1);
+        group_end();
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c)
-            dq[c] = mma(at_lane.column(k_tile, b * 32 + 16 * u, c), e, dq[c]);
+        for (int x = 0; x < 2 * (D / 32); ++x) {
+          const Frag<NT> column = columns[x % kAhead];
+          if (x + kAhead < 2 * (D / 32)) read_column(x + kAhead);
+          dq[x % (D / 32)] = mma(column, e[x / (D / 32)], dq[x % (D / 32)]);
+          group_end();
         }
       }
     }
@@ -235,8 +263,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
 #pragma unroll
         for (int s = 0; s < WAVES; ++s) sum += sums[s * pitch + x - x0];
       if (lane < WAVES) {
-        if (b == 0) sum += blocks[lane * 32 * kBlockPitch];
-        if (b == intervals - 1) sum += blocks[lane * 32 * kBlockPitch + 1];
+        if (b == 0) sum += blocks[lane * kBlockFloats];
+        if (b == intervals - 1) sum += blocks[lane * kBlockFloats + 1];
       }
 #pragma unroll
       for (int o = 32; o >= 1; o /= 2) sum += __shfl_xor(sum, o);
@@ -246,12 +274,14 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
 }
 
 // dk (DK) and dv (DV) of 32 keys to a wave.
-template <int DT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT, bool DK, bool DV>
+template <int NT, int D, int WAVES, int STEP, int EU, bool V_LDS, bool BIAS, bool SPLIT, bool DK, bool DV>
 __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
-  typedef typename Elem<DT>::T T;
-  typedef Tile<DT, D> Tl;
+  constexpr int DT = storage(NT);
+  typedef Tile<NT, D> Tl;
+  typedef typename Tl::T T;
   constexpr int QT = STEP, QB = QT / 32, KT = kRows * WAVES;
-  __shared__ __align__(128) T q_tile[QT * Tl::kPitch], do_tile[QT * Tl::kPitch];
+  __shared__ typename Tl::template Store<QT> q_tile, do_tile;
+  __shared__ typename Tl::template Store<QT> v_tile[V_LDS ? KT / QT : 1];
   __shared__ __align__(16) float refs[QT], deltas[QT];
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
@@ -279,18 +309,26 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
     const int share = (steps + p.splits - 1) / p.splits;
     n = min(steps, split * share), end = min(steps, n + share);
   }
-  Bias bias{lut, p.lut_first, p.lut_size};
+  const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
 
-  Frag<DT> k[D / 16], v[DK ? D / 16 : 1];
-  load_row<DT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
-  if constexpr (DK)
-    load_row<DT, D>((const T*)f.v.p + token * f.v.ld + (int64_t)kv * p.dim, valid, half, p.dim, v);
+  Frag<NT> k[D / 16], v[DK && !V_LDS ? D / 16 : 1];
+  load_row<NT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
+  if constexpr (DK && !V_LDS)
+    load_row<NT, D>((const T*)f.v.p + token * f.v.ld + (int64_t)kv * p.dim, valid, half, p.dim, v);
   f32x16 dk[DK ? D / 32 : 1] = {}, dv[DV ? D / 32 : 1] = {};
 
   const T* q0 = (const T*)f.q.p + at.other.begin * f.q.ld + (int64_t)kv * p.group * p.dim;
   const T* do0 = (const T*)f.dout.p + at.other.begin * f.dout.ld + (int64_t)kv * p.group * p.dim;
   const Tl at_lane(lane);
-  Stage<DT, D, QT, 64 * WAVES> qs, ds;
+  Stage<NT, D, QT, 64 * WAVES> qs, ds;
+  if constexpr (DK && V_LDS) {
+    const T* v0 = (const T*)f.v.p + at.here.begin * f.v.ld + (int64_t)kv * p.dim;
+#pragma unroll 1
+    for (int r = 0; r < KT / QT; ++r) {
+      qs.load(v0, f.v.ld, j0 + r * QT, lk, p.dim);
+      qs.store(v_tile[r], v0, f.v.ld, j0 + r * QT, lk, p.dim);
+    }
+  }
   float ref = kInf, del = 0.0f;  // of query threadIdx.x of the tile
   auto load = [&](int step) {
     const int g = step / tiles, i0 = start + (step - g * tiles) * QT;
@@ -321,17 +359,39 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
         f32x16 s = {}, dp = {};
+        struct Rows {
+          Frag<NT> q, dout, v;
+        } rows[2];
+        auto read = [&](int c, Rows& r) {
+          r.q = at_lane.row(q_tile, b * 32, c);
+          if constexpr (DK) r.dout = at_lane.row(do_tile, b * 32, c);
+          if constexpr (DK && V_LDS) r.v = at_lane.row(v_tile[wave * kRows / QT], wave * kRows % QT, c);
+        };
+        read(0, rows[0]);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          s = mma(at_lane.row(q_tile, b * 32, c), k[c], s);
-          if constexpr (DK) dp = mma(at_lane.row(do_tile, b * 32, c), v[c], dp);
+          Rows& r = rows[c % 2];
+          if (c + 1 < D / 16) read(c + 1, rows[(c + 1) % 2]);
+          s = mma(r.q, k[c], s);
+          if constexpr (DK) dp = mma(r.dout, V_LDS ? r.v : v[V_LDS ? 0 : c], dp);
+          group_end();
         }
+        // the first columns are on their way during the exponentials
+        struct Columns {
+          Frag<NT> q, dout;
+        } columns[2];
+        auto read_columns = [&](int x, Columns& r) {
+          const int u = x / (D / 32), c = x % (D / 32);
+          if constexpr (DV) r.dout = at_lane.column(do_tile, b * 32 + 16 * u, c);
+          if constexpr (DK) r.q = at_lane.column(q_tile, b * 32 + 16 * u, c);
+        };
+        read_columns(0, columns[0]);
         const int ib = i0 + b * 32;
         if (BIAS)
-          add_bias(s, p.scale2, bias,
-                   bias.uniform(__builtin_amdgcn_readlane(j, 0) - (ib + 31 + shift),
-                                __builtin_amdgcn_readlane(j, 31) - (ib + shift)),
-                   [&](int r) { return j - (ib + block_row(r, half) + shift); });
+          add_bias<-1>(s, p.scale2, bias,
+                       bias.uniform(__builtin_amdgcn_readlane(j, 0) - (ib + 31 + shift),
+                                    __builtin_amdgcn_readlane(j, 31) - (ib + shift)),
+                       j - (ib + 4 * half + shift));
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
           const f32x4 ref4 = *(const f32x4*)&refs[b * 32 + block_row(r, half)];
@@ -354,19 +414,24 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
           }
         }
         // p and ds rounded to bf16 (half a step of 2^-8, as dv and dk are)
+        Frag<NT> e[2], de[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          Frag<DT> e, de;
           float x[8], y[8];
 #pragma unroll
           for (int z = 0; z < 8; ++z) x[z] = s[8 * u + z], y[z] = dp[8 * u + z];
-          e.set(x);
-          de.set(y);
+          e[u].set(x);
+          de[u].set(y);
+        }
+        group_end();
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            if constexpr (DV) dv[c] = mma(at_lane.column(do_tile, b * 32 + 16 * u, c), e, dv[c]);
-            if constexpr (DK) dk[c] = mma(at_lane.column(q_tile, b * 32 + 16 * u, c), de, dk[c]);
-          }
+        for (int x = 0; x < 2 * (D / 32); ++x) {
+          const int u = x / (D / 32), c = x % (D / 32);
+          const Columns& r = columns[x % 2];
+          if (x + 1 < 2 * (D / 32)) read_columns(x + 1, columns[(x + 1) % 2]);
+          if constexpr (DV) dv[c] = mma(r.dout, e[u], dv[c]);
+          if constexpr (DK) dk[c] = mma(r.q, de[u], dk[c]);
+          group_end();
         }
       }
     }
@@ -435,35 +500,29 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buck
   Elem<DT>::store(g, accumulate ? Elem<DT>::load(g) + sum : sum);
 }
 
-// Variants: waves of a workgroup, rows of a tile of the other axis, waves to a SIMD
-// that the registers have to leave room for.
-template <int DT, int D>
-struct Shape {
-  static constexpr int kDqWaves = dq_waves(DT == RIP_BF16, D), kDkvWaves = dkv_waves(DT == RIP_BF16, D);
-  static constexpr int kDqStep = DT == RIP_BF16 && D <= 64 ? 64 : 32;
-  static constexpr int kDkvStep = kDqStep;
-  static constexpr int kDqUnits = DT == RIP_BF16 && D <= 128 ? 2 : 1;
-  static constexpr int kDkvUnits = DT == RIP_BF16 && D == 128 ? 2 : 1;
-};
-template <int DT, int D, bool BIAS, bool SPLIT>
+// Variants: rows of a tile of the other axis, and waves to a SIMD that the registers
+// have to leave room for.
+template <int NT, int D, bool BIAS, bool SPLIT>
 const void* dq_of() {
-  typedef Shape<DT, D> S;
-  return (const void*)dq_kernel<DT, D, S::kDqWaves, S::kDqStep, S::kDqUnits, BIAS, SPLIT>;
+  constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
+  constexpr int step = wide ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
+  return (const void*)dq_kernel<NT, D, dq_waves(NT == kBf16, D), step, units, BIAS, SPLIT>;
 }
-template <int DT, int D>
+template <int NT, int D>
 const void* dq_of(bool bias, bool split) {
-  return bias ? (split ? dq_of<DT, D, true, true>() : dq_of<DT, D, true, false>())
-              : (split ? dq_of<DT, D, false, true>() : dq_of<DT, D, false, false>());
+  return bias ? (split ? dq_of<NT, D, true, true>() : dq_of<NT, D, true, false>())
+              : (split ? dq_of<NT, D, false, true>() : dq_of<NT, D, false, false>());
 }
-template <int DT, int D, bool BIAS, bool SPLIT, bool DK, bool DV>
+template <int NT, int D, int WAVES, bool BIAS, bool SPLIT, bool DK, bool DV>
 const void* dkv_of() {
-  typedef Shape<DT, D> S;
-  return (const void*)dkv_kernel<DT, D, S::kDkvWaves, S::kDkvStep, S::kDkvUnits, BIAS, SPLIT, DK, DV>;
+  constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
+  constexpr int step = NT == kBf16 && D <= 64 ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
+  return (const void*)dkv_kernel<NT, D, WAVES, step, units, wide, BIAS, SPLIT, DK, DV>;
 }
-template <int DT, int D, bool DK, bool DV>
+template <int NT, int D, int WAVES, bool DK = true, bool DV = true>
 const void* dkv_of(bool bias, bool split) {
-  return bias ? (split ? dkv_of<DT, D, true, true, DK, DV>() : dkv_of<DT, D, true, false, DK, DV>())
-              : (split ? dkv_of<DT, D, false, true, DK, DV>() : dkv_of<DT, D, false, false, DK, DV>());
+  return bias ? (split ? dkv_of<NT, D, WAVES, true, true, DK, DV>() : dkv_of<NT, D, WAVES, true, false, DK, DV>())
+              : (split ? dkv_of<NT, D, WAVES, false, true, DK, DV>() : dkv_of<NT, D, WAVES, false, false, DK, DV>());
 }
 template <int DT>
 int32_t add(const float* part, int splits, int64_t tokens, int width, Heads to, void* stream) {
@@ -480,11 +539,13 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& pl
   {
     f.a = over_q;
     const bool split = f.a.splits > 1;
-    const void* fn = width == 64    ? dq_of<DT, 64>(bias, split)
-                     : width == 128 ? dq_of<DT, 128>(bias, split)
-                                    : dq_of<DT, 256>(bias, split);
+    constexpr int NT = DT == RIP_BF16 ? kBf16 : kSplit, kWide = DT == RIP_BF16 ? kBf16 : kFp32;
+    const void* fn = width == 64    ? dq_of<NT, 64>(bias, split)
+                     : width == 96  ? dq_of<NT, 96>(bias, split)
+                     : width == 128 ? dq_of<NT, 128>(bias, split)
+                                    : dq_of<kWide, 256>(bias, split);
     const size_t lds =
-        bias ? 4 * (f.a.lut_size + plan.q.waves * (sums_size(f.a.lut_size) + 32 * kBlockPitch)) : 0;
+        bias ? 4 * (lut_floats(f.a.lut_size) + plan.q.waves * (sums_size(f.a.lut_size) + kBlockFloats)) : 0;
     void* args[] = {&f};
     if ((rc = launch(fn, grid_of(f.a, f.a.heads / f.a.pack), dim3(64 * plan.q.waves), args, lds, stream, "rip_attn_backward: queries")))
       return rc;
@@ -495,20 +556,27 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& pl
   const int kv_heads = f.a.heads / f.a.group;
   const bool split = f.a.splits > 1;
   const dim3 grid = grid_of(f.a, kv_heads);
-  const size_t lds = bias ? 4 * f.a.lut_size : 0;
+  const size_t lds = bias ? 4 * lut_floats(f.a.lut_size) : 0;
   void* args[] = {&f};
   const char* what = "rip_attn_backward: keys";
-  if (DT == RIP_FP32 && width == 256) {
+  if (width == 256) {
     // dk and dv with the operands of both do not fit the registers: one after the other
-    if ((rc = launch(dkv_of<RIP_FP32, 256, false, true>(bias, split), grid, dim3(64 * plan.k.waves), args, lds,
-                     stream, what)) ||
-        (rc = launch(dkv_of<RIP_FP32, 256, true, false>(bias, split), grid, dim3(64 * plan.k.waves), args, lds,
-                     stream, what)))
+    constexpr int kWide = DT == RIP_BF16 ? kBf16 : kFp32;
+    if ((rc = launch(dkv_of<kWide, 256, 4, false, true>(bias, split), grid, dim3(64 * plan.k.waves), args,
+                     lds, stream, what)) ||
+        (rc = launch(dkv_of<kWide, 256, 4, true, false>(bias, split), grid, dim3(64 * plan.k.waves), args,
+                     lds, stream, what)))
       return rc;
   } else {
-    const void* fn = width == 64    ? dkv_of<DT, 64, true, true>(bias, split)
-                     : width == 128 ? dkv_of<DT, 128, true, true>(bias, split)
-                                    : dkv_of<RIP_BF16, 256, true, true>(bias, split);
+    const void* fn;
+    if constexpr (DT == RIP_BF16)
+      fn = width == 64 ? (plan.k.waves == 4 ? dkv_of<kBf16, 64, 4>(bias, split) : dkv_of<kBf16, 64, 8>(bias, split))
+           : width == 96 ? dkv_of<kBf16, 96, 8>(bias, split)
+                         : dkv_of<kBf16, 128, 8>(bias, split);
+    else
+      fn = width == 64   ? dkv_of<kSplit, 64, 4>(bias, split)
+           : width == 96 ? dkv_of<kSplit, 96, 4>(bias, split)
+                         : dkv_of<kSplit, 128, 4>(bias, split);
     if ((rc = launch(fn, grid, dim3(64 * plan.k.waves), args, lds, stream, what))) return rc;
   }
   if (!split) return RIP_OK;

@@ -15,8 +15,8 @@ namespace attn {
 namespace {
 
 // Keys of a tile.  A wave by itself holds a whole tile on its way in its registers.
-template <int DT, int D, int WAVES>
-constexpr int kKeys = DT == RIP_BF16 && D <= 128 && (WAVES > 1 || D <= 64) ? 64 : 32;
+template <int NT, int D, int WAVES>
+constexpr int kKeys = NT == kBf16 && D <= 128 && (WAVES > 1 || D <= 64) ? 64 : 32;
 
 // Without a bias, with one, and with one whose gradient will be wanted: that sums ds
 // in fp32, and its row sums delta come from out, which must not hold the rounding of
@@ -25,14 +25,15 @@ enum { kPlain, kBias, kExact };
 
 constexpr float kSlack = 6.0f;  // growth of a maximum (log2) that needs no rescaling
 
-template <int DT, int D, int WAVES, int MODE, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) void forward_kernel(
+template <int NT, int D, int WAVES, int MODE, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, NT == kBf16 && D <= 128 ? 2 : 1) void forward_kernel(
     Forward f) {
-  typedef typename Elem<DT>::T T;
-  typedef Tile<DT, D> Tl;
-  constexpr int KT = kKeys<DT, D, WAVES>, KB = KT / 32, QT = kRows * WAVES;
+  constexpr int DT = storage(NT);
+  typedef Tile<NT, D> Tl;
+  typedef typename Tl::T T;
+  constexpr int KT = kKeys<NT, D, WAVES>, KB = KT / 32, QT = kRows * WAVES;
   constexpr bool BIAS = MODE != kPlain, EXACT = MODE == kExact;
-  __shared__ __align__(128) T k_tile[KT * Tl::kPitch], v_tile[KT * Tl::kPitch];
+  __shared__ typename Tl::template Store<KT> k_tile, v_tile;
   extern __shared__ __align__(16) float lut[];
   const Args& p = f.a;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, half = lane / 32;
@@ -60,18 +61,18 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
     const int share = (((keys + KT - 1) / KT + p.splits - 1) / p.splits) * KT;
     t = min(keys, split * share), end = min(keys, t + share);
   }
-  Bias bias{lut, p.lut_first, p.lut_size};
+  const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
   if (BIAS) load_lut(p, head0, lut);
 
-  Frag<DT> q[D / 16];
-  load_row<DT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
+  Frag<NT> q[D / 16];
+  load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
   const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
   const Tl at_lane(lane);
 
   f32x16 o[D / 32] = {};
   float m = -kInf, l = 0.0f;  // reference (log2); the sum of this half's keys
-  Stage<DT, D, KT, 64 * WAVES> ks, vs;
+  Stage<NT, D, KT, 64 * WAVES> ks, vs;
   if (t < end) {
     ks.load(k0, f.k.ld, t, end, p.dim);
     vs.load(v0, f.v.ld, t, end, p.dim);
@@ -86,18 +87,32 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
     }
     if (wq < rows && t < most) {
       f32x16 s[KB] = {};
+      Frag<NT> rows[2][KB];
+      auto read = [&](int c) {
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c)
+        for (int b = 0; b < KB; ++b) rows[c % 2][b] = at_lane.row(k_tile, b * 32, c);
+      };
+      read(0);
 #pragma unroll
-        for (int b = 0; b < KB; ++b)
-          s[b] = mma(at_lane.row(k_tile, b * 32, c), q[c], s[b]);
+      for (int c = 0; c < D / 16; ++c) {
+        if (c + 1 < D / 16) read(c + 1);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) s[b] = mma(rows[c % 2][b], q[c], s[b]);
+        group_end();
+      }
+      constexpr int kAhead = 2, kColumns = KB * 2 * (D / 32);  // columns on their way; all
+      Frag<NT> columns[kAhead];
+      auto read_column = [&](int x) {
+        columns[x % kAhead] = at_lane.column(v_tile, 16 * (x / (D / 32)), x % (D / 32));
+      };
+      read_column(0);
       if (BIAS) {
         const int first = __builtin_amdgcn_readlane(pos, 0), last = __builtin_amdgcn_readlane(pos, 31);
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
           const int key = t + b * 32;
-          add_bias(s[b], p.scale2, bias, bias.uniform(key - last, key + 31 - first),
-                   [&](int r) { return key + block_row(r, half) - pos; });
+          add_bias<1>(s[b], p.scale2, bias, bias.uniform(key - last, key + 31 - first),
+                      key + 4 * half - pos);
         }
       }
       if (t + KT > least || t + KT > end) {
@@ -134,30 +149,32 @@ __global__ __launch_bounds__(64 * WAVES, DT == RIP_BF16 && D <= 128 ? 2 : 1) voi
         }
       // e^x rounded to bf16 (half a step of 2^-8, as out is; their sum is not) so that
       // the product runs at bf16's rate
+      Frag<NT> e[KB * 2], rest[EXACT ? KB * 2 : 1];
 #pragma unroll
-      for (int b = 0; b < KB; ++b)
+      for (int u = 0; u < KB * 2; ++u) {
+        float x[8];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Frag<DT> e;
-          float x[8];
+        for (int j = 0; j < 8; ++j) x[j] = s[u / 2][8 * (u % 2) + j];
+        e[u].set(x);
+        if constexpr (EXACT) {
+          float y[8];
+          e[u].get(y);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = s[b][8 * u + j];
-          e.set(x);
-          Frag<DT> rest;
-          if constexpr (EXACT) {
-            float y[8];
-            e.get(y);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] -= y[j];
-            rest.set(x);
-          }
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            const Frag<DT> v = at_lane.column(v_tile, b * 32 + 16 * u, c);
-            o[c] = mma(v, e, o[c]);
-            if constexpr (EXACT) o[c] = mma(v, rest, o[c]);
-          }
+          for (int j = 0; j < 8; ++j) x[j] -= y[j];
+          rest[u].set(x);
         }
+      }
+      read_column(1);
+      group_end();
+#pragma unroll
+      for (int x = 0; x < kColumns; ++x) {
+        const int u = x / (D / 32), c = x % (D / 32);
+        const Frag<NT> v = columns[x % kAhead];
+        if (x + kAhead < kColumns) read_column(x + kAhead);
+        o[c] = mma(v, e[u], o[c]);
+        if constexpr (EXACT) o[c] = mma(v, rest[u], o[c]);
+        group_end();
+      }
     }
     lds_barrier();
   }
@@ -230,7 +247,6 @@ __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   constexpr int kColumns = RIP_MAX_HEAD_DIM / 64;
   float x[kColumns] = {};
   const float* from = f.part + row * p.dim + lane;
-#pragma unroll 4
   for (int s = wave; s < p.splits; s += 4) {
     const float w = __shfl(weight, s);
 #pragma unroll
@@ -253,23 +269,27 @@ __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   if (f.lse && c == 0) f.lse[row] = l == 0.0f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int DT, int D, int WAVES, int MODE>
+template <int NT, int D, int WAVES, int MODE>
 const void* variant(bool split) {
-  return split ? (const void*)forward_kernel<DT, D, WAVES, MODE, true>
-               : (const void*)forward_kernel<DT, D, WAVES, MODE, false>;
+  return split ? (const void*)forward_kernel<NT, D, WAVES, MODE, true>
+               : (const void*)forward_kernel<NT, D, WAVES, MODE, false>;
 }
-template <int DT, int D, int WAVES>
+template <int NT, int D, int WAVES>
 const void* variant(int mode, bool split) {
-  if (DT == RIP_BF16 && mode == kExact) return variant<RIP_BF16, D, WAVES, kExact>(split);
-  return mode == kPlain ? variant<DT, D, WAVES, kPlain>(split) : variant<DT, D, WAVES, kBias>(split);
+  if (NT == kBf16 && mode == kExact) return variant<kBf16, D, WAVES, kExact>(split);
+  return mode == kPlain ? variant<NT, D, WAVES, kPlain>(split) : variant<NT, D, WAVES, kBias>(split);
 }
-template <int DT>
-const void* kernel_of(int width, int waves, int mode, bool split) {
-  const bool one = waves == 1;
+template <int NT, int D>
+const void* variant(int waves, int mode, bool split) {
+  return waves == 1 ? variant<NT, D, 1>(mode, split) : variant<NT, D, 4>(mode, split);
+}
+const void* kernel_of(int32_t dtype, int width, int waves, int mode, bool split) {
+  const bool bf16 = dtype == RIP_BF16;
   switch (width) {
-    case 64: return one ? variant<DT, 64, 1>(mode, split) : variant<DT, 64, 4>(mode, split);
-    case 128: return one ? variant<DT, 128, 1>(mode, split) : variant<DT, 128, 4>(mode, split);
-    default: return one ? variant<DT, 256, 1>(mode, split) : variant<DT, 256, 4>(mode, split);
+    case 64: return bf16 ? variant<kBf16, 64>(waves, mode, split) : variant<kSplit, 64>(waves, mode, split);
+    case 96: return bf16 ? variant<kBf16, 96>(waves, mode, split) : variant<kSplit, 96>(waves, mode, split);
+    case 128: return bf16 ? variant<kBf16, 128>(waves, mode, split) : variant<kSplit, 128>(waves, mode, split);
+    default: return bf16 ? variant<kBf16, 256>(waves, mode, split) : variant<kFp32, 256>(waves, mode, split);
   }
 }
 
@@ -280,9 +300,8 @@ int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* strea
   void* args[] = {&f};
   const bool split = p.splits > 1;
   const int mode = !p.lut ? kPlain : f.low.p ? kExact : kBias;
-  const void* fn = dtype == RIP_BF16 ? kernel_of<RIP_BF16>(width, waves, mode, split)
-                                     : kernel_of<RIP_FP32>(width, waves, mode, split);
-  int32_t rc = launch(fn, grid_of(p, p.heads / p.pack), dim3(64 * waves), args, p.lut ? p.lut_size * 4 : 0, stream, "rip_attn_forward");
+  const void* fn = kernel_of(dtype, width, waves, mode, split);
+  int32_t rc = launch(fn, grid_of(p, p.heads / p.pack), dim3(64 * waves), args, p.lut ? 4 * lut_floats(p.lut_size) : 0, stream, "rip_attn_forward");
   if (rc || !split) return rc;
   return launch(dtype == RIP_BF16 ? (const void*)join_kernel<RIP_BF16> : (const void*)join_kernel<RIP_FP32>,
                 dim3((uint32_t)(p.heads * p.q.tokens)), dim3(256), args, 0, stream,

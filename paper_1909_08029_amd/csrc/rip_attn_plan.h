@@ -14,8 +14,8 @@ constexpr int kRows = 32;         // queries (or keys) of a wave
 constexpr int kMaxSplits = 64;
 constexpr int kScan = 1024;       // offsets that every workgroup puts in order by itself
 
-constexpr int kWidths = 3;
-constexpr int kWidth[kWidths] = {64, 128, 256};  // of a head, padded with zeros
+constexpr int kWidths = 4;
+constexpr int kWidth[kWidths] = {64, 96, 128, 256};  // of a head, padded with zeros
 inline int width_of(int dim) {
   for (int i = 0; i < kWidths; ++i)
     if (dim <= kWidth[i]) return kWidth[i];
@@ -46,12 +46,13 @@ constexpr Kernel kForward = {2, 0.12}, kDq = {3, 0.16}, kDkv = {4, 0.2};
 // them where causal) in `splits` parts, from the time of a block on a SIMD (1024 of
 // them, shared by `resident` waves): what all SIMDs have to do, or one tile's chain,
 // whichever is longer; then the parts' way through memory and the launch that adds
-// them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us (bf16; 8192
-// clocks for 128 columns and four in fp32) a column each with two waves to a SIMD, half as
-// long again alone; a tile costs about four us before its first block.
+// them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us a
+// column each in bf16 with two waves to a SIMD (six times that for fp32 as three parts,
+// sixteen times for fp32's own instructions), half as long again alone; a tile costs
+// about four us before its first block.
 inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int64_t axis,
                       int splits, double part) {
-  const double product = (s.bf16 ? 0.0021 : 0.0134) * width, block = k.products * product + k.softmax;
+  const double product = (s.bf16 ? 0.0021 : width <= 128 ? 0.0126 : 0.0336) * width, block = k.products * product + k.softmax;
   const double alone = (s.bf16 ? 1.5 : 1.0) * block * (waves == 1 ? 1.25 : 1.0);
   const double blocks = (double)ceil_div(axis, kRows);
   const double all = (double)units * waves * (blocks * (s.causal ? 0.5 : 1.0) * block + 2.0 * splits) / 1024;
@@ -99,18 +100,24 @@ inline Plan over_keys(const Sizes& s, int waves) {
   return best;
 }
 
-// Waves of a workgroup.
+// Waves of a workgroup.  Narrow heads take eight over the keys where sequences are long
+// (8192 tokens, 16 heads of 64, causal: 608 us for the backward pass, 739 with four) and
+// four where they are short (32 sequences: 115 and 105).
 inline Plan plan_forward(const Sizes& s) {
   constexpr int waves[] = {4, 1};
   return over_queries(s, kForward, waves, 2);
 }
-constexpr int dq_waves(bool bf16, int width) { return bf16 && width == 128 ? 8 : 4; }
-constexpr int dkv_waves(bool bf16, int width) { return bf16 && width == 128 ? 8 : 4; }
+constexpr int dq_waves(bool bf16, int width) { return bf16 && width > 64 && width <= 128 ? 8 : 4; }
+inline int dkv_waves(bool bf16, int width, int64_t keys) {
+  return bf16 && (width == 64 ? keys >= 512 : width <= 128) ? 8 : 4;
+}
 inline Plan plan_dq(const Sizes& s) {
   const int waves[] = {dq_waves(s.bf16, width_of(s.dim))};
   return over_queries(s, kDq, waves, 1);
 }
-inline Plan plan_dkv(const Sizes& s) { return over_keys(s, dkv_waves(s.bf16, width_of(s.dim))); }
+inline Plan plan_dkv(const Sizes& s) {
+  return over_keys(s, dkv_waves(s.bf16, width_of(s.dim), ceil_div(s.k_tokens, std::max(1, s.n))));
+}
 
 }  // namespace attn
 }  // namespace rip

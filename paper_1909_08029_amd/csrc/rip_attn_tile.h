@@ -28,11 +28,18 @@ constexpr float kInf = __builtin_inff();
 
 __device__ __forceinline__ int block_row(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
 
+// How numbers enter the matrix instructions: bf16 as they are; fp32 as three bf16
+// numbers whose sum they are (24 bits = 8 + 8 + 8), with the six products of parts that
+// reach fp32's last bit, at six times the cost of bf16; or, where those do not fit the
+// registers, fp32's own instructions, at sixteen times.
+enum { kBf16 = RIP_BF16, kSplit = 2, kFp32 = 3 };
+constexpr int storage(int number) { return number == kBf16 ? RIP_BF16 : RIP_FP32; }
+
 // Eight operands of a lane, and a product of 16 steps of the summed axis.
-template <int DT>
+template <int NT>
 struct Frag;
 template <>
-struct Frag<RIP_BF16> {
+struct Frag<kBf16> {
   bf16x8 x;
   __device__ __forceinline__ void set(u32x4 v) { x = __builtin_bit_cast(bf16x8, v); }
   __device__ __forceinline__ void set(const float (&f)[8]) {
@@ -44,9 +51,53 @@ struct Frag<RIP_BF16> {
   __device__ __forceinline__ void get(float (&f)[8]) const {
     Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x), f);
   }
+  __device__ __forceinline__ void load(const uint16_t* p) { set(*(const u32x4_any*)p); }
 };
 template <>
-struct Frag<RIP_FP32> {
+struct Frag<kSplit> {
+  bf16x8 x[3];
+  // The leading eight bits, cut (so that nothing rounds to an infinity), the next eight
+  // rounded, and the rest, which is exact.  An infinity is its first part alone.
+  static __device__ __forceinline__ void cut(const float (&f)[8], u32x4 (&part)[3]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float r[2];
+      uint32_t lead[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        lead[h] = __float_as_uint(f[2 * j + h]);
+        r[h] = f[2 * j + h] - __uint_as_float(lead[h] & 0xffff0000u);
+        r[h] = __builtin_isinf(f[2 * j + h]) ? 0.0f : r[h];
+      }
+      part[0][j] = __builtin_amdgcn_perm(lead[1], lead[0], 0x07060302u);
+      const uint32_t next = Elem<RIP_BF16>::pack2(r[0], r[1]);
+      part[1][j] = next;
+      part[2][j] = Elem<RIP_BF16>::pack2(r[0] - __uint_as_float(next << 16),
+                                         r[1] - __uint_as_float(next & 0xffff0000u));
+    }
+  }
+  __device__ __forceinline__ void set(const float (&f)[8]) {
+    u32x4 part[3];
+    cut(f, part);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) x[i] = __builtin_bit_cast(bf16x8, part[i]);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    float a[8], b[8];
+    Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x[0]), f);
+    Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x[1]), a);
+    Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x[2]), b);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] += a[j] + b[j];
+  }
+  __device__ __forceinline__ void load(const float* p) {
+    float f[8];
+    Elem<RIP_FP32>::load8(p, f);
+    set(f);
+  }
+};
+template <>
+struct Frag<kFp32> {
   float x[8];
   __device__ __forceinline__ void set(const float (&f)[8]) {
 #pragma unroll
@@ -56,12 +107,22 @@ struct Frag<RIP_FP32> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = x[j];
   }
+  __device__ __forceinline__ void load(const float* p) { Elem<RIP_FP32>::load8(p, x); }
 };
-__device__ __forceinline__ f32x16 mma(const Frag<RIP_BF16>& a, const Frag<RIP_BF16>& b, f32x16 c) {
+__device__ __forceinline__ f32x16 mma(const Frag<kBf16>& a, const Frag<kBf16>& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
 }
-// fp32: eight instructions of two steps each; the order of the summed axis is free.
-__device__ __forceinline__ f32x16 mma(const Frag<RIP_FP32>& a, const Frag<RIP_FP32>& b, f32x16 c) {
+// The smallest products first.
+__device__ __forceinline__ f32x16 mma(const Frag<kSplit>& a, const Frag<kSplit>& b, f32x16 c) {
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[0], b.x[2], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[1], b.x[1], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[2], b.x[0], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[0], b.x[1], c, 0, 0, 0);
+  c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[1], b.x[0], c, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x[0], b.x[0], c, 0, 0, 0);
+}
+// Eight instructions of two steps each; the order of the summed axis is free.
+__device__ __forceinline__ f32x16 mma(const Frag<kFp32>& a, const Frag<kFp32>& b, f32x16 c) {
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[j], b.x[j], c, 0, 0, 0);
@@ -88,14 +149,19 @@ __device__ __forceinline__ int swizzle(int row) { return (row & 3) << 1 | (row >
 // Swizzles change the lowest three bits of a piece's number alone, and those of a
 // lane's rows are the same in every block, so few addresses (bytes) serve all blocks:
 // the rest of an address is known when the code is compiled.
-template <int DT, int D>
+// A Tile is what the kernels hold in LDS: ROWS rows of D numbers.
+constexpr int pitch_of(int d, int bytes) { return (d * bytes + 127) / 128 * 128; }
+
+template <int NT, int D>
 struct Tile;
 template <int D>
-struct Tile<RIP_BF16, D> {
+struct Tile<kBf16, D> {
   typedef uint16_t T;
-  static constexpr int kPiece = 8;                    // elements of 16 bytes
-  static constexpr int kPitch = D < 64 ? 64 : D;
-  static constexpr int kBytes = kPitch * 2;
+  static constexpr int kBytes = pitch_of(D, 2);   // of a row
+  template <int ROWS>
+  struct Store {
+    __align__(128) char x[ROWS * kBytes];
+  };
   uint32_t rows[4], columns[2];
   __device__ __forceinline__ explicit Tile(int lane) {
     const int r = lane % 32, half = lane / 32;
@@ -107,29 +173,80 @@ struct Tile<RIP_BF16, D> {
     for (int c = 0; c < 2; ++c)
       columns[c] = row * kBytes + ((4 * c + group % 2 * 2 + in % 4 / 2) ^ swizzle(row)) * 16 + in % 2 * 8;
   }
+  __device__ __forceinline__ u32x4 row_piece(const char* tile, int first, int s) const {
+    return *(const u32x4*)(tile + first * kBytes + rows[s % 4] + s / 4 * 128);
+  }
+  __device__ __forceinline__ u32x4 column_piece(const char* tile, int first, int c) const {
+    const char* p = tile + first * kBytes + columns[c % 2] + c / 2 * 128;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kBytes));
+    return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
   // Operand of row `first` + lane % 32, elements 16 s + 8 half .. (first: of 32)
-  __device__ __forceinline__ Frag<RIP_BF16> row(const T* tile, int first, int s) const {
-    Frag<RIP_BF16> f;
-    f.set(*(const u32x4*)((const char*)tile + first * kBytes + rows[s % 4] + s / 4 * 128));
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kBf16> row(const Store<ROWS>& tile, int first, int s) const {
+    Frag<kBf16> f;
+    f.set(row_piece(tile.x, first, s));
     return f;
   }
   // Operand of column 32 c + lane % 32 over the 16 rows from `first` (a multiple of
   // 16), in block_row's order: rows first + 4 half .. + 3, then those 8 further.
-  __device__ __forceinline__ Frag<RIP_BF16> column(const T* tile, int first, int c) const {
-    const char* p = (const char*)tile + first * kBytes + columns[c % 2] + c / 2 * 128;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kBytes));
-    Frag<RIP_BF16> f;
-    f.set(__builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7)));
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kBf16> column(const Store<ROWS>& tile, int first, int c) const {
+    Frag<kBf16> f;
+    f.set(column_piece(tile.x, first, c));
     return f;
+  }
+  template <int ROWS>  // eight elements of a row from column 8 `unit` on
+  static __device__ __forceinline__ void put(Store<ROWS>& tile, int row, int unit, const u32x4 (&x)[1]) {
+    *(u32x4*)(tile.x + row * kBytes + (unit ^ swizzle(row)) * 16) = x[0];
   }
 };
 template <int D>
-struct Tile<RIP_FP32, D> {
+struct Tile<kSplit, D> {
   typedef float T;
-  static constexpr int kPiece = 4;
-  static constexpr int kPitch = D < 32 ? 32 : D;
-  static constexpr int kBytes = kPitch * 4;
+  typedef Tile<kBf16, D> Part;
+  template <int ROWS>
+  struct Store {
+    typename Part::template Store<ROWS> part[3];
+  };
+  Part at;
+  __device__ __forceinline__ explicit Tile(int lane) : at(lane) {}
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kSplit> row(const Store<ROWS>& tile, int first, int s) const {
+    Frag<kSplit> f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) f.x[i] = __builtin_bit_cast(bf16x8, at.row_piece(tile.part[i].x, first, s));
+    return f;
+  }
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kSplit> column(const Store<ROWS>& tile, int first, int c) const {
+    Frag<kSplit> f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      f.x[i] = __builtin_bit_cast(bf16x8, at.column_piece(tile.part[i].x, first, c));
+    return f;
+  }
+  template <int ROWS>
+  static __device__ __forceinline__ void put(Store<ROWS>& tile, int row, int unit, const u32x4 (&x)[2]) {
+    float f[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(x[j / 4][j % 4]);
+    u32x4 part[3];
+    Frag<kSplit>::cut(f, part);
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      *(u32x4*)(tile.part[i].x + row * Part::kBytes + (unit ^ swizzle(row)) * 16) = part[i];
+  }
+};
+template <int D>
+struct Tile<kFp32, D> {
+  typedef float T;
+  static constexpr int kBytes = pitch_of(D, 4);
+  template <int ROWS>
+  struct Store {
+    __align__(128) char x[ROWS * kBytes];
+  };
   uint32_t rows[4], columns[4];
   __device__ __forceinline__ explicit Tile(int lane) {
     const int r = lane % 32, half = lane / 32;
@@ -142,20 +259,28 @@ struct Tile<RIP_FP32, D> {
       columns[j] = row * kBytes + (lane % 32 / 4 ^ swizzle(row)) * 16 + lane % 4 * 4;
     }
   }
-  __device__ __forceinline__ Frag<RIP_FP32> row(const T* tile, int first, int s) const {
-    const char* p = (const char*)tile + first * kBytes + s / 2 * 128;
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kFp32> row(const Store<ROWS>& tile, int first, int s) const {
+    const char* p = tile.x + first * kBytes + s / 2 * 128;
     const f32x4 a = *(const f32x4*)(p + rows[s % 2 * 2]), b = *(const f32x4*)(p + rows[s % 2 * 2 + 1]);
-    Frag<RIP_FP32> f;
+    Frag<kFp32> f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) f.x[j] = a[j], f.x[4 + j] = b[j];
     return f;
   }
-  __device__ __forceinline__ Frag<RIP_FP32> column(const T* tile, int first, int c) const {
-    Frag<RIP_FP32> f;
+  template <int ROWS>
+  __device__ __forceinline__ Frag<kFp32> column(const Store<ROWS>& tile, int first, int c) const {
+    Frag<kFp32> f;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      f.x[j] = *(const float*)((const char*)tile + (first + j / 4 * 8) * kBytes + columns[j % 4] + c * 128);
+      f.x[j] = *(const float*)(tile.x + (first + j / 4 * 8) * kBytes + columns[j % 4] + c * 128);
     return f;
+  }
+  template <int ROWS>
+  static __device__ __forceinline__ void put(Store<ROWS>& tile, int row, int unit, const u32x4 (&x)[2]) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+      *(u32x4*)(tile.x + row * kBytes + ((2 * unit + w) ^ swizzle(row)) * 16) = x[w];
   }
 };
 
@@ -171,13 +296,19 @@ __device__ __forceinline__ void load_tail(const typename Elem<DT>::T* p, int n, 
 
 // Rows on their way to LDS: ROWS rows of d <= D elements, by THREADS threads, in units
 // of eight elements.  Rows of a width that eight does not divide go straight there.
-template <int DT, int D, int ROWS, int THREADS>
+constexpr int two_power(int n) { return n <= 1 ? 1 : 2 * two_power((n + 1) / 2); }
+
+template <int NT, int D, int ROWS, int THREADS>
 struct Stage {
-  typedef typename Elem<DT>::T T;
-  typedef Tile<DT, D> Tl;
-  static constexpr int kPerRow = D / kLane, kAtOnce = THREADS / kPerRow;  // rows
+  typedef Tile<NT, D> Tl;
+  typedef typename Tl::T T;
+  typedef typename Tl::template Store<ROWS> Store;
+  static constexpr int DT = storage(NT);
+  static constexpr int kPerRow = two_power(D / kLane);   // threads
+  static constexpr int kAtOnce = THREADS / kPerRow;      // rows
   static constexpr int kUnits = ROWS / kAtOnce;
   static constexpr int kWords = DT == RIP_BF16 ? 1 : 2;  // 16 bytes each
+  static constexpr int kPiece = 16 / (int)sizeof(T);
   static_assert(THREADS % kPerRow == 0 && ROWS % kAtOnce == 0, "whole rows at once");
   u32x4 x[kUnits][kWords];
 
@@ -188,12 +319,12 @@ struct Stage {
     const int r = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * kLane;
     const T* first = base + row * ld;                 // the same in every lane
     const uint32_t at = (uint32_t)r * (uint32_t)ld + c;
-    if (row + ROWS <= rows && d == D) {
+    if (row + ROWS <= rows && d == kPerRow * kLane) {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i)
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
-          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * Tl::kPiece);
+          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * kPiece);
       return;
     }
 #pragma unroll
@@ -203,74 +334,65 @@ struct Stage {
       if (row + r + i * kAtOnce < rows && c < d) {
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
-          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * Tl::kPiece);
+          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * kPiece);
       }
     }
   }
   // What load() took; the arguments are the same.
-  __device__ __forceinline__ void store(T* tile, const T* base, int64_t ld, int row, int rows, int d) const {
+  __device__ __forceinline__ void store(Store& tile, const T* base, int64_t ld, int row, int rows,
+                                        int d) const {
+    const int r = threadIdx.x / kPerRow, unit = threadIdx.x % kPerRow;
+    if (kPerRow * kLane != D && unit * kLane >= D) return;
     if (d % kLane) {
+      const int c = unit * kLane;
 #pragma unroll 1
-      for (int u = threadIdx.x; u < ROWS * kPerRow; u += THREADS) {
-        const int r = u / kPerRow, c = u % kPerRow * kLane;
+      for (int i = 0; i < kUnits; ++i) {
+        const int at = row + r + i * kAtOnce;
         float f[kLane] = {};
-        if (row + r < rows && c < d) {
-          const T* p = base + (row + r) * ld + c;
+        if (at < rows && c < d) {
+          const T* p = base + at * ld + c;
           if (c + kLane <= d)
             Elem<DT>::load8(p, f);
           else
             load_tail<DT>(p, d - c, f);
         }
+        u32x4 v[kWords];
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          u32x4 v;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if constexpr (DT == RIP_BF16)
-              v[j] = Elem<RIP_BF16>::pack2(f[2 * j], f[2 * j + 1]);
-            else
-              v[j] = __float_as_uint(f[4 * w + j]);
-          }
-          *(u32x4*)((char*)tile + r * Tl::kBytes + ((c / Tl::kPiece + w) ^ swizzle(r)) * 16) = v;
+        for (int j = 0; j < kLane; ++j) {
+          if constexpr (DT == RIP_FP32)
+            v[j / 4][j % 4] = __float_as_uint(f[j]);
+          else if (j % 2)
+            v[0][j / 2] = Elem<RIP_BF16>::pack2(f[j - 1], f[j]);
         }
+        Tl::put(tile, r + i * kAtOnce, unit, v);
       }
       return;
     }
-    const int r = threadIdx.x / kPerRow, piece = threadIdx.x % kPerRow * (kLane / Tl::kPiece);
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      const int row = r + i * kAtOnce;
-#pragma unroll
-      for (int w = 0; w < kWords; ++w)
-        *(u32x4*)((char*)tile + row * Tl::kBytes + ((piece + w) ^ swizzle(row)) * 16) = x[i][w];
-    }
+    for (int i = 0; i < kUnits; ++i) Tl::put(tile, r + i * kAtOnce, unit, x[i]);
   }
 };
 
 // Operands of one row in registers: elements 16 s + 8 half .. for every s.
-template <int DT, int D>
-__device__ __forceinline__ void load_row(const typename Elem<DT>::T* row, bool valid, int half, int d,
-                                         Frag<DT> (&f)[D / 16]) {
+template <int NT, int D>
+__device__ __forceinline__ void load_row(const typename Tile<NT, D>::T* row, bool valid, int half, int d,
+                                         Frag<NT> (&f)[D / 16]) {
+  constexpr int DT = storage(NT);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s) {
-    float x[kLane] = {};
     const int c = 16 * s + 8 * half;
-    if (valid && c + kLane <= d) Elem<DT>::load8(row + c, x);
-    f[s].set(x);
+    f[s] = Frag<NT>{};
+    if (valid && c + kLane <= d) f[s].load(row + c);
   }
   if (d % kLane == 0) return;
   const int unit = d / kLane;  // the one that ends inside
   float x[kLane] = {};
   if (valid && half == unit % 2) load_tail<DT>(row + unit * kLane, d % kLane, x);
+  Frag<NT> tail;
+  tail.set(x);
 #pragma unroll
   for (int s = 0; s < D / 16; ++s)
-    if (s == unit / 2) {
-      float y[kLane];
-      f[s].get(y);
-#pragma unroll
-      for (int j = 0; j < kLane; ++j) y[j] = half == unit % 2 ? x[j] : y[j];
-      f[s].set(y);
-    }
+    if (s == unit / 2 && half == unit % 2) f[s] = tail;
 }
 
 // The 4 consecutive elements that a lane holds of its row: c .. c + 3 below d.
@@ -382,6 +504,12 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// Ends a group of instructions: the compiler orders those of a group, and moves none
+// into another.  A group reads the operands of the next one and multiplies its own, so
+// that LDS's latency lies beside products; left to itself the compiler reads each
+// operand right before its product.
+__device__ __forceinline__ void group_end() { __builtin_amdgcn_sched_barrier(0); }
+
 // A workgroup's head (of `heads`), split and slot.  Heads go fastest: workgroups go to
 // the eight XCDs, each with an L2 of its own, in turn, so that where 8 divides the
 // heads (or they divide 8) a head's rows are read by one (or few) of them; and the
@@ -399,36 +527,41 @@ __device__ __forceinline__ bool my_share(const Args& p, int heads, Share* s) {
 
 // ---------------------------------------------------------------------------
 // Bias by distance, times log2(e), in LDS: lut[0] holds for every distance (key -
-// query) up to first, lut[size - 1] for all from first + size - 1 on.
+// query) up to first, lut[size - 1] for all from first + size - 1 on, and kLutPad
+// copies of each beside them, so that a block that lies partly in between needs no look
+// at its ends: its distances reach 62 past them.
 // ---------------------------------------------------------------------------
+constexpr int kLutPad = 64;
 struct Bias {
-  const float* lut;
+  const float* lut;  // of distance first
   int first, size;
   // Distances from `a` to `b` all have lut[0] (-1) or lut[size - 1] (1); 0: neither.
   __device__ __forceinline__ int uniform(int a, int b) const {
     return b <= first ? -1 : a >= first + size - 1 ? 1 : 0;
   }
   __device__ __forceinline__ float far(int side) const { return lut[side < 0 ? 0 : size - 1]; }
-  __device__ __forceinline__ float near(int rel) const {
-    return lut[min(max(rel - first, 0), size - 1)];
-  }
 };
+// LDS: kLutPad + lut_size + kLutPad numbers from `lut` on.
 __device__ __forceinline__ void load_lut(const Args& p, int head, float* lut) {
   const float* from = p.lut + (int64_t)head * p.lut_size;
-  for (int i = threadIdx.x; i < p.lut_size; i += blockDim.x) lut[i] = from[i];
+  for (int i = threadIdx.x; i < p.lut_size + 2 * kLutPad; i += blockDim.x)
+    lut[i] = from[min(max(i - kLutPad, 0), p.lut_size - 1)];
 }
+__host__ __device__ constexpr int lut_floats(int lut_size) { return lut_size + 2 * kLutPad; }
 
-// Scores of a block in the log2 domain with the bias; side: Bias::uniform of the block,
-// rel(r): the distance of register r.
-template <typename Rel>
-__device__ __forceinline__ void add_bias(f32x16& s, float scale2, const Bias& bias, int side, Rel rel) {
+// Scores of a block in the log2 domain with the bias; side: Bias::uniform of the block.
+// Register r is at distance rel + SIGN * row, row = block_row(r, 0) (rel has the half).
+template <int SIGN>
+__device__ __forceinline__ void add_bias(f32x16& s, float scale2, const Bias& bias, int side, int rel) {
   if (side) {
     const float b = bias.far(side);
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], scale2, b);
   } else {
+    // lanes whose query (or key) does not exist repeat the last one's place
+    const float* at = bias.lut + (rel - bias.first);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], scale2, bias.near(rel(r)));
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], scale2, at[SIGN * block_row(r, 0)]);
   }
 }
 
