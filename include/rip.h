@@ -512,6 +512,7 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
  *   q, out, dout, dq  [q_tokens][heads * head_dim], head h at columns h * head_dim
  *   k, v, dk, dv      [k_tokens][kv_heads * head_dim]; head h of q reads head
  *                     h / (heads / kv_heads)
+ * with row strides of at most RIP_MAX_WIDTH.
  * Sequence s has the queries q_offsets[s] .. q_offsets[s+1]-1 and the keys
  * k_offsets[s] .. k_offsets[s+1]-1 (int32, on the device; k_offsets NULL: as
  * q_offsets).  Offsets out of order are cut to fit as in rip_pref_loss.  With L_q

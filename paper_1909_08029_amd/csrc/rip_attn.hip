@@ -20,7 +20,7 @@ struct Prepare {
   Buckets buckets;
 };
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 1024;
 constexpr float kHides = -65536.0f;  // a bias below hides its keys
 
 // Workgroups 0 .. cleans-1 make the running maximum of a side's offsets; the others
@@ -151,6 +151,15 @@ int32_t check(const rip_attn* a, const char* name) {
   return check_matrix(a->bias, "bias", a->bias_dtype, a->buckets, a->heads, a->ld_bias);
 }
 
+// A matrix of a call; the kernels count the elements of a tile's rows in 32 bits.
+int32_t check_rows(const void* p, const char* what, int32_t dtype, int64_t rows, int64_t width, int64_t ld) {
+  const int32_t rc = check_matrix(p, what, dtype, rows, width, ld);
+  if (rc) return rc;
+  if (rows > 1 && ld > RIP_MAX_WIDTH)
+    return fail(RIP_E_UNSUPPORTED, "%s: row stride %lld is above the limit", what, (long long)ld);
+  return RIP_OK;
+}
+
 // Workgroups are counted in 32 bits.
 int32_t check_grid(const Plan& p, int64_t heads, const char* name) {
   if (p.slots * p.splits * heads >= (int64_t)1 << 31)
@@ -252,11 +261,11 @@ extern "C" int32_t rip_attn_forward(const rip_attn* a, const void* q, int64_t ld
   const int64_t wide = (int64_t)a->heads * a->head_dim, narrow = (int64_t)a->kv_heads * a->head_dim;
   const int32_t t = a->dtype;
   if (t == RIP_FP32) low = nullptr;
-  if ((rc = check_matrix(q, "q", t, a->q_tokens, wide, ld_q)) ||
-      (rc = check_matrix(k, "k", t, a->k_tokens, narrow, ld_k)) ||
-      (rc = check_matrix(v, "v", t, a->k_tokens, narrow, ld_v)) ||
-      (rc = check_matrix(out, "out", t, a->q_tokens, wide, ld_out)) ||
-      (low && (rc = check_matrix(low, "low", t, a->q_tokens, wide, ld_low))))
+  if ((rc = check_rows(q, "q", t, a->q_tokens, wide, ld_q)) ||
+      (rc = check_rows(k, "k", t, a->k_tokens, narrow, ld_k)) ||
+      (rc = check_rows(v, "v", t, a->k_tokens, narrow, ld_v)) ||
+      (rc = check_rows(out, "out", t, a->q_tokens, wide, ld_out)) ||
+      (low && (rc = check_rows(low, "low", t, a->q_tokens, wide, ld_low))))
     return rc;
   if (reinterpret_cast<uintptr_t>(lse) % 4)
     return fail(RIP_E_ALIGN, "%s: lse = %p is not 4-byte aligned", name, (const void*)lse);
@@ -306,15 +315,15 @@ extern "C" int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t l
   const int64_t wide = (int64_t)a->heads * a->head_dim, narrow = (int64_t)a->kv_heads * a->head_dim;
   const int32_t t = a->dtype;
   if (t == RIP_FP32) low = nullptr;
-  if ((rc = check_matrix(q, "q", t, a->q_tokens, wide, ld_q)) ||
-      (rc = check_matrix(k, "k", t, a->k_tokens, narrow, ld_k)) ||
-      (rc = check_matrix(v, "v", t, a->k_tokens, narrow, ld_v)) ||
-      (rc = check_matrix(out, "out", t, a->q_tokens, wide, ld_out)) ||
-      (rc = check_matrix(dout, "dout", t, a->q_tokens, wide, ld_dout)) ||
-      (low && (rc = check_matrix(low, "low", t, a->q_tokens, wide, ld_low))) ||
-      (rc = check_matrix(dq, "dq", t, a->q_tokens, wide, ld_dq)) ||
-      (rc = check_matrix(dk, "dk", t, a->k_tokens, narrow, ld_dk)) ||
-      (rc = check_matrix(dv, "dv", t, a->k_tokens, narrow, ld_dv)))
+  if ((rc = check_rows(q, "q", t, a->q_tokens, wide, ld_q)) ||
+      (rc = check_rows(k, "k", t, a->k_tokens, narrow, ld_k)) ||
+      (rc = check_rows(v, "v", t, a->k_tokens, narrow, ld_v)) ||
+      (rc = check_rows(out, "out", t, a->q_tokens, wide, ld_out)) ||
+      (rc = check_rows(dout, "dout", t, a->q_tokens, wide, ld_dout)) ||
+      (low && (rc = check_rows(low, "low", t, a->q_tokens, wide, ld_low))) ||
+      (rc = check_rows(dq, "dq", t, a->q_tokens, wide, ld_dq)) ||
+      (rc = check_rows(dk, "dk", t, a->k_tokens, narrow, ld_dk)) ||
+      (rc = check_rows(dv, "dv", t, a->k_tokens, narrow, ld_dv)))
     return rc;
   if (dbias && !a->bias) return fail(RIP_E_INVAL, "%s: dbias without a bias", name);
   if (dbias && (rc = check_matrix(dbias, "dbias", dbias_dtype, a->buckets, a->heads, ld_dbias))) return rc;

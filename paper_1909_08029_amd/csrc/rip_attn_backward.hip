@@ -105,6 +105,16 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
     for (int x = lane; x < kBlockFloats; x += 64) block[x] = 0.0f;
   }
 
+  const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
+  const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
+  const Tl at_lane(lane);
+
+  f32x16 dq[D / 32] = {};
+  Stage<NT, D, KT, 64 * WAVES> ks, vs;
+  if (t < end) {
+    ks.load(k0, f.k.ld, t, end, p.dim);
+    vs.load(v0, f.v.ld, t, end, p.dim);
+  }
   Frag<NT> q[D / 16], dout[D / 16];
   load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   load_row<NT, D>((const T*)f.dout.p + token * f.dout.ld + (int64_t)head * p.dim, valid, half, p.dim,
@@ -128,18 +138,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
     delta = add_halves(delta);
   }
   const int64_t row = (int64_t)head * p.q.tokens + token;
-  const float ref = valid ? reference(f.lse[row]) : kInf;
+  const float lse = f.lse[row], ref = valid ? reference(lse) : kInf;
   if (valid && half == 0 && split == 0) f.delta[row] = delta;
-  const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
-  const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
-  const Tl at_lane(lane);
-
-  f32x16 dq[D / 32] = {};
-  Stage<NT, D, KT, 64 * WAVES> ks, vs;
-  if (t < end) {
-    ks.load(k0, f.k.ld, t, end, p.dim);
-    vs.load(v0, f.v.ld, t, end, p.dim);
-  }
   for (; t < end; t += KT) {
     ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
     vs.store(v_tile, v0, f.v.ld, t, end, p.dim);
@@ -311,10 +311,6 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
   }
   const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
 
-  Frag<NT> k[D / 16], v[DK && !V_LDS ? D / 16 : 1];
-  load_row<NT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
-  if constexpr (DK && !V_LDS)
-    load_row<NT, D>((const T*)f.v.p + token * f.v.ld + (int64_t)kv * p.dim, valid, half, p.dim, v);
   f32x16 dk[DK ? D / 32 : 1] = {}, dv[DV ? D / 32 : 1] = {};
 
   const T* q0 = (const T*)f.q.p + at.other.begin * f.q.ld + (int64_t)kv * p.group * p.dim;
@@ -329,26 +325,29 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
       qs.store(v_tile[r], v0, f.v.ld, j0 + r * QT, lk, p.dim);
     }
   }
-  float ref = kInf, del = 0.0f;  // of query threadIdx.x of the tile
+  float lse = 0.0f, del = 0.0f;  // of query threadIdx.x of the tile
   auto load = [&](int step) {
     const int g = step / tiles, i0 = start + (step - g * tiles) * QT;
     qs.load(q0 + (int64_t)g * p.dim, f.q.ld, i0, lq, p.dim);
     ds.load(do0 + (int64_t)g * p.dim, f.dout.ld, i0, lq, p.dim);
-    const int i = i0 + threadIdx.x;
-    ref = kInf, del = 0.0f;
-    if (threadIdx.x < QT && i < lq) {
-      const int64_t row = ((int64_t)kv * p.group + g) * p.q.tokens + at.other.begin + i;
-      ref = reference(f.lse[row]);
-      if (DK) del = f.delta[row];
-    }
+    const int64_t row = ((int64_t)kv * p.group + g) * p.q.tokens + at.other.begin + min(i0 + (int)threadIdx.x, lq - 1);
+    lse = f.lse[row];
+    if (DK) del = f.delta[row];
   };
   if (n < end) load(n);
+  Frag<NT> k[D / 16], v[DK && !V_LDS ? D / 16 : 1];
+  load_row<NT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
+  if constexpr (DK && !V_LDS)
+    load_row<NT, D>((const T*)f.v.p + token * f.v.ld + (int64_t)kv * p.dim, valid, half, p.dim, v);
   int lut_head = -1;
   for (; n < end; ++n) {
     const int g = n / tiles, i0 = start + (n - g * tiles) * QT;
     qs.store(q_tile, q0 + (int64_t)g * p.dim, f.q.ld, i0, lq, p.dim);
     ds.store(do_tile, do0 + (int64_t)g * p.dim, f.dout.ld, i0, lq, p.dim);
-    if (threadIdx.x < QT) refs[threadIdx.x] = ref, deltas[threadIdx.x] = del;
+    if (threadIdx.x < QT) {
+      refs[threadIdx.x] = i0 + (int)threadIdx.x < lq ? reference(lse) : kInf;
+      deltas[threadIdx.x] = del;
+    }
     if (BIAS && lut_head != g) {
       load_lut(p, kv * p.group + g, lut);
       lut_head = g;

@@ -64,8 +64,6 @@ __global__ __launch_bounds__(64 * WAVES, NT == kBf16 && D <= 128 ? 2 : 1) void f
   const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
   if (BIAS) load_lut(p, head0, lut);
 
-  Frag<NT> q[D / 16];
-  load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
   const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
   const Tl at_lane(lane);
@@ -77,6 +75,8 @@ __global__ __launch_bounds__(64 * WAVES, NT == kBf16 && D <= 128 ? 2 : 1) void f
     ks.load(k0, f.k.ld, t, end, p.dim);
     vs.load(v0, f.v.ld, t, end, p.dim);
   }
+  Frag<NT> q[D / 16];
+  load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   for (; t < end; t += KT) {
     ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
     vs.store(v_tile, v0, f.v.ld, t, end, p.dim);

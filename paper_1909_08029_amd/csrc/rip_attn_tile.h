@@ -35,6 +35,22 @@ __device__ __forceinline__ int block_row(int r, int half) { return 8 * (r / 4) +
 enum { kBf16 = RIP_BF16, kSplit = 2, kFp32 = 3 };
 constexpr int storage(int number) { return number == kBf16 ? RIP_BF16 : RIP_FP32; }
 
+// Eight elements as they are loaded.
+struct RawBf16 {
+  u32x4 x;
+  __device__ __forceinline__ void load(const uint16_t* p) { x = *(const u32x4_any*)p; }
+};
+struct RawFp32 {
+  u32x4 x[2];
+  __device__ __forceinline__ void load(const float* p) {
+    x[0] = *(const u32x4_any*)p, x[1] = *(const u32x4_any*)(p + 4);
+  }
+  __device__ __forceinline__ void get(bool in, float (&f)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = in ? __uint_as_float(x[j / 4][j % 4]) : 0.0f;
+  }
+};
+
 // Eight operands of a lane, and a product of 16 steps of the summed axis.
 template <int NT>
 struct Frag;
@@ -51,7 +67,8 @@ struct Frag<kBf16> {
   __device__ __forceinline__ void get(float (&f)[8]) const {
     Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x), f);
   }
-  __device__ __forceinline__ void load(const uint16_t* p) { set(*(const u32x4_any*)p); }
+  typedef RawBf16 Raw;
+  __device__ __forceinline__ void set(const Raw& r, bool in) { set(in ? r.x : u32x4{0, 0, 0, 0}); }
 };
 template <>
 struct Frag<kSplit> {
@@ -90,9 +107,10 @@ struct Frag<kSplit> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] += a[j] + b[j];
   }
-  __device__ __forceinline__ void load(const float* p) {
+  typedef RawFp32 Raw;
+  __device__ __forceinline__ void set(const Raw& r, bool in) {
     float f[8];
-    Elem<RIP_FP32>::load8(p, f);
+    r.get(in, f);
     set(f);
   }
 };
@@ -107,7 +125,8 @@ struct Frag<kFp32> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = x[j];
   }
-  __device__ __forceinline__ void load(const float* p) { Elem<RIP_FP32>::load8(p, x); }
+  typedef RawFp32 Raw;
+  __device__ __forceinline__ void set(const Raw& r, bool in) { r.get(in, x); }
 };
 __device__ __forceinline__ f32x16 mma(const Frag<kBf16>& a, const Frag<kBf16>& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
@@ -312,39 +331,35 @@ struct Stage {
   static_assert(THREADS % kPerRow == 0 && ROWS % kAtOnce == 0, "whole rows at once");
   u32x4 x[kUnits][kWords];
 
-  // Rows row .. of the `rows` from `base` on; those past the end and columns past d
-  // are zeros.
+  // Rows row .. of the `rows` (at least one) from `base` on.  What lies past the end or past
+  // column d is loaded from inside, without a branch, and left out by store().
   __device__ __forceinline__ void load(const T* base, int64_t ld, int row, int rows, int d) {
     if (d % kLane) return;
     const int r = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * kLane;
-    const T* first = base + row * ld;                 // the same in every lane
-    const uint32_t at = (uint32_t)r * (uint32_t)ld + c;
-    if (row + ROWS <= rows && d == kPerRow * kLane) {
+    const int from = min(row, rows - 1);              // a tile may lie past the end
+    const T* first = base + from * ld;                // the same in every lane
+    if (row + ROWS <= rows) {
+      const uint32_t at = (uint32_t)r * (uint32_t)ld + (c < d ? c : 0);
 #pragma unroll
       for (int i = 0; i < kUnits; ++i)
 #pragma unroll
         for (int w = 0; w < kWords; ++w)
           x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * kPiece);
-      return;
-    }
+    } else {
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
+      for (int i = 0; i < kUnits; ++i) {
+        const uint32_t at = (uint32_t)min(r + i * kAtOnce, rows - 1 - from) * (uint32_t)ld + (c < d ? c : 0);
 #pragma unroll
-      for (int w = 0; w < kWords; ++w) x[i][w] = u32x4{0, 0, 0, 0};
-      if (row + r + i * kAtOnce < rows && c < d) {
-#pragma unroll
-        for (int w = 0; w < kWords; ++w)
-          x[i][w] = *(const u32x4_any*)(first + i * kAtOnce * ld + at + w * kPiece);
+        for (int w = 0; w < kWords; ++w) x[i][w] = *(const u32x4_any*)(first + at + w * kPiece);
       }
     }
   }
-  // What load() took; the arguments are the same.
-  __device__ __forceinline__ void store(Store& tile, const T* base, int64_t ld, int row, int rows,
-                                        int d) const {
-    const int r = threadIdx.x / kPerRow, unit = threadIdx.x % kPerRow;
-    if (kPerRow * kLane != D && unit * kLane >= D) return;
+  // What load() took, with zeros past the end and past column d; the arguments are the
+  // same.
+  __device__ __forceinline__ void store(Store& tile, const T* base, int64_t ld, int row, int rows, int d) {
+    const int r = threadIdx.x / kPerRow, unit = threadIdx.x % kPerRow, c = unit * kLane;
+    if (kPerRow * kLane != D && c >= D) return;
     if (d % kLane) {
-      const int c = unit * kLane;
 #pragma unroll 1
       for (int i = 0; i < kUnits; ++i) {
         const int at = row + r + i * kAtOnce;
@@ -368,21 +383,36 @@ struct Stage {
       }
       return;
     }
+    if (row + ROWS > rows || d != D) {
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+        for (int w = 0; w < kWords; ++w)
+          x[i][w] = row + r + i * kAtOnce < rows && c < d ? x[i][w] : u32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) Tl::put(tile, r + i * kAtOnce, unit, x[i]);
   }
 };
 
-// Operands of one row in registers: elements 16 s + 8 half .. for every s.
+// Operands of one row in registers: elements 16 s + 8 half .. for every s, zeros unless
+// `valid` (the row is readable all the same; no load waits behind a branch).
 template <int NT, int D>
 __device__ __forceinline__ void load_row(const typename Tile<NT, D>::T* row, bool valid, int half, int d,
                                          Frag<NT> (&f)[D / 16]) {
   constexpr int DT = storage(NT);
+  if (d >= kLane) {
+    typename Frag<NT>::Raw raw[D / 16];
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    const int c = 16 * s + 8 * half;
-    f[s] = Frag<NT>{};
-    if (valid && c + kLane <= d) f[s].load(row + c);
+    for (int s = 0; s < D / 16; ++s) {
+      const int c = 16 * s + 8 * half;
+      raw[s].load(row + (c + kLane <= d ? c : 0));
+    }
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) f[s].set(raw[s], valid && 16 * s + 8 * half + kLane <= d);
+  } else {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) f[s] = Frag<NT>{};
   }
   if (d % kLane == 0) return;
   const int unit = d / kLane;  // the one that ends inside
