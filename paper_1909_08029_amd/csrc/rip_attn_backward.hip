@@ -504,7 +504,8 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buck
 template <int NT, int D, bool BIAS, bool SPLIT>
 const void* dq_of() {
   constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
-  constexpr int step = wide ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
+  constexpr int step = wide || (D <= 64 && (BIAS || NT == kSplit)) ? 64 : 32;
+  constexpr int units = NT == kBf16 && D <= 128 ? 2 : 1;
   return (const void*)dq_kernel<NT, D, dq_waves(NT == kBf16, D), step, units, BIAS, SPLIT>;
 }
 template <int NT, int D>
@@ -515,7 +516,7 @@ const void* dq_of(bool bias, bool split) {
 template <int NT, int D, int WAVES, bool BIAS, bool SPLIT, bool DK, bool DV>
 const void* dkv_of() {
   constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
-  constexpr int step = NT == kBf16 && D <= 64 ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
+  constexpr int step = D <= 64 ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
   return (const void*)dkv_kernel<NT, D, WAVES, step, units, wide, BIAS, SPLIT, DK, DV>;
 }
 template <int NT, int D, int WAVES, bool DK = true, bool DV = true>

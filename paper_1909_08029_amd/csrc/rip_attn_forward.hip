@@ -14,10 +14,6 @@ namespace rip {
 namespace attn {
 namespace {
 
-// Keys of a tile.  A wave by itself holds a whole tile on its way in its registers.
-template <int NT, int D, int WAVES>
-constexpr int kKeys = NT == kBf16 && D <= 128 && (WAVES > 1 || D <= 64) ? 64 : 32;
-
 // Without a bias, with one, and with one whose gradient will be wanted: that sums ds
 // in fp32, and its row sums delta come from out, which must not hold the rounding of
 // the exponentials then.  They enter the product as two bf16 numbers (16 bits).
@@ -25,13 +21,12 @@ enum { kPlain, kBias, kExact };
 
 constexpr float kSlack = 6.0f;  // growth of a maximum (log2) that needs no rescaling
 
-template <int NT, int D, int WAVES, int MODE, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, NT == kBf16 && D <= 128 ? 2 : 1) void forward_kernel(
-    Forward f) {
+template <int NT, int D, int WAVES, int KT, int EU, int MODE, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(Forward f) {
   constexpr int DT = storage(NT);
   typedef Tile<NT, D> Tl;
   typedef typename Tl::T T;
-  constexpr int KT = kKeys<NT, D, WAVES>, KB = KT / 32, QT = kRows * WAVES;
+  constexpr int KB = KT / 32, QT = kRows * WAVES;
   constexpr bool BIAS = MODE != kPlain, EXACT = MODE == kExact;
   __shared__ typename Tl::template Store<KT> k_tile, v_tile;
   extern __shared__ __align__(16) float lut[];
@@ -244,14 +239,23 @@ __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   l *= weight;
 #pragma unroll
   for (int o = 32; o >= 1; o /= 2) l += __shfl_xor(l, o);
-  constexpr int kColumns = RIP_MAX_HEAD_DIM / 64;
+  constexpr int kColumns = RIP_MAX_HEAD_DIM / 64, kAtOnce = 4;  // splits of a wave
   float x[kColumns] = {};
   const float* from = f.part + row * p.dim + lane;
-  for (int s = wave; s < p.splits; s += 4) {
-    const float w = __shfl(weight, s);
+  for (int s0 = wave; s0 < p.splits; s0 += 4 * kAtOnce) {
+    float y[kAtOnce][kColumns];
 #pragma unroll
-    for (int c = 0; c < kColumns; ++c)
-      if (lane + 64 * c < p.dim) x[c] += from[s * all * p.dim + 64 * c] * w;
+    for (int i = 0; i < kAtOnce; ++i)
+#pragma unroll
+      for (int c = 0; c < kColumns; ++c)
+        y[i][c] = lane + 64 * c < p.dim ? from[min(s0 + 4 * i, p.splits - 1) * all * p.dim + 64 * c] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float w = __shfl(weight, min(s0 + 4 * i, 63));
+      if (s0 + 4 * i < p.splits)
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) x[c] += y[i][c] * w;
+    }
   }
 #pragma unroll
   for (int c = 0; c < kColumns; ++c) sums[wave][lane + 64 * c] = x[c];
@@ -269,10 +273,16 @@ __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   if (f.lse && c == 0) f.lse[row] = l == 0.0f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// Keys of a tile (a wave by itself holds a whole tile on its way in its registers), and
+// waves to a SIMD that the registers have to leave room for.
 template <int NT, int D, int WAVES, int MODE>
 const void* variant(bool split) {
-  return split ? (const void*)forward_kernel<NT, D, WAVES, MODE, true>
-               : (const void*)forward_kernel<NT, D, WAVES, MODE, false>;
+  constexpr bool wide = (NT == kBf16 && D <= 128 && (WAVES > 1 || D <= 64)) ||
+                        (NT == kSplit && D <= 64 && WAVES > 1);
+  constexpr int keys = wide ? 64 : 32;
+  constexpr int units = NT != kBf16 || D > 128 ? 1 : D <= 64 && WAVES == 4 ? 3 : 2;
+  return split ? (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, true>
+               : (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, false>;
 }
 template <int NT, int D, int WAVES>
 const void* variant(int mode, bool split) {
@@ -281,6 +291,8 @@ const void* variant(int mode, bool split) {
 }
 template <int NT, int D>
 const void* variant(int waves, int mode, bool split) {
+  if constexpr (NT == kBf16 && (D == 96 || D == 128))
+    if (waves == 8) return variant<NT, D, 8>(mode, split);
   return waves == 1 ? variant<NT, D, 1>(mode, split) : variant<NT, D, 4>(mode, split);
 }
 const void* kernel_of(int32_t dtype, int width, int waves, int mode, bool split) {

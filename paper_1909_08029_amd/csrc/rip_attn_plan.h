@@ -47,15 +47,18 @@ constexpr Kernel kForward = {2, 0.12}, kDq = {3, 0.16}, kDkv = {4, 0.2};
 // them, shared by `resident` waves): what all SIMDs have to do, or one tile's chain,
 // whichever is longer; then the parts' way through memory and the launch that adds
 // them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us a
-// column each in bf16 with two waves to a SIMD (six times that for fp32 as three parts,
-// sixteen times for fp32's own instructions), half as long again alone; a tile costs
-// about four us before its first block.
+// column each in bf16 (six times that for fp32 as three parts, sixteen times for fp32's
+// own instructions); a tile costs about four us before its first block.
 inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int64_t axis,
                       int splits, double part) {
   const double product = (s.bf16 ? 0.0021 : width <= 128 ? 0.0126 : 0.0336) * width, block = k.products * product + k.softmax;
-  const double alone = (s.bf16 ? 1.5 : 1.0) * block * (waves == 1 ? 1.25 : 1.0);
+  // eight waves share a tile's way to LDS (16384 tokens of 128 columns: 1089 us for the
+  // forward pass, 1306 with four); a wave by itself waits for it (one query each over
+  // 200003 keys: 190 us in 64 parts, 159 with four waves in 32)
+  const double alone = block * (waves == 1 ? 2.0 : 1.0);
   const double blocks = (double)ceil_div(axis, kRows);
-  const double all = (double)units * waves * (blocks * (s.causal ? 0.5 : 1.0) * block + 2.0 * splits) / 1024;
+  const double all = (double)units * waves * (waves == 8 ? 0.9 : 1.0) *
+                     (blocks * (s.causal ? 0.5 : 1.0) * block + 2.0 * splits) / 1024;
   const double chain = blocks / splits * alone + 4.0;
   return std::max(all, chain) + (splits > 1 ? 5.0 + splits * part / 2e6 : 0.0);
 }
@@ -104,8 +107,9 @@ inline Plan over_keys(const Sizes& s, int waves) {
 // (8192 tokens, 16 heads of 64, causal: 608 us for the backward pass, 739 with four) and
 // four where they are short (32 sequences: 115 and 105).
 inline Plan plan_forward(const Sizes& s) {
-  constexpr int waves[] = {4, 1};
-  return over_queries(s, kForward, waves, 2);
+  const int width = width_of(s.dim);
+  constexpr int waves[] = {4, 1, 8};
+  return over_queries(s, kForward, waves, s.bf16 && (width == 96 || width == 128) ? 3 : 2);
 }
 constexpr int dq_waves(bool bf16, int width) { return bf16 && width > 64 && width <= 128 ? 8 : 4; }
 inline int dkv_waves(bool bf16, int width, int64_t keys) {
