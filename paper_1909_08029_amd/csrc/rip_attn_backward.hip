@@ -503,9 +503,8 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buck
 // have to leave room for.
 template <int NT, int D, bool BIAS, bool SPLIT>
 const void* dq_of() {
-  constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
-  constexpr int step = wide || (D <= 64 && (BIAS || NT == kSplit)) ? 64 : 32;
-  constexpr int units = NT == kBf16 && D <= 128 ? 2 : 1;
+  constexpr int step = NT == kBf16 && D <= 128 && (D > 64 || BIAS) ? 64 : 32;
+  constexpr int units = D <= (NT == kBf16 ? 128 : 64) ? 2 : 1;
   return (const void*)dq_kernel<NT, D, dq_waves(NT == kBf16, D), step, units, BIAS, SPLIT>;
 }
 template <int NT, int D>
@@ -515,9 +514,11 @@ const void* dq_of(bool bias, bool split) {
 }
 template <int NT, int D, int WAVES, bool BIAS, bool SPLIT, bool DK, bool DV>
 const void* dkv_of() {
-  constexpr bool wide = NT == kBf16 && D > 64 && D <= 128;
-  constexpr int step = D <= 64 ? 64 : 32, units = NT == kBf16 && D <= 128 ? 2 : 1;
-  return (const void*)dkv_kernel<NT, D, WAVES, step, units, wide, BIAS, SPLIT, DK, DV>;
+  constexpr int step = NT == kBf16 && D <= 64 ? 64 : 32;
+  constexpr int units = D <= (NT == kBf16 ? 128 : 64) ? 2 : 1;
+  // the keys' values in LDS where the registers hold too much beside them
+  constexpr bool v_lds = (NT == kBf16 && D > 64 && D <= 128) || (NT == kSplit && D != 96);
+  return (const void*)dkv_kernel<NT, D, WAVES, step, units, v_lds, BIAS, SPLIT, DK, DV>;
 }
 template <int NT, int D, int WAVES, bool DK = true, bool DV = true>
 const void* dkv_of(bool bias, bool split) {

@@ -280,7 +280,7 @@ const void* variant(bool split) {
   constexpr bool wide = (NT == kBf16 && D <= 128 && (WAVES > 1 || D <= 64)) ||
                         (NT == kSplit && D <= 64 && WAVES > 1);
   constexpr int keys = wide ? 64 : 32;
-  constexpr int units = NT != kBf16 || D > 128 ? 1 : D <= 64 && WAVES == 4 ? 3 : 2;
+  constexpr int units = D > (NT == kBf16 ? 128 : WAVES == 1 ? 64 : 96) ? 1 : NT == kBf16 && D <= 64 && WAVES == 4 ? 3 : 2;
   return split ? (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, true>
                : (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, false>;
 }

@@ -42,25 +42,31 @@ struct Kernel {
 };
 constexpr Kernel kForward = {2, 0.12}, kDq = {3, 0.16}, kDkv = {4, 0.2};
 
-// Time (us) of `units` tiles of `waves` waves that go over `axis` elements each (half of
-// them where causal) in `splits` parts, from the time of a block on a SIMD (1024 of
+// Time (us) of `units` tiles of `waves` waves (of which `busy` have work) that go over `axis` elements each (`share`
+// of them where causal) in `splits` parts, from the time of a block on a SIMD (1024 of
 // them, shared by `resident` waves): what all SIMDs have to do, or one tile's chain,
 // whichever is longer; then the parts' way through memory and the launch that adds
 // them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us a
 // column each in bf16 (six times that for fp32 as three parts, sixteen times for fp32's
 // own instructions); a tile costs about four us before its first block.
-inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int64_t axis,
-                      int splits, double part) {
+inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int busy,
+                      int64_t axis, double share, int splits, double part) {
   const double product = (s.bf16 ? 0.0021 : width <= 128 ? 0.0126 : 0.0336) * width, block = k.products * product + k.softmax;
   // eight waves share a tile's way to LDS (16384 tokens of 128 columns: 1089 us for the
   // forward pass, 1306 with four); a wave by itself waits for it (one query each over
-  // 200003 keys: 190 us in 64 parts, 159 with four waves in 32)
-  const double alone = block * (waves == 1 ? 2.0 : 1.0);
+  // 200003 keys: 190 us in 64 parts, 159 with four waves in 32); of eight, two share a SIMD
+  const double alone = block * (busy == 8 ? 1.8 : (waves == 1 ? 2.0 : 1.0) * (s.bf16 ? 1.1 : 1.25));
   const double blocks = (double)ceil_div(axis, kRows);
-  const double all = (double)units * waves * (waves == 8 ? 0.9 : 1.0) *
-                     (blocks * (s.causal ? 0.5 : 1.0) * block + 2.0 * splits) / 1024;
+  const double all = (double)units * busy * (waves == 8 ? 0.9 : 1.0) *
+                     (blocks * share * block + 2.0 * splits) / 1024;
   const double chain = blocks / splits * alone + 4.0;
   return std::max(all, chain) + (splits > 1 ? 5.0 + splits * part / 2e6 : 0.0);
+}
+
+// Of all pairs of a query and a key, those that the query sees: its sequence's queries
+// are the last of its keys.
+inline double share_of(const Sizes& s, int64_t q, int64_t k) {
+  return s.causal ? 1.0 - 0.5 * std::min(1.0, (double)q / std::max<int64_t>(1, k)) : 1.0;
 }
 
 constexpr int kTrySplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
@@ -74,10 +80,13 @@ inline Plan over_queries(const Sizes& s, const Kernel& kernel, const int* waves,
   if (!s.bias && s.group > 1 && q < kRows * 4 && s.q_tokens * s.group < (int64_t)1 << 30) best.pack = s.group;
   double least = 1e30;
   for (int i = 0; i < options; ++i) {
+    if (waves[i] == 8 && options > 1 && q * best.pack <= 4 * kRows) continue;
     const int64_t units = n * ceil_div(q * best.pack, kRows * waves[i]) * (s.heads / best.pack);
     for (int splits : kTrySplits) {
       if (splits > 1 && splits * 64 > k) break;
-      const double us = time_of(kernel, s, best.width, units, waves[i], k, splits,
+      // waves without a query wait, and cost nothing
+      const int busy = (int)std::min<int64_t>(waves[i], ceil_div(q * best.pack, kRows));
+      const double us = time_of(kernel, s, best.width, units, waves[i], busy, k, share_of(s, q, k), splits,
                                 4.0 * s.q_tokens * s.heads * s.dim);
       if (us < least) least = us, best.waves = waves[i], best.splits = splits;
     }
@@ -95,7 +104,7 @@ inline Plan over_keys(const Sizes& s, int waves) {
   double least = 1e30;
   for (int splits : kTrySplits) {
     if (splits > 1 && splits * 64 > axis) break;
-    const double us = time_of(kDkv, s, best.width, units, waves, axis, splits,
+    const double us = time_of(kDkv, s, best.width, units, waves, waves, axis, share_of(s, q, k), splits,
                               8.0 * s.k_tokens * (s.heads / s.group) * s.dim);
     if (us < least) least = us, best.splits = splits;
   }
