@@ -111,7 +111,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
 
   f32x16 dq[D / 32] = {};
   Stage<NT, D, KT, 64 * WAVES> ks, vs;
-  if (t < end) {
+  constexpr bool kOnTheWay = NT != kFp32;  // as in the forward pass
+  if (kOnTheWay && t < end) {
     ks.load(k0, f.k.ld, t, end, p.dim);
     vs.load(v0, f.v.ld, t, end, p.dim);
   }
@@ -141,10 +142,14 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   const float lse = f.lse[row], ref = valid ? reference(lse) : kInf;
   if (valid && half == 0 && split == 0) f.delta[row] = delta;
   for (; t < end; t += KT) {
+    if (!kOnTheWay) {
+      ks.load(k0, f.k.ld, t, end, p.dim);
+      vs.load(v0, f.v.ld, t, end, p.dim);
+    }
     ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
     vs.store(v_tile, v0, f.v.ld, t, end, p.dim);
     lds_barrier();
-    if (t + KT < end) {
+    if (kOnTheWay && t + KT < end) {
       ks.load(k0, f.k.ld, t + KT, end, p.dim);
       vs.load(v0, f.v.ld, t + KT, end, p.dim);
     }
@@ -334,7 +339,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
     lse = f.lse[row];
     if (DK) del = f.delta[row];
   };
-  if (n < end) load(n);
+  constexpr bool kOnTheWay = NT != kFp32;
+  if (kOnTheWay && n < end) load(n);
   Frag<NT> k[D / 16], v[DK && !V_LDS ? D / 16 : 1];
   load_row<NT, D>((const T*)f.k.p + token * f.k.ld + (int64_t)kv * p.dim, valid, half, p.dim, k);
   if constexpr (DK && !V_LDS)
@@ -342,6 +348,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
   int lut_head = -1;
   for (; n < end; ++n) {
     const int g = n / tiles, i0 = start + (n - g * tiles) * QT;
+    if (!kOnTheWay) load(n);
     qs.store(q_tile, q0 + (int64_t)g * p.dim, f.q.ld, i0, lq, p.dim);
     ds.store(do_tile, do0 + (int64_t)g * p.dim, f.dout.ld, i0, lq, p.dim);
     if (threadIdx.x < QT) {
@@ -353,7 +360,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
       lut_head = g;
     }
     lds_barrier();
-    if (n + 1 < end) load(n + 1);
+    if (kOnTheWay && n + 1 < end) load(n + 1);
     if (jw < lk && i0 + QT > first_wave) {
 #pragma unroll
       for (int b = 0; b < QB; ++b) {

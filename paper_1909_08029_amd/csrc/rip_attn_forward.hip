@@ -66,17 +66,23 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(Forward f) {
   f32x16 o[D / 32] = {};
   float m = -kInf, l = 0.0f;  // reference (log2); the sum of this half's keys
   Stage<NT, D, KT, 64 * WAVES> ks, vs;
-  if (t < end) {
+  // (fp32 of 256 columns has no registers for tiles on their way)
+  constexpr bool kOnTheWay = NT != kFp32;
+  if (kOnTheWay && t < end) {
     ks.load(k0, f.k.ld, t, end, p.dim);
     vs.load(v0, f.v.ld, t, end, p.dim);
   }
   Frag<NT> q[D / 16];
   load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
   for (; t < end; t += KT) {
+    if (!kOnTheWay) {
+      ks.load(k0, f.k.ld, t, end, p.dim);
+      vs.load(v0, f.v.ld, t, end, p.dim);
+    }
     ks.store(k_tile, k0, f.k.ld, t, end, p.dim);
     vs.store(v_tile, v0, f.v.ld, t, end, p.dim);
     lds_barrier();
-    if (t + KT < end) {
+    if (kOnTheWay && t + KT < end) {
       ks.load(k0, f.k.ld, t + KT, end, p.dim);
       vs.load(v0, f.v.ld, t + KT, end, p.dim);
     }
@@ -293,7 +299,9 @@ template <int NT, int D>
 const void* variant(int waves, int mode, bool split) {
   if constexpr (NT == kBf16 && (D == 96 || D == 128))
     if (waves == 8) return variant<NT, D, 8>(mode, split);
-  return waves == 1 ? variant<NT, D, 1>(mode, split) : variant<NT, D, 4>(mode, split);
+  if constexpr (D < 256)
+    if (waves == 1) return variant<NT, D, 1>(mode, split);
+  return variant<NT, D, 4>(mode, split);
 }
 const void* kernel_of(int32_t dtype, int width, int waves, int mode, bool split) {
   const bool bf16 = dtype == RIP_BF16;

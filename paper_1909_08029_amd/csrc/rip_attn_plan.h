@@ -118,7 +118,7 @@ inline Plan over_keys(const Sizes& s, int waves) {
 inline Plan plan_forward(const Sizes& s) {
   const int width = width_of(s.dim);
   constexpr int waves[] = {4, 1, 8};
-  return over_queries(s, kForward, waves, s.bf16 && (width == 96 || width == 128) ? 3 : 2);
+  return over_queries(s, kForward, waves, width == 256 ? 1 : s.bf16 && width > 64 ? 3 : 2);
 }
 constexpr int dq_waves(bool bf16, int width) { return bf16 && width > 64 && width <= 128 ? 8 : 4; }
 inline int dkv_waves(bool bf16, int width, int64_t keys) {

@@ -35,21 +35,39 @@ __device__ __forceinline__ int block_row(int r, int half) { return 8 * (r / 4) +
 enum { kBf16 = RIP_BF16, kSplit = 2, kFp32 = 3 };
 constexpr int storage(int number) { return number == kBf16 ? RIP_BF16 : RIP_FP32; }
 
-// Eight elements as they are loaded.
-struct RawBf16 {
-  u32x4 x;
-  __device__ __forceinline__ void load(const uint16_t* p) { x = *(const u32x4_any*)p; }
-};
-struct RawFp32 {
-  u32x4 x[2];
-  __device__ __forceinline__ void load(const float* p) {
-    x[0] = *(const u32x4_any*)p, x[1] = *(const u32x4_any*)(p + 4);
-  }
-  __device__ __forceinline__ void get(bool in, float (&f)[8]) const {
+// Eight elements as they are loaded, 16 bytes a word (RAW[1] bf16, RAW[2] fp32).
+//
+// Columns c .. c + 7 of a row of d: where they end past d, the row's last eight are
+// loaded instead, and dropped at the front, which leaves zeros at the end (d >= 8).
+__device__ __forceinline__ int first_column(int c, int d) { return c < d ? min(c, d - kLane) : 0; }
+template <int WORDS>
+__device__ __forceinline__ void drop_front(u32x4 (&x)[WORDS], int n) {
+  constexpr int N = 4 * WORDS;
+  uint32_t w[N];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = in ? __uint_as_float(x[j / 4][j % 4]) : 0.0f;
+  for (int i = 0; i < N; ++i) w[i] = x[i / 4][i % 4];
+  const int words = WORDS == 1 ? n / 2 : n;
+#pragma unroll
+  for (int by = N / 2; by >= 1; by /= 2)
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = words & by ? (i + by < N ? w[i + by] : 0u) : w[i];
+  if (WORDS == 1) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t next = i + 1 < N ? w[i + 1] : 0u;
+      w[i] = n & 1 ? w[i] >> 16 | next << 16 : w[i];
+    }
   }
-};
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i / 4][i % 4] = w[i];
+}
+// What columns c .. c + 7 of a row of d are, from what first_column() loaded.
+template <int WORDS>
+__device__ __forceinline__ void cut_columns(u32x4 (&x)[WORDS], int c, int d, bool row) {
+  if (d % kLane) drop_front<WORDS>(x, c < d && c + kLane > d ? c + kLane - d : 0);
+#pragma unroll
+  for (int w = 0; w < WORDS; ++w) x[w] = row && c < d ? x[w] : u32x4{0, 0, 0, 0};
+}
 
 // Eight operands of a lane, and a product of 16 steps of the summed axis.
 template <int NT>
@@ -67,8 +85,7 @@ struct Frag<kBf16> {
   __device__ __forceinline__ void get(float (&f)[8]) const {
     Elem<RIP_BF16>::unpack8(__builtin_bit_cast(u32x4, x), f);
   }
-  typedef RawBf16 Raw;
-  __device__ __forceinline__ void set(const Raw& r, bool in) { set(in ? r.x : u32x4{0, 0, 0, 0}); }
+  __device__ __forceinline__ void set(const u32x4 (&raw)[1]) { set(raw[0]); }
 };
 template <>
 struct Frag<kSplit> {
@@ -107,10 +124,10 @@ struct Frag<kSplit> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] += a[j] + b[j];
   }
-  typedef RawFp32 Raw;
-  __device__ __forceinline__ void set(const Raw& r, bool in) {
+  __device__ __forceinline__ void set(const u32x4 (&raw)[2]) {
     float f[8];
-    r.get(in, f);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(raw[j / 4][j % 4]);
     set(f);
   }
 };
@@ -125,8 +142,10 @@ struct Frag<kFp32> {
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = x[j];
   }
-  typedef RawFp32 Raw;
-  __device__ __forceinline__ void set(const Raw& r, bool in) { r.get(in, x); }
+  __device__ __forceinline__ void set(const u32x4 (&raw)[2]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(raw[j / 4][j % 4]);
+  }
 };
 __device__ __forceinline__ f32x16 mma(const Frag<kBf16>& a, const Frag<kBf16>& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.x, b.x, c, 0, 0, 0);
@@ -313,10 +332,10 @@ __device__ __forceinline__ void load_tail(const typename Elem<DT>::T* p, int n, 
   }
 }
 
-// Rows on their way to LDS: ROWS rows of d <= D elements, by THREADS threads, in units
-// of eight elements.  Rows of a width that eight does not divide go straight there.
 constexpr int two_power(int n) { return n <= 1 ? 1 : 2 * two_power((n + 1) / 2); }
 
+// Rows on their way to LDS: ROWS rows of d <= D elements, by THREADS threads, in units
+// of eight elements.  Rows shorter than that go straight there.
 template <int NT, int D, int ROWS, int THREADS>
 struct Stage {
   typedef Tile<NT, D> Tl;
@@ -334,12 +353,12 @@ struct Stage {
   // Rows row .. of the `rows` (at least one) from `base` on.  What lies past the end or past
   // column d is loaded from inside, without a branch, and left out by store().
   __device__ __forceinline__ void load(const T* base, int64_t ld, int row, int rows, int d) {
-    if (d % kLane) return;
-    const int r = threadIdx.x / kPerRow, c = threadIdx.x % kPerRow * kLane;
+    if (d < kLane) return;
+    const int r = threadIdx.x / kPerRow, c = first_column(threadIdx.x % kPerRow * kLane, d);
     const int from = min(row, rows - 1);              // a tile may lie past the end
     const T* first = base + from * ld;                // the same in every lane
     if (row + ROWS <= rows) {
-      const uint32_t at = (uint32_t)r * (uint32_t)ld + (c < d ? c : 0);
+      const uint32_t at = (uint32_t)r * (uint32_t)ld + c;
 #pragma unroll
       for (int i = 0; i < kUnits; ++i)
 #pragma unroll
@@ -348,7 +367,7 @@ struct Stage {
     } else {
 #pragma unroll
       for (int i = 0; i < kUnits; ++i) {
-        const uint32_t at = (uint32_t)min(r + i * kAtOnce, rows - 1 - from) * (uint32_t)ld + (c < d ? c : 0);
+        const uint32_t at = (uint32_t)min(r + i * kAtOnce, rows - 1 - from) * (uint32_t)ld + c;
 #pragma unroll
         for (int w = 0; w < kWords; ++w) x[i][w] = *(const u32x4_any*)(first + at + w * kPiece);
       }
@@ -359,18 +378,12 @@ struct Stage {
   __device__ __forceinline__ void store(Store& tile, const T* base, int64_t ld, int row, int rows, int d) {
     const int r = threadIdx.x / kPerRow, unit = threadIdx.x % kPerRow, c = unit * kLane;
     if (kPerRow * kLane != D && c >= D) return;
-    if (d % kLane) {
+    if (d < kLane) {
 #pragma unroll 1
       for (int i = 0; i < kUnits; ++i) {
         const int at = row + r + i * kAtOnce;
         float f[kLane] = {};
-        if (at < rows && c < d) {
-          const T* p = base + at * ld + c;
-          if (c + kLane <= d)
-            Elem<DT>::load8(p, f);
-          else
-            load_tail<DT>(p, d - c, f);
-        }
+        if (at < rows && unit == 0) load_tail<DT>(base + at * ld, d, f);
         u32x4 v[kWords];
 #pragma unroll
         for (int j = 0; j < kLane; ++j) {
@@ -385,10 +398,7 @@ struct Stage {
     }
     if (row + ROWS > rows || d != D) {
 #pragma unroll
-      for (int i = 0; i < kUnits; ++i)
-#pragma unroll
-        for (int w = 0; w < kWords; ++w)
-          x[i][w] = row + r + i * kAtOnce < rows && c < d ? x[i][w] : u32x4{0, 0, 0, 0};
+      for (int i = 0; i < kUnits; ++i) cut_columns<kWords>(x[i], c, d, row + r + i * kAtOnce < rows);
     }
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) Tl::put(tile, r + i * kAtOnce, unit, x[i]);
@@ -400,29 +410,33 @@ struct Stage {
 template <int NT, int D>
 __device__ __forceinline__ void load_row(const typename Tile<NT, D>::T* row, bool valid, int half, int d,
                                          Frag<NT> (&f)[D / 16]) {
-  constexpr int DT = storage(NT);
+  constexpr int DT = storage(NT), WORDS = DT == RIP_BF16 ? 1 : 2;
   if (d >= kLane) {
-    typename Frag<NT>::Raw raw[D / 16];
+    u32x4 raw[D / 16][WORDS];
 #pragma unroll
     for (int s = 0; s < D / 16; ++s) {
-      const int c = 16 * s + 8 * half;
-      raw[s].load(row + (c + kLane <= d ? c : 0));
+      const auto* p = row + first_column(16 * s + 8 * half, d);
+#pragma unroll
+      for (int w = 0; w < WORDS; ++w) raw[s][w] = *(const u32x4_any*)(p + 4 * w);
+    }
+    if (d == D) {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s)
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) raw[s][w] = valid ? raw[s][w] : u32x4{0, 0, 0, 0};
+    } else {
+#pragma unroll
+      for (int s = 0; s < D / 16; ++s) cut_columns<WORDS>(raw[s], 16 * s + 8 * half, d, valid);
     }
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) f[s].set(raw[s], valid && 16 * s + 8 * half + kLane <= d);
+    for (int s = 0; s < D / 16; ++s) f[s].set(raw[s]);
   } else {
+    float x[kLane] = {};
+    if (valid && half == 0) load_tail<DT>(row, d, x);
+    f[0].set(x);
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) f[s] = Frag<NT>{};
+    for (int s = 1; s < D / 16; ++s) f[s] = Frag<NT>{};
   }
-  if (d % kLane == 0) return;
-  const int unit = d / kLane;  // the one that ends inside
-  float x[kLane] = {};
-  if (valid && half == unit % 2) load_tail<DT>(row + unit * kLane, d % kLane, x);
-  Frag<NT> tail;
-  tail.set(x);
-#pragma unroll
-  for (int s = 0; s < D / 16; ++s)
-    if (s == unit / 2 && half == unit % 2) f[s] = tail;
 }
 
 // The 4 consecutive elements that a lane holds of its row: c .. c + 3 below d.
