@@ -279,14 +279,12 @@ __global__ __launch_bounds__(256) void join_kernel(Forward f) {
   if (f.lse && c == 0) f.lse[row] = l == 0.0f ? -kInf : (top + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// Keys of a tile (a wave by itself holds a whole tile on its way in its registers), and
-// waves to a SIMD that the registers have to leave room for.
+// Variants: keys of a tile, and waves to a SIMD that the registers have to leave room for
+// (three for 64 columns: 8192 tokens, 16 heads, causal 184 us, 212 with two).
 template <int NT, int D, int WAVES, int MODE>
 const void* variant(bool split) {
-  constexpr bool wide = (NT == kBf16 && D <= 128 && (WAVES > 1 || D <= 64)) ||
-                        (NT == kSplit && D <= 64 && WAVES > 1);
-  constexpr int keys = wide ? 64 : 32;
-  constexpr int units = D > (NT == kBf16 ? 128 : WAVES == 1 ? 64 : 96) ? 1 : NT == kBf16 && D <= 64 && WAVES == 4 ? 3 : 2;
+  constexpr int keys = (NT == kBf16 && D <= 128) || (NT == kSplit && D <= 64) ? 64 : 32;
+  constexpr int units = NT == kBf16 ? (D <= 64 ? 3 : D <= 128 ? 2 : 1) : D <= 96 ? 2 : 1;
   return split ? (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, true>
                : (const void*)forward_kernel<NT, D, WAVES, keys, units, MODE, false>;
 }
@@ -299,8 +297,6 @@ template <int NT, int D>
 const void* variant(int waves, int mode, bool split) {
   if constexpr (NT == kBf16 && (D == 96 || D == 128))
     if (waves == 8) return variant<NT, D, 8>(mode, split);
-  if constexpr (D < 256)
-    if (waves == 1) return variant<NT, D, 1>(mode, split);
   return variant<NT, D, 4>(mode, split);
 }
 const void* kernel_of(int32_t dtype, int width, int waves, int mode, bool split) {

@@ -42,20 +42,22 @@ struct Kernel {
 };
 constexpr Kernel kForward = {2, 0.12}, kDq = {3, 0.16}, kDkv = {4, 0.2};
 
-// Time (us) of `units` tiles of `waves` waves (of which `busy` have work) that go over `axis` elements each (`share`
-// of them where causal) in `splits` parts, from the time of a block on a SIMD (1024 of
-// them, shared by `resident` waves): what all SIMDs have to do, or one tile's chain,
-// whichever is longer; then the parts' way through memory and the launch that adds
-// them.  `part`: bytes of a split's parts.  A block's products take 0.0021 us a
-// column each in bf16 (six times that for fp32 as three parts, sixteen times for fp32's
-// own instructions); a tile costs about four us before its first block.
+// Time (us) of `units` tiles of `waves` waves (of which `busy` have work) that go over
+// `axis` elements each (`share` of them where causal) in `splits` parts: what all 1024
+// SIMDs have to do, or one tile's chain, whichever is longer; then the parts' way through
+// memory and the launch that adds them (`part`: bytes of a split's parts).
+//
+// Measured: a block's products take 0.0021 us a column each in bf16 (six times that for
+// fp32 as three parts, sixteen times for fp32's own instructions); a tile costs about four
+// us before its first block.  Eight waves share a tile's way to LDS (16384 tokens of
+// 128 columns: 1089 us for the forward pass, 1306 with four), but two share a SIMD.
+// One query each over 200003 keys: 1512 us in one part, 404 in 4, 159 in 32, 164 in 64;
+// 2049 tokens of 72 columns in fp32: 150, 76 in 4, 84 in 16.
 inline double time_of(const Kernel& k, const Sizes& s, int width, int64_t units, int waves, int busy,
                       int64_t axis, double share, int splits, double part) {
-  const double product = (s.bf16 ? 0.0021 : width <= 128 ? 0.0126 : 0.0336) * width, block = k.products * product + k.softmax;
-  // eight waves share a tile's way to LDS (16384 tokens of 128 columns: 1089 us for the
-  // forward pass, 1306 with four); a wave by itself waits for it (one query each over
-  // 200003 keys: 190 us in 64 parts, 159 with four waves in 32); of eight, two share a SIMD
-  const double alone = block * (busy == 8 ? 1.8 : (waves == 1 ? 2.0 : 1.0) * (s.bf16 ? 1.1 : 1.25));
+  const double product = (s.bf16 ? 0.0021 : width <= 128 ? 0.0126 : 0.0336) * width;
+  const double block = k.products * product + k.softmax;
+  const double alone = block * (busy == 8 ? 1.8 : s.bf16 ? 1.1 : 1.25);
   const double blocks = (double)ceil_div(axis, kRows);
   const double all = (double)units * busy * (waves == 8 ? 0.9 : 1.0) *
                      (blocks * share * block + 2.0 * splits) / 1024;
@@ -71,8 +73,8 @@ inline double share_of(const Sizes& s, int64_t q, int64_t k) {
 
 constexpr int kTrySplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
 
-// Over the queries (forward; dq).  A tile that the queries of a head would not fill
-// takes those of all heads that share k and v.
+// Over the queries (forward; dq) with tiles of the given waves.  A tile that the queries
+// of a head would not fill takes those of all heads that share k and v.
 inline Plan over_queries(const Sizes& s, const Kernel& kernel, const int* waves, int options) {
   Plan best{width_of(s.dim), waves[0], 1, 1, 0};
   const int n = std::max(1, s.n);
@@ -80,12 +82,12 @@ inline Plan over_queries(const Sizes& s, const Kernel& kernel, const int* waves,
   if (!s.bias && s.group > 1 && q < kRows * 4 && s.q_tokens * s.group < (int64_t)1 << 30) best.pack = s.group;
   double least = 1e30;
   for (int i = 0; i < options; ++i) {
-    if (waves[i] == 8 && options > 1 && q * best.pack <= 4 * kRows) continue;
+    // waves without a query wait, and cost nothing; no tile is twice as long as they need
+    const int busy = (int)std::min<int64_t>(waves[i], ceil_div(q * best.pack, kRows));
+    if (i > 0 && busy <= waves[i] / 2) continue;
     const int64_t units = n * ceil_div(q * best.pack, kRows * waves[i]) * (s.heads / best.pack);
     for (int splits : kTrySplits) {
       if (splits > 1 && splits * 64 > k) break;
-      // waves without a query wait, and cost nothing
-      const int busy = (int)std::min<int64_t>(waves[i], ceil_div(q * best.pack, kRows));
       const double us = time_of(kernel, s, best.width, units, waves[i], busy, k, share_of(s, q, k), splits,
                                 4.0 * s.q_tokens * s.heads * s.dim);
       if (us < least) least = us, best.waves = waves[i], best.splits = splits;
@@ -112,13 +114,15 @@ inline Plan over_keys(const Sizes& s, int waves) {
   return best;
 }
 
-// Waves of a workgroup.  Narrow heads take eight over the keys where sequences are long
-// (8192 tokens, 16 heads of 64, causal: 608 us for the backward pass, 739 with four) and
-// four where they are short (32 sequences: 115 and 105).
+// Waves of a workgroup.  Eight for 96 and 128 columns, whose registers leave two to a SIMD
+// room (with four the forward pass takes them where sequences are short).  Over the keys of
+// narrow heads eight where sequences are long (8192 tokens, 16 heads of 64, causal: 608 us
+// for the backward pass, 739 with four) and four where they are short (32 sequences: 115
+// and 105).
 inline Plan plan_forward(const Sizes& s) {
   const int width = width_of(s.dim);
-  constexpr int waves[] = {4, 1, 8};
-  return over_queries(s, kForward, waves, width == 256 ? 1 : s.bf16 && width > 64 ? 3 : 2);
+  constexpr int waves[] = {4, 8};
+  return over_queries(s, kForward, waves, s.bf16 && (width == 96 || width == 128) ? 2 : 1);
 }
 constexpr int dq_waves(bool bf16, int width) { return bf16 && width > 64 && width <= 128 ? 8 : 4; }
 inline int dkv_waves(bool bf16, int width, int64_t keys) {
