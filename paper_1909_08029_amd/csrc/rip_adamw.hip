@@ -62,14 +62,29 @@ struct Update {
   float b1, c1, b2, c2, eps;      // c = 1 - b
   rip_adamw_scalars s;
   const rip_adamw_scalars* live;  // device; replaces s unless NULL
-  uint8_t active[RIP_MAX_REPLICAS];
+  uint32_t active[RIP_MAX_REPLICAS / 4];  // a byte each, in words that scalar loads reach
 };
 
 // Second moment in 8 bits: code 16 x + y stands for y steps (x = 0) or
 // (16 + y) 2^(x - 1), a step being 2^(exp - 127); the largest is 31 * 2^14.
-__device__ __forceinline__ float second_value(uint32_t c, float step) {
-  const float f = c < 16 ? (float)c : __uint_as_float((c + (130u << 4)) << 19);
-  return f * step;
+// Shifted to a float's place a code is its value times 2^-130 (x = 0 a subnormal).
+// `nan`: bits of a NaN for a block that stands for it, else 0.
+__device__ __forceinline__ float second_value(uint32_t codes, int j, int exp, uint32_t nan) {
+  const uint32_t at = j < 3 ? codes << (19 - 8 * j) : codes >> 5;
+  return __builtin_amdgcn_ldexpf(__uint_as_float((at & 0xffu << 19) | nan), exp + 3);
+}
+__device__ __forceinline__ uint32_t nan_of(int exp) { return exp == kCkptNan ? 0x7fc00000u : 0; }
+
+// The square root rounded to nearest, for 0 and from kRootLeast on, where the residuals
+// below are exact.  The hardware's is within one step; the root lies above the middle
+// of y and its neighbour z if x > y z.  (Smaller numbers have to be scaled first, which
+// costs as much again: seven of the 88 instructions that an element would take.)
+constexpr float kRootLeast = 0x1p-96f;
+__device__ __forceinline__ float root_of(float x) {
+  const float y = __builtin_amdgcn_sqrtf(x);
+  const float down = __uint_as_float(__float_as_uint(y) - 1), up = __uint_as_float(__float_as_uint(y) + 1);
+  const float z = __builtin_fmaf(-down, y, x) <= 0.0f ? down : y;
+  return __builtin_fmaf(-up, y, x) > 0.0f ? up : z;
 }
 // Exponent byte of a block whose largest value has the bits `top` (>= 0).
 __device__ __forceinline__ uint32_t second_exponent(uint32_t top) {
@@ -77,13 +92,19 @@ __device__ __forceinline__ uint32_t second_exponent(uint32_t top) {
   const int e = (int)(top >> 23) - 18 + ((top & 0x7fffffu) > 0x780000u ? 1 : 0);
   return top >= 0x7f800000u ? kCkptNan : (uint32_t)max(1, e);
 }
-// Code of x >= 0 with 1 / step = inv, rounded up with the probability r / 2^16 of
-// a remainder.
+// Code (its low byte) of x >= 0 with 1 / step = inv, rounded up with the probability
+// r / 2^16 of a remainder.
 __device__ __forceinline__ uint32_t second_code(float x, float inv, uint32_t r) {
   const float t = x * inv;
-  const uint32_t low = (uint32_t)(t + (float)r * 0x1p-16f);
-  const uint32_t high = ((__float_as_uint(t) + (r << 3)) >> 19) - (130u << 4);
-  return max(t < 16.0f ? low : min(high, 255u), x > 0.0f ? 1u : 0u);
+  const uint32_t low = (uint32_t)__builtin_fmaf((float)r, 0x1p-16f, t);
+  const uint32_t high = min((__float_as_uint(t) + (r << 3)) >> 19, (130u << 4) + 255) - (130u << 4);
+  return max(t < 16.0f ? low : high, min(__float_as_uint(x), 1u));
+}
+// The low bytes of four numbers.
+__device__ __forceinline__ uint32_t pack4(const uint32_t (&x)[kLane], int j) {
+  const uint32_t a = __builtin_amdgcn_perm(x[j + 1], x[j], 0x0c0c0400u);
+  const uint32_t b = __builtin_amdgcn_perm(x[j + 3], x[j + 2], 0x0c0c0400u);
+  return __builtin_amdgcn_perm(b, a, 0x05040100u);
 }
 
 // Finalizer of MurmurHash3 (Appleby), a bijection of 32 bits.
@@ -95,14 +116,14 @@ __device__ __forceinline__ uint32_t scramble(uint32_t x) {
   return x ^ (x >> 16);
 }
 
-template <int N>
-__device__ __forceinline__ uint32_t block_max(const float (&x)[N]) {
+// Largest magnitude (bits) of the 32 elements that four neighbouring lanes hold.
+__device__ __forceinline__ uint32_t block_max(const float (&x)[kLane]) {
+  static_assert(kCkptBlock == 4 * kLane, "a block is a quad of lanes");
   uint32_t top = 0;
 #pragma unroll
-  for (int j = 0; j < N; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
-#pragma unroll
-  for (int o = 1; o < kCkptBlock / N; o *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, o));
-  return top;
+  for (int j = 0; j < kLane; ++j) top = max(top, __float_as_uint(x[j]) & 0x7fffffffu);
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xf, 0xf, true));  // lane ^ 1
+  return max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xf, 0xf, true)); // lane ^ 2
 }
 __device__ __forceinline__ float inverse_step(uint32_t e) {
   return e == kCkptNan ? 0.0f : __uint_as_float((254 - e) << 23);
@@ -114,76 +135,125 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 struct Unit {
   float w[kLane], g[kLane], m[kLane], v[kLane];
 };
-template <int DT, int FORMAT>
+template <int DT, bool FULL>
+__device__ __forceinline__ void get(uint64_t p, int64_t at, int c, int width, float (&f)[kLane]) {
+  const typename Elem<DT>::T* from = (const typename Elem<DT>::T*)p + at;
+  if (FULL)
+    Elem<DT>::template load8<true>(from + c, f);
+  else
+    load_unit<DT>(from, c, width, f);
+}
+template <int DT, bool FULL>
+__device__ __forceinline__ void put(uint64_t p, int64_t at, int c, int width, const float (&f)[kLane]) {
+  typename Elem<DT>::T* to = (typename Elem<DT>::T*)p + at;
+  if (FULL)
+    Elem<DT>::store8(to + c, f);
+  else
+    store_unit<DT>(to, c, width, f);
+}
+template <int DT, int FORMAT, bool FULL>
 __device__ __forceinline__ void load(const Row& row, int64_t at, int width, int c, Unit& u) {
-  typedef typename Elem<DT>::T T;
-  load_unit<DT>((const T*)row.param + at, c, width, u.w);
-  load_unit<DT>((const T*)row.grad + at, c, width, u.g);
+  get<DT, FULL>(row.param, at, c, width, u.w);
+  get<DT, FULL>(row.grad, at, c, width, u.g);
   if constexpr (FORMAT == RIP_STATE_FP32) {
-    load_unit<RIP_FP32>((const float*)row.m + at, c, width, u.m);
-    load_unit<RIP_FP32>((const float*)row.v + at, c, width, u.v);
+    get<RIP_FP32, FULL>(row.m, at, c, width, u.m);
+    get<RIP_FP32, FULL>(row.v, at, c, width, u.v);
   } else {
     const u32x2 mc = *(const u32x2*)((const int8_t*)row.m + at + c);
     const u32x2 vc = *(const u32x2*)((const uint8_t*)row.v + at + c);
-    const int64_t block = (at + c) / kCkptBlock;
     const uint32_t codes[2] = {mc[0], mc[1]};
-    ckpt_unpack<kLane>(codes, ((const uint8_t*)row.m_exps)[block], u.m);
-    const float step = ckpt_step(((const uint8_t*)row.v_exps)[block]);
+    ckpt_unpack<kLane>(codes, ((const uint8_t*)row.m_exps + at / kCkptBlock)[c / kCkptBlock], u.m);
+    const int exp = ((const uint8_t*)row.v_exps + at / kCkptBlock)[c / kCkptBlock];
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) u.v[j] = second_value(vc[j / 4] >> (8 * (j % 4)) & 0xff, step);
+    for (int j = 0; j < kLane; ++j) u.v[j] = second_value(vc[j / 4], j % 4, exp, nan_of(exp));
   }
 }
 
-// A tile of one replica's segment.  Bound by memory.
-template <int DT, int FORMAT>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Update u) {
-  typedef typename Elem<DT>::T T;
-  const int rep = u.active[blockIdx.y];
-  const TileAt tile = u.table[blockIdx.x];
-  const Row row = u.rows[(int64_t)tile.segment * u.n_rep + rep];
-  const rip_adamw_scalars s = u.live ? *u.live : u.s;
-  const int64_t at = (int64_t)tile.tile * kTile, left = row.numel - at;
-  const int width = left < kTile ? (int)left : kTile;
+// The weights from the new moments.
+template <bool PLAIN>
+__device__ __forceinline__ void step(const Update& u, const rip_adamw_scalars& s, Unit& x) {
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    const float root = PLAIN ? root_of(x.v[j]) : __builtin_sqrtf(x.v[j]);
+    x.w[j] = x.w[j] * s.decay - (s.rate * x.m[j]) / (root * s.root + u.eps);
+  }
+}
+
+// Eight elements of a tile; FULL: no segment ends in it.
+template <int DT, int FORMAT, bool FULL>
+__device__ __forceinline__ void update(const Update& u, const rip_adamw_scalars& s, const Row& row, int rep,
+                                       uint32_t segment, int64_t at, int width) {
   const int c = threadIdx.x * kLane;
-  if (c >= (FORMAT == RIP_STATE_FP32 ? width : (width + kCkptBlock - 1) / kCkptBlock * kCkptBlock))
+  if (!FULL && c >= (FORMAT == RIP_STATE_FP32 ? width : (width + kCkptBlock - 1) / kCkptBlock * kCkptBlock))
     return;
   Unit x;
-  load<DT, FORMAT>(row, at, width, c, x);
+  load<DT, FORMAT, FULL>(row, at, width, c, x);
 #pragma unroll
   for (int j = 0; j < kLane; ++j) {
     const float g = s.grad_scale * x.g[j];
     x.m[j] = u.b1 * x.m[j] + u.c1 * g;
     x.v[j] = u.b2 * x.v[j] + (u.c2 * g) * g;
-    x.w[j] = x.w[j] * s.decay - (s.rate * x.m[j]) / (__builtin_sqrtf(x.v[j]) * s.root + u.eps);
   }
-  store_unit<DT>((T*)row.param + at, c, width, x.w);
+  float least = x.v[0];
+#pragma unroll
+  for (int j = 1; j < kLane; ++j) least = fminf(least, x.v[j]);
+  if (FORMAT == RIP_STATE_8BIT && __all(least >= kRootLeast))
+    step<true>(u, s, x);
+  else
+    step<false>(u, s, x);
+  put<DT, FULL>(row.param, at, c, width, x.w);
   if constexpr (FORMAT == RIP_STATE_FP32) {
-    store_unit<RIP_FP32>((float*)row.m + at, c, width, x.m);
-    store_unit<RIP_FP32>((float*)row.v + at, c, width, x.v);
+    put<RIP_FP32, FULL>(row.m, at, c, width, x.m);
+    put<RIP_FP32, FULL>(row.v, at, c, width, x.v);
   } else {
-    const uint64_t key = fold(fold(s.key[0] | (uint64_t)s.key[1] << 32, (uint64_t)rep), tile.segment);
-    const int64_t i = at + c;
-    const uint32_t seed = (uint32_t)key + (uint32_t)(i >> 32) * 0x9E3779B9u;
+    const uint64_t key = fold(fold(s.key[0] | (uint64_t)s.key[1] << 32, (uint64_t)rep), segment);
+    const uint32_t seed = (uint32_t)key + (uint32_t)(at >> 32) * 0x9E3779B9u;  // (a tile's)
+    const uint32_t i = (uint32_t)at + c;
     const uint32_t me = ckpt_exponent(block_max(x.m)), ve = second_exponent(block_max(x.v));
     const float mi = inverse_step(me), vi = inverse_step(ve);
-    u32x2 mc = {0, 0}, vc = {0, 0};
+    uint32_t ms[kLane], vs[kLane];
 #pragma unroll
     for (int j = 0; j < kLane; ++j) {
-      const uint32_t h = scramble((uint32_t)(i + j) ^ seed);
-      const float q = floorf(x.m[j] * mi + (float)(h & 0xffff) * 0x1p-16f);
-      const uint32_t code = (uint32_t)(int)fminf(fmaxf(q, -127.0f), 127.0f) & 0xff;
-      mc[j / 4] |= code << (8 * (j % 4));
-      vc[j / 4] |= second_code(x.v[j], vi, h >> 16) << (8 * (j % 4));
+      const uint32_t h = scramble((i + j) ^ seed);
+      const float q = floorf(__builtin_fmaf((float)(h & 0xffff), 0x1p-16f, x.m[j] * mi));
+      ms[j] = (uint32_t)(int)__builtin_amdgcn_fmed3f(q, -127.0f, 127.0f);
+      vs[j] = second_code(x.v[j], vi, h >> 16);
     }
+    u32x2 mc = {pack4(ms, 0), pack4(ms, 4)}, vc = {pack4(vs, 0), pack4(vs, 4)};
     if (me == kCkptNan) mc = u32x2{0, 0};
     if (ve == kCkptNan) vc = u32x2{0, 0};
-    *(u32x2*)((int8_t*)row.m + i) = mc;
-    *(u32x2*)((uint8_t*)row.v + i) = vc;
+    *(u32x2*)((int8_t*)row.m + at + c) = mc;
+    *(u32x2*)((uint8_t*)row.v + at + c) = vc;
     if (threadIdx.x % (kCkptBlock / kLane) == 0) {
-      ((uint8_t*)row.m_exps)[i / kCkptBlock] = (uint8_t)me;
-      ((uint8_t*)row.v_exps)[i / kCkptBlock] = (uint8_t)ve;
+      ((uint8_t*)row.m_exps + at / kCkptBlock)[c / kCkptBlock] = (uint8_t)me;
+      ((uint8_t*)row.v_exps + at / kCkptBlock)[c / kCkptBlock] = (uint8_t)ve;
     }
   }
+}
+
+// A tile of one replica's segment.  Moments in fp32: bound by memory (5.4 TB/s).  In 8
+// bits: by instructions, 80 an element, half of them the root and the quotient to the
+// last bit, a third the codes (two replicas of 400 M: 1702 us, 4.8 TB/s; 2021 with roots
+// scaled always, with branches around each load, and keys made in every lane).
+template <int DT, int FORMAT>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Update u) {
+  const int rep = u.active[blockIdx.y / 4] >> (8 * (blockIdx.y % 4)) & 0xff;
+  const TileAt tile = u.table[blockIdx.x];
+  const Row row = u.rows[(int64_t)tile.segment * u.n_rep + rep];
+  rip_adamw_scalars s = u.s;
+  if (u.live) {  // (word by word: one pointer to both kinds of memory would make them a lane's)
+    s.decay = u.live->decay, s.rate = u.live->rate, s.root = u.live->root;
+    s.grad_scale = u.live->grad_scale, s.key[0] = u.live->key[0], s.key[1] = u.live->key[1];
+  }
+  const int64_t at = (int64_t)tile.tile * kTile, left = row.numel - at;
+  const int width = left < kTile ? (int)left : kTile;
+  // Whole tiles of 8-bit moments load without branches.  With moments in fp32 that is
+  // slower: more loads in flight than memory serves well (541 us for four replicas of
+  // 25.6 M, 527 with one array's loads after another's).
+  if (FORMAT == RIP_STATE_8BIT && width == kTile)
+    update<DT, FORMAT, true>(u, s, row, rep, tile.segment, at, width);
+  else
+    update<DT, FORMAT, false>(u, s, row, rep, tile.segment, at, width);
 }
 
 struct Moments {
@@ -208,9 +278,9 @@ __global__ __launch_bounds__(kThreads) void moments_kernel(Moments p, typename E
   ckpt_unpack<kLane>(codes, ((const uint8_t*)row.m_exps)[i / kCkptBlock], x);
   const int64_t to = blockIdx.y * p.packed + row.place + i;
   Elem<DT>::store8(m + to, x);
-  const float step = ckpt_step(((const uint8_t*)row.v_exps)[i / kCkptBlock]);
+  const int exp = ((const uint8_t*)row.v_exps)[i / kCkptBlock];
 #pragma unroll
-  for (int j = 0; j < kLane; ++j) x[j] = second_value(vc[j / 4] >> (8 * (j % 4)) & 0xff, step);
+  for (int j = 0; j < kLane; ++j) x[j] = second_value(vc[j / 4], j % 4, exp, nan_of(exp));
   Elem<DT>::store8(v + to, x);
 }
 
@@ -378,7 +448,7 @@ extern "C" int32_t rip_adamw_step(const rip_adamw_state* s, const int32_t* activ
       return fail(RIP_E_INVAL, "active id %d out of range", active[i]);
     if (seen[active[i]]) return fail(RIP_E_INVAL, "active id %d listed twice", active[i]);
     seen[active[i]] = 1;
-    u.active[i] = (uint8_t)active[i];
+    u.active[i / 4] |= (uint32_t)active[i] << (8 * (i % 4));
   }
   if (!n_active || !s->tiles) return RIP_OK;
   if ((rc = check_device(s))) return rc;

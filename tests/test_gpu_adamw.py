@@ -133,6 +133,27 @@ def test_extremes(bits):
         x.check(before, x.snapshot(), [0], step, HYPER)
 
 
+def test_roots_of_all_magnitudes():
+    """Second moments from far below the smallest normal number to 2^100, waves of one
+    magnitude, of all, and with zeros among them; eps so small that the root counts."""
+    import torch
+    import paper_1909_08029_amd as rip
+    h = dict(HYPER, eps=1e-37, weight_decay=0.0, grad_scale=1.0)
+    x = Setup("f32", 8, sizes=[1 << 18, 1 << 16, 6145], n=1)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for k, g in enumerate(x.grad[0]):
+        power = torch.randint(-74, 51, (len(g),), generator=gen, device="cuda")
+        if k == 0:                                  # a power for each 512 elements
+            power = power[:len(g) // 512].repeat_interleave(512)
+        g.copy_((1 + torch.rand(len(g), generator=gen, device="cuda")) * 2.0 ** power.float())
+        if k == 2:
+            g[torch.rand(len(g), generator=gen, device="cuda") < 0.01] = 0
+    for step in (1, 2):
+        before = x.snapshot()
+        rip.rip_adamw_step(x.state, [0], step, **h)
+        x.check(before, x.snapshot(), [0], step, h)
+
+
 def test_roundings_keep_the_mean():
     """A second moment that shrinks by 0.1% a step, between codes 3 to 6% apart, and a
     first moment of a few steps of its block follow their exact values on average."""
