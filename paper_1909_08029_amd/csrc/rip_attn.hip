@@ -80,7 +80,10 @@ struct Layout {
   }
 };
 
-bool two_sided(const rip_attn& a) { return a.k_offsets && a.k_offsets != a.q_offsets; }
+// One list for both sides is cut to each side's tokens.
+bool two_sided(const rip_attn& a) {
+  return a.k_offsets && (a.k_offsets != a.q_offsets || a.k_tokens != a.q_tokens);
+}
 
 Sizes sizes_of(const rip_attn& a) {
   return {a.q_tokens, a.k_tokens, a.n_sequences, a.heads, a.heads / a.kv_heads, a.head_dim,

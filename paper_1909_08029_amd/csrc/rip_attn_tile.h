@@ -523,7 +523,7 @@ __device__ __forceinline__ Place find(const Args& p, const Side& here, const Sid
   at.tile = slot - (lo * pack / PER + e);
   if (e == 0 || e == n + 1) {
     at.other = {0, 0};
-  } else if (other.offsets != here.offsets) {
+  } else if (other.offsets != here.offsets || other.tokens != here.tokens) {
     if (p.cleaned) {
       at.other = {other.offsets[e - 1], other.offsets[e]};
     } else {

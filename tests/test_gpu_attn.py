@@ -189,6 +189,24 @@ def test_offsets_out_of_order():
     assert torch.cuda.is_available()
 
 
+@pytest.mark.parametrize("sequences", [2, 1100])
+def test_one_list_for_both_sides(sequences):
+    """The same tensor as both offsets, with other numbers of queries and keys: it is cut
+    to each side's tokens."""
+    import paper_1909_08029_amd as rip
+    import torch
+    at = [0, 90, 200] if sequences == 2 else [0] * (sequences - 1) + [90, 200]
+    o = offsets(at)
+    for dtype in ("f32", "bf16"):
+        for nq, nk in ((200, 150), (120, 200)):
+            q, k, v, dout = tensors(dtype, 2, 1, 64, nq, nk)
+            out, kept = rip.rip_attn_forward(q, k, v, o, o, causal=False)
+            dq, dk, dv = rip.rip_attn_backward(dout, q, k, v, out, kept, o, o, causal=False)
+            Attention(q, k, v, at, at, causal=False, dout=dout).check(
+                dict(out=out, lse=kept.lse, dq=dq, dk=dk, dv=dv))
+    assert torch.cuda.is_available()
+
+
 def test_many_sequences():
     """More than every workgroup puts in order by itself; one and two tokens each."""
     at = [0]
