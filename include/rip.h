@@ -537,6 +537,7 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
 #define RIP_MAX_HEAD_DIM 256
 #define RIP_MAX_SEQUENCES (1 << 20)
 #define RIP_MAX_INTERVALS 128
+#define RIP_MAX_BUCKETS (1 << 20)
 #define RIP_MAX_BIAS_SPAN 2048   /* last start - first start + 2 */
 
 typedef struct rip_rel_buckets {
@@ -557,7 +558,7 @@ typedef struct rip_attn {
   const void* bias;         /* device [buckets][heads], or NULL: none */
   int32_t bias_dtype;
   int64_t ld_bias;
-  int32_t buckets;
+  int32_t buckets;          /* 1 .. RIP_MAX_BUCKETS */
   const rip_rel_buckets* rel;
 } rip_attn;
 

@@ -87,7 +87,7 @@ bool two_sided(const rip_attn& a) {
 
 Sizes sizes_of(const rip_attn& a) {
   return {a.q_tokens, a.k_tokens, a.n_sequences, a.heads, a.heads / a.kv_heads, a.head_dim,
-          a.dtype == RIP_BF16, a.causal != 0, a.bias != nullptr};
+          a.dtype == RIP_BF16, a.causal != 0, a.bias != nullptr, a.bias ? lut_size(a) : 0};
 }
 
 Layout layout_of(const rip_attn& a, const Plans& plan, bool backward) {
@@ -138,8 +138,8 @@ int32_t check(const rip_attn* a, const char* name) {
       a->buckets < 1)
     return fail(RIP_E_INVAL, "%s: a bias needs buckets, intervals and their rows", name);
   const int n = a->rel->n_intervals;
-  if (n > RIP_MAX_INTERVALS)
-    return fail(RIP_E_UNSUPPORTED, "%s: %d intervals are above the limit", name, n);
+  if (n > RIP_MAX_INTERVALS || a->buckets > RIP_MAX_BUCKETS)
+    return fail(RIP_E_UNSUPPORTED, "%s: %d intervals, %d buckets are above the limit", name, n, a->buckets);
   for (int b = 0; b < n; ++b)
     if (a->rel->rows[b] < 0 || a->rel->rows[b] >= a->buckets)
       return fail(RIP_E_INVAL, "%s: interval %d has row %d of %d", name, b, a->rel->rows[b], a->buckets);

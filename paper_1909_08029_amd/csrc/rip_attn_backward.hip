@@ -509,16 +509,24 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buck
 
 // Variants: rows of a tile of the other axis, and waves to a SIMD that the registers
 // have to leave room for.
-template <int NT, int D, bool BIAS, bool SPLIT>
+template <int NT, int D, int WAVES, bool BIAS, bool SPLIT>
 const void* dq_of() {
   constexpr int step = NT == kBf16 && D <= 128 && (D > 64 || BIAS) ? 64 : 32;
   constexpr int units = D <= (NT == kBf16 ? 128 : 64) ? 2 : 1;
-  return (const void*)dq_kernel<NT, D, dq_waves(NT == kBf16, D), step, units, BIAS, SPLIT>;
+  static_assert(!BIAS || sizeof(typename Tile<NT, D>::template Store<step>) * 2 +
+                                 4 * (lut_floats(WAVES == 8 ? kSpanOfEight : RIP_MAX_BIAS_SPAN) +
+                                      WAVES * (sums_size(WAVES == 8 ? kSpanOfEight : RIP_MAX_BIAS_SPAN) +
+                                               kBlockFloats)) <= 160 * 1024,
+                "the LDS holds tiles, the bias and the sums");
+  return (const void*)dq_kernel<NT, D, WAVES, step, units, BIAS, SPLIT>;
 }
 template <int NT, int D>
-const void* dq_of(bool bias, bool split) {
-  return bias ? (split ? dq_of<NT, D, true, true>() : dq_of<NT, D, true, false>())
-              : (split ? dq_of<NT, D, false, true>() : dq_of<NT, D, false, false>());
+const void* dq_of(int waves, bool bias, bool split) {
+  constexpr int kWaves = dq_waves(NT == kBf16, D, 0);
+  if (bias && waves != kWaves)
+    return split ? dq_of<NT, D, 4, true, true>() : dq_of<NT, D, 4, true, false>();
+  return bias ? (split ? dq_of<NT, D, kWaves, true, true>() : dq_of<NT, D, kWaves, true, false>())
+              : (split ? dq_of<NT, D, kWaves, false, true>() : dq_of<NT, D, kWaves, false, false>());
 }
 template <int NT, int D, int WAVES, bool BIAS, bool SPLIT, bool DK, bool DV>
 const void* dkv_of() {
@@ -549,10 +557,11 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& pl
     f.a = over_q;
     const bool split = f.a.splits > 1;
     constexpr int NT = DT == RIP_BF16 ? kBf16 : kSplit, kWide = DT == RIP_BF16 ? kBf16 : kFp32;
-    const void* fn = width == 64    ? dq_of<NT, 64>(bias, split)
-                     : width == 96  ? dq_of<NT, 96>(bias, split)
-                     : width == 128 ? dq_of<NT, 128>(bias, split)
-                                    : dq_of<kWide, 256>(bias, split);
+    const int waves = plan.q.waves;
+    const void* fn = width == 64    ? dq_of<NT, 64>(waves, bias, split)
+                     : width == 96  ? dq_of<NT, 96>(waves, bias, split)
+                     : width == 128 ? dq_of<NT, 128>(waves, bias, split)
+                                    : dq_of<kWide, 256>(waves, bias, split);
     const size_t lds =
         bias ? 4 * (lut_floats(f.a.lut_size) + plan.q.waves * (sums_size(f.a.lut_size) + kBlockFloats)) : 0;
     void* args[] = {&f};

@@ -27,6 +27,7 @@ struct Sizes {
   int64_t q_tokens, k_tokens;
   int n, heads, group, dim;
   bool bf16, causal, bias;
+  int span;  // of the bias: numbers by distance
 };
 struct Plan {
   int width, waves, pack, splits;
@@ -124,12 +125,17 @@ inline Plan plan_forward(const Sizes& s) {
   constexpr int waves[] = {4, 8};
   return over_queries(s, kForward, waves, s.bf16 && (width == 96 || width == 128) ? 2 : 1);
 }
-constexpr int dq_waves(bool bf16, int width) { return bf16 && width > 64 && width <= 128 ? 8 : 4; }
+// dq sums the bias's gradient by distance in every wave: the LDS of eight waves' sums
+// beside the tiles (128 rows of 256 bytes) and the waves' blocks holds spans up to 1468.
+constexpr int kSpanOfEight = 1468;
+constexpr int dq_waves(bool bf16, int width, int span) {
+  return bf16 && width > 64 && width <= 128 && span <= kSpanOfEight ? 8 : 4;
+}
 inline int dkv_waves(bool bf16, int width, int64_t keys) {
   return bf16 && (width == 64 ? keys >= 512 : width <= 128) ? 8 : 4;
 }
 inline Plan plan_dq(const Sizes& s) {
-  const int waves[] = {dq_waves(s.bf16, width_of(s.dim))};
+  const int waves[] = {dq_waves(s.bf16, width_of(s.dim), s.span)};
   return over_queries(s, kDq, waves, 1);
 }
 inline Plan plan_dkv(const Sizes& s) {

@@ -58,6 +58,7 @@ BOTH = [
     (dict(q_offsets=A + 2), ALIGN), (dict(k_offsets=A + 4097), ALIGN),
     (dict(BIAS, rel=False), INVAL), (dict(BIAS, intervals=0), INVAL), (dict(BIAS, no_rows=True), INVAL),
     (dict(BIAS, no_starts=True), INVAL), (dict(BIAS, buckets=0), INVAL),
+    (dict(BIAS, buckets=(1 << 20) + 1), UNSUP),
     (dict(BIAS, starts=range(128), rows=[0] * 129), UNSUP),
     (dict(BIAS, rows=(0, 3, 1)), INVAL), (dict(BIAS, rows=(0, -1, 1)), INVAL),
     (dict(BIAS, starts=(4, 4)), INVAL), (dict(BIAS, starts=(4, -4)), INVAL),

@@ -21,10 +21,10 @@ static void show(const Plan& p) {
   std::printf("%d %d %d %d %lld ", p.width, p.waves, p.pack, p.splits, (long long)p.slots);
 }
 int main(int argc, char** argv) {
-  for (int i = 1; i + 8 < argc; i += 9) {
-    long long v[9];
-    for (int j = 0; j < 9; ++j) v[j] = std::atoll(argv[i + j]);
-    const Sizes s{v[1], v[2], (int)v[0], (int)v[3], (int)v[4], (int)v[5], v[6] != 0, v[7] != 0, v[8] != 0};
+  for (int i = 1; i + 9 < argc; i += 10) {
+    long long v[10];
+    for (int j = 0; j < 10; ++j) v[j] = std::atoll(argv[i + j]);
+    const Sizes s{v[1], v[2], (int)v[0], (int)v[3], (int)v[4], (int)v[5], v[6] != 0, v[7] != 0, v[8] != 0, (int)v[9]};
     show(plan_forward(s));
     show(plan_dq(s));
     show(plan_dkv(s));
@@ -45,7 +45,7 @@ def plans(tmp_path_factory):
                     str(d / "p.cpp"), "-o", str(d / "p")], check=True, timeout=120)
 
     def run(queries):
-        """(sequences, queries, keys, heads, group, dim, bf16, causal, bias) each, in all."""
+        """(sequences, queries, keys, heads, group, dim, bf16, causal, bias, span) each, in all."""
         args = [str(int(v)) for q in queries for v in q]
         out = subprocess.run([str(d / "p"), *args], capture_output=True, text=True, timeout=60, check=True)
         return [[tuple(int(v) for v in line.split()[5 * i:5 * i + 5]) for i in range(3)]
@@ -56,7 +56,7 @@ def plans(tmp_path_factory):
 def test_every_variant_is_taken(plans):
     seen = set()
     cases = list(itertools.product(WIDTHS.items(), (0, 1), (0, 1), SHAPES.values()))
-    got = plans([(n, n * q, n * k, heads, group, dim, bf16, causal, bias)
+    got = plans([(n, n * q, n * k, heads, group, dim, bf16, causal, bias, 100 * bias)
                  for (width, dim), bf16, bias, (n, q, k, heads, group, causal) in cases])
     for ((width, dim), bf16, bias, shape), plan in zip(cases, got):
         for kind, (w, waves, pack, splits, slots) in zip(("forward", "dq", "dkv"), plan):
@@ -75,13 +75,21 @@ def test_every_variant_is_taken(plans):
         assert ("pack", kind, packed) in seen
 
 
+def test_wide_spans_take_four_waves(plans):
+    spans = [1, 1468, 1469, 2048]
+    for width, dim in WIDTHS.items():
+        got = plans([(2, 2000, 2000, 4, 1, dim, 1, 0, 1, s) for s in spans])
+        most = 8 if width in (96, 128) else 4
+        assert [p[1][1] for p in got] == [most, most, 4, 4]
+
+
 def test_plans_cover_their_rows(plans):
-    sizes = [(n, q, k, heads, group, dim, bf16, causal, bias)
+    sizes = [(n, q, k, heads, group, dim, bf16, causal, bias, span)
              for n in (0, 1, 7, 1 << 20) for q in (0, 1, 130, 70001, 1 << 23) for k in (0, 3, 4097, 1 << 23)
              for heads, group in ((1, 1), (32, 8), (256, 256)) for dim in (1, 64, 96, 250)
-             for bf16, causal, bias in ((0, 0, 0), (1, 1, 0), (1, 0, 1))]
+             for bf16, causal, bias, span in ((0, 0, 0, 0), (1, 1, 0, 0), (1, 0, 1, 1), (1, 0, 1, 2048))]
     for size, plan in zip(sizes, plans(sizes)):
-        n, q, k, heads, group, dim, bf16, causal, bias = size
+        n, q, k, heads, group, dim, bf16, causal, bias, span = size
         for kind, (width, waves, pack, splits, slots) in zip(("forward", "dq", "dkv"), plan):
             assert dim <= width and waves in (4, 8) and 1 <= splits <= 64, size
             assert pack == 1 or (pack == group and not bias and kind != "dkv"), size

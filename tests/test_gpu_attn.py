@@ -131,6 +131,17 @@ def test_intervals(starts, rows):
                 buckets=rip.RelBuckets(starts, rows))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 80, 128, 256])
+@pytest.mark.parametrize("span", [1468, 1469, 2048])
+def test_wide_spans(dtype, dim, span):
+    """Sums of many distances in LDS beside the tiles, at every width; one and many tiles."""
+    import paper_1909_08029_amd as rip
+    first = 1 - span // 2
+    b = rip.RelBuckets([first, -3, 0, first + span - 2], [3, 1, 0, 2, 4])
+    against(*tensors(dtype, 2, 1, dim, 1301, 1301), [0, 1200, 1301], causal=False, bias=table(5, 2), buckets=b)
+
+
 def test_a_bias_that_hides_keys():
     """-inf in the table is a mask; queries that it leaves nothing have zeros."""
     import torch
