@@ -20,7 +20,11 @@ def key_of(seed, step, replica, segment):
 
 
 def hashes(n, key):
-    x = np.arange(n, dtype=np.uint64)
+    return hashes_from(0, n, key)
+
+
+def hashes_from(first, n, key):
+    x = np.arange(first, first + n, dtype=np.uint64)
     x = (x & np.uint64(0xffffffff)) ^ np.uint64(key)
     for shift, mul in ((16, 0x85ebca6b), (13, 0xc2b2ae35)):
         x = ((x ^ (x >> np.uint64(shift))) * np.uint64(mul)) & np.uint64(0xffffffff)
