@@ -26,8 +26,8 @@ struct Args {
   float scale2, scale;  // scale2 = scale * log2(e)
   int splits;         // of the axis that a workgroup goes over
   int slots;          // tiles of the grid
-  const float* lut;   // [heads][lut_size], or NULL
-  int lut_size, lut_first;
+  const float* lut;   // the bias by distance, [heads][lut_size], or NULL: made by the workgroup
+  int lut_size, lut_first;  // lut_size 0: no bias
 };
 
 // A matrix of heads side by side.
@@ -40,12 +40,39 @@ struct ConstHeads {
   int64_t ld;
 };
 
-// The map from distances to rows of the table, by value.
+// The table, and which of its rows a distance reads, by value: what the kernels with a
+// bias take behind their other arguments.
 struct Buckets {
+  const void* table;
+  int64_t ld;
+  int bf16;
   int n;                           // intervals
   int32_t start[kMaxStarts];       // first distance of intervals 1 ..
   int32_t row[RIP_MAX_INTERVALS];
 };
+template <typename T>
+struct WithBias : T {
+  Buckets map;
+};
+template <typename T, bool BIAS>
+struct KernelArgs {
+  typedef T type;
+};
+template <typename T>
+struct KernelArgs<T, true> {
+  typedef WithBias<T> type;
+};
+
+// A bias's value in the log2 domain.  Masks of a type's lowest value hide their keys as
+// -inf does: the log-sum of a row of such scores would not hold what tells them apart.
+constexpr float kHides = -65536.0f;
+__device__ __forceinline__ float bias_at(const Buckets& map, int distance, int head) {
+  int row = map.row[0];
+  for (int b = 1; b < map.n; ++b) row = distance >= map.start[b - 1] ? map.row[b] : row;
+  const int64_t at = row * map.ld + head;
+  const float x = map.bf16 ? Elem<RIP_BF16>::load((const uint16_t*)map.table + at) : ((const float*)map.table)[at];
+  return x < kHides ? -__builtin_inff() : x * 1.44269504f;
+}
 
 struct Forward {
   Args a;
@@ -62,7 +89,6 @@ struct Backward {
   float* delta;     // [heads][q tokens]
   float* part;      // splits: parts of dq, or of dk and dv
   float* bias_part; // [heads][slots * splits][intervals]
-  const Buckets* buckets;  // device
 };
 
 // The grid of a launch over slots, splits and heads: as many rows as its 32-bit sizes
@@ -73,13 +99,13 @@ inline dim3 grid_of(const Args& p, int heads) {
 }
 
 // Launches by type and width (rip_attn_forward.hip, rip_attn_backward.hip).
-int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* stream);
+int32_t run_forward(WithBias<Forward>& f, int32_t dtype, int width, int waves, void* stream);
 struct Plans {
   Plan q, k;
 };
-int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype,
+int32_t run_backward(WithBias<Backward>& f, const Args& over_q, const Args& over_k, int32_t dtype,
                      const Plans& plan, void* stream);
-int32_t run_bias_grad(const Backward& f, int64_t parts, int32_t buckets, int32_t heads,
+int32_t run_bias_grad(const WithBias<Backward>& f, int64_t parts, int32_t buckets, int32_t heads,
                       int32_t dtype, void* grad, int64_t ld, int32_t accumulate, void* stream);
 
 }  // namespace attn

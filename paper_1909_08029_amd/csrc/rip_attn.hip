@@ -11,17 +11,12 @@ struct Prepare {
   int32_t tokens[2];
   int32_t* cleaned[2];  // or NULL
   int32_t n_seqs, cleans;
-  const void* bias;
-  int32_t bias_bf16;
-  int64_t ld_bias;
   float* lut;
   int32_t lut_size;
-  Buckets* buckets_out;  // or NULL
-  Buckets buckets;
+  Buckets map;
 };
 
 constexpr int kThreads = 1024;
-constexpr float kHides = -65536.0f;  // a bias below hides its keys
 
 // Workgroups 0 .. cleans-1 make the running maximum of a side's offsets; the others
 // write a head's bias by distance.
@@ -47,21 +42,9 @@ __global__ __launch_bounds__(kThreads) void prepare_kernel(Prepare p) {
     }
     return;
   }
-  const int head = blockIdx.x - p.cleans, n = p.buckets.n;
-  const int first = n > 1 ? p.buckets.start[0] - 1 : 0;
-  for (int i = threadIdx.x; i < p.lut_size; i += kThreads) {
-    int row = p.buckets.row[0];
-    for (int b = 1; b < n; ++b) row = first + i >= p.buckets.start[b - 1] ? p.buckets.row[b] : row;
-    const int64_t at = row * p.ld_bias + head;
-    const float x = p.bias_bf16 ? Elem<RIP_BF16>::load((const uint16_t*)p.bias + at)
-                                : ((const float*)p.bias)[at];
-    // masks of a type's lowest value too: the log-sum of a row of such scores would not
-    // hold what tells them apart
-    p.lut[(int64_t)head * p.lut_size + i] = x < kHides ? -__builtin_inff() : x * 1.44269504f;
-  }
-  if (head == 0 && p.buckets_out)
-    for (int i = threadIdx.x; i < (int)(sizeof(Buckets) / 4); i += kThreads)
-      ((int32_t*)p.buckets_out)[i] = ((const int32_t*)&p.buckets)[i];
+  const int head = blockIdx.x - p.cleans, first = p.map.n > 1 ? p.map.start[0] - 1 : 0;
+  for (int i = threadIdx.x; i < p.lut_size; i += kThreads)
+    p.lut[(int64_t)head * p.lut_size + i] = bias_at(p.map, first + i, head);
 }
 
 int64_t align16(int64_t bytes) { return ceil_div(bytes, 16) * 16; }
@@ -71,9 +54,27 @@ int lut_size(const rip_attn& a) {
   return n > 1 ? a.rel->starts[n - 2] - a.rel->starts[0] + 2 : 1;
 }
 
+// Whether a launch before makes the bias by distance: where a workgroup would compare a
+// lane's distances with more than 16 starts in all (8 of 37 tokens' case: 39.4 us, 44.3
+// with the launches; 62 of 8192 tokens in 1024 workgroups: 330 us, 290 with them).
+bool lut_before(const rip_attn& a) {
+  return a.bias && ceil_div(lut_size(a) + 128, 256) * a.rel->n_intervals > 16;
+}
+Buckets map_of(const rip_attn& a) {
+  Buckets m{};
+  if (!a.bias) return m;
+  m.table = a.bias, m.ld = a.ld_bias, m.bf16 = a.bias_dtype == RIP_BF16;
+  m.n = a.rel->n_intervals;
+  for (int b = 0; b < m.n; ++b) {
+    m.row[b] = a.rel->rows[b];
+    if (b) m.start[b - 1] = a.rel->starts[b - 1];
+  }
+  return m;
+}
+
 // What a call takes of its workspace, in bytes from its start.
 struct Layout {
-  int64_t cleaned[2] = {-1, -1}, lut = -1, buckets = -1, delta = -1, bias_part = -1, part = -1, end = 0;
+  int64_t cleaned[2] = {-1, -1}, lut = -1, delta = -1, bias_part = -1, part = -1, end = 0;
   void take(int64_t& at, int64_t bytes) {
     at = end;
     end += align16(bytes);
@@ -94,17 +95,14 @@ Layout layout_of(const rip_attn& a, const Plans& plan, bool backward) {
   Layout l;
   if (a.n_sequences > kScan)
     for (int s = 0; s < (two_sided(a) ? 2 : 1); ++s) l.take(l.cleaned[s], 4 * ((int64_t)a.n_sequences + 1));
-  if (a.bias) l.take(l.lut, 4 * (int64_t)a.heads * lut_size(a));
+  if (lut_before(a)) l.take(l.lut, 4 * (int64_t)a.heads * lut_size(a));
   const int64_t rows = (int64_t)a.heads * a.q_tokens;
   if (!backward) {
     if (plan.q.splits > 1) l.take(l.part, 4 * rows * plan.q.splits * (a.head_dim + 2));
     return l;
   }
   l.take(l.delta, 4 * rows);
-  if (a.bias) {
-    l.take(l.buckets, sizeof(Buckets));
-    l.take(l.bias_part, 4 * a.heads * plan.q.slots * plan.q.splits * a.rel->n_intervals);
-  }
+  if (a.bias) l.take(l.bias_part, 4 * a.heads * plan.q.slots * plan.q.splits * a.rel->n_intervals);
   const int64_t dq = plan.q.splits > 1 ? plan.q.splits * rows * a.head_dim : 0;
   const int64_t dkv =
       plan.k.splits > 1 ? 2 * plan.k.splits * a.k_tokens * (int64_t)a.kv_heads * a.head_dim : 0;
@@ -187,7 +185,7 @@ Args args_of(const rip_attn& a, const Plan& plan, const Layout& l, char* ws) {
   p.scale = a.scale, p.scale2 = a.scale * 1.44269504f;
   p.splits = plan.splits, p.slots = (int)plan.slots;
   if (a.bias) {
-    p.lut = (const float*)(ws + l.lut);
+    if (l.lut >= 0) p.lut = (const float*)(ws + l.lut);
     p.lut_size = lut_size(a);
     p.lut_first = a.rel->n_intervals > 1 ? a.rel->starts[0] - 1 : 0;
   }
@@ -201,17 +199,11 @@ int32_t prepare(const rip_attn& a, const Layout& l, char* ws, void* stream) {
   for (int s = 0; s < 2; ++s)
     if (l.cleaned[s] >= 0) p.cleaned[s] = (int32_t*)(ws + l.cleaned[s]), p.cleans = s + 1;
   p.n_seqs = a.n_sequences;
-  if (a.bias) {
-    p.bias = a.bias, p.bias_bf16 = a.bias_dtype == RIP_BF16, p.ld_bias = a.ld_bias;
+  if (l.lut >= 0) {
     p.lut = (float*)(ws + l.lut), p.lut_size = lut_size(a);
-    p.buckets.n = a.rel->n_intervals;
-    for (int b = 0; b < p.buckets.n; ++b) {
-      p.buckets.row[b] = a.rel->rows[b];
-      if (b) p.buckets.start[b - 1] = a.rel->starts[b - 1];
-    }
-    if (l.buckets >= 0) p.buckets_out = (Buckets*)(ws + l.buckets);
+    p.map = map_of(a);
   }
-  const int groups = p.cleans + (a.bias ? a.heads : 0);
+  const int groups = p.cleans + (l.lut >= 0 ? a.heads : 0);
   if (!groups) return RIP_OK;
   void* args[] = {&p};
   return launch((const void*)prepare_kernel, dim3((uint32_t)groups), dim3(kThreads), args, 0, stream,
@@ -290,7 +282,8 @@ extern "C" int32_t rip_attn_forward(const rip_attn* a, const void* q, int64_t ld
   if (a->q_tokens == 0) return RIP_OK;
   char* ws = static_cast<char*>(workspace);
   if ((rc = prepare(*a, l, ws, stream))) return rc;
-  Forward f{};
+  WithBias<Forward> f{};
+  f.map = map_of(*a);
   f.a = args_of(*a, plan.q, l, ws);
   f.q = {q, ld_q}, f.k = {k, ld_k}, f.v = {v, ld_v};
   f.out = {out, ld_out}, f.low = {low, ld_low};
@@ -354,7 +347,8 @@ extern "C" int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t l
   if (dbias) b.matrix(dbias, dbias_dtype, a->buckets, a->heads, ld_dbias, "dbias", true);
   b.range(workspace, l.end, "workspace", true);
   if ((rc = b.check())) return rc;
-  Backward f{};
+  WithBias<Backward> f{};
+  f.map = map_of(*a);
   if (a->q_tokens == 0 && a->k_tokens == 0)
     return !dbias || accumulate
                ? RIP_OK
@@ -367,10 +361,7 @@ extern "C" int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t l
   f.lse = lse;
   f.delta = (float*)(ws + l.delta);
   f.part = l.part >= 0 ? (float*)(ws + l.part) : nullptr;
-  if (a->bias) {
-    f.bias_part = (float*)(ws + l.bias_part);
-    f.buckets = (const Buckets*)(ws + l.buckets);
-  }
+  if (a->bias) f.bias_part = (float*)(ws + l.bias_part);
   if ((rc = run_backward(f, args_of(*a, plan.q, l, ws), args_of(*a, plan.k, l, ws), t, plan, stream)) ||
       !dbias)
     return rc;

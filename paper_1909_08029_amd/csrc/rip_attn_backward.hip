@@ -53,7 +53,8 @@ __device__ __forceinline__ void add_diagonals(const f32x16& ds, int rel, int fir
 }
 
 template <int NT, int D, int WAVES, int STEP, int EU, bool BIAS, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
+__global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(
+    typename KernelArgs<Backward, BIAS>::type f) {
   constexpr int DT = storage(NT);
   typedef Tile<NT, D> Tl;
   typedef typename Tl::T T;
@@ -75,7 +76,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   float* const sums = lut + lut_floats(p.lut_size);
   float* const mine = sums + wave * pitch;
   float* const block = sums + WAVES * pitch + wave * kBlockFloats;
-  const int intervals = BIAS ? f.buckets->n : 0;
+  int intervals = 0;
+  if constexpr (BIAS) intervals = f.map.n;
   float* const bias_part =
       BIAS ? f.bias_part + ((int64_t)hz * p.slots * p.splits + slot * p.splits + split) * intervals
            : nullptr;
@@ -100,8 +102,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
   }
   const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
   float below = 0.0f, above = 0.0f;  // ds of blocks all in the first (last) interval
-  if (BIAS) {
-    load_lut(p, head0, lut);
+  if constexpr (BIAS) {
+    load_lut(p, f.map, head0, lut);
     for (int x = lane; x < pitch; x += 64) mine[x] = 0.0f;
     for (int x = lane; x < kBlockFloats; x += 64) block[x] = 0.0f;
   }
@@ -262,8 +264,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
     const float* const blocks = sums + WAVES * pitch;
     const int x0 = p.lut_first - 62;  // distance of the first sum
     for (int b = wave; b < intervals; b += WAVES) {
-      const int from = b == 0 ? x0 : f.buckets->start[b - 1];
-      const int to = b == intervals - 1 ? x0 + pitch : f.buckets->start[b];
+      const int from = b == 0 ? x0 : f.map.start[b - 1];
+      const int to = b == intervals - 1 ? x0 + pitch : f.map.start[b];
       float sum = 0.0f;
       for (int x = from + lane; x < to; x += 64)
 #pragma unroll
@@ -281,7 +283,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dq_kernel(Backward f) {
 
 // dk (DK) and dv (DV) of 32 keys to a wave.
 template <int NT, int D, int WAVES, int STEP, int EU, bool V_LDS, bool BIAS, bool SPLIT, bool DK, bool DV>
-__global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
+__global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(
+    typename KernelArgs<Backward, BIAS>::type f) {
   constexpr int DT = storage(NT);
   typedef Tile<NT, D> Tl;
   typedef typename Tl::T T;
@@ -356,8 +359,8 @@ __global__ __launch_bounds__(64 * WAVES, EU) void dkv_kernel(Backward f) {
       refs[threadIdx.x] = i0 + (int)threadIdx.x < lq ? reference(lse) : kInf;
       deltas[threadIdx.x] = del;
     }
-    if (BIAS && lut_head != g) {
-      load_lut(p, kv * p.group + g, lut);
+    if constexpr (BIAS) {
+      if (lut_head != g) load_lut(p, f.map, kv * p.group + g, lut);
       lut_head = g;
     }
     lds_barrier();
@@ -487,14 +490,14 @@ __global__ __launch_bounds__(256) void add_kernel(const float* part, int splits,
 
 // The bias's gradient: a workgroup adds the parts of one row of the table and one head.
 template <int DT>
-__global__ __launch_bounds__(256) void bias_kernel(const float* part, const Buckets* buckets,
+__global__ __launch_bounds__(256) void bias_kernel(const float* part, Buckets map,
                                                    int64_t parts, typename Elem<DT>::T* grad,
                                                    int64_t ld, int accumulate) {
   __shared__ float sums[4];
-  const int row = blockIdx.x, head = blockIdx.y, n = parts ? buckets->n : 0;
+  const int row = blockIdx.x, head = blockIdx.y, n = parts ? map.n : 0;
   float sum = 0.0f;
   for (int b = 0; b < n; ++b) {
-    if (buckets->row[b] != row) continue;
+    if (map.row[b] != row) continue;
     for (int64_t x = threadIdx.x; x < parts; x += 256) sum += part[(head * parts + x) * n + b];
   }
 #pragma unroll
@@ -549,9 +552,9 @@ int32_t add(const float* part, int splits, int64_t tokens, int width, Heads to, 
 }
 
 template <int DT>
-int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& plan, void* stream) {
+int32_t run(WithBias<Backward>& f, const Args& over_q, const Args& over_k, const Plans& plan, void* stream) {
   int32_t rc;
-  const bool bias = over_q.lut;
+  const bool bias = over_q.lut_size;
   const int width = plan.q.width;
   {
     f.a = over_q;
@@ -606,15 +609,15 @@ int32_t run(Backward& f, const Args& over_q, const Args& over_k, const Plans& pl
 
 }  // namespace
 
-int32_t run_backward(Backward& f, const Args& over_q, const Args& over_k, int32_t dtype, const Plans& plan,
+int32_t run_backward(WithBias<Backward>& f, const Args& over_q, const Args& over_k, int32_t dtype, const Plans& plan,
                      void* stream) {
   return dtype == RIP_BF16 ? run<RIP_BF16>(f, over_q, over_k, plan, stream)
                            : run<RIP_FP32>(f, over_q, over_k, plan, stream);
 }
 
-int32_t run_bias_grad(const Backward& f, int64_t parts, int32_t buckets, int32_t heads, int32_t dtype,
+int32_t run_bias_grad(const WithBias<Backward>& f, int64_t parts, int32_t buckets, int32_t heads, int32_t dtype,
                       void* grad, int64_t ld, int32_t accumulate, void* stream) {
-  void* args[] = {(void*)&f.bias_part, (void*)&f.buckets, &parts, &grad, &ld, &accumulate};
+  void* args[] = {(void*)&f.bias_part, (void*)&f.map, &parts, &grad, &ld, &accumulate};
   return launch(dtype == RIP_BF16 ? (const void*)bias_kernel<RIP_BF16> : (const void*)bias_kernel<RIP_FP32>,
                 dim3((uint32_t)buckets, (uint32_t)heads), dim3(256), args, 0, stream,
                 "rip_attn_backward: bias");

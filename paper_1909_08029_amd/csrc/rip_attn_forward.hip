@@ -22,12 +22,15 @@ namespace {
 // Without a bias, with one, and with one whose gradient will be wanted: that sums ds
 // in fp32, and its row sums delta come from out, which must not hold the rounding of
 // the exponentials then.  They enter the product as two bf16 numbers (16 bits).
+// (A kernel's name holds what its parameters' types depend on: plain numbers, as an
+// unnamed type's place is counted differently for the host and the device.)
 enum { kPlain, kBias, kExact };
 
 constexpr float kSlack = 6.0f;  // growth of a maximum (log2) that needs no rescaling
 
 template <int NT, int D, int WAVES, int KT, int EU, int MODE, bool SPLIT>
-__global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(Forward f) {
+__global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(
+    typename KernelArgs<Forward, MODE != 0>::type f) {
   constexpr int DT = storage(NT);
   typedef Tile<NT, D> Tl;
   typedef typename Tl::T T;
@@ -62,7 +65,6 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(Forward f) {
     t = min(keys, split * share), end = min(keys, t + share);
   }
   const Bias bias{lut + kLutPad, p.lut_first, p.lut_size};
-  if (BIAS) load_lut(p, head0, lut);
 
   const T* k0 = (const T*)f.k.p + at.other.begin * f.k.ld + (int64_t)kv * p.dim;
   const T* v0 = (const T*)f.v.p + at.other.begin * f.v.ld + (int64_t)kv * p.dim;
@@ -79,6 +81,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(Forward f) {
   }
   Frag<NT> q[D / 16];
   load_row<NT, D>((const T*)f.q.p + token * f.q.ld + (int64_t)head * p.dim, valid, half, p.dim, q);
+  if constexpr (BIAS) load_lut(p, f.map, head0, lut);
   for (; t < end; t += KT) {
     if (!kOnTheWay) {
       ks.load(k0, f.k.ld, t, end, p.dim);
@@ -316,13 +319,13 @@ const void* kernel_of(int32_t dtype, int width, int waves, int mode, bool split)
 
 }  // namespace
 
-int32_t run_forward(Forward& f, int32_t dtype, int width, int waves, void* stream) {
+int32_t run_forward(WithBias<Forward>& f, int32_t dtype, int width, int waves, void* stream) {
   const Args& p = f.a;
   void* args[] = {&f};
   const bool split = p.splits > 1;
-  const int mode = !p.lut ? kPlain : f.low.p ? kExact : kBias;
+  const int mode = !p.lut_size ? kPlain : f.low.p ? kExact : kBias;
   const void* fn = kernel_of(dtype, width, waves, mode, split);
-  int32_t rc = launch(fn, grid_of(p, p.heads / p.pack), dim3(64 * waves), args, p.lut ? 4 * lut_floats(p.lut_size) : 0, stream, "rip_attn_forward");
+  int32_t rc = launch(fn, grid_of(p, p.heads / p.pack), dim3(64 * waves), args, p.lut_size ? 4 * lut_floats(p.lut_size) : 0, stream, "rip_attn_forward");
   if (rc || !split) return rc;
   return launch(dtype == RIP_BF16 ? (const void*)join_kernel<RIP_BF16> : (const void*)join_kernel<RIP_FP32>,
                 dim3((uint32_t)(p.heads * p.q.tokens)), dim3(256), args, 0, stream,

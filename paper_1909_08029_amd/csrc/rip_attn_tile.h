@@ -586,10 +586,11 @@ struct Bias {
   __device__ __forceinline__ float far(int side) const { return lut[side < 0 ? 0 : size - 1]; }
 };
 // LDS: kLutPad + lut_size + kLutPad numbers from `lut` on.
-__device__ __forceinline__ void load_lut(const Args& p, int head, float* lut) {
-  const float* from = p.lut + (int64_t)head * p.lut_size;
-  for (int i = threadIdx.x; i < p.lut_size + 2 * kLutPad; i += blockDim.x)
-    lut[i] = from[min(max(i - kLutPad, 0), p.lut_size - 1)];
+__device__ __forceinline__ void load_lut(const Args& p, const Buckets& map, int head, float* lut) {
+  for (int i = threadIdx.x; i < p.lut_size + 2 * kLutPad; i += blockDim.x) {
+    const int at = min(max(i - kLutPad, 0), p.lut_size - 1);
+    lut[i] = p.lut ? p.lut[(int64_t)head * p.lut_size + at] : bias_at(map, p.lut_first + at, head);
+  }
 }
 __host__ __device__ constexpr int lut_floats(int lut_size) { return lut_size + 2 * kLutPad; }
 

@@ -54,3 +54,14 @@ def test_matrix_instructions(asm):
     for source in ("rip_attn_forward", "rip_attn_backward"):
         assert set(re.findall(r"v_mfma_\w+", asm[source])) == forms
         assert "ds_read_b64_tr_b16" in asm[source] and "v_cvt_pk_bf16_f32" in asm[source]
+
+
+def test_every_kernel_is_found_by_its_name():
+    """Names that the host registers in the built library are names of its device code (one
+    that is not ends the process at its first launch)."""
+    data = open(os.path.join(ROOT, "paper_1909_08029_amd", "librip.so"), "rb").read()
+    names = set(re.findall(rb"\0(_Z[A-Za-z0-9_$]*_kernel[A-Za-z0-9_$]*)(?=\0)", data))
+    kernels = set(re.findall(rb"\0(_Z[A-Za-z0-9_$]*_kernel[A-Za-z0-9_$]*)\.kd(?=\0)", data))
+    assert len(kernels) > 100
+    stubs = {n for n in names if b"__device_stub__" in n}
+    assert names - stubs == kernels, sorted(names - stubs ^ kernels)[:4]
