@@ -515,7 +515,8 @@ __global__ __launch_bounds__(256) void bias_kernel(const float* part, Buckets ma
 template <int NT, int D, int WAVES, bool BIAS, bool SPLIT>
 const void* dq_of() {
   constexpr int step = NT == kBf16 && D <= 128 && (D > 64 || BIAS) ? 64 : 32;
-  constexpr int units = D <= (NT == kBf16 ? 128 : 64) ? 2 : 1;
+  // (four waves to a tile of 96 or 128 bf16 columns: their LDS leaves no room for more)
+  constexpr int units = D <= 64 || WAVES == 8 ? 2 : 1;
   static_assert(!BIAS || sizeof(typename Tile<NT, D>::template Store<step>) * 2 +
                                  4 * (lut_floats(WAVES == 8 ? kSpanOfEight : RIP_MAX_BIAS_SPAN) +
                                       WAVES * (sums_size(WAVES == 8 ? kSpanOfEight : RIP_MAX_BIAS_SPAN) +

@@ -5,7 +5,7 @@ to AMDGPU assembly with the library's own flags).
 * attention's products are matrix instructions, of bf16 on operands that transposing LDS
   reads deliver, and of fp32 for the widest heads alone;
 * no private memory but for the widest fp32 heads, whose rows and sums alone take 384
-  registers, and a few values of loops' surroundings in others.
+  registers, and at most sixteen values of loops' surroundings in others.
 """
 import importlib.util
 import os
@@ -46,7 +46,7 @@ def test_arithmetic_and_registers(asm, source):
     assert kernels
     for name, private in kernels:
         if not re.search(r"(forward|dq|dkv)_kernelILi3ELi256E", name):   # (fp32, 256)
-            assert int(private) <= (32 if "attn_" in source else 0), name
+            assert int(private) <= (64 if "attn_" in source else 0), name
 
 
 def test_matrix_instructions(asm):
