@@ -515,10 +515,11 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
  * with row strides of at most RIP_MAX_WIDTH.
  * Sequence s has the queries q_offsets[s] .. q_offsets[s+1]-1 and the keys
  * k_offsets[s] .. k_offsets[s+1]-1 (int32, on the device; k_offsets NULL: as
- * q_offsets; one list for both is cut to each side's tokens).  Offsets out of order are cut to fit as in rip_pref_loss.  With L_q
- * queries and L_k keys, query i stands at position i + L_k - L_q (its sequence's
- * queries are the last of its keys) and sees every key j of its sequence, or with
- * `causal` those with j <= i + L_k - L_q.
+ * q_offsets; one list for both is cut to each side's tokens).  Offsets out of
+ * order are cut to fit as in rip_pref_loss.  With L_q queries and L_k keys,
+ * query i stands at position i + L_k - L_q (its sequence's queries are the last
+ * of its keys) and sees every key j of its sequence, or with `causal` those with
+ * j <= i + L_k - L_q.
  *   x_ij   = scale * q_i . k_j + bias[row of (j - position of i)][h]
  *   lse_i  = log sum_j e^x_ij,  p_ij = e^(x_ij - lse_i),  out_i = sum_j p_ij v_j
  * A bias below -65536 (-inf, a type's lowest value) hides its keys.  A query that sees no
