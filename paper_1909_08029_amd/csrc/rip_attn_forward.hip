@@ -71,7 +71,9 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(
   const Tl at_lane(lane);
 
   f32x16 o[D / 32] = {};
-  float m = -kInf, l = 0.0f;  // reference (log2); the sum of this half's keys
+  // reference (log2); the sum of this half's keys, and what its last rounding added (Kahan
+  // 1965): equal terms all round the same way, so that 100000 plain additions err by 1e-3
+  float m = -kInf, l = 0.0f, over = 0.0f;
   Stage<NT, D, KT, 64 * WAVES> ks, vs;
   // (fp32 of 256 columns has no registers for tiles on their way)
   constexpr bool kOnTheWay = NT != kFp32;
@@ -141,21 +143,25 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(
       if (__any(top > m + kSlack)) {
         const float next = fmaxf(m, top), scale = m == next ? 1.0f : __builtin_amdgcn_exp2f(m - next);
         m = next;
-        l *= scale;
+        l *= scale, over *= scale;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c)
 #pragma unroll
           for (int r = 0; r < 16; ++r) o[c][r] *= scale;
       }
       const float ref = m == -kInf ? 0.0f : m;  // no key seen so far: every exponential is 0
+      float sums[4];  // of the tile
 #pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const float x = BIAS ? s[b][r] - ref : __builtin_fmaf(s[b][r], p.scale2, -ref);
           s[b][r] = __builtin_amdgcn_exp2f(x);
-          l += s[b][r];
+          sums[r % 4] = b == 0 && r < 4 ? s[b][r] : sums[r % 4] + s[b][r];
         }
+      const float more = ((sums[0] + sums[1]) + (sums[2] + sums[3])) - over, sum = l + more;
+      over = (sum - l) - more;
+      l = sum;
       // e^x rounded to bf16 (half a step of 2^-8, as out is; their sum is not) so that
       // the product runs at bf16's rate
       Frag<NT> e[KB * 2], rest[EXACT ? KB * 2 : 1];
@@ -188,7 +194,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(
     lds_barrier();
   }
   if (!valid) return;
-  l = add_halves(l);
+  l = add_halves(l - over);
   if constexpr (SPLIT) {
     const int64_t row = ((int64_t)split * p.heads + head) * p.q.tokens + token;
     const int64_t all = (int64_t)p.splits * p.heads * p.q.tokens;
