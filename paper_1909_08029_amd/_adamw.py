@@ -3,7 +3,8 @@ argument marshalling only)."""
 from __future__ import annotations
 
 import ctypes
-import functools
+import operator
+import struct
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -15,12 +16,6 @@ STATE_FP32 = 0
 STATE_8BIT = 1
 
 BLOCK = 32  # elements that share an exponent
-
-
-class _Adamw(ctypes.Structure):
-    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double),
-                ("grad_scale", ctypes.c_double), ("seed", ctypes.c_uint64)]
 
 
 class _Scalars(ctypes.Structure):
@@ -139,11 +134,17 @@ class AdamwState:
     __del__ = close
 
 
-@functools.lru_cache(maxsize=64)
-def _cfg(lr, betas, eps, weight_decay, grad_scale, seed):
-    """A reference to the struct of these values, built once."""
-    return ctypes.byref(_Adamw(lr, betas[0], betas[1], eps, weight_decay, grad_scale,
-                               seed & (2 ** 64 - 1)))
+_PACK = struct.Struct("=6dQ").pack  # of struct rip_adamw: lr .. grad_scale, seed
+
+
+def _cfg(lr, betas, eps, weight_decay, grad_scale, seed) -> bytes:
+    """struct rip_adamw of these values as they are now (a tensor may change in place)."""
+    beta1, beta2 = betas
+    seed = operator.index(seed) & (2 ** 64 - 1)
+    try:
+        return _PACK(lr, beta1, beta2, eps, weight_decay, grad_scale, seed)
+    except struct.error as e:
+        raise TypeError(f"AdamW's settings must be real numbers: {e}") from None
 
 
 def rip_adamw_scalars(step: int, lr: float, betas: Tuple[float, float] = (0.9, 0.999),
@@ -153,7 +154,7 @@ def rip_adamw_scalars(step: int, lr: float, betas: Tuple[float, float] = (0.9, 0
     grad_scale and two words of a key.  A copy on the device is rip_adamw_step's
     ``scalars``."""
     out = torch.empty(6, dtype=torch.float32)
-    _check(lib.rip_adamw_scalars_at(_cfg(lr, tuple(betas), eps, weight_decay, grad_scale, seed), step,
+    _check(lib.rip_adamw_scalars_at(_cfg(lr, betas, eps, weight_decay, grad_scale, seed), step,
                                     out.data_ptr()))
     return out
 
@@ -175,7 +176,7 @@ def rip_adamw_step(state: AdamwState, active: Sequence[int], step: int, lr: floa
         live = scalars.data_ptr()
     act, _keep = _i32_call(list(active))
     rc = lib.rip_adamw_step(state._h, act, len(active),
-                            _cfg(lr, tuple(betas), eps, weight_decay, grad_scale, seed), step, live,
+                            _cfg(lr, betas, eps, weight_decay, grad_scale, seed), step, live,
                             _stream(stream, _device()))
     if rc:
         _check(rc)
