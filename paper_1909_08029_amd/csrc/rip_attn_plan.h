@@ -73,6 +73,11 @@ inline double share_of(const Sizes& s, int64_t q, int64_t k) {
 }
 
 constexpr int kTrySplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+// A part has 64 elements of the axis or more.  Without a tile there is nothing to join, nor
+// a row for the launch that would (a grid of no workgroups is an error).
+inline bool may_split(int splits, int64_t axis, int64_t units) {
+  return splits == 1 || (units > 0 && splits * 64 <= axis);
+}
 
 // Over the queries (forward; dq) with tiles of the given waves.  A tile that the queries
 // of a head would not fill takes those of all heads that share k and v.
@@ -88,7 +93,7 @@ inline Plan over_queries(const Sizes& s, const Kernel& kernel, const int* waves,
     if (i > 0 && busy <= waves[i] / 2) continue;
     const int64_t units = n * ceil_div(q * best.pack, kRows * waves[i]) * (s.heads / best.pack);
     for (int splits : kTrySplits) {
-      if (splits > 1 && splits * 64 > k) break;
+      if (!may_split(splits, k, units)) break;
       const double us = time_of(kernel, s, best.width, units, waves[i], busy, k, share_of(s, q, k), splits,
                                 4.0 * s.q_tokens * s.heads * s.dim);
       if (us < least) least = us, best.waves = waves[i], best.splits = splits;
@@ -106,7 +111,7 @@ inline Plan over_keys(const Sizes& s, int waves) {
   const int64_t units = n * ceil_div(k, kRows * waves) * (s.heads / s.group), axis = ceil_div(q, kRows) * kRows * s.group;
   double least = 1e30;
   for (int splits : kTrySplits) {
-    if (splits > 1 && splits * 64 > axis) break;
+    if (!may_split(splits, axis, units)) break;
     const double us = time_of(kDkv, s, best.width, units, waves, waves, axis, share_of(s, q, k), splits,
                               8.0 * s.k_tokens * (s.heads / s.group) * s.dim);
     if (us < least) least = us, best.splits = splits;

@@ -97,3 +97,15 @@ def test_plans_cover_their_rows(plans):
             # tokens before the first and behind the last)
             rows = (k if kind == "dkv" else q) * pack
             assert rows < 1 << 31 and slots == rows // (32 * waves) + n + 2, size
+
+
+def test_an_empty_side_is_not_split(plans):
+    """Nothing to sum into: one part, whatever the other side's length (a second launch over
+    no rows would have no workgroups)."""
+    sizes = [(n, q, k, heads, group, dim, bf16, causal, bias, bias)
+             for n in (0, 1, 7) for q, k in ((0, 128), (0, 600), (0, 100000), (300, 0), (4096, 0), (0, 0))
+             for heads, group in ((1, 1), (8, 1), (32, 8)) for dim in (32, 80, 128, 200)
+             for bf16 in (0, 1) for causal in (0, 1) for bias in (0, 1)]
+    for size, (forward, dq, dkv) in zip(sizes, plans(sizes)):
+        assert size[1] or forward[3] == dq[3] == 1, size
+        assert size[2] or dkv[3] == 1, size

@@ -404,3 +404,24 @@ def test_refusals_of_the_binding():
             bwd(**bad)
         assert e.value.code == rip.RIP_E_OVERLAP
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nq,nk", [(0, 600), (600, 0), (0, 5000), (5000, 0)])
+def test_one_empty_side(dtype, dim, nq, nk):
+    """Queries without keys and keys without queries, more than a split is made for: every
+    row of every output is written, with zeros (log-sums: -inf)."""
+    import torch
+    import paper_1909_08029_amd as rip
+    q, k, v, dout = tensors(dtype, 4, 2, dim, nq, nk)
+    at = [0, nq // 2, nq], [0, nk // 3, nk]
+    bias, b = table(4, 4), rip.RelBuckets([-1, 0, 1], [0, 1, 2, 3])
+    for args in (dict(), dict(bias=bias, buckets=b)):
+        grads = [torch.full_like(t, float("nan")) for t in (q, k, v)]
+        got = run(q, k, v, dout, *at, **args, dq=grads[0], dk=grads[1], dv=grads[2])
+        for name, t in got.items():
+            assert (t == (-math.inf if name == "lse" else 0)).all(), name
+    kept = torch.full_like(bias, 3.0)
+    run(q, k, v, dout, *at, bias=bias, buckets=b, dbias=kept, accumulate=True)
+    assert (kept == 3).all()
