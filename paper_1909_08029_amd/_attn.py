@@ -8,6 +8,7 @@ and autograd: as for the operators that fill gradient buffers.
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
@@ -61,7 +62,12 @@ class RelBuckets:
     def __init__(self, starts: Sequence[int], rows: Sequence[int]):
         if len(rows) != len(starts) + 1:
             raise ValueError(f"{len(starts)} starts make {len(starts) + 1} intervals, not {len(rows)}")
-        self.starts, self.rows = tuple(starts), tuple(rows)
+        self.starts, self.rows = tuple(map(operator.index, starts)), tuple(map(operator.index, rows))
+        # the library's lists are int32
+        if any(not -2 ** 31 <= x < 2 ** 31 for x in self.starts):
+            raise ValueError(f"a start beyond 32 bits: {self.starts}")
+        if any(not 0 <= x < 2 ** 31 for x in self.rows):
+            raise ValueError(f"rows must be 0 .. 2^31 - 1: {self.rows}")
         self._starts = (ctypes.c_int32 * max(1, len(starts)))(*self.starts)
         self._rows = (ctypes.c_int32 * len(rows))(*self.rows)
         self._rel = _Rel(len(rows), ctypes.addressof(self._starts), ctypes.addressof(self._rows))

@@ -159,3 +159,28 @@ def test_bucket_arguments():
         rip.RelBuckets([], [])
     one = rip.RelBuckets([], [0])
     assert one.starts == () and one.rows == (0,)
+
+
+FAR = 2 ** 32
+
+
+@pytest.mark.parametrize("starts,rows", [
+    ([FAR + 5], [0, 1]), ([2 ** 31], [0, 1]), ([-2 ** 31 - 1], [0, 1]), ([0, 2 ** 63 - 1], [0, 1, 2]),
+    ([0, FAR], [0, 1, 2]), ([0], [0, FAR]), ([0], [0, 2 ** 31]), ([0], [-1, 0]), ([0], [-FAR, 0]),
+])
+def test_buckets_beyond_32_bits(starts, rows):
+    """Numbers that the library's int32 lists would hold as others."""
+    with pytest.raises(ValueError):
+        rip.RelBuckets(starts, rows)
+
+
+@pytest.mark.parametrize("starts,rows", [([1.5], [0, 1]), ([0], [0, 1.0]), (["1"], [0, 1]), ([None], [0, 1])])
+def test_buckets_that_are_no_integers(starts, rows):
+    with pytest.raises(TypeError):
+        rip.RelBuckets(starts, rows)
+
+
+def test_buckets_hold_what_they_show():
+    import numpy as np
+    b = rip.RelBuckets(np.array([-2 ** 31, 7]), [np.int64(3), 2 ** 31 - 1, True])
+    assert b.starts == (-2 ** 31, 7) == tuple(b._starts) and b.rows == (3, 2 ** 31 - 1, 1) == tuple(b._rows)
