@@ -10,7 +10,7 @@ from typing import Optional, Sequence, Tuple
 import torch
 
 from . import LIB_PATH, Replicas, _check, _i32_call, lib
-from ._train_ops import _CODES, _device, _elsewhere, _empty, _stream
+from ._train_ops import _CODES, _device, _elsewhere, _empty, _stream, _wrote
 
 STATE_FP32 = 0
 STATE_8BIT = 1
@@ -43,6 +43,12 @@ def _declare():
 
 
 _declare()
+
+
+def _counted(tensors):
+    """One tensor for each version counter of these: a view has its base's."""
+    bases = [t if t._base is None else t._base for t in tensors]
+    return list({id(t): t for t in bases}.values())
 
 
 class AdamwState:
@@ -91,6 +97,9 @@ class AdamwState:
                                           ctypes.byref(h)))
         self._h = h
         self._destroy = lib.rip_adamw_state_destroy  # still reachable at interpreter exit
+        kinds = [rows for rows in (param, m, v, m_exps, v_exps) if rows is not None]
+        self._written = [_counted(t for rows in kinds for t in rows[r]) for r in range(rep.n)]
+        self._all_written = _counted(t for row in self._written for t in row)
 
     @classmethod
     def zeros(cls, rep: Replicas, bits: int = 32) -> "AdamwState":
@@ -166,7 +175,8 @@ def rip_adamw_step(state: AdamwState, active: Sequence[int], step: int, lr: floa
     """AdamW step ``step`` (1, 2, ...) of the ``active`` workers in one launch (see
     include/rip.h).  ``scalars`` on the device (rip_adamw_scalars) takes the place
     of what lr, weight_decay, grad_scale, seed and step say, read when the launch
-    runs: for graphs replayed with later steps' scalars."""
+    runs: for graphs replayed with later steps' scalars.  The workers' parameters and
+    moments count as modified in place."""
     live = None
     if scalars is not None:
         if scalars.get_device() != _device():
@@ -174,9 +184,13 @@ def rip_adamw_step(state: AdamwState, active: Sequence[int], step: int, lr: floa
         if scalars.dtype is not torch.float32 or scalars.numel() != 6 or not scalars.is_contiguous():
             raise ValueError("scalars must hold six contiguous float32 values (rip_adamw_scalars)")
         live = scalars.data_ptr()
-    act, _keep = _i32_call(list(active))
+    act, ids = _i32_call(list(active))
     rc = lib.rip_adamw_step(state._h, act, len(active),
                             _cfg(lr, betas, eps, weight_decay, grad_scale, seed), step, live,
                             _stream(stream, _device()))
     if rc:
         _check(rc)
+    if len(active) == state.rep.n:
+        _wrote(state._all_written)
+    else:
+        _wrote([t for r in ids[:len(active)] for t in state._written[r]])
