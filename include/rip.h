@@ -528,7 +528,8 @@ int32_t rip_policy_loss(const void* logits, int32_t dtype, int64_t ld, int64_t n
  * no other sequence; within one, an infinity or a NaN may reach any of its rows.
  *
  * Products are taken of the inputs as they are and of p and ds rounded to the
- * inputs' type; sums, scores and statistics are fp32.
+ * inputs' type; sums, scores and statistics are fp32 (the sum of e^x compensated, so
+ * that lse's error does not grow with the number of keys).
  *
  * The bias.  Distances j - position fall into n_intervals intervals: those below
  * starts[0], from starts[0] to starts[1] - 1, ..., from starts[n_intervals - 2] on
@@ -575,7 +576,11 @@ int32_t rip_attn_forward(const rip_attn* a, const void* q, int64_t ld_q, const v
 
 /* dq, dk and dv from dout and what the forward pass gave (low may be NULL), and with a
  * bias, unless dbias is NULL, its gradient dbias [buckets][heads] of dbias_dtype (rows
- * of no interval: zeros), added to what it holds if `accumulate` is nonzero. */
+ * of no interval: zeros), added to what it holds if `accumulate` is nonzero.  With a
+ * bias the workspace holds its gradient's parts, 4 bytes for each head, interval, split
+ * and tile of queries (q_tokens / 128 + n_sequences + 2 of these at most): 134 MB a head
+ * for 2^20 sequences and 32 intervals.  A call without dbias takes them, and the time
+ * of their sums, all the same. */
 int64_t rip_attn_backward_workspace(const rip_attn* a);
 int32_t rip_attn_backward(const rip_attn* a, const void* q, int64_t ld_q, const void* k,
                           int64_t ld_k, const void* v, int64_t ld_v, const void* out,

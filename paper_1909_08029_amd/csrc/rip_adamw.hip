@@ -77,7 +77,8 @@ __device__ __forceinline__ uint32_t nan_of(int exp) { return exp == kCkptNan ? 0
 
 // The square root rounded to nearest, for 0 and from kRootLeast on, where the residuals
 // below are exact.  The hardware's is within one step; the root lies above the middle
-// of y and its neighbour z if x > y z.  (Smaller numbers have to be scaled first, which
+// of y and its neighbour z if x > y z (Tuckerman's test; Agarwal, Cooley, Gustavson,
+// Shearer, Slishman and Tuckerman 1986).  (Smaller numbers have to be scaled first, which
 // costs as much again: seven of the 88 instructions that an element would take.)
 constexpr float kRootLeast = 0x1p-96f;
 __device__ __forceinline__ float root_of(float x) {

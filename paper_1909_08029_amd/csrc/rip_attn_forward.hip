@@ -10,9 +10,10 @@
 // leaves the sums within fp32's range and saves rescaling them.
 //
 // Long sequences are bound by the matrix units and what lies between their
-// instructions (16384 causal tokens, 16 heads of 128: 1.22 ms, 900 TFLOP/s), single
-// queries over long caches by memory (819 MB in 161 us), short ones by their own
-// beginning and end (256 tokens, 64 columns: half of 33 us for 32 x 16 of them).
+// instructions (16384 causal tokens, 16 heads of 128: 1.2 ms repeated by itself, 1.3 in
+// passes with the backward pass, whose clock is lower: 920 and 840 TFLOP/s), single
+// queries over long caches by memory (819 MB in 177 to 184 us), short ones by their own
+// beginning and end (256 tokens, 64 columns: half of 36 us for 32 x 16 of them).
 #include "rip_attn_tile.h"
 
 namespace rip {
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(64 * WAVES, EU) void forward_kernel(
 
   f32x16 o[D / 32] = {};
   // reference (log2); the sum of this half's keys, and what its last rounding added (Kahan
-  // 1965): equal terms all round the same way, so that 100000 plain additions err by 1e-3
+  // 1965): equal terms all round the same way, so that 100000 plain additions err by 3e-4
   float m = -kInf, l = 0.0f, over = 0.0f;
   Stage<NT, D, KT, 64 * WAVES> ks, vs;
   // (fp32 of 256 columns has no registers for tiles on their way)
